@@ -479,6 +479,163 @@ STAR_API star_status_t star_group_update_host_ex(float *h_params, float *h_momen
                                                  size_t workspace_bytes, void *cuda_stream);
 
 /* ---------------------------------------------------------------------------
+ * A worker's step: the loss over the vocabulary with the gradient of the
+ * logits, and activations kept in 8 bits whose backward pass writes the
+ * worker's gradient buffers -- what a worker does before its gradients reach
+ * star_group_update.
+ *
+ * Matrices are row-major with a row stride (`ld`, in elements, at least the
+ * number of columns); any element-aligned base and any stride is taken, rows
+ * that share one phase modulo 16 bytes and whose stride keeps it are the fast
+ * case.  Sizes of zero are successful no-ops (sums and losses are still
+ * written: zero).  Written buffers must not overlap any other buffer of the
+ * call, except where an in-place form is named.  All sums, softmax statistics
+ * and activation values are held in binary32; results are rounded once.  The
+ * same call on the same inputs gives the same bits.
+ * ------------------------------------------------------------------------- */
+
+/* Rows of logits x[t][0 .. vocab), one label each.  With z = x / temperature,
+ *     lse = log(sum_j exp(z[j])),  p[j] = exp(z[j] - lse),  logp = z[label] - lse.
+ * A row is ACTIVE iff its label lies in [0, vocab) (a prompt or padding token
+ * carries any other value, -100 by custom), its weight, where weights are
+ * given, is not 0, and not every logit of it is -inf.  The logits of a row that
+ * its label or weight makes inactive are not read: they may hold anything.  An
+ * inactive row has logp = lse = loss = 0 and a zero gradient.  A NaN or +inf
+ * logit makes its own row's results NaN and the totals with them.
+ *
+ * star_token_logprobs: logp[rows] and, unless NULL, lse[rows].
+ * temperature finite, > 0.  One kernel launch. */
+STAR_API star_status_t star_token_logprobs(const void *logits, star_dtype_t dtype, int64_t rows,
+                                           int64_t vocab, int64_t ld, const int64_t *labels,
+                                           float temperature, float *logp, float *lse,
+                                           void *cuda_stream);
+
+/* Device workspace of the two losses below: bytes for `rows` rows in
+ * `sequences` sequences (0 for the policy loss).  Need not be initialized. */
+STAR_API star_status_t star_loss_workspace_bytes(int64_t rows, int64_t sequences, size_t *bytes_out);
+
+/* Clipped policy loss with a KL term, forward and backward in one pass over the
+ * logits.  Per active row t, with A = advantages[t] and w = weights[t] (1
+ * without weights):
+ *     r    = exp(logp - old_logp[t])                 (1 if old_logp is NULL)
+ *     u    = r A,   c = clamp(r, 1 - clip_low, 1 + clip_high) A
+ *     kl   = exp(ref_logp[t] - logp) - (ref_logp[t] - logp) - 1      (0 if ref_logp is NULL)
+ *     token_loss[t] = -min(u, c) + kl_coef kl
+ *     dlogits[t][j] = w / temperature * ((j == label) - p[j]) *
+ *                     (-(u <= c) r A + kl_coef (1 - exp(ref_logp[t] - logp)))
+ *     sums = { sum w token_loss, sum w (-min(u, c)), sum w kl, sum w (c < u) }
+ * dlogits is the gradient of sums[0]; the caller puts the mean's 1 / n (per
+ * token or per sequence) and any loss scale into weights.
+ *   old_logp NULL differentiates the ratio as if old_logp were logp itself.
+ *   dlogits   : rows x vocab of dtype with stride ld_dlogits, or NULL for the
+ *               forward pass alone; may be the logits themselves (same pointer
+ *               and stride), which are then replaced by their gradient
+ *   logp, token_loss : rows entries each; sums : 4 entries
+ *   workspace : device, 16-byte aligned, star_loss_workspace_bytes(rows, 0) bytes
+ * 0 <= clip_low <= 1, clip_high >= 0, kl_coef finite. */
+STAR_API star_status_t star_policy_loss(const void *logits, star_dtype_t dtype, int64_t rows, int64_t vocab,
+                                        int64_t ld, const int64_t *labels, const float *weights,
+                                        const float *advantages, const float *old_logp,
+                                        const float *ref_logp, float temperature, float clip_low,
+                                        float clip_high, float kl_coef, float *logp, float *token_loss,
+                                        float *sums, void *dlogits, int64_t ld_dlogits, void *workspace,
+                                        size_t workspace_bytes, void *cuda_stream);
+
+/* Preference loss on pairs of sequences (paired log ratios), forward and
+ * backward.  Rows seq_offsets[s] .. seq_offsets[s + 1] are sequence s; sequence
+ * 2 i is pair i's chosen answer, 2 i + 1 its rejected one.  With L_s the sum of
+ * logp over the active rows of sequence s, divided by their number if average
+ * != 0 (an empty sequence has L = 0), and ref_s = ref_seq_logp[s] (0 if NULL):
+ *     h    = (L_2i - L_2i+1) - (ref_2i - ref_2i+1),   margin[i] = beta h
+ *     pair_loss[i] = -(1 - e) log sigmoid(beta h) - e log sigmoid(-beta h),   e = label_smoothing
+ *     loss[0] = loss_scale * sum_i pair_loss[i]
+ * and dlogits is the gradient of loss[0] (rows x vocab, as for the policy loss;
+ * NULL: forward alone; may be the logits themselves).  Rows outside every
+ * sequence are inactive.
+ *   seq_offsets : DEVICE, 2 pairs + 1 entries, ascending, in [0, rows].  It is
+ *                 not read on the host; entries are clamped to [0, rows], so
+ *                 that a wrong array gives wrong results but no access outside
+ *                 the buffers
+ *   seq_logp    : 2 pairs entries (L_s);  pair_loss, margin : pairs entries
+ *   workspace   : star_loss_workspace_bytes(rows, 2 * pairs) bytes, 16-byte aligned
+ * beta and loss_scale finite, 0 <= label_smoothing <= 1. */
+STAR_API star_status_t star_preference_loss(const void *logits, star_dtype_t dtype, int64_t rows,
+                                            int64_t vocab, int64_t ld, const int64_t *labels,
+                                            const int32_t *seq_offsets, int64_t pairs,
+                                            const float *ref_seq_logp, float temperature, float beta,
+                                            float label_smoothing, int average, float loss_scale,
+                                            float *seq_logp, float *pair_loss, float *margin, float *loss,
+                                            void *dlogits, int64_t ld_dlogits, void *workspace,
+                                            size_t workspace_bytes, void *cuda_stream);
+
+/* Activations kept in 8 bits.  A checkpoint of x (rows x cols) holds, for every
+ * block of 32 consecutive columns of a row (the last block of a row may be
+ * shorter), a scale 2^e and a code per element,
+ *     e    = the smallest integer >= -126 for which every code of the block is
+ *            within -127 .. 127
+ *     code = round(x / 2^e)   nearest, ties to even;     value = code * 2^e
+ * so a value is off by at most half a step, 1/127 of the block's largest
+ * magnitude at worst and 1/254 at best, and stands exactly in bf16 and fp32: whoever
+ * reads it, the tensor cores included, rounds nothing further.  A block that
+ * holds a NaN, an infinity or a magnitude of 127.5 * 2^104 (2.6e33) or more has
+ * codes 0 and the scale byte 255: all its values are NaN, so that an overflow
+ * reaches the gradients as it would without the checkpoint.
+ *   codes  : int8, row-major, `pitch` bytes from row to row: cols rounded up to a
+ *            multiple of 16 (bytes past cols are 0).  16-byte aligned
+ *   scales : bytes e + 127, four neighbouring blocks side by side for one row,
+ *            then the next row: byte ((c / 128) * tall + t) * 4 + (c / 32) % 4 for
+ *            element (t, c), tall = rows rounded up to a multiple of 64 (bytes of
+ *            rows past `rows` and of blocks past cols are not used).  16-byte aligned
+ * star_checkpoint_sizes gives pitch and the bytes of both (8.25 bits an element). */
+STAR_API star_status_t star_checkpoint_sizes(int64_t rows, int64_t cols, int64_t *pitch_out,
+                                             size_t *code_bytes_out, size_t *scale_bytes_out);
+
+/* Elementwise activations.  GELU_TANH is the tanh form (GPT-2),
+ * 0.5 x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))); GELU_ERF is x Phi(x) (BERT);
+ * SILU is x / (1 + exp(-x)). */
+typedef enum {
+    STAR_ACT_NONE = 0,
+    STAR_ACT_GELU_TANH = 1,
+    STAR_ACT_GELU_ERF = 2,
+    STAR_ACT_SILU = 3
+} star_activation_t;
+
+/* Forward pass: keeps x (rows x cols of dtype, stride ld) in codes and scales
+ * and, where act_out is given, writes act(x) to it in the same pass over x
+ * (rows x cols of dtype, stride ld_act; the activation of x itself, not of its
+ * kept value; may be x: same pointer and stride).  One kernel launch. */
+STAR_API star_status_t star_checkpoint_pack(int8_t *codes, uint8_t *scales, const void *x, star_dtype_t dtype,
+                                            int64_t rows, int64_t cols, int64_t ld, star_activation_t act,
+                                            void *act_out, int64_t ld_act, void *cuda_stream);
+
+/* out = act(value) for every kept value (STAR_ACT_NONE: the value itself,
+ * exact).  out: rows x cols of dtype, stride ld.  One kernel launch. */
+STAR_API star_status_t star_checkpoint_unpack(void *out, star_dtype_t dtype, int64_t ld, const int8_t *codes,
+                                              const uint8_t *scales, int64_t rows, int64_t cols,
+                                              star_activation_t act, void *cuda_stream);
+
+/* Backward pass of an activation whose input was kept: dx = dy * act'(value).
+ * dx, dy: rows x cols of dtype; dx may be dy (same pointer and stride).  One
+ * kernel launch. */
+STAR_API star_status_t star_checkpoint_act_backward(void *dx, int64_t ld_dx, const void *dy, int64_t ld_dy,
+                                                    star_dtype_t dtype, const int8_t *codes,
+                                                    const uint8_t *scales, int64_t rows, int64_t cols,
+                                                    star_activation_t act, void *cuda_stream);
+
+/* Weight gradient of a linear layer whose input was kept:
+ *     dw[o][c] = sum_t dy[t][o] * value[t][c]       (+ dw[o][c] before, if accumulate != 0)
+ *   dy : rows x outs of dy_dtype, stride ld_dy
+ *   dw : dw_dtype, outs x cols with stride ld_dw; with transposed != 0 it is
+ *        stored as cols x outs (the layout of a layer y = x W with W[in][out]).
+ *        Usually the worker's gradient buffer that a round reads
+ * rows == 0 gives zeros (or leaves dw, when accumulating). */
+STAR_API star_status_t star_checkpoint_weight_grad(void *dw, star_dtype_t dw_dtype, int64_t ld_dw, int transposed,
+                                                   const void *dy, star_dtype_t dy_dtype, int64_t ld_dy,
+                                                   const int8_t *codes, const uint8_t *scales, int64_t rows,
+                                                   int64_t cols, int64_t outs, int accumulate,
+                                                   void *cuda_stream);
+
+/* ---------------------------------------------------------------------------
  * Tensor-list round for callers that cannot allocate device memory.
  *
  * The paper has no counterpart to this entry point; it exists for integration.

@@ -135,6 +135,27 @@ def _load() -> ctypes.CDLL:
     lib.star_multi_prepare_ex.restype = c_int
     lib.star_group_update_multi_ex.argtypes = [c_vp, c_vp, c_vp, c_int, c_vp, c_f, c_f, c_vp, c_int, c_vp]
     lib.star_group_update_multi_ex.restype = c_int
+    lib.star_token_logprobs.argtypes = [c_vp, c_int, c_i64, c_i64, c_i64, c_vp, c_f, c_vp, c_vp, c_vp]
+    lib.star_token_logprobs.restype = c_int
+    lib.star_loss_workspace_bytes.argtypes = [c_i64, c_i64, c_vp]
+    lib.star_loss_workspace_bytes.restype = c_int
+    lib.star_policy_loss.argtypes = ([c_vp, c_int, c_i64, c_i64, c_i64] + [c_vp] * 5 + [c_f] * 4 + [c_vp] * 4
+                                     + [c_i64, c_vp, ctypes.c_size_t, c_vp])
+    lib.star_policy_loss.restype = c_int
+    lib.star_preference_loss.argtypes = ([c_vp, c_int, c_i64, c_i64, c_i64, c_vp, c_vp, c_i64, c_vp, c_f, c_f, c_f, c_int,
+                                          c_f] + [c_vp] * 5 + [c_i64, c_vp, ctypes.c_size_t, c_vp])
+    lib.star_preference_loss.restype = c_int
+    lib.star_checkpoint_sizes.argtypes = [c_i64, c_i64, c_vp, c_vp, c_vp]
+    lib.star_checkpoint_sizes.restype = c_int
+    lib.star_checkpoint_pack.argtypes = [c_vp, c_vp, c_vp, c_int, c_i64, c_i64, c_i64, c_int, c_vp, c_i64, c_vp]
+    lib.star_checkpoint_pack.restype = c_int
+    lib.star_checkpoint_unpack.argtypes = [c_vp, c_int, c_i64, c_vp, c_vp, c_i64, c_i64, c_int, c_vp]
+    lib.star_checkpoint_unpack.restype = c_int
+    lib.star_checkpoint_act_backward.argtypes = [c_vp, c_i64, c_vp, c_i64, c_int, c_vp, c_vp, c_i64, c_i64, c_int, c_vp]
+    lib.star_checkpoint_act_backward.restype = c_int
+    lib.star_checkpoint_weight_grad.argtypes = [c_vp, c_int, c_i64, c_int, c_vp, c_int, c_i64, c_vp, c_vp, c_i64, c_i64,
+                                                c_i64, c_int, c_vp]
+    lib.star_checkpoint_weight_grad.restype = c_int
     for name in ("star_schedule_validate", "star_schedule_static_x", "star_schedule_from_labels",
                  "star_schedule_dynamic_x", "star_group_update", "star_multi_workspace_bytes",
                  "star_multi_prepare", "star_group_update_multi"):
@@ -773,3 +794,180 @@ def star_group_update_multi_noalloc(params: Sequence[torch.Tensor], momentum: Se
     _check(_lib.star_group_update_multi_noalloc(T, P, V, G, S, W, STAR_DTYPE_F32 if dt is None else dt,
                                                 _i32(group_offsets), _i32(group_members), K, lr, mu, wd,
                                                 _stream(stream)), "star_group_update_multi_noalloc")
+
+
+# ---------------------------------------------------------------------------
+# a worker's step: losses over the vocabulary, activations kept in 8 bits
+# ---------------------------------------------------------------------------
+STAR_ACT_NONE = 0
+STAR_ACT_GELU_TANH = 1
+STAR_ACT_GELU_ERF = 2
+STAR_ACT_SILU = 3
+_ACTS = {"none": STAR_ACT_NONE, "gelu_tanh": STAR_ACT_GELU_TANH, "gelu_erf": STAR_ACT_GELU_ERF, "silu": STAR_ACT_SILU}
+_DTYPES = {torch.float32: STAR_DTYPE_F32, torch.bfloat16: STAR_DTYPE_BF16}
+
+
+def _matrix(t: torch.Tensor, what: str, shape=None, dtype=None) -> Tuple[int, int, int]:
+    """(address, dtype code, row stride) of a CUDA matrix whose rows are contiguous."""
+    code = _DTYPES.get(t.dtype)
+    if code is None or t.dim() != 2 or not t.is_cuda or (dtype is not None and t.dtype != dtype):
+        raise TypeError("%s must be a 2-D %s CUDA tensor" % (what, "float32 or bfloat16" if dtype is None else dtype))
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError("%s has shape %s, expected %s" % (what, tuple(t.shape), shape))
+    rows, cols = t.shape
+    ld, step = t.stride()
+    if (step != 1 and cols > 1) or (ld < cols and rows > 1):
+        raise TypeError("%s must have contiguous rows that do not overlap" % what)
+    return t.data_ptr(), code, max(ld, cols)
+
+
+def _vector(t: Optional[torch.Tensor], n: int, what: str, dtype=torch.float32) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+        raise TypeError("%s must be a contiguous %s CUDA tensor" % (what, dtype))
+    if t.numel() != n:
+        raise ValueError("%s has %d elements, expected %d" % (what, t.numel(), n))
+    return t.data_ptr()
+
+
+def _act(act) -> int:
+    if act not in _ACTS:
+        raise ValueError("unknown activation %r (one of %s)" % (act, ", ".join(_ACTS)))
+    return _ACTS[act]
+
+
+def star_token_logprobs(logits: torch.Tensor, labels: torch.Tensor, logp: torch.Tensor,
+                        lse: Optional[torch.Tensor] = None, temperature: float = 1.0, stream=None) -> None:
+    """logp (and lse) of every row's label; labels outside [0, vocab) give 0."""
+    rows, vocab = logits.shape
+    x, dtype, ld = _matrix(logits, "logits")
+    _check(_lib.star_token_logprobs(x, dtype, rows, vocab, ld, _vector(labels, rows, "labels", torch.int64),
+                                    temperature, _vector(logp, rows, "logp"), _vector(lse, rows, "lse"),
+                                    _stream(stream)), "star_token_logprobs")
+
+
+def star_loss_workspace_bytes(rows: int, sequences: int = 0) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.star_loss_workspace_bytes(rows, sequences, ctypes.byref(out)), "star_loss_workspace_bytes")
+    return out.value
+
+
+def _workspace(t: torch.Tensor) -> Tuple[int, int]:
+    if not t.is_cuda or not t.is_contiguous():
+        raise TypeError("workspace must be a contiguous CUDA tensor")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def star_policy_loss(logits: torch.Tensor, labels: torch.Tensor, advantages: torch.Tensor, logp: torch.Tensor,
+                     token_loss: torch.Tensor, sums: torch.Tensor, workspace: torch.Tensor,
+                     dlogits: Optional[torch.Tensor] = None, weights: Optional[torch.Tensor] = None,
+                     old_logp: Optional[torch.Tensor] = None, ref_logp: Optional[torch.Tensor] = None,
+                     clip_low: float = 0.2, clip_high: float = 0.2, kl_coef: float = 0.0, temperature: float = 1.0,
+                     stream=None) -> None:
+    """Clipped policy loss with a KL term: logp, token_loss, the four sums and,
+    unless None, the gradient of the logits (which may be the logits)."""
+    rows, vocab = logits.shape
+    x, dtype, ld = _matrix(logits, "logits")
+    d, _, ld_d = (None, dtype, vocab) if dlogits is None else _matrix(dlogits, "dlogits", (rows, vocab), logits.dtype)
+    ws, ws_bytes = _workspace(workspace)
+    _check(_lib.star_policy_loss(x, dtype, rows, vocab, ld, _vector(labels, rows, "labels", torch.int64),
+                                 _vector(weights, rows, "weights"), _vector(advantages, rows, "advantages"),
+                                 _vector(old_logp, rows, "old_logp"), _vector(ref_logp, rows, "ref_logp"), temperature,
+                                 clip_low, clip_high, kl_coef, _vector(logp, rows, "logp"),
+                                 _vector(token_loss, rows, "token_loss"), _vector(sums, 4, "sums"), d, ld_d, ws,
+                                 ws_bytes, _stream(stream)), "star_policy_loss")
+
+
+def star_preference_loss(logits: torch.Tensor, labels: torch.Tensor, seq_offsets: torch.Tensor, seq_logp: torch.Tensor,
+                         pair_loss: torch.Tensor, margin: torch.Tensor, loss: torch.Tensor, workspace: torch.Tensor,
+                         dlogits: Optional[torch.Tensor] = None, ref_logp: Optional[torch.Tensor] = None,
+                         beta: float = 0.1, label_smoothing: float = 0.0, average: bool = False,
+                         loss_scale: float = 1.0, temperature: float = 1.0, stream=None) -> None:
+    """Preference loss of pairs of sequences (chosen, rejected, chosen, ...):
+    sequence log-probabilities, losses, margins, the total and, unless None, the
+    gradient of the logits (which may be the logits)."""
+    rows, vocab = logits.shape
+    pairs = pair_loss.numel()
+    x, dtype, ld = _matrix(logits, "logits")
+    d, _, ld_d = (None, dtype, vocab) if dlogits is None else _matrix(dlogits, "dlogits", (rows, vocab), logits.dtype)
+    ws, ws_bytes = _workspace(workspace)
+    _check(_lib.star_preference_loss(x, dtype, rows, vocab, ld, _vector(labels, rows, "labels", torch.int64),
+                                     _vector(seq_offsets, 2 * pairs + 1, "seq_offsets", torch.int32), pairs,
+                                     _vector(ref_logp, 2 * pairs, "ref_logp"), temperature, beta, label_smoothing,
+                                     int(average), loss_scale, _vector(seq_logp, 2 * pairs, "seq_logp"),
+                                     _vector(pair_loss, pairs, "pair_loss"), _vector(margin, pairs, "margin"),
+                                     _vector(loss, 1, "loss"), d, ld_d, ws, ws_bytes, _stream(stream)),
+           "star_preference_loss")
+
+
+def star_checkpoint_sizes(rows: int, cols: int) -> Tuple[int, int, int]:
+    """(pitch, bytes of codes, bytes of scales) of a checkpoint of rows x cols values."""
+    pitch, code_bytes, scale_bytes = ctypes.c_int64(0), ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(_lib.star_checkpoint_sizes(rows, cols, ctypes.byref(pitch), ctypes.byref(code_bytes), ctypes.byref(scale_bytes)),
+           "star_checkpoint_sizes")
+    return pitch.value, code_bytes.value, scale_bytes.value
+
+
+def star_checkpoint_empty(rows: int, cols: int, device="cuda") -> Tuple[torch.Tensor, torch.Tensor]:
+    """Uninitialized codes (int8, rows x pitch) and scales (uint8, tiles x tall x 4) for rows x cols values."""
+    pitch, _, scale_bytes = star_checkpoint_sizes(rows, cols)
+    tiles = (cols + 127) // 128
+    return (torch.empty((rows, pitch), dtype=torch.int8, device=device),
+            torch.empty((tiles, scale_bytes // (4 * max(tiles, 1)), 4), dtype=torch.uint8, device=device))
+
+
+def _kept(codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int) -> Tuple[int, int]:
+    pitch, tiles, tall = (cols + 15) // 16 * 16, (cols + 127) // 128, (rows + 63) // 64 * 64
+    if codes.dtype != torch.int8 or scales.dtype != torch.uint8 or not codes.is_cuda or not scales.is_cuda \
+            or not codes.is_contiguous() or not scales.is_contiguous():
+        raise TypeError("codes / scales must be contiguous int8 / uint8 CUDA tensors")
+    if codes.numel() != rows * pitch or scales.numel() != tiles * tall * 4:
+        raise ValueError("codes / scales do not have the sizes of a checkpoint of %d x %d values" % (rows, cols))
+    return codes.data_ptr(), scales.data_ptr()
+
+
+def star_checkpoint_pack(codes: torch.Tensor, scales: torch.Tensor, x: torch.Tensor, act: str = "none",
+                         act_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Keep x in 8 bits; with act_out also write act(x) (which may be x)."""
+    rows, cols = x.shape
+    p, dtype, ld = _matrix(x, "x")
+    q, s = _kept(codes, scales, rows, cols)
+    h, _, ld_h = (None, dtype, cols) if act_out is None else _matrix(act_out, "act_out", (rows, cols), x.dtype)
+    _check(_lib.star_checkpoint_pack(q, s, p, dtype, rows, cols, ld, _act(act), h, ld_h, _stream(stream)),
+           "star_checkpoint_pack")
+
+
+def star_checkpoint_unpack(out: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, act: str = "none",
+                           stream=None) -> None:
+    """out = act(kept value)."""
+    rows, cols = out.shape
+    p, dtype, ld = _matrix(out, "out")
+    q, s = _kept(codes, scales, rows, cols)
+    _check(_lib.star_checkpoint_unpack(p, dtype, ld, q, s, rows, cols, _act(act), _stream(stream)),
+           "star_checkpoint_unpack")
+
+
+def star_checkpoint_act_backward(dx: torch.Tensor, dy: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
+                                 act: str, stream=None) -> None:
+    """dx = dy * act'(kept value); dx may be dy."""
+    rows, cols = dy.shape
+    p, dtype, ld = _matrix(dy, "dy")
+    d, _, ld_d = _matrix(dx, "dx", (rows, cols), dy.dtype)
+    q, s = _kept(codes, scales, rows, cols)
+    _check(_lib.star_checkpoint_act_backward(d, ld_d, p, ld, dtype, q, s, rows, cols, _act(act), _stream(stream)),
+           "star_checkpoint_act_backward")
+
+
+def star_checkpoint_weight_grad(dw: torch.Tensor, dy: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
+                                transposed: bool = False, accumulate: bool = False, stream=None) -> None:
+    """dw (outs x cols, or cols x outs if transposed) = or += dy^T times the kept values."""
+    rows, outs = dy.shape
+    w, w_dtype, ld_w = _matrix(dw, "dw")
+    cols = dw.shape[0 if transposed else 1]
+    if dw.shape[1 if transposed else 0] != outs:
+        raise ValueError("dw has shape %s, dy has %d columns" % (tuple(dw.shape), outs))
+    p, dtype, ld = _matrix(dy, "dy")
+    q, s = _kept(codes, scales, rows, cols)
+    _check(_lib.star_checkpoint_weight_grad(w, w_dtype, ld_w, int(transposed), p, dtype, ld, q, s, rows, cols, outs,
+                                            int(accumulate), _stream(stream)), "star_checkpoint_weight_grad")

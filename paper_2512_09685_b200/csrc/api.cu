@@ -8,21 +8,32 @@
 
 #include <cuda_runtime.h>
 
+#include "internal.h"
 #include "kernels.cuh"
 #include "star.h"
 
 namespace {
 
-using namespace star;
-
 thread_local int g_last_cuda_error = 0;
 std::atomic<int64_t> g_launches{0};
+
+}  // namespace
+
+namespace star {
 
 star_status_t cuda_failed(cudaError_t e)
 {
     g_last_cuda_error = static_cast<int>(e);
     return STAR_ERR_CUDA;
 }
+
+void count_launch() { g_launches.fetch_add(1, std::memory_order_relaxed); }
+
+}  // namespace star
+
+namespace {
+
+using namespace star;
 
 constexpr uint64_t kPlanMagic = 0x53544152504c414eull;   // "STARPLAN"
 constexpr size_t kWorkspaceAlign = 256;

@@ -1,0 +1,44 @@
+// Device helpers shared by the operators of a worker's step (sm_100a).
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "kernels.cuh"
+
+namespace star {
+
+// 2^x, 2 ulp; -inf gives 0, NaN stays NaN.
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+constexpr float kLog2e = 1.44269504088896340736f;
+// Element i of a buffer of type G (GradF32 or GradBF16), widened.
+template <typename G> __device__ __forceinline__ float load_value(const void *base, int64_t i)
+{
+    if constexpr (G::kBytes == 2)
+        return __uint_as_float(static_cast<uint32_t>(static_cast<const unsigned short *>(base)[i]) << 16);
+    else
+        return static_cast<const float *>(base)[i];
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+template <typename G> __device__ __forceinline__ void store_value(void *base, int64_t i, float x)
+{
+    if constexpr (G::kBytes == 2)
+        static_cast<unsigned short *>(base)[i] = static_cast<unsigned short>(pack_bf16(x, 0.0f));
+    else
+        static_cast<float *>(base)[i] = x;
+}
+
+}  // namespace star

@@ -1,0 +1,84 @@
+// What the library's source files share: error and launch bookkeeping (defined
+// in api.cu) and the argument checks of operators on matrices with a row stride.
+#pragma once
+
+#include <cstddef>
+#include <cstdint>
+
+#include <cuda_runtime.h>
+
+#include "star.h"
+
+namespace star {
+
+// Notes the error for star_last_cuda_error() and returns STAR_ERR_CUDA.
+star_status_t cuda_failed(cudaError_t e);
+// One more kernel launched (star_launch_count).
+void count_launch();
+
+inline bool is_dtype(int dt) { return dt == STAR_DTYPE_F32 || dt == STAR_DTYPE_BF16; }
+inline int dtype_size(int dt) { return dt == STAR_DTYPE_BF16 ? 2 : 4; }
+
+// A device buffer of an argument list: where it starts and how many bytes of
+// address space it spans.
+struct Extent {
+    uintptr_t begin = 0;
+    uint64_t bytes = 0;
+};
+
+inline bool overlap(const Extent &a, const Extent &b)
+{
+    return a.bytes && b.bytes && a.begin < b.begin + b.bytes && b.begin < a.begin + a.bytes;
+}
+
+inline Extent extent(const void *p, uint64_t bytes)
+{
+    return p ? Extent{reinterpret_cast<uintptr_t>(p), bytes} : Extent{};
+}
+
+// Largest byte count a matrix argument may span: far beyond any device's
+// memory, and small enough that no sum of offsets overflows 64 bits.
+constexpr uint64_t kMaxBytes = uint64_t{1} << 56;
+
+// rows x cols elements of `size` bytes, `ld` elements from row to row.  Checks
+// the pointer's alignment, the stride and the size; *out spans the matrix.
+inline star_status_t check_matrix(const void *p, int64_t rows, int64_t cols, int64_t ld, int size, Extent *out)
+{
+    if (rows < 0 || cols < 0 || ld < cols) return STAR_ERR_INVALID_ARG;
+    *out = Extent{};
+    if (rows == 0 || cols == 0) return STAR_OK;
+    if (!p) return STAR_ERR_NULL_POINTER;
+    if (reinterpret_cast<uintptr_t>(p) % static_cast<unsigned>(size) != 0) return STAR_ERR_INVALID_ARG;
+    if (static_cast<uint64_t>(ld) > kMaxBytes / static_cast<unsigned>(size) ||
+        static_cast<uint64_t>(rows) > kMaxBytes / static_cast<unsigned>(size) / static_cast<uint64_t>(ld))
+        return STAR_ERR_INVALID_ARG;
+    *out = extent(p, (static_cast<uint64_t>(rows - 1) * static_cast<uint64_t>(ld) + static_cast<uint64_t>(cols)) *
+                         static_cast<unsigned>(size));
+    return STAR_OK;
+}
+
+// A vector of n elements; optional ones may be NULL.
+inline star_status_t check_vector(const void *p, int64_t n, int size, bool optional, Extent *out)
+{
+    *out = Extent{};
+    if (!p && optional) return STAR_OK;
+    return check_matrix(p, 1, n, n, size, out);
+}
+
+// Whether a written buffer shares memory with any of the others.
+inline bool overlaps_any(const Extent &written, const Extent *others, int n)
+{
+    for (int i = 0; i < n; ++i)
+        if (overlap(written, others[i])) return true;
+    return false;
+}
+
+inline int sm_count(int *out)
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(out, cudaDevAttrMultiProcessorCount, dev);
+    return static_cast<int>(e);
+}
+
+}  // namespace star
