@@ -16,8 +16,9 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libstar.so")
-SOURCES = ["api.cu", "losses.cu", "checkpoint.cu", "schedule.cc", "mode_decision.cc"]
-HEADERS = [os.path.join(CSRC, h) for h in ("internal.h", "kernels.cuh", "device.cuh", "losses.cuh", "checkpoint.cuh")]
+SOURCES = ["api.cu", "losses.cu", "checkpoint.cu", "weight_grad.cu", "schedule.cc", "mode_decision.cc"]
+HEADERS = [os.path.join(CSRC, h) for h in ("internal.h", "kernels.cuh", "device.cuh", "losses.cuh", "checkpoint.cuh",
+                                           "checkpoint_host.h", "weight_grad.cuh")]
 HEADERS.append(os.path.join(ROOT, "include", "star.h"))
 
 NVCC_FLAGS = [

@@ -3,37 +3,11 @@
 #include <type_traits>
 
 #include "checkpoint.cuh"
-#include "internal.h"
+#include "checkpoint_host.h"
 
 namespace {
 
 using namespace star;
-
-star_status_t launched()
-{
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return cuda_failed(e);
-    count_launch();
-    return STAR_OK;
-}
-
-// Checks a checkpoint's buffers; *codes and *scales span them.
-star_status_t check_kept(const int8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, Kept *out, Extent *at)
-{
-    size_t code_bytes = 0, scale_bytes = 0;
-    int64_t pitch = 0;
-    const star_status_t st = star_checkpoint_sizes(rows, cols, &pitch, &code_bytes, &scale_bytes);
-    if (st != STAR_OK) return st;
-    at[0] = at[1] = Extent{};
-    *out = Kept{const_cast<int8_t *>(codes), const_cast<uint8_t *>(scales), rows, cols, pitch, (rows + 63) / 64 * 64};
-    if (code_bytes == 0) return STAR_OK;
-    if (!codes || !scales) return STAR_ERR_NULL_POINTER;
-    if (reinterpret_cast<uintptr_t>(codes) % 16 != 0 || reinterpret_cast<uintptr_t>(scales) % 16 != 0)
-        return STAR_ERR_INVALID_ARG;
-    at[0] = extent(codes, code_bytes);
-    at[1] = extent(scales, scale_bytes);
-    return overlap(at[0], at[1]) ? STAR_ERR_INVALID_ARG : STAR_OK;
-}
 
 bool is_act(int act) { return act >= STAR_ACT_NONE && act <= STAR_ACT_SILU; }
 
@@ -150,41 +124,4 @@ extern "C" star_status_t star_checkpoint_act_backward(void *dx, int64_t ld_dx, c
     a.dy = dy;
     a.ld_dy = ld_dy;
     return read_kept<true>(a, dtype, act, cuda_stream);
-}
-
-extern "C" star_status_t star_checkpoint_weight_grad(void *dw, star_dtype_t dw_dtype, int64_t ld_dw, int transposed,
-                                                     const void *dy, star_dtype_t dy_dtype, int64_t ld_dy,
-                                                     const int8_t *codes, const uint8_t *scales, int64_t rows,
-                                                     int64_t cols, int64_t outs, int accumulate, void *cuda_stream)
-{
-    if (!is_dtype(dw_dtype) || !is_dtype(dy_dtype) || outs < 0) return STAR_ERR_INVALID_ARG;
-    WeightGradArgs a{};
-    Extent read[3], written;
-    star_status_t st = check_kept(codes, scales, rows, cols, &a.kept, read);
-    if (st == STAR_OK) st = check_matrix(dy, rows, outs, ld_dy, dtype_size(dy_dtype), &read[2]);
-    if (st == STAR_OK)
-        st = check_matrix(dw, transposed ? cols : outs, transposed ? outs : cols, ld_dw, dtype_size(dw_dtype), &written);
-    if (st == STAR_OK && overlaps_any(written, read, 3)) st = STAR_ERR_INVALID_ARG;
-    if (st != STAR_OK || cols == 0 || outs == 0 || (rows == 0 && accumulate)) return st;
-    a.dy = dy;
-    a.ld_dy = ld_dy;
-    a.dw = dw;
-    a.stride_o = transposed ? 1 : ld_dw;
-    a.stride_c = transposed ? ld_dw : 1;
-    a.outs = outs;
-    a.accumulate = accumulate;
-    const int64_t across = (cols + 31) / 32, down = (outs + 31) / 32;
-    if (across > 0x7fffffff) return STAR_ERR_UNSUPPORTED;
-    const dim3 grid(static_cast<unsigned>(across), static_cast<unsigned>(down < 65535 ? down : 65535));
-    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    const bool y16 = dy_dtype == STAR_DTYPE_BF16, w16 = dw_dtype == STAR_DTYPE_BF16;
-    if (y16 && w16)
-        star_weight_grad_kernel<GradBF16, GradBF16><<<grid, 256, 0, stream>>>(a);
-    else if (y16)
-        star_weight_grad_kernel<GradBF16, GradF32><<<grid, 256, 0, stream>>>(a);
-    else if (w16)
-        star_weight_grad_kernel<GradF32, GradBF16><<<grid, 256, 0, stream>>>(a);
-    else
-        star_weight_grad_kernel<GradF32, GradF32><<<grid, 256, 0, stream>>>(a);
-    return launched();
 }

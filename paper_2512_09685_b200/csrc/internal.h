@@ -16,6 +16,15 @@ star_status_t cuda_failed(cudaError_t e);
 // One more kernel launched (star_launch_count).
 void count_launch();
 
+// The status of the launch just made.
+inline star_status_t launched()
+{
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_failed(e);
+    count_launch();
+    return STAR_OK;
+}
+
 inline bool is_dtype(int dt) { return dt == STAR_DTYPE_F32 || dt == STAR_DTYPE_BF16; }
 inline int dtype_size(int dt) { return dt == STAR_DTYPE_BF16 ? 2 : 4; }
 
@@ -71,14 +80,6 @@ inline bool overlaps_any(const Extent &written, const Extent *others, int n)
     for (int i = 0; i < n; ++i)
         if (overlap(written, others[i])) return true;
     return false;
-}
-
-inline int sm_count(int *out)
-{
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(out, cudaDevAttrMultiProcessorCount, dev);
-    return static_cast<int>(e);
 }
 
 }  // namespace star

@@ -12,14 +12,6 @@ using namespace star;
 // Blocks of a grid over `rows` rows (every kernel strides over the rest).
 int row_grid(int64_t rows) { return static_cast<int>(rows < 148 * 64 ? rows : 148 * 64); }
 
-star_status_t launched()
-{
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return cuda_failed(e);
-    count_launch();
-    return STAR_OK;
-}
-
 // The checks that the three operators share.  read[0] is the logits' extent.
 star_status_t check_rows(const void *logits, star_dtype_t dtype, int64_t rows, int64_t vocab, int64_t ld,
                          const int64_t *labels, float temperature, RowArgs *out, Extent *read)
