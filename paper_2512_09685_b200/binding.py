@@ -343,8 +343,9 @@ def _state(t: torch.Tensor, what: str) -> int:
 
 
 def _stream(stream) -> int:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    if stream is None:                                  # the current stream's handle, without a Stream object around it
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream
 
 
 def star_group_update(params: torch.Tensor, momentum: torch.Tensor,

@@ -46,47 +46,137 @@ bool make_map(CUtensorMap *map, CUtensorMapDataType type, const void *base, int6
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int BN, int STAGES>
-star_status_t launch_tensor(const WeightGradTile &tile, const CUtensorMap &codes, const CUtensorMap &dy, bool dw_bf16, int parts,
-                            cudaStream_t stream)
+// The kernel comes in three shapes.  Shared memory and TMEM hold one block on an
+// SM in all of them.
+//   kWide   a pair of blocks, 256 columns x 512 outputs: a widened code serves 512
+//           outputs, 0.73 us a step of 64 rows (1.47 PFLOP/s over 148 SMs)
+//   kNarrow a pair, 256 x 256: 0.56 us, bound by the widening
+//   kSingle a block, 128 x 256: 0.56 us
+enum Shape { kWide = 0, kNarrow = 1, kSingle = 2, kShapes = 3 };
+constexpr int kMostParts = 8;
+
+template <int SHAPE> struct ShapeOf;
+template <> struct ShapeOf<kWide> {
+    static constexpr int kOuts = 512, kBlocks = 2;
+    using Smem = GradSmem<512, 4, 3, true>;
+    static constexpr auto kernel() { return star_weight_grad_tensor_kernel<512, 4, 3, true>; }
+};
+template <> struct ShapeOf<kNarrow> {
+    static constexpr int kOuts = 256, kBlocks = 2;
+    using Smem = GradSmem<256, 7, 3, true>;
+    static constexpr auto kernel() { return star_weight_grad_tensor_kernel<256, 7, 3, true>; }
+};
+template <> struct ShapeOf<kSingle> {
+    static constexpr int kOuts = 256, kBlocks = 1;
+    using Smem = GradSmem<256, 4, 3, false>;
+    static constexpr auto kernel() { return star_weight_grad_tensor_kernel<256, 4, 3, false>; }
+};
+
+void fill_config(cudaLaunchConfig_t *config, cudaLaunchAttribute *attribute, int64_t columns, int64_t down, int blocks, int parts,
+                 int smem, cudaStream_t stream)
 {
-    const auto kernel = star_weight_grad_tensor_kernel<BN, STAGES>;
-    constexpr int smem = GradSmem<BN, STAGES>::kDynamic;
-    static std::atomic<bool> ready[kMaxDevices];
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return cuda_failed(e);
-    if (dev >= kMaxDevices) return STAR_ERR_UNSUPPORTED;
-    if (!ready[dev].load(std::memory_order_acquire)) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        if (e != cudaSuccess) return cuda_failed(e);
-        ready[dev].store(true, std::memory_order_release);
-    }
-    cudaLaunchConfig_t config{};
-    config.gridDim = dim3(static_cast<unsigned>((tile.a.kept.cols + kTileC - 1) / kTileC), static_cast<unsigned>((tile.a.outs + BN - 1) / BN),
-                          static_cast<unsigned>(parts));
-    config.blockDim = dim3(kGradThreads);
-    config.dynamicSmemBytes = smem;
-    config.stream = stream;
-    cudaLaunchAttribute attribute{};
-    attribute.id = cudaLaunchAttributeClusterDimension;
-    attribute.val.clusterDim.x = 1;
-    attribute.val.clusterDim.y = 1;
-    attribute.val.clusterDim.z = static_cast<unsigned>(parts);
-    config.attrs = &attribute;
-    config.numAttrs = 1;
-    e = cudaLaunchKernelEx(&config, kernel, tile, codes, dy, static_cast<int>(dw_bf16));
-    if (e != cudaSuccess) return cuda_failed(e);
-    return launched();
+    *config = cudaLaunchConfig_t{};
+    config->gridDim = dim3(static_cast<unsigned>(columns * blocks), static_cast<unsigned>(down), static_cast<unsigned>(parts));
+    config->blockDim = dim3(kGradThreads);
+    config->dynamicSmemBytes = static_cast<size_t>(smem);
+    config->stream = stream;
+    *attribute = cudaLaunchAttribute{};
+    attribute->id = cudaLaunchAttributeClusterDimension;
+    attribute->val.clusterDim.x = static_cast<unsigned>(blocks);
+    attribute->val.clusterDim.y = 1;
+    attribute->val.clusterDim.z = static_cast<unsigned>(parts);
+    config->attrs = attribute;
+    config->numAttrs = 1;
 }
 
-// Into how many parts the rows are split: enough blocks for the device, but at
-// least 4 steps each.
-int row_parts(int64_t tiles, int64_t steps)
+// Per device and shape: how many clusters of `parts` tiles the device holds at
+// once (GPUs of one kind differ: their SMs come in groups of uneven size, and a
+// cluster stays within a group).  0: not asked yet.
+struct Device {
+    std::atomic<int> clusters[kShapes][kMostParts + 1];
+    std::atomic<bool> ready{false};
+};
+Device g_devices[kMaxDevices];
+
+template <int SHAPE> cudaError_t prepare_shape(Device &d)
 {
-    int parts = 1;
-    while (parts < 8 && tiles * parts * 2 <= 148 && steps >= 4 * parts * 2) parts *= 2;
-    return parts;
+    using S = ShapeOf<SHAPE>;
+    const auto kernel = S::kernel();
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::Smem::kDynamic);
+    for (int parts = 1; e == cudaSuccess && parts * S::kBlocks <= 8; ++parts) {
+        cudaLaunchConfig_t config;
+        cudaLaunchAttribute attribute;
+        fill_config(&config, &attribute, 64, 1, S::kBlocks, parts, S::Smem::kDynamic, nullptr);
+        int n = 0;
+        e = cudaOccupancyMaxActiveClusters(&n, kernel, &config);
+        d.clusters[SHAPE][parts].store(n, std::memory_order_relaxed);
+    }
+    return e;
+}
+
+cudaError_t prepared_device(Device **out)
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+    Device &d = g_devices[dev];
+    if (!d.ready.load(std::memory_order_acquire)) {
+        e = prepare_shape<kWide>(d);
+        if (e == cudaSuccess) e = prepare_shape<kNarrow>(d);
+        if (e == cudaSuccess) e = prepare_shape<kSingle>(d);
+        if (e != cudaSuccess) return e;
+        d.ready.store(true, std::memory_order_release);
+    }
+    *out = &d;
+    return cudaSuccess;
+}
+
+template <int SHAPE>
+star_status_t launch_shape(const WeightGradTile &tile, const CUtensorMap &codes, const CUtensorMap &dy, bool dw_bf16, int parts,
+                           cudaStream_t stream)
+{
+    using S = ShapeOf<SHAPE>;
+    cudaLaunchConfig_t config;
+    cudaLaunchAttribute attribute;
+    constexpr int64_t columns = S::kBlocks * kTileC;
+    fill_config(&config, &attribute, (tile.a.kept.cols + columns - 1) / columns, (tile.a.outs + S::kOuts - 1) / S::kOuts, S::kBlocks,
+                parts, S::Smem::kDynamic, stream);
+    const cudaError_t e = cudaLaunchKernelEx(&config, S::kernel(), tile, codes, dy, static_cast<int>(dw_bf16));
+    return e == cudaSuccess ? launched() : cuda_failed(e);
+}
+
+// Shape and number of parts with the least expected time: the waves of tiles the
+// device needs, each the steps of one part and what a tile costs beside them.
+// Measured (us; 8 to 256 steps, 128 to 4096 columns): a step takes 0.73 / 0.56 /
+// 0.56, the rest 5 and, split, 17 / 12 / 12 (accumulators through distributed
+// shared memory).  16384 rows, 1024 -> 4096: kWide in 2 parts 114 us, in 1 part
+// 191, kNarrow 150, kSingle 148.  8192 rows, 1024 -> 1024: kSingle in 4 parts 31
+// us, in 1 part 77, kWide in 4 parts 41.
+struct Plan {
+    Shape shape;
+    int parts;
+};
+
+Plan choose(const Device &d, int64_t cols, int64_t outs, int64_t steps)
+{
+    constexpr double step_us[kShapes] = {0.73, 0.56, 0.56}, split_us[kShapes] = {17.0, 12.0, 12.0};
+    Plan best{kSingle, 1};
+    double least = -1.0;
+    for (int shape = kWide; shape < kShapes; ++shape) {
+        const int blocks = shape == kSingle ? 1 : 2, outs_tile = shape == kWide ? 512 : 256;
+        const int64_t tiles = ((cols + blocks * kTileC - 1) / (blocks * kTileC)) * ((outs + outs_tile - 1) / outs_tile);
+        for (int parts = 1; parts * blocks <= 8 && parts <= steps; ++parts) {
+            const int held = std::max(d.clusters[shape][parts].load(std::memory_order_relaxed), 1);
+            const double waves = static_cast<double>((tiles + held - 1) / held);
+            const double cost = waves * (static_cast<double>((steps + parts - 1) / parts) * step_us[shape] + (parts > 1 ? split_us[shape] : 5.0));
+            if (least < 0.0 || cost < least) {
+                least = cost;
+                best = Plan{static_cast<Shape>(shape), parts};
+            }
+        }
+    }
+    return best;
 }
 
 }  // namespace
@@ -112,14 +202,11 @@ extern "C" star_status_t star_checkpoint_weight_grad(void *dw, star_dtype_t dw_d
     a.stride_c = transposed ? ld_dw : 1;
     a.outs = outs;
     a.accumulate = accumulate;
-    const int64_t across = (cols + 31) / 32, down = (outs + 31) / 32;
-    if (across > 0x7fffffff) return STAR_ERR_UNSUPPORTED;
-    const dim3 grid(static_cast<unsigned>(across), static_cast<unsigned>(down < 65535 ? down : 65535));
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const bool y16 = dy_dtype == STAR_DTYPE_BF16, w16 = dw_dtype == STAR_DTYPE_BF16;
     // The TMA reads dy in place: 16-byte aligned rows, coordinates of 32 bits.
     const bool tiled = y16 && rows > 0 && reinterpret_cast<uintptr_t>(dy) % 16 == 0 && ld_dy % 8 == 0 && rows < 0x7fffff00 &&
-                       cols < 0x7fffff00 && outs < 0x7fffff00 && (outs + 255) / 256 <= 65535;
+                       cols < 0x7fffff00 && outs < 0x7fffff00 && (outs + kTileO - 1) / kTileO <= 65535;
     if (tiled) {
         CUtensorMap codes_map, dy_map;
         if (!make_map(&codes_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, a.kept.pitch, rows, static_cast<uint64_t>(a.kept.pitch), kTileC,
@@ -129,9 +216,19 @@ extern "C" star_status_t star_checkpoint_weight_grad(void *dw, star_dtype_t dw_d
             return cuda_failed(cudaErrorInvalidValue);
         const int64_t steps = (rows + kTileT - 1) / kTileT;
         const WeightGradTile tile{a, static_cast<int>(steps)};
-        const int64_t tiles = ((cols + kTileC - 1) / kTileC) * ((outs + 255) / 256);
-        return launch_tensor<256, 4>(tile, codes_map, dy_map, w16, row_parts(tiles, steps), stream);
+        Device *device = nullptr;
+        const cudaError_t e = prepared_device(&device);
+        if (e != cudaSuccess) return cuda_failed(e);
+        const Plan plan = choose(*device, cols, outs, steps);
+        switch (plan.shape) {
+        case kWide: return launch_shape<kWide>(tile, codes_map, dy_map, w16, plan.parts, stream);
+        case kNarrow: return launch_shape<kNarrow>(tile, codes_map, dy_map, w16, plan.parts, stream);
+        default: return launch_shape<kSingle>(tile, codes_map, dy_map, w16, plan.parts, stream);
+        }
     }
+    const int64_t across = (cols + 31) / 32, down = (outs + 31) / 32;
+    if (across > 0x7fffffff) return STAR_ERR_UNSUPPORTED;
+    const dim3 grid(static_cast<unsigned>(across), static_cast<unsigned>(down < 65535 ? down : 65535));
     if (y16 && w16)
         star_weight_grad_kernel<GradBF16, GradBF16><<<grid, 256, 0, stream>>>(a);
     else if (y16)

@@ -24,7 +24,10 @@ namespace star {
 
 constexpr int kTileC = 128;          // columns (M of the matrix instruction)
 constexpr int kTileT = 64;           // rows per step
-constexpr int kConvertWarps = 8;
+constexpr int kTileO = 256;          // most outputs (N) of one matrix instruction
+constexpr int kGroups = 2;           // groups of converting warps, taking the steps in turn
+constexpr int kGroupWarps = 8;
+constexpr int kConvertWarps = kGroups * kGroupWarps;
 constexpr int kFirstConvert = 4;     // warps 0: TMA, 1: matrix instructions, 2: TMEM, 3: idle
 constexpr int kGradThreads = 32 * (kFirstConvert + kConvertWarps);
 
@@ -34,10 +37,10 @@ struct WeightGradTile {
 };
 
 // ---------------------------------------------------------------------------
-// Barriers in shared memory.  Every wait ends: after kWaitNs it reports failure,
+// Barriers in shared memory.  Every wait ends: after kWaitCycles it reports failure,
 // the block stops issuing, drains its copies, and leaves without a result.
 // ---------------------------------------------------------------------------
-constexpr uint64_t kWaitNs = 4000000000ull;
+constexpr long long kWaitCycles = 4000000000ll;      // two seconds and more
 __device__ int g_wait_expired;       // set by a block that gave up waiting
 
 __device__ __forceinline__ uint32_t smem_address(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
@@ -50,9 +53,10 @@ __device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
 }
+// `bar` is a barrier of any block of the cluster.
 __device__ __forceinline__ void barrier_arrive(uint32_t bar)
 {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
 }
 __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity)
 {
@@ -62,16 +66,10 @@ __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity)
                  "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
-__device__ __forceinline__ uint64_t now_ns()
-{
-    uint64_t t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
-}
 __device__ __noinline__ bool barrier_wait_long(uint32_t bar, uint32_t parity)
 {
-    const uint64_t start = now_ns();
-    while (now_ns() - start < kWaitNs)
+    const long long start = clock64();
+    while (clock64() - start < kWaitCycles)
         for (int i = 0; i < 64; ++i)
             if (barrier_try(bar, parity)) return true;
     atomicExch(&g_wait_expired, 1);
@@ -79,7 +77,7 @@ __device__ __noinline__ bool barrier_wait_long(uint32_t bar, uint32_t parity)
 }
 __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity)
 {
-    for (int i = 0; i < 32; ++i)
+    for (int i = 0; i < 16; ++i)
         if (barrier_try(bar, parity)) return true;
     return barrier_wait_long(bar, parity);
 }
@@ -107,23 +105,53 @@ __device__ __forceinline__ uint64_t operand_descriptor(uint32_t address)
     return static_cast<uint64_t>((address >> 4) & 0x3fff) | leading << 16 | stride << 32 | uint64_t{1} << 46 | uint64_t{2} << 61;
 }
 
-// bf16 x bf16 -> fp32, both operands MN-major, M = 128.
-template <int BN> __device__ __forceinline__ constexpr uint32_t instruction_descriptor()
+// bf16 x bf16 -> fp32, both operands MN-major.  M = 128, or 256 over a pair of blocks.
+template <bool PAIR> __device__ __forceinline__ constexpr uint32_t instruction_descriptor()
 {
-    return 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | static_cast<uint32_t>(BN / 8) << 17 | static_cast<uint32_t>(kTileC / 16) << 24;
+    return 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | static_cast<uint32_t>(kTileO / 8) << 17 |
+           static_cast<uint32_t>((PAIR ? 2 : 1) * kTileC / 16) << 24;
 }
 
-__device__ __forceinline__ void matrix_multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate)
+template <bool PAIR> __device__ __forceinline__ void matrix_multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate)
 {
-    asm volatile("{\n\t.reg .pred p;\n\t"
-                 "setp.ne.u32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(accumulate)) : "memory");
+    if constexpr (PAIR)
+        asm volatile("{\n\t.reg .pred p;\n\t"
+                     "setp.ne.u32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(accumulate)) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\t"
+                     "setp.ne.u32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(accumulate)) : "memory");
 }
-// The barrier's phase advances once every matrix instruction issued so far is done.
-__device__ __forceinline__ void matrix_commit(uint32_t bar)
+// The barrier's phase advances once every matrix instruction issued so far is
+// done; in a pair, that of the barrier at the same place in both blocks (mask).
+template <bool PAIR> __device__ __forceinline__ void matrix_commit(uint32_t bar, uint32_t mask)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+    if constexpr (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     :: "r"(bar), "h"(static_cast<uint16_t>(mask)) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+// Accumulator memory of BN columns; whole warps, both blocks of a pair.
+template <int BN, bool PAIR> __device__ __forceinline__ void tensor_alloc(uint32_t at)
+{
+    if constexpr (PAIR) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(at), "n"(BN) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(at), "n"(BN) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+}
+template <int BN, bool PAIR> __device__ __forceinline__ void tensor_free(uint32_t tmem)
+{
+    if constexpr (PAIR)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmem), "n"(BN));
+    else
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "n"(BN));
 }
 __device__ __forceinline__ void tensor_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tensor_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -155,12 +183,11 @@ __device__ __forceinline__ void load_accumulator(uint32_t address, float (&out)[
 // Widening.  With u = code + 128 in 0 .. 255, the float with bits 0x4b0000uu is
 // 2^23 + u; fma(that, 2^e, -(2^23 + 128) 2^e) = code * 2^e, exact, and exact in
 // bf16: its upper half.  A byte permutation, an fma per code and half a
-// permutation to pack: 2.5 instructions a code.
+// permutation to pack: 2.75 instructions a code.
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ uint2 widen_codes(uint32_t four, float scale)
+__device__ __forceinline__ uint2 widen_codes(uint32_t four, float scale, float off)
 {
     const uint32_t u = four ^ 0x80808080u;
-    const float off = __fmul_rn(scale, -8388736.0f);
     float f[4];
     f[0] = __fmaf_rn(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7650)), scale, off);
     f[1] = __fmaf_rn(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7651)), scale, off);
@@ -169,20 +196,32 @@ __device__ __forceinline__ uint2 widen_codes(uint32_t four, float scale)
     return make_uint2(__byte_perm(__float_as_uint(f[0]), __float_as_uint(f[1]), 0x7632),
                       __byte_perm(__float_as_uint(f[2]), __float_as_uint(f[3]), 0x7632));
 }
+__device__ __forceinline__ uint4 widen_codes(uint2 eight, float scale, float off)
+{
+    const uint2 a = widen_codes(eight.x, scale, off), b = widen_codes(eight.y, scale, off);
+    return make_uint4(a.x, a.y, b.x, b.y);
+}
 
-// Shared memory of a block, from a 1024-byte aligned base.
-template <int BN, int STAGES> struct GradSmem {
+// Shared memory of a block, from a 1024-byte aligned base: a ring of LOADS steps
+// as they are fetched (codes, scale bytes, dy), and a shorter one of WIDE steps
+// of the widened operand.  A step's copies take a microsecond or more under load
+// and its products a quarter of one, so the first ring has to be deep.
+template <int BN, int LOADS, int WIDE, bool PAIR> struct GradSmem {
+    static_assert(BN % kTileO == 0, "whole instructions");
+    static constexpr int kOuts = PAIR ? BN / 2 : BN;             // outputs whose dy this block holds
+    static constexpr int kRun = PAIR ? kTileO / 2 : kTileO;      // of them, side by side: this block's share of one instruction
     static constexpr int kA = kTileC * kTileT * 2;
-    static constexpr int kB = BN * kTileT * 2;
+    static constexpr int kB = kOuts * kTileT * 2;
     static constexpr int kRaw = kTileC * kTileT;
     static constexpr int kScale = kTileT * 4;
-    static constexpr int kOffB = STAGES * kA;
-    static constexpr int kOffRaw = kOffB + STAGES * kB;
-    static constexpr int kOffScale = kOffRaw + STAGES * kRaw;
-    static constexpr int kOffBarrier = kOffScale + STAGES * kScale;
+    static constexpr int kOffB = WIDE * kA;
+    static constexpr int kOffRaw = kOffB + LOADS * kB;
+    static constexpr int kOffScale = kOffRaw + LOADS * kRaw;
+    static constexpr int kOffBarrier = kOffScale + LOADS * kScale;
     static constexpr int kBytes = kOffBarrier + 256;
     static constexpr int kDynamic = kBytes + 1024;               // room to align the base
-    static_assert(kTileC * BN * 4 <= kOffBarrier, "the accumulators of a split tile reuse the stages");
+    static_assert(WIDE <= LOADS && 8 * (2 * LOADS + WIDE + 2) <= 256, "barriers");
+    static_assert(kTileC * kTileO * 4 <= kOffBarrier, "the accumulators of a split tile reuse the rings");
     static_assert(kDynamic <= 232448, "more shared memory than a block may have");
 };
 
@@ -202,11 +241,33 @@ __device__ __forceinline__ uint32_t peer_address(uint32_t address, uint32_t rank
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(address), "r"(rank));
     return r;
 }
-__device__ __forceinline__ float peer_load(uint32_t address)
+__device__ __forceinline__ float4 peer_load(uint32_t address)
 {
-    float x;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(address) : "memory");
+    float4 x;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(address));
     return x;
+}
+
+// The sums of a split tile: part `part` adds its share of the columns over the
+// parts' accumulators (in their shared memory, [kTileO][kTileC]), in the order of
+// the parts, all loads of a sum in flight together.
+template <int PARTS, typename Store>
+__device__ __forceinline__ void join_parts(uint32_t sums, int part, uint32_t of_pair, uint32_t blocks, Store store)
+{
+    const int first = kTileO * part / PARTS, last = kTileO * (part + 1) / PARTS;
+    for (int i = first * (kTileC / 4) + threadIdx.x; i < last * (kTileC / 4); i += kGradThreads) {
+        float4 x[PARTS];
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) x[q] = peer_load(peer_address(sums + static_cast<uint32_t>(i) * 16, of_pair + blocks * q));
+#pragma unroll
+        for (int q = 1; q < PARTS; ++q) {
+            x[0].x = __fadd_rn(x[0].x, x[q].x);
+            x[0].y = __fadd_rn(x[0].y, x[q].y);
+            x[0].z = __fadd_rn(x[0].z, x[q].z);
+            x[0].w = __fadd_rn(x[0].w, x[q].w);
+        }
+        store(i / (kTileC / 4), i % (kTileC / 4) * 4, x[0]);
+    }
 }
 
 __device__ __forceinline__ void store_weight(const WeightGradArgs &a, bool bf16, int64_t o, int64_t c, float x)
@@ -221,40 +282,52 @@ __device__ __forceinline__ void store_weight(const WeightGradArgs &a, bool bf16,
     }
 }
 
-// grid: (column tiles, output tiles, parts of the rows); cluster: (1, 1, parts).
-template <int BN, int STAGES>
+// grid: (column tiles, output tiles, parts of the rows); cluster: (1 or 2, 1, parts).
+//
+// PAIR: two blocks with neighbouring column tiles work as one (cta_group::2).
+// Each widens its own 128 columns and fetches half of the dy tile; the matrix
+// instructions, issued by the first of the two, read both halves from both
+// blocks.  One block alone is bound by its shared memory: per step of 64 rows
+// the matrix instructions read 48 KB, the copies write 40 KB and the widening
+// moves 24 KB, 112 KB where 128 B a cycle give 64 KB in the 512 cycles of the
+// products.  In a pair that is 80 KB.
+template <int BN, int LOADS, int WIDE, bool PAIR>
 __global__ void __launch_bounds__(kGradThreads, 1)
 star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const __grid_constant__ CUtensorMap codes_map,
                                const __grid_constant__ CUtensorMap dy_map, int dw_bf16)
 {
-    using S = GradSmem<BN, STAGES>;
+    using S = GradSmem<BN, LOADS, WIDE, PAIR>;
+    constexpr int kShare = BN / (kConvertWarps / 4);             // accumulator columns a converting warp reads at the end
+    static_assert(kShare % 32 == 0, "whole loads");
+    constexpr uint32_t kBlocks = PAIR ? 2 : 1;
     extern __shared__ uint8_t dynamic[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~uintptr_t{1023});
     const uint32_t base = smem_address(smem);
     const uint32_t bars = base + S::kOffBarrier;
-    const auto loaded = [&](int s) { return bars + 8 * s; };                     // the step's copies have landed
-    const auto widened = [&](int s) { return bars + 8 * (STAGES + s); };         // its A operand is written
-    const auto used = [&](int s) { return bars + 8 * (2 * STAGES + s); };        // its matrix instructions are done
-    const uint32_t finished = bars + 8 * (3 * STAGES);
-    uint32_t *tmem_at = reinterpret_cast<uint32_t *>(smem + S::kOffBarrier + 8 * (3 * STAGES + 1));
+    const auto loaded = [&](int i) { return bars + 8 * (i % LOADS); };                       // step i's copies have landed
+    const auto used = [&](int i) { return bars + 8 * (LOADS + i % LOADS); };                 // its matrix instructions are done
+    const auto widened = [&](int i) { return bars + 8 * (2 * LOADS + i % WIDE); };           // its A operand is written (in both blocks)
+    const auto load_phase = [](int i) { return static_cast<uint32_t>(i / LOADS) & 1; };
+    const auto wide_phase = [](int i) { return static_cast<uint32_t>(i / WIDE) & 1; };
+    const uint32_t finished = bars + 8 * (2 * LOADS + WIDE);
+    uint32_t *tmem_at = reinterpret_cast<uint32_t *>(smem + S::kOffBarrier + 8 * (2 * LOADS + WIDE + 1));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t rank = cluster_rank(), of_pair = rank % kBlocks, leader = rank - of_pair;
+    const uint32_t mask = 3u << leader;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < STAGES; ++s) {
-            barrier_init(loaded(s), 1);
-            barrier_init(widened(s), kConvertWarps);
-            barrier_init(used(s), 1);
+        for (int i = 0; i < LOADS; ++i) {
+            barrier_init(loaded(i), 1);
+            barrier_init(used(i), 1);
         }
+        for (int i = 0; i < WIDE; ++i) barrier_init(widened(i), kBlocks * kGroupWarps);
         barrier_init(finished, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 2) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                     :: "r"(smem_address(tmem_at)), "n"(BN) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-    }
+    if (warp == 2) tensor_alloc<BN, PAIR>(smem_address(tmem_at));
     tensor_fence_before();
     __syncthreads();
+    if constexpr (PAIR) cluster_sync();                          // the other block's barriers are ready
     tensor_fence_after();
     const uint32_t tmem = *tmem_at;
 
@@ -266,65 +339,77 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
 
     if (warp == 0) {
         if (lane == 0) {
+            // The second block of a pair may lie past the last column tile: its
+            // codes read as zero, its scales are those of the last tile.
+            const int64_t scale_tile = min(static_cast<int64_t>(blockIdx.x), (p.a.kept.cols - 1) / kTileC);
+            const uint8_t *scales = p.a.kept.scales + scale_tile * p.a.kept.tall * 4;
+            const int outs0 = static_cast<int>(o0) + static_cast<int>(of_pair) * S::kRun;
             int issued = 0;
             for (int k = first; k < last; ++k) {
-                const int i = k - first, s = i % STAGES;
-                if (i >= STAGES && !barrier_wait(used(s), (i / STAGES - 1) & 1)) break;
-                barrier_expect(loaded(s), S::kRaw + S::kScale + S::kB);
+                const int i = k - first, s = i % LOADS;
+                if (i >= LOADS && !barrier_wait(used(i - LOADS), load_phase(i - LOADS))) break;
+                barrier_expect(loaded(i), S::kRaw + S::kScale + S::kB);
                 const int t = k * kTileT;
-                tma_load_2d(base + S::kOffRaw + s * S::kRaw, &codes_map, static_cast<int>(c0), t, loaded(s));
-                bulk_load(base + S::kOffScale + s * S::kScale, p.a.kept.scales + (blockIdx.x * p.a.kept.tall + t) * 4, S::kScale, loaded(s));
+                tma_load_2d(base + S::kOffRaw + s * S::kRaw, &codes_map, static_cast<int>(c0), t, loaded(i));
+                bulk_load(base + S::kOffScale + s * S::kScale, scales + static_cast<int64_t>(t) * 4, S::kScale, loaded(i));
 #pragma unroll
-                for (int q = 0; q < BN / 64; ++q)
-                    tma_load_2d(base + S::kOffB + s * S::kB + q * (kTileT * 128), &dy_map, static_cast<int>(o0) + 64 * q, t, loaded(s));
+                for (int q = 0; q < S::kOuts / 64; ++q)
+                    tma_load_2d(base + S::kOffB + s * S::kB + q * (kTileT * 128), &dy_map, outs0 + 64 * q / S::kRun * kTileO + 64 * q % S::kRun, t,
+                                loaded(i));
                 issued = i + 1;
             }
             // Copies still in flight land before the block goes on (they have, unless a wait ran out).
-            for (int i = issued > STAGES ? issued - STAGES : 0; i < issued; ++i) barrier_wait(loaded(i % STAGES), (i / STAGES) & 1);
+            for (int i = issued > LOADS ? issued - LOADS : 0; i < issued; ++i) barrier_wait(loaded(i), load_phase(i));
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            constexpr uint32_t idesc = instruction_descriptor<BN>();
+        if (lane == 0 && of_pair == 0) {
+            constexpr uint32_t idesc = instruction_descriptor<PAIR>();
             for (int k = first; k < last && ok; ++k) {
-                const int i = k - first, s = i % STAGES;
-                const uint32_t parity = (i / STAGES) & 1;
-                ok = barrier_wait(loaded(s), parity) && barrier_wait(widened(s), parity);
+                const int i = k - first;
+                // The widening warps of both blocks have seen their block's copies land.
+                ok = barrier_wait(loaded(i), load_phase(i)) && barrier_wait(widened(i), wide_phase(i));
                 if (!ok) break;
                 tensor_fence_after();
-                const uint32_t as = base + s * S::kA, bs = base + S::kOffB + s * S::kB;
+                const uint32_t as = base + (i % WIDE) * S::kA, bs = base + S::kOffB + (i % LOADS) * S::kB;
 #pragma unroll
                 for (int q = 0; q < kTileT / 16; ++q)                // 16 rows an instruction
-                    matrix_multiply(tmem, operand_descriptor(as + q * 2048), operand_descriptor(bs + q * 2048), idesc, i > 0 || q > 0);
-                matrix_commit(used(s));
+#pragma unroll
+                    for (int n = 0; n < BN / kTileO; ++n)
+                        matrix_multiply<PAIR>(tmem + n * kTileO, operand_descriptor(as + q * 2048),
+                                              operand_descriptor(bs + n * (S::kRun * kTileT * 2) + q * 2048), idesc, i > 0 || q > 0);
+                matrix_commit<PAIR>(used(i), mask);
             }
-            if (last > first) matrix_commit(finished);
+            if (last > first) matrix_commit<PAIR>(finished, mask);
         }
     } else if (warp >= kFirstConvert) {
-        const int w = threadIdx.x - 32 * kFirstConvert;
-        for (int k = first; k < last; ++k) {
-            const int i = k - first, s = i % STAGES;
-            ok = barrier_wait(loaded(s), (i / STAGES) & 1);
+        // Thread w of a group widens 16 codes of rows w / 8 + 32 h: their place is the
+        // same in every step.  Eight neighbouring threads fill one 128-byte row in
+        // each half of the operand; those of the upper half start with their second
+        // eight codes, so that no bank is hit twice.
+        constexpr int kRows = 32 * kGroupWarps / 8;
+        const int w = (threadIdx.x - 32 * kFirstConvert) % (32 * kGroupWarps), t0 = w / 8, j = w % 8, swap = j / 4;
+        static_assert(kRows % 8 == 0, "the swizzle depends on the row modulo 8");
+        const int from = t0 * kTileC + j * 16, to = swap * (kTileT * 128) + t0 * 128;
+        const int to0 = to + (((2 * (j % 4) + swap) ^ (t0 % 8)) << 4), to1 = to + (((2 * (j % 4) + 1 - swap) ^ (t0 % 8)) << 4);
+        for (int k = first + (warp - kFirstConvert) / kGroupWarps; k < last; k += kGroups) {
+            const int i = k - first, s = i % LOADS;
+            ok = (i < WIDE || barrier_wait(used(i - WIDE), load_phase(i - WIDE))) && barrier_wait(loaded(i), load_phase(i));
             if (!ok) break;
-            const uint8_t *raw = smem + S::kOffRaw + s * S::kRaw, *scale = smem + S::kOffScale + s * S::kScale;
-            uint8_t *as = smem + s * S::kA;
+            const uint8_t *raw = smem + S::kOffRaw + s * S::kRaw + from, *scale = smem + S::kOffScale + s * S::kScale + t0 * 4 + j / 2;
+            uint8_t *as = smem + (i % WIDE) * S::kA;
+            const int64_t left = p.a.kept.rows - static_cast<int64_t>(k) * kTileT;   // rows past the end have codes 0 and no scale
+            const int rows = static_cast<int>(min(left, static_cast<int64_t>(kTileT)));
 #pragma unroll
-            for (int h = 0; h < kTileT * 8 / (32 * kConvertWarps); ++h) {
-                const int unit = w + h * 32 * kConvertWarps, t = unit / 8, j = unit % 8;       // 16 codes of row t
-                const uint4 codes = *reinterpret_cast<const uint4 *>(raw + t * kTileC + j * 16);
-                // Rows past the end have codes 0 and no scale.
-                const float f = static_cast<int64_t>(k) * kTileT + t < p.a.kept.rows ? scale_value(scale[t * 4 + j / 2]) : 0.0f;
-                const uint2 q0 = widen_codes(codes.x, f), q1 = widen_codes(codes.y, f), q2 = widen_codes(codes.z, f), q3 = widen_codes(codes.w, f);
-                const uint4 lo = make_uint4(q0.x, q0.y, q1.x, q1.y), hi = make_uint4(q2.x, q2.y, q3.x, q3.y);
-                // Eight neighbouring threads fill one 128-byte row in each half; the upper
-                // half starts with its odd 16 bytes, so that no bank is hit twice.
-                uint8_t *row = as + (j / 4) * (kTileT * 128) + t * 128;
-                const int odd = j / 4, even_at = ((2 * (j % 4)) ^ (t % 8)) * 16, odd_at = ((2 * (j % 4) + 1) ^ (t % 8)) * 16;
-                *reinterpret_cast<uint4 *>(row + (odd ? odd_at : even_at)) = odd ? hi : lo;
-                *reinterpret_cast<uint4 *>(row + (odd ? even_at : odd_at)) = odd ? lo : hi;
+            for (int h = 0; h < kTileT / kRows; ++h) {
+                const uint2 c0 = *reinterpret_cast<const uint2 *>(raw + h * kRows * kTileC + 8 * swap);
+                const uint2 c1 = *reinterpret_cast<const uint2 *>(raw + h * kRows * kTileC + 8 - 8 * swap);
+                const float f = t0 + h * kRows < rows ? scale_value(scale[h * kRows * 4]) : 0.0f, off = __fmul_rn(f, -8388736.0f);
+                *reinterpret_cast<uint4 *>(as + h * kRows * 128 + to0) = widen_codes(c0, f, off);
+                *reinterpret_cast<uint4 *>(as + h * kRows * 128 + to1) = widen_codes(c1, f, off);
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0) barrier_arrive(widened(s));
+            if (lane == 0) barrier_arrive(peer_address(widened(i), leader));
         }
     }
 
@@ -334,11 +419,11 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
     if (any) ok = barrier_wait(finished, 0) && ok;
     const bool whole = __syncthreads_and(ok);
     tensor_fence_after();
+    const int quarter = warp % 4, share = (warp - kFirstConvert) / 4;            // of a converting warp
     if (parts == 1) {
         if (whole && warp >= kFirstConvert) {
-            const int quarter = warp % 4, half = (warp - kFirstConvert) / 4;
             const int64_t c = c0 + quarter * 32 + lane;
-            for (int col = half * (BN / 2); col < (half + 1) * (BN / 2); col += 32) {
+            for (int col = share * kShare; col < (share + 1) * kShare; col += 32) {
                 float x[32];
                 if (any) {
                     load_accumulator(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + col, x);
@@ -354,36 +439,48 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
             }
         }
     } else {
-        float *sums = reinterpret_cast<float *>(smem);               // [BN][kTileC]
-        if (warp >= kFirstConvert) {
-            const int quarter = warp % 4, half = (warp - kFirstConvert) / 4;
-            for (int col = half * (BN / 2); col < (half + 1) * (BN / 2); col += 32) {
-                float x[32];
-                load_accumulator(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + col, x);
+        float *sums = reinterpret_cast<float *>(smem);               // [kTileO][kTileC]
+        constexpr int kPart = kTileO / (kConvertWarps / 4);
+        for (int n = 0; n < BN / kTileO; ++n) {
+            if (warp >= kFirstConvert) {
+                for (int col = share * kPart; col < (share + 1) * kPart; col += 32) {
+                    float x[32];
+                    load_accumulator(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + n * kTileO + col, x);
 #pragma unroll
-                for (int r = 0; r < 32; ++r) sums[(col + r) * kTileC + quarter * 32 + lane] = x[r];
+                    for (int r = 0; r < 32; ++r) sums[(col + r) * kTileC + quarter * 32 + lane] = x[r];
+                }
+            }
+            __syncthreads();
+            cluster_sync();
+            if (whole) {
+                const auto store = [&](int col, int r, float4 x) {
+                    const int64_t o = o0 + n * kTileO + col;
+                    if (o >= p.a.outs) return;
+                    const float v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (c0 + r + e < p.a.kept.cols) store_weight(p.a, dw_bf16, o, c0 + r + e, v[e]);
+                };
+                switch (parts) {
+                case 2: join_parts<2>(base, part, of_pair, kBlocks, store); break;
+                case 3: join_parts<3>(base, part, of_pair, kBlocks, store); break;
+                case 4: join_parts<4>(base, part, of_pair, kBlocks, store); break;
+                case 5: join_parts<5>(base, part, of_pair, kBlocks, store); break;
+                case 6: join_parts<6>(base, part, of_pair, kBlocks, store); break;
+                case 7: join_parts<7>(base, part, of_pair, kBlocks, store); break;
+                default: join_parts<8>(base, part, of_pair, kBlocks, store); break;
+                }
+            }
+            if (n + 1 < BN / kTileO) {
+                __syncthreads();
+                cluster_sync();                                      // the sums are read before the next ones come
             }
         }
-        __syncthreads();
-        cluster_sync();
-        const int mine = BN / parts;
-        const uint32_t rank = cluster_rank();
-        if (whole) {
-            for (int i = threadIdx.x; i < mine * kTileC; i += kGradThreads) {
-                const int col = static_cast<int>(rank) * mine + i / kTileC, r = i % kTileC;
-                const uint32_t at = base + static_cast<uint32_t>(col * kTileC + r) * 4;
-                float x = peer_load(peer_address(at, 0));
-                for (int q = 1; q < parts; ++q) x = __fadd_rn(x, peer_load(peer_address(at, q)));
-                if (c0 + r < p.a.kept.cols && o0 + col < p.a.outs) store_weight(p.a, dw_bf16, o0 + col, c0 + r, x);
-            }
-        }
-        __syncthreads();
-        cluster_sync();                                              // nobody leaves while its memory is read
     }
     tensor_fence_before();
     __syncthreads();
-    if (warp == 2)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "n"(BN));
+    if (PAIR || parts > 1) cluster_sync();                           // nobody leaves while a peer reads its memory or signals it
+    if (warp == 2) tensor_free<BN, PAIR>(tmem);
 }
 
 }  // namespace star
