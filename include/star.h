@@ -504,7 +504,8 @@ STAR_API star_status_t star_group_update_host_ex(float *h_params, float *h_momen
  * logit makes its own row's results NaN and the totals with them.
  *
  * star_token_logprobs: logp[rows] and, unless NULL, lse[rows].
- * temperature finite, > 0.  One kernel launch. */
+ * temperature finite, > 0; vocab at most 2^31 - 1 (STAR_ERR_UNSUPPORTED beyond).
+ * One kernel launch. */
 STAR_API star_status_t star_token_logprobs(const void *logits, star_dtype_t dtype, int64_t rows,
                                            int64_t vocab, int64_t ld, const int64_t *labels,
                                            float temperature, float *logp, float *lse,

@@ -1,5 +1,7 @@
 // Entry points of the losses over the vocabulary: argument checks on the host,
 // then the launches.
+#include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "internal.h"
@@ -9,14 +11,145 @@ namespace {
 
 using namespace star;
 
-// Blocks of a grid over `rows` rows (every kernel strides over the rest).
-int row_grid(int64_t rows) { return static_cast<int>(rows < 148 * 64 ? rows : 148 * 64); }
+constexpr int kMaxDevices = 64;
+
+// Shape of the launch that walks the rows.
+struct RowPlan {
+    int cluster = 1;             // blocks that hold a row; 0: rows too long for that
+    int threads = 128;
+    int stages = 2;
+    int granules = 0;            // a block holds at most this many of a row
+};
+
+// A block's share of a row, twice (one row worked on, one in flight), has to fit
+// its shared memory; beyond that, more blocks per row where there are fewer rows
+// than the device has room for.
+constexpr int kRingBytes = 224 * 1024;
+
+RowPlan plan_rows(int64_t rows, int64_t vocab, int size)
+{
+    RowPlan p;
+    const int64_t granules = vocab * size / 16;
+    const auto share = [&](int c) { return (granules + c - 1) / c; };
+    while (p.cluster <= 8 && share(p.cluster) * 16 * 2 > kRingBytes) p.cluster *= 2;
+    if (p.cluster > 8) {
+        p.cluster = 0;
+        return p;
+    }
+    while (p.cluster < 8 && rows * p.cluster * 2 <= 148 && share(p.cluster) >= 512) p.cluster *= 2;
+    p.granules = static_cast<int>(share(p.cluster));
+    p.threads = p.granules >= 3072 ? 1024 : p.granules >= 1536 ? 512 : p.granules >= 768 ? 256 : 128;
+    p.stages = p.granules * 16 * 4 <= 40 * 1024 ? 4 : 2;
+    return p;
+}
+
+// Launches `kernel` as the dependent of the kernel in front of it in the stream
+// (programmatic: it may start early and waits by itself) or in order.
+template <typename... Params, typename... Args>
+star_status_t launch(void (*kernel)(Params...), int64_t grid, int threads, size_t smem, int cluster, bool dependent, cudaStream_t stream,
+                     const Args &...args)
+{
+    cudaLaunchConfig_t config{};
+    config.gridDim = dim3(static_cast<unsigned>(grid));
+    config.blockDim = dim3(static_cast<unsigned>(threads));
+    config.dynamicSmemBytes = smem;
+    config.stream = stream;
+    cudaLaunchAttribute attributes[2] = {};
+    int n = 0;
+    if (cluster > 1) {
+        attributes[n].id = cudaLaunchAttributeClusterDimension;
+        attributes[n].val.clusterDim.x = static_cast<unsigned>(cluster);
+        attributes[n].val.clusterDim.y = 1;
+        attributes[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (dependent) {
+        attributes[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attributes[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
+    config.attrs = attributes;
+    config.numAttrs = static_cast<unsigned>(n);
+    const cudaError_t e = cudaLaunchKernelEx(&config, kernel, args...);
+    return e == cudaSuccess ? launched() : cuda_failed(e);
+}
+
+// Clusters of the kernel that the device holds at once.
+template <typename Kernel> cudaError_t held_clusters(Kernel kernel, const RowPlan &p, size_t smem, int *out)
+{
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t config{};
+    config.gridDim = dim3(static_cast<unsigned>(p.cluster) * 64);
+    config.blockDim = dim3(static_cast<unsigned>(p.threads));
+    config.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attribute{};
+    attribute.id = cudaLaunchAttributeClusterDimension;
+    attribute.val.clusterDim.x = static_cast<unsigned>(p.cluster);
+    attribute.val.clusterDim.y = 1;
+    attribute.val.clusterDim.z = 1;
+    config.attrs = &attribute;
+    config.numAttrs = 1;
+    return cudaOccupancyMaxActiveClusters(out, kernel, &config);
+}
+
+// One kernel's occupancy per device, cluster size and ring size (in KiB), asked
+// once: the question takes longer than a small launch.
+struct Held {
+    std::atomic<int> clusters[kMaxDevices][4][kRingBytes / 1024 + 1];
+};
+
+template <typename G, bool POLICY, int THREADS, int STAGES>
+star_status_t launch_ring(RowWork &a, const RowPlan &p, int *clusters_out, cudaStream_t stream)
+{
+    static Held held;
+    const auto kernel = star_row_kernel<G, POLICY, THREADS, STAGES>;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return cuda_failed(e);
+    if (dev < 0 || dev >= kMaxDevices) return STAR_ERR_UNSUPPORTED;
+    a.granules = p.granules;
+    const size_t kib = (static_cast<size_t>(p.granules) * 16 * STAGES + 1023) / 1024;
+    std::atomic<int> &known = held.clusters[dev][p.cluster == 1 ? 0 : p.cluster == 2 ? 1 : p.cluster == 4 ? 2 : 3][kib];
+    int n = known.load(std::memory_order_relaxed);
+    if (n == 0) {
+        e = held_clusters(kernel, p, kib * 1024, &n);
+        if (e != cudaSuccess) return cuda_failed(e);
+        if (n < 1) return cuda_failed(cudaErrorInvalidConfiguration);
+        known.store(n, std::memory_order_relaxed);
+    }
+    const int64_t clusters = std::min<int64_t>(a.row.rows, n);
+    *clusters_out = static_cast<int>(clusters);
+    return launch(kernel, clusters * p.cluster, THREADS, kib * 1024, p.cluster, false, stream, a);
+}
+
+// The pass over the rows; *clusters_out: how many partial sums it leaves.
+template <typename G, bool POLICY> star_status_t walk_rows(RowWork &a, int *clusters_out, cudaStream_t stream)
+{
+    const RowPlan p = plan_rows(a.row.rows, a.row.vocab, G::kBytes);
+    if (p.cluster == 0) {
+        const int64_t grid = std::min<int64_t>(a.row.rows, 148 * 8);
+        *clusters_out = static_cast<int>(grid);
+        return launch(star_long_row_kernel<G, POLICY>, grid, kRowThreads, 0, 1, false, stream, a);
+    }
+    if (p.stages == 4) {
+        if (p.threads == 128) return launch_ring<G, POLICY, 128, 4>(a, p, clusters_out, stream);
+        return launch_ring<G, POLICY, 256, 4>(a, p, clusters_out, stream);
+    }
+    switch (p.threads) {
+    case 128: return launch_ring<G, POLICY, 128, 2>(a, p, clusters_out, stream);
+    case 256: return launch_ring<G, POLICY, 256, 2>(a, p, clusters_out, stream);
+    case 512: return launch_ring<G, POLICY, 512, 2>(a, p, clusters_out, stream);
+    default: return launch_ring<G, POLICY, 1024, 2>(a, p, clusters_out, stream);
+    }
+}
 
 // The checks that the three operators share.  read[0] is the logits' extent.
 star_status_t check_rows(const void *logits, star_dtype_t dtype, int64_t rows, int64_t vocab, int64_t ld,
                          const int64_t *labels, float temperature, RowArgs *out, Extent *read)
 {
     if (!is_dtype(dtype) || vocab < 0) return STAR_ERR_INVALID_ARG;
+    if (vocab > 0x7fffffff) return STAR_ERR_UNSUPPORTED;
     if (!(temperature > 0.0f) || !std::isfinite(temperature) || !std::isfinite(1.0f / temperature) ||
         !std::isfinite(1.0f / temperature * kLog2e))
         return STAR_ERR_INVALID_ARG;
@@ -65,7 +198,7 @@ extern "C" star_status_t star_token_logprobs(const void *logits, star_dtype_t dt
                                              int64_t ld, const int64_t *labels, float temperature, float *logp,
                                              float *lse, void *cuda_stream)
 {
-    LogprobArgs a{};
+    RowWork a{};
     Extent read[2], written[2];
     star_status_t st = check_rows(logits, dtype, rows, vocab, ld, labels, temperature, &a.row, read);
     if (st == STAR_OK) st = check_vector(logp, rows, 4, false, &written[0]);
@@ -75,11 +208,8 @@ extern "C" star_status_t star_token_logprobs(const void *logits, star_dtype_t dt
     a.logp = logp;
     a.lse = lse;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (dtype == STAR_DTYPE_BF16)
-        star_logprob_kernel<GradBF16><<<row_grid(rows), kRowThreads, 0, stream>>>(a);
-    else
-        star_logprob_kernel<GradF32><<<row_grid(rows), kRowThreads, 0, stream>>>(a);
-    return launched();
+    int clusters = 0;
+    return dtype == STAR_DTYPE_BF16 ? walk_rows<GradBF16, false>(a, &clusters, stream) : walk_rows<GradF32, false>(a, &clusters, stream);
 }
 
 extern "C" star_status_t star_loss_workspace_bytes(int64_t rows, int64_t sequences, size_t *bytes_out)
@@ -102,7 +232,7 @@ extern "C" star_status_t star_policy_loss(const void *logits, star_dtype_t dtype
 {
     if (!(clip_low >= 0.0f && clip_low <= 1.0f) || !(clip_high >= 0.0f) || !std::isfinite(kl_coef))
         return STAR_ERR_INVALID_ARG;
-    PolicyArgs a{};
+    RowWork a{};
     Extent read[6], written[5];
     star_status_t st = check_rows(logits, dtype, rows, vocab, ld, labels, temperature, &a.row, read);
     if (st == STAR_OK) st = check_vector(weights, rows, 4, true, &read[2]);
@@ -127,20 +257,17 @@ extern "C" star_status_t star_policy_loss(const void *logits, star_dtype_t dtype
     a.kl_coef = kl_coef;
     a.logp = logp;
     a.token_loss = token_loss;
-    a.terms = static_cast<float4 *>(workspace);
+    a.partial = static_cast<float4 *>(workspace);
     a.dlogits = dlogits;
     a.ld_dlogits = ld_dlogits;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    int clusters = 0;
     if (rows > 0) {
-        if (dtype == STAR_DTYPE_BF16)
-            star_policy_kernel<GradBF16><<<row_grid(rows), kRowThreads, 0, stream>>>(a);
-        else
-            star_policy_kernel<GradF32><<<row_grid(rows), kRowThreads, 0, stream>>>(a);
-        st = launched();
+        st = dtype == STAR_DTYPE_BF16 ? walk_rows<GradBF16, true>(a, &clusters, stream) : walk_rows<GradF32, true>(a, &clusters, stream);
         if (st != STAR_OK) return st;
     }
-    star_policy_sums_kernel<<<1, kSumThreads, 0, stream>>>(a.terms, rows, sums);
-    return launched();
+    return launch(star_policy_sums_kernel, 1, kSumThreads, 0, 1, rows > 0, stream, static_cast<const float4 *>(a.partial),
+                  static_cast<int64_t>(clusters), sums);
 }
 
 extern "C" star_status_t star_preference_loss(const void *logits, star_dtype_t dtype, int64_t rows, int64_t vocab,
@@ -186,26 +313,21 @@ extern "C" star_status_t star_preference_loss(const void *logits, star_dtype_t d
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const bool bf16 = dtype == STAR_DTYPE_BF16;
     if (rows > 0) {
-        LogprobArgs p{};
+        RowWork p{};
         p.row = a.row;
         p.kept = a.kept;
-        if (bf16)
-            star_logprob_kernel<GradBF16><<<row_grid(rows), kRowThreads, 0, stream>>>(p);
-        else
-            star_logprob_kernel<GradF32><<<row_grid(rows), kRowThreads, 0, stream>>>(p);
-        if ((st = launched()) != STAR_OK) return st;
+        int clusters = 0;
+        st = bf16 ? walk_rows<GradBF16, false>(p, &clusters, stream) : walk_rows<GradF32, false>(p, &clusters, stream);
+        if (st != STAR_OK) return st;
     }
     if (pairs > 0) {
-        star_preference_pair_kernel<<<static_cast<int>(pairs < 65536 ? pairs : 65536), kPairThreads, 0, stream>>>(a);
-        if ((st = launched()) != STAR_OK) return st;
+        st = launch(star_preference_pair_kernel, std::min<int64_t>(pairs, 65536), kPairThreads, 0, 1, rows > 0, stream, a);
+        if (st != STAR_OK) return st;
     }
-    if (dlogits && rows > 0) {
-        if (bf16)
-            star_preference_grad_kernel<GradBF16><<<row_grid(rows), kRowThreads, 0, stream>>>(a);
-        else
-            star_preference_grad_kernel<GradF32><<<row_grid(rows), kRowThreads, 0, stream>>>(a);
-    } else {
-        star_preference_total_kernel<<<1, kPairThreads, 0, stream>>>(a);
-    }
-    return launched();
+    const bool follows = rows > 0 || pairs > 0;
+    if (!dlogits || rows == 0) return launch(star_preference_total_kernel, 1, kPairThreads, 0, 1, follows, stream, a);
+    const int64_t per_row = vocab * dtype_size(dtype) / 16 / kGradGranules + 1;
+    const int64_t grid = std::min<int64_t>(rows > 148 * 64 / per_row ? 148 * 64 : rows * per_row, 148 * 64);
+    return bf16 ? launch(star_preference_grad_kernel<GradBF16>, grid, kRowThreads, 0, 1, follows, stream, a)
+                : launch(star_preference_grad_kernel<GradF32>, grid, kRowThreads, 0, 1, follows, stream, a);
 }

@@ -43,8 +43,6 @@ struct WeightGradTile {
 constexpr long long kWaitCycles = 4000000000ll;      // two seconds and more
 __device__ int g_wait_expired;       // set by a block that gave up waiting
 
-__device__ __forceinline__ uint32_t smem_address(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
-
 __device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count)
 {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar), "r"(count) : "memory");
@@ -225,22 +223,6 @@ template <int BN, int LOADS, int WIDE, bool PAIR> struct GradSmem {
     static_assert(kDynamic <= 232448, "more shared memory than a block may have");
 };
 
-__device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t cluster_rank()
-{
-    uint32_t r;
-    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t peer_address(uint32_t address, uint32_t rank)
-{
-    uint32_t r;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(address), "r"(rank));
-    return r;
-}
 __device__ __forceinline__ float4 peer_load(uint32_t address)
 {
     float4 x;

@@ -43,7 +43,7 @@ COMMON_ROWS = [(dict(dtype=2), INVALID), (dict(dtype=-1), INVALID), (dict(rows=-
                (dict(ld=99), INVALID), (dict(logits=None), NULL), (dict(labels=None), NULL), (dict(logits=address(0) + 1), INVALID),
                (dict(labels=address(1) + 4), INVALID), (dict(temperature=0.0), INVALID), (dict(temperature=-1.0), INVALID),
                (dict(temperature=math.nan), INVALID), (dict(temperature=math.inf), INVALID), (dict(temperature=1e-40), INVALID),
-               (dict(rows=1 << 50, ld=1 << 30), INVALID), (dict(logp=address(0) + 4), INVALID), (dict(logp=address(1)), INVALID)]
+               (dict(rows=1 << 50, ld=1 << 30), INVALID), (dict(vocab=1 << 31, ld=1 << 31), B.STAR_ERR_UNSUPPORTED), (dict(logp=address(0) + 4), INVALID), (dict(logp=address(1)), INVALID)]
 
 REFUSED = {
     "star_token_logprobs": COMMON_ROWS + [(dict(logp=None), NULL), (dict(lse=address(2)), INVALID), (dict(logp=address(2) + 2), INVALID)],
