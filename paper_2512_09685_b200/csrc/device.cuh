@@ -68,6 +68,52 @@ __device__ __forceinline__ uint32_t cluster_size()
     return r;
 }
 
+// ---------------------------------------------------------------------------
+// Barriers in shared memory.  Every wait ends: after kWaitTries attempts it reports failure,
+// sets a flag that star_check_waits reads, and the kernel ends without a valid
+// result, its copies drained.
+// ---------------------------------------------------------------------------
+// An attempt takes 20 ns or more (the hardware holds it for a while), so a wait
+// ends after some tenths of a second at the earliest: waits for memory take
+// microseconds.
+constexpr int kWaitTries = 1 << 24;
+static __device__ int g_wait_expired;        // of this source file's kernels
+
+__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
+}
+// `bar` is a barrier of any block of the cluster.
+__device__ __forceinline__ void barrier_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
+}
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity)
+{
+    for (int i = 0; i < kWaitTries; ++i)
+        if (barrier_try(bar, parity)) return true;
+    atomicExch(&g_wait_expired, 1);
+    return false;
+}
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 :: "r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
 // A kernel launched as a programmatic dependent may start before the kernel in
 // front of it in the stream is done; wait_for_primary() returns once that one is
 // complete and its writes are visible.  launch_dependents() lets it start.

@@ -13,36 +13,6 @@ using namespace star;
 
 constexpr int kMaxDevices = 64;
 
-// Shape of the launch that walks the rows.
-struct RowPlan {
-    int cluster = 1;             // blocks that hold a row; 0: rows too long for that
-    int threads = 128;
-    int stages = 2;
-    int granules = 0;            // a block holds at most this many of a row
-};
-
-// A block's share of a row, twice (one row worked on, one in flight), has to fit
-// its shared memory; beyond that, more blocks per row where there are fewer rows
-// than the device has room for.
-constexpr int kRingBytes = 224 * 1024;
-
-RowPlan plan_rows(int64_t rows, int64_t vocab, int size)
-{
-    RowPlan p;
-    const int64_t granules = vocab * size / 16;
-    const auto share = [&](int c) { return (granules + c - 1) / c; };
-    while (p.cluster <= 8 && share(p.cluster) * 16 * 2 > kRingBytes) p.cluster *= 2;
-    if (p.cluster > 8) {
-        p.cluster = 0;
-        return p;
-    }
-    while (p.cluster < 8 && rows * p.cluster * 2 <= 148 && share(p.cluster) >= 512) p.cluster *= 2;
-    p.granules = static_cast<int>(share(p.cluster));
-    p.threads = p.granules >= 3072 ? 1024 : p.granules >= 1536 ? 512 : p.granules >= 768 ? 256 : 128;
-    p.stages = p.granules * 16 * 4 <= 40 * 1024 ? 4 : 2;
-    return p;
-}
-
 // Launches `kernel` as the dependent of the kernel in front of it in the stream
 // (programmatic: it may start early and waits by itself) or in order.
 template <typename... Params, typename... Args>
@@ -74,74 +44,131 @@ star_status_t launch(void (*kernel)(Params...), int64_t grid, int threads, size_
     return e == cudaSuccess ? launched() : cuda_failed(e);
 }
 
-// Clusters of the kernel that the device holds at once.
-template <typename Kernel> cudaError_t held_clusters(Kernel kernel, const RowPlan &p, size_t smem, int *out)
-{
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes);
-    if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t config{};
-    config.gridDim = dim3(static_cast<unsigned>(p.cluster) * 64);
-    config.blockDim = dim3(static_cast<unsigned>(p.threads));
-    config.dynamicSmemBytes = smem;
-    cudaLaunchAttribute attribute{};
-    attribute.id = cudaLaunchAttributeClusterDimension;
-    attribute.val.clusterDim.x = static_cast<unsigned>(p.cluster);
-    attribute.val.clusterDim.y = 1;
-    attribute.val.clusterDim.z = 1;
-    config.attrs = &attribute;
-    config.numAttrs = 1;
-    return cudaOccupancyMaxActiveClusters(out, kernel, &config);
-}
-
-// One kernel's occupancy per device, cluster size and ring size (in KiB), asked
-// once: the question takes longer than a small launch.
+// Clusters of a kernel that the device holds at once, per device, cluster size
+// and shared memory (in KiB), asked once: the question takes longer than a small
+// launch.
 struct Held {
-    std::atomic<int> clusters[kMaxDevices][4][kRingBytes / 1024 + 1];
+    std::atomic<int> clusters[kMaxDevices][4][kKeepBytesPerThread + 1];
 };
 
-template <typename G, bool POLICY, int THREADS, int STAGES>
-star_status_t launch_ring(RowWork &a, const RowPlan &p, int *clusters_out, cudaStream_t stream)
+template <typename Kernel> cudaError_t held_clusters(Kernel kernel, Held &known, int threads, int cluster, int kib, int *out)
 {
-    static Held held;
-    const auto kernel = star_row_kernel<G, POLICY, THREADS, STAGES>;
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return cuda_failed(e);
-    if (dev < 0 || dev >= kMaxDevices) return STAR_ERR_UNSUPPORTED;
-    a.granules = p.granules;
-    const size_t kib = (static_cast<size_t>(p.granules) * 16 * STAGES + 1023) / 1024;
-    std::atomic<int> &known = held.clusters[dev][p.cluster == 1 ? 0 : p.cluster == 2 ? 1 : p.cluster == 4 ? 2 : 3][kib];
-    int n = known.load(std::memory_order_relaxed);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+    std::atomic<int> &slot = known.clusters[dev][cluster == 1 ? 0 : cluster == 2 ? 1 : cluster == 4 ? 2 : 3][kib];
+    int n = slot.load(std::memory_order_relaxed);
     if (n == 0) {
-        e = held_clusters(kernel, p, kib * 1024, &n);
-        if (e != cudaSuccess) return cuda_failed(e);
-        if (n < 1) return cuda_failed(cudaErrorInvalidConfiguration);
-        known.store(n, std::memory_order_relaxed);
+        if (kib > 0) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kKeepBytesPerThread * 1024);
+        if (e != cudaSuccess) return e;
+        if (cluster == 1) {
+            int sms = 0, per_sm = 0;
+            e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+            if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, static_cast<size_t>(kib) * 1024);
+            n = sms * per_sm;
+        } else {
+            cudaLaunchConfig_t config{};
+            config.gridDim = dim3(static_cast<unsigned>(cluster) * 64);
+            config.blockDim = dim3(static_cast<unsigned>(threads));
+            cudaLaunchAttribute attribute{};
+            attribute.id = cudaLaunchAttributeClusterDimension;
+            attribute.val.clusterDim.x = static_cast<unsigned>(cluster);
+            attribute.val.clusterDim.y = 1;
+            attribute.val.clusterDim.z = 1;
+            config.attrs = &attribute;
+            config.numAttrs = 1;
+            e = cudaOccupancyMaxActiveClusters(&n, kernel, &config);
+        }
+        if (e != cudaSuccess) return e;
+        if (n < 1) return cudaErrorInvalidConfiguration;
+        slot.store(n, std::memory_order_relaxed);
     }
-    const int64_t clusters = std::min<int64_t>(a.row.rows, n);
-    *clusters_out = static_cast<int>(clusters);
-    return launch(kernel, clusters * p.cluster, THREADS, kib * 1024, p.cluster, false, stream, a);
+    *out = n;
+    return cudaSuccess;
 }
 
-// The pass over the rows; *clusters_out: how many partial sums it leaves.
-template <typename G, bool POLICY> star_status_t walk_rows(RowWork &a, int *clusters_out, cudaStream_t stream)
+// The rows' statistics: blocks of 32 to 256 threads with two batches of granules
+// or more for each thread, and a cluster of blocks per row where there are fewer
+// rows than half the SMs.
+template <typename G, bool POLICY, int THREADS>
+star_status_t launch_rows(const RowWork &a, int cluster, int *parts_out, cudaStream_t stream)
 {
-    const RowPlan p = plan_rows(a.row.rows, a.row.vocab, G::kBytes);
-    if (p.cluster == 0) {
-        const int64_t grid = std::min<int64_t>(a.row.rows, 148 * 8);
-        *clusters_out = static_cast<int>(grid);
-        return launch(star_long_row_kernel<G, POLICY>, grid, kRowThreads, 0, 1, false, stream, a);
+    static Held known;
+    constexpr auto kernel = star_row_kernel<G, POLICY, THREADS>;
+    int held = 0;
+    const cudaError_t e = held_clusters(kernel, known, THREADS, cluster, 0, &held);
+    if (e != cudaSuccess) return cuda_failed(e);
+    // Short rows: as many blocks as the device holds, each with many rows.  Long
+    // rows: a block each, which evens out rows that are skipped.
+    const int64_t most = a.row.vocab * G::kBytes < 16384 ? held : int64_t{1} << 20, clusters = std::min(a.row.rows, most);
+    *parts_out = static_cast<int>(clusters);
+    return launch(kernel, clusters * cluster, THREADS, 0, cluster, false, stream, a);
+}
+
+template <typename G, bool POLICY> star_status_t walk_rows(const RowWork &a, int *parts_out, cudaStream_t stream)
+{
+    const int64_t granules = a.row.vocab * G::kBytes / 16;
+    int cluster = 1, threads = 32;
+    while (cluster < 8 && a.row.rows * cluster * 2 <= 148 && granules / (cluster * 2) >= 512) cluster *= 2;
+    while (threads < 256 && granules / cluster > static_cast<int64_t>(threads) * 2 * kBatch) threads *= 2;
+    switch (threads) {
+    case 32: return launch_rows<G, POLICY, 32>(a, cluster, parts_out, stream);
+    case 64: return launch_rows<G, POLICY, 64>(a, cluster, parts_out, stream);
+    case 128: return launch_rows<G, POLICY, 128>(a, cluster, parts_out, stream);
+    default: return launch_rows<G, POLICY, 256>(a, cluster, parts_out, stream);
     }
-    if (p.stages == 4) {
-        if (p.threads == 128) return launch_ring<G, POLICY, 128, 4>(a, p, clusters_out, stream);
-        return launch_ring<G, POLICY, 256, 4>(a, p, clusters_out, stream);
+}
+
+// The policy loss in one reading of the rows.
+template <typename G, int THREADS> star_status_t launch_policy(const RowWork &a, int *parts_out, cudaStream_t stream)
+{
+    static Held known;
+    constexpr auto kernel = star_policy_kernel<G, THREADS>;
+    const int kib = static_cast<int>((a.row.vocab * G::kBytes / 16 * 16 + 1023) / 1024);
+    int held = 0;
+    const cudaError_t e = held_clusters(kernel, known, THREADS, 1, kib, &held);
+    if (e != cudaSuccess) return cuda_failed(e);
+    const int64_t blocks = std::min<int64_t>(a.row.rows, held);
+    *parts_out = static_cast<int>(blocks);
+    return launch(kernel, blocks, THREADS, static_cast<size_t>(kib) * 1024, 1, false, stream, a);
+}
+
+// Whether the policy loss is made in one reading (and the smallest block whose
+// part of the SM's shared memory holds a row): rows of up to 224 KB, and enough
+// of them to fill half the SMs with a block each.  Fewer rows are shared by
+// clusters and read twice.  The same with and without a gradient, so that both
+// give the same bits.
+bool one_reading(int64_t rows, int64_t vocab, int size, int *threads)
+{
+    const int64_t bytes = vocab * size;
+    if (rows * 2 <= 148) return false;
+    for (int t : {32, 64, 128, 256, 512, 1024}) {
+        *threads = t;
+        if (bytes <= kKeepBytesPerThread * t) return true;
     }
-    switch (p.threads) {
-    case 128: return launch_ring<G, POLICY, 128, 2>(a, p, clusters_out, stream);
-    case 256: return launch_ring<G, POLICY, 256, 2>(a, p, clusters_out, stream);
-    case 512: return launch_ring<G, POLICY, 512, 2>(a, p, clusters_out, stream);
-    default: return launch_ring<G, POLICY, 1024, 2>(a, p, clusters_out, stream);
+    return false;
+}
+
+template <typename G> star_status_t run_policy(const RowWork &a, int threads, int *parts_out, cudaStream_t stream)
+{
+    switch (threads) {
+    case 32: return launch_policy<G, 32>(a, parts_out, stream);
+    case 64: return launch_policy<G, 64>(a, parts_out, stream);
+    case 128: return launch_policy<G, 128>(a, parts_out, stream);
+    case 256: return launch_policy<G, 256>(a, parts_out, stream);
+    case 512: return launch_policy<G, 512>(a, parts_out, stream);
+    default: return launch_policy<G, 1024>(a, parts_out, stream);
     }
+}
+
+// The gradient from what was kept of the rows.
+template <bool POLICY> star_status_t launch_gradient(const GradArgs &g, star_dtype_t dtype, bool follows, cudaStream_t stream)
+{
+    const int64_t per_row = g.row.vocab * dtype_size(dtype) / 16 / kGradGranules + 1;
+    const int64_t most = 148 * 64, grid = g.row.rows > most / per_row ? most : g.row.rows * per_row;
+    return dtype == STAR_DTYPE_BF16 ? launch(star_row_gradient_kernel<GradBF16, POLICY>, grid, kRowThreads, 0, 1, follows, stream, g)
+                                    : launch(star_row_gradient_kernel<GradF32, POLICY>, grid, kRowThreads, 0, 1, follows, stream, g);
 }
 
 // The checks that the three operators share.  read[0] is the logits' extent.
@@ -218,7 +245,8 @@ extern "C" star_status_t star_loss_workspace_bytes(int64_t rows, int64_t sequenc
     if (rows < 0 || sequences < 0 || static_cast<uint64_t>(rows) > kMaxBytes / 16 ||
         static_cast<uint64_t>(sequences) > kMaxBytes / 16)
         return STAR_ERR_INVALID_ARG;
-    *bytes_out = static_cast<size_t>(rows) * 16 + 16;
+    // What is kept of every row, and the partial sums of up to as many blocks.
+    *bytes_out = static_cast<size_t>(rows) * 32 + 16;
     return STAR_OK;
 }
 
@@ -261,13 +289,29 @@ extern "C" star_status_t star_policy_loss(const void *logits, star_dtype_t dtype
     a.dlogits = dlogits;
     a.ld_dlogits = ld_dlogits;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    int clusters = 0;
-    if (rows > 0) {
-        st = dtype == STAR_DTYPE_BF16 ? walk_rows<GradBF16, true>(a, &clusters, stream) : walk_rows<GradF32, true>(a, &clusters, stream);
-        if (st != STAR_OK) return st;
+    const bool bf16 = dtype == STAR_DTYPE_BF16;
+    int parts = 0, threads = 0;
+    const bool once = one_reading(rows, vocab, dtype_size(dtype), &threads);
+    if (once) {
+        st = bf16 ? run_policy<GradBF16>(a, threads, &parts, stream) : run_policy<GradF32>(a, threads, &parts, stream);
+    } else if (rows > 0) {
+        if (dlogits) a.kept = reinterpret_cast<RowKept *>(a.partial + rows);
+        st = bf16 ? walk_rows<GradBF16, true>(a, &parts, stream) : walk_rows<GradF32, true>(a, &parts, stream);
+    }
+    if (st != STAR_OK) return st;
+    if (!once && rows > 0 && dlogits) {
+        GradArgs g{};
+        g.row = a.row;
+        g.kept = a.kept;
+        g.dlogits = dlogits;
+        g.ld_dlogits = ld_dlogits;
+        g.partial = a.partial;
+        g.parts = parts;
+        g.sums = sums;
+        return launch_gradient<true>(g, dtype, true, stream);
     }
     return launch(star_policy_sums_kernel, 1, kSumThreads, 0, 1, rows > 0, stream, static_cast<const float4 *>(a.partial),
-                  static_cast<int64_t>(clusters), sums);
+                  static_cast<int64_t>(parts), sums);
 }
 
 extern "C" star_status_t star_preference_loss(const void *logits, star_dtype_t dtype, int64_t rows, int64_t vocab,
@@ -311,8 +355,8 @@ extern "C" star_status_t star_preference_loss(const void *logits, star_dtype_t d
     a.dlogits = dlogits;
     a.ld_dlogits = ld_dlogits;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    const bool bf16 = dtype == STAR_DTYPE_BF16;
     if (rows > 0) {
+        const bool bf16 = dtype == STAR_DTYPE_BF16;
         RowWork p{};
         p.row = a.row;
         p.kept = a.kept;
@@ -326,8 +370,14 @@ extern "C" star_status_t star_preference_loss(const void *logits, star_dtype_t d
     }
     const bool follows = rows > 0 || pairs > 0;
     if (!dlogits || rows == 0) return launch(star_preference_total_kernel, 1, kPairThreads, 0, 1, follows, stream, a);
-    const int64_t per_row = vocab * dtype_size(dtype) / 16 / kGradGranules + 1;
-    const int64_t grid = std::min<int64_t>(rows > 148 * 64 / per_row ? 148 * 64 : rows * per_row, 148 * 64);
-    return bf16 ? launch(star_preference_grad_kernel<GradBF16>, grid, kRowThreads, 0, 1, follows, stream, a)
-                : launch(star_preference_grad_kernel<GradF32>, grid, kRowThreads, 0, 1, follows, stream, a);
+    GradArgs g{};
+    g.row = a.row;
+    g.kept = a.kept;
+    g.dlogits = dlogits;
+    g.ld_dlogits = ld_dlogits;
+    g.pair_loss = pair_loss;
+    g.pairs = pairs;
+    g.loss_scale = loss_scale;
+    g.loss = loss;
+    return launch_gradient<false>(g, dtype, follows, stream);
 }

@@ -37,50 +37,6 @@ struct WeightGradTile {
 };
 
 // ---------------------------------------------------------------------------
-// Barriers in shared memory.  Every wait ends: after kWaitCycles it reports failure,
-// the block stops issuing, drains its copies, and leaves without a result.
-// ---------------------------------------------------------------------------
-constexpr long long kWaitCycles = 4000000000ll;      // two seconds and more
-__device__ int g_wait_expired;       // set by a block that gave up waiting
-
-__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
-}
-// `bar` is a barrier of any block of the cluster.
-__device__ __forceinline__ void barrier_arrive(uint32_t bar)
-{
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
-}
-__device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity)
-{
-    uint32_t done;
-    asm volatile("{\n\t.reg .pred p;\n\t"
-                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-                 "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    return done != 0;
-}
-__device__ __noinline__ bool barrier_wait_long(uint32_t bar, uint32_t parity)
-{
-    const long long start = clock64();
-    while (clock64() - start < kWaitCycles)
-        for (int i = 0; i < 64; ++i)
-            if (barrier_try(bar, parity)) return true;
-    atomicExch(&g_wait_expired, 1);
-    return false;
-}
-__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity)
-{
-    for (int i = 0; i < 16; ++i)
-        if (barrier_try(bar, parity)) return true;
-    return barrier_wait_long(bar, parity);
-}
-
-// ---------------------------------------------------------------------------
 // Copies and matrix instructions.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
@@ -88,12 +44,6 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 :: "r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
-}
-
 // Descriptor of an operand tile stored as 128-byte rows (64 bf16 of one t), 64
 // rows to a chunk of 64 columns, 128-byte swizzle.  Leading offset: from chunk
 // to chunk; stride offset: from 8 rows to the next 8.
