@@ -1,5 +1,6 @@
 // Entry points of activations kept in 8 bits: argument checks on the host, then
 // one kernel launch.
+#include <algorithm>
 #include <type_traits>
 
 #include "checkpoint.cuh"
@@ -11,7 +12,45 @@ using namespace star;
 
 bool is_act(int act) { return act >= STAR_ACT_NONE && act <= STAR_ACT_SILU; }
 
-int grid_for(int64_t work) { return static_cast<int>(work < 1 ? 1 : work < 148 * 32 ? work : 148 * 32); }
+int grid_for(int64_t blocks) { return static_cast<int>(blocks < 1 ? 1 : blocks < 148 * 64 ? blocks : 148 * 64); }
+
+// Whether every row of a matrix starts on a 16-byte boundary.
+bool on_grid(const void *p, int64_t ld, int size) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (ld * size) % 16 == 0; }
+
+// i / d = (i * magic) >> (32 + shift) for all i < 2^31: magic = floor(2^(32 + shift) / d) + 1
+// with 2^shift the power of two at or below d - 1, so that it fits 32 bits.
+Divisor make_divisor(uint32_t d)
+{
+    Divisor r{d, 0, 0};
+    while (d > 1 && (uint64_t{1} << (r.shift + 1)) < d) ++r.shift;
+    r.magic = static_cast<uint32_t>((uint64_t{1} << (32 + r.shift)) / d + 1);
+    return r;
+}
+
+// Runs launch(halves, grid) on the rows in runs of less than 2^31 halves (one,
+// for all but checkpoints of 32 GB and more).
+template <typename F> star_status_t by_halves(int64_t rows, int64_t cols, F launch)
+{
+    const int64_t per_row = (cols + 31) / 32 * 2;
+    const int64_t most = (int64_t{1} << 30) / per_row;
+    for (int64_t first = 0; first < rows; first += most) {
+        const int64_t n = std::min(most, rows - first) * per_row;
+        launch(Halves{make_divisor(static_cast<uint32_t>(per_row)), static_cast<uint32_t>(first), static_cast<uint32_t>(n)},
+               grid_for((n + kKeepThreads - 1) / kKeepThreads));
+        const star_status_t st = launched();
+        if (st != STAR_OK) return st;
+    }
+    return STAR_OK;
+}
+
+// The 16-byte kernels number rows and halves of a row in 32 bits.
+bool countable(int64_t rows, int64_t cols) { return rows <= 0x7fffffff && cols <= (int64_t{1} << 32); }
+
+int loose_grid(int64_t rows, int64_t cols)
+{
+    const int64_t groups = ((cols + 31) / 32 + kLoose - 1) / kLoose, per_block = kKeepThreads / 32;
+    return grid_for(rows > (148 * 64 * per_block) / groups ? 148 * 64 : (rows * groups + per_block - 1) / per_block);
+}
 
 // Calls f with the activation as a compile-time number.
 template <typename F> void with_act(int act, F f)
@@ -60,31 +99,48 @@ extern "C" star_status_t star_checkpoint_pack(int8_t *codes, uint8_t *scales, co
     a.act_out = act_out;
     a.ld_act = ld_act;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    const int grid = grid_for((rows * ((cols + 31) / 32) + 7) / 8);
+    const int size = dtype_size(dtype);
+    const bool vector = on_grid(x, ld, size) && (!act_out || on_grid(act_out, ld_act, size)) && countable(rows, cols);
     with_act(act, [&](auto k) {
         constexpr int ACT = decltype(k)::value;
-        if (dtype == STAR_DTYPE_BF16)
-            star_checkpoint_pack_kernel<GradBF16, ACT><<<grid, kPackThreads, 0, stream>>>(a);
+        if (vector)
+            st = by_halves(rows, cols, [&](const Halves &h, int grid) {
+                if (dtype == STAR_DTYPE_BF16)
+                    star_checkpoint_pack_kernel<GradBF16, ACT><<<grid, kKeepThreads, 0, stream>>>(a, h);
+                else
+                    star_checkpoint_pack_kernel<GradF32, ACT><<<grid, kKeepThreads, 0, stream>>>(a, h);
+            });
+        else if (dtype == STAR_DTYPE_BF16)
+            star_checkpoint_pack_loose_kernel<GradBF16, ACT><<<loose_grid(rows, cols), kKeepThreads, 0, stream>>>(a);
         else
-            star_checkpoint_pack_kernel<GradF32, ACT><<<grid, kPackThreads, 0, stream>>>(a);
+            star_checkpoint_pack_loose_kernel<GradF32, ACT><<<loose_grid(rows, cols), kKeepThreads, 0, stream>>>(a);
     });
-    return launched();
+    return vector ? st : launched();
 }
 
 namespace {
 
-template <bool BACKWARD> star_status_t read_kept(UnpackArgs &a, star_dtype_t dtype, int act, void *cuda_stream)
+template <bool BACKWARD> star_status_t read_kept(const ReadArgs &a, star_dtype_t dtype, int act, void *cuda_stream)
 {
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    const int grid = grid_for((a.kept.rows * a.kept.cols + kPackThreads - 1) / kPackThreads);
+    const int size = dtype_size(dtype);
+    const bool vector = on_grid(a.out, a.ld, size) && (!BACKWARD || on_grid(a.dy, a.ld_dy, size)) && countable(a.kept.rows, a.kept.cols);
+    star_status_t st = STAR_OK;
     with_act(act, [&](auto k) {
         constexpr int ACT = decltype(k)::value;
-        if (dtype == STAR_DTYPE_BF16)
-            star_checkpoint_read_kernel<GradBF16, ACT, BACKWARD><<<grid, kPackThreads, 0, stream>>>(a);
+        if (vector)
+            st = by_halves(a.kept.rows, a.kept.cols, [&](const Halves &h, int grid) {
+                if (dtype == STAR_DTYPE_BF16)
+                    star_checkpoint_read_kernel<GradBF16, ACT, BACKWARD><<<grid, kKeepThreads, 0, stream>>>(a, h);
+                else
+                    star_checkpoint_read_kernel<GradF32, ACT, BACKWARD><<<grid, kKeepThreads, 0, stream>>>(a, h);
+            });
+        else if (dtype == STAR_DTYPE_BF16)
+            star_checkpoint_read_loose_kernel<GradBF16, ACT, BACKWARD><<<loose_grid(a.kept.rows, a.kept.cols), kKeepThreads, 0, stream>>>(a);
         else
-            star_checkpoint_read_kernel<GradF32, ACT, BACKWARD><<<grid, kPackThreads, 0, stream>>>(a);
+            star_checkpoint_read_loose_kernel<GradF32, ACT, BACKWARD><<<loose_grid(a.kept.rows, a.kept.cols), kKeepThreads, 0, stream>>>(a);
     });
-    return launched();
+    return vector ? st : launched();
 }
 
 }  // namespace
@@ -94,7 +150,7 @@ extern "C" star_status_t star_checkpoint_unpack(void *out, star_dtype_t dtype, i
                                                 star_activation_t act, void *cuda_stream)
 {
     if (!is_dtype(dtype) || !is_act(act)) return STAR_ERR_INVALID_ARG;
-    UnpackArgs a{};
+    ReadArgs a{};
     Extent read[2], written;
     star_status_t st = check_kept(codes, scales, rows, cols, &a.kept, read);
     if (st == STAR_OK) st = check_matrix(out, rows, cols, ld, dtype_size(dtype), &written);
@@ -111,7 +167,7 @@ extern "C" star_status_t star_checkpoint_act_backward(void *dx, int64_t ld_dx, c
                                                       void *cuda_stream)
 {
     if (!is_dtype(dtype) || !is_act(act)) return STAR_ERR_INVALID_ARG;
-    UnpackArgs a{};
+    ReadArgs a{};
     Extent read[3], written;
     star_status_t st = check_kept(codes, scales, rows, cols, &a.kept, read);
     if (st == STAR_OK) st = check_matrix(dy, rows, cols, ld_dy, dtype_size(dtype), &read[2]);

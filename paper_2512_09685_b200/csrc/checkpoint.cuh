@@ -104,24 +104,228 @@ struct PackArgs {
     int64_t ld_act;
 };
 
-constexpr int kPackThreads = 256;
+struct ReadArgs {
+    Kept kept;
+    void *out;
+    int64_t ld;
+    const void *dy;      // BACKWARD only
+    int64_t ld_dy;
+};
 
-// One warp per block of 32 columns, one lane per element.
-template <typename G, int ACT> __global__ void __launch_bounds__(kPackThreads) star_checkpoint_pack_kernel(const __grid_constant__ PackArgs a)
+constexpr int kKeepThreads = 256;
+
+// ---------------------------------------------------------------------------
+// Rows whose values start on 16-byte boundaries: a thread takes half a block, 16
+// columns, and its neighbour the other half; all accesses are 16 bytes.  The
+// work is numbered row by row, an even number of halves to a row, so that two
+// neighbouring lanes always share a block.
+//
+// Bound by memory: 16384 x 4096 bf16, kept with GELU forward (5.03 bytes an
+// element), restored (3.03), GELU backward (5.03).  An exponential and a
+// reciprocal per element take 70 % of the forward's time on their unit.
+// ---------------------------------------------------------------------------
+
+// i / d for i < 2^31 and the divisor the host made `magic` and `shift` from.
+struct Divisor {
+    uint32_t d, magic;
+    int shift;
+};
+__device__ __forceinline__ uint32_t divide(uint32_t i, const Divisor &d) { return d.d == 1 ? i : __umulhi(i, d.magic) >> d.shift; }
+
+struct Halves {
+    Divisor per_row;     // halves of a row: an even number
+    uint32_t first_row;  // rows in front of this launch
+    uint32_t n;          // halves of this launch
+};
+
+template <typename G> struct Sixteen {
+    static constexpr int kWords = G::kBytes * 4;
+    // 16 values of a row from column c on; columns past the end read as 0.
+    static __device__ __forceinline__ void load(const void *row, int64_t c, int64_t cols, uint32_t (&w)[kWords])
+    {
+        const char *p = static_cast<const char *>(row) + c * G::kBytes;
+        if (c + 16 <= cols) {
+#pragma unroll
+            for (int q = 0; q < kWords / 4; ++q) {
+                const uint4 v = reinterpret_cast<const uint4 *>(p)[q];
+                w[4 * q] = v.x; w[4 * q + 1] = v.y; w[4 * q + 2] = v.z; w[4 * q + 3] = v.w;
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < kWords; ++q) w[q] = 0;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                if (c + e < cols) {
+                    if constexpr (G::kBytes == 2)
+                        w[e / 2] |= static_cast<uint32_t>(reinterpret_cast<const unsigned short *>(p)[e]) << (e % 2 * 16);
+                    else
+                        w[e] = reinterpret_cast<const uint32_t *>(p)[e];
+                }
+            }
+        }
+    }
+    static __device__ __forceinline__ void widen(const uint32_t (&w)[kWords], float (&f)[16])
+    {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            if constexpr (G::kBytes == 2)
+                f[e] = __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+            else
+                f[e] = __uint_as_float(w[e]);
+        }
+    }
+    // Bits of the largest magnitude as a binary32 (NaN above infinity above the rest).
+    static __device__ __forceinline__ uint32_t largest(const uint32_t (&w)[kWords])
+    {
+        uint32_t m = 0;
+        if constexpr (G::kBytes == 2) {
+#pragma unroll
+            for (int q = 0; q < kWords; ++q) m = __vmaxu2(m, w[q] & 0x7fff7fffu);
+            return max(m << 16, m & 0xffff0000u);
+        } else {
+#pragma unroll
+            for (int q = 0; q < kWords; ++q) m = max(m, w[q] & 0x7fffffffu);
+            return m;
+        }
+    }
+    static __device__ __forceinline__ void store(void *row, int64_t c, int64_t cols, const float (&f)[16])
+    {
+        char *p = static_cast<char *>(row) + c * G::kBytes;
+        uint32_t w[kWords];
+#pragma unroll
+        for (int q = 0; q < kWords; ++q) {
+            if constexpr (G::kBytes == 2)
+                w[q] = pack_bf16(f[2 * q], f[2 * q + 1]);
+            else
+                w[q] = __float_as_uint(f[q]);
+        }
+        if (c + 16 <= cols) {
+#pragma unroll
+            for (int q = 0; q < kWords / 4; ++q) reinterpret_cast<uint4 *>(p)[q] = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                if (c + e < cols) {
+                    if constexpr (G::kBytes == 2)
+                        reinterpret_cast<unsigned short *>(p)[e] = static_cast<unsigned short>(w[e / 2] >> (e % 2 * 16));
+                    else
+                        reinterpret_cast<uint32_t *>(p)[e] = w[e];
+                }
+            }
+        }
+    }
+};
+
+template <typename G, int ACT>
+__global__ void __launch_bounds__(kKeepThreads) star_checkpoint_pack_kernel(const __grid_constant__ PackArgs a, const __grid_constant__ Halves h)
+{
+    // Whole warps go round the loop: neighbours exchange their magnitudes.
+    for (uint32_t base = blockIdx.x * kKeepThreads; base < h.n; base += gridDim.x * kKeepThreads) {
+        const uint32_t i = base + threadIdx.x;
+        const uint32_t row = divide(i, h.per_row), half = i - row * h.per_row.d;
+        const int64_t t = static_cast<int64_t>(h.first_row) + row, c = static_cast<int64_t>(half) * 16;
+        const bool in = i < h.n && c < a.kept.cols;
+        uint32_t w[Sixteen<G>::kWords];
+        uint32_t largest = 0;
+        if (in) {
+            Sixteen<G>::load(static_cast<const char *>(a.x) + t * a.ld * G::kBytes, c, a.kept.cols, w);
+            largest = Sixteen<G>::largest(w);
+        }
+        largest = max(largest, __shfl_xor_sync(0xffffffffu, largest, 1));
+        if (!in) continue;
+        const int s = scale_byte(largest);
+        const float inverse = scale_inverse(s);
+        float f[16];
+        Sixteen<G>::widen(w, f);
+        uint32_t codes[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t lo = __byte_perm(code_bits(f[4 * q], inverse), code_bits(f[4 * q + 1], inverse), 0x0040);
+            const uint32_t hi = __byte_perm(code_bits(f[4 * q + 2], inverse), code_bits(f[4 * q + 3], inverse), 0x0040);
+            codes[q] = s == 255 ? 0u : __byte_perm(lo, hi, 0x5410);
+        }
+        *reinterpret_cast<uint4 *>(a.kept.codes + t * a.kept.pitch + c) = make_uint4(codes[0], codes[1], codes[2], codes[3]);
+        if (half % 2 == 0) a.kept.scales[scale_at(a.kept, t, half / 2)] = static_cast<uint8_t>(s);
+        if (a.act_out) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) f[e] = activation<ACT>(f[e]);
+            Sixteen<G>::store(static_cast<char *>(a.act_out) + t * a.ld_act * G::kBytes, c, a.kept.cols, f);
+        }
+    }
+}
+
+// Values of 16 codes; see weight_grad.cuh for the arithmetic.
+__device__ __forceinline__ void widen_sixteen(const uint4 &codes, float scale, float (&f)[16])
+{
+    const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
+    const float off = __fmul_rn(scale, -8388736.0f);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const uint32_t u = w[q] ^ 0x80808080u;
+        f[4 * q] = __fmaf_rn(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7650)), scale, off);
+        f[4 * q + 1] = __fmaf_rn(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7651)), scale, off);
+        f[4 * q + 2] = __fmaf_rn(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7652)), scale, off);
+        f[4 * q + 3] = __fmaf_rn(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7653)), scale, off);
+    }
+}
+
+// out = act(value), or dy * act'(value).
+template <typename G, int ACT, bool BACKWARD>
+__global__ void __launch_bounds__(kKeepThreads) star_checkpoint_read_kernel(const __grid_constant__ ReadArgs a, const __grid_constant__ Halves h)
+{
+    for (uint32_t i = blockIdx.x * kKeepThreads + threadIdx.x; i < h.n; i += gridDim.x * kKeepThreads) {
+        const uint32_t row = divide(i, h.per_row), half = i - row * h.per_row.d;
+        const int64_t t = static_cast<int64_t>(h.first_row) + row, c = static_cast<int64_t>(half) * 16;
+        if (c >= a.kept.cols) continue;
+        const uint4 codes = *reinterpret_cast<const uint4 *>(a.kept.codes + t * a.kept.pitch + c);
+        const float scale = scale_value(a.kept.scales[scale_at(a.kept, t, half / 2)]);
+        uint32_t w[Sixteen<G>::kWords];
+        if constexpr (BACKWARD) Sixteen<G>::load(static_cast<const char *>(a.dy) + t * a.ld_dy * G::kBytes, c, a.kept.cols, w);
+        float f[16];
+        widen_sixteen(codes, scale, f);
+        if constexpr (BACKWARD) {
+            float dy[16];
+            Sixteen<G>::widen(w, dy);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) f[e] = __fmul_rn(dy[e], activation_slope<ACT>(f[e]));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) f[e] = activation<ACT>(f[e]);
+        }
+        Sixteen<G>::store(static_cast<char *>(a.out) + t * a.ld * G::kBytes, c, a.kept.cols, f);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Any alignment: one warp per block, one lane per element, kLoose blocks of a
+// warp's in flight.
+// ---------------------------------------------------------------------------
+constexpr int kLoose = 4;
+
+template <typename G, int ACT> __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_pack_loose_kernel(const __grid_constant__ PackArgs a)
 {
     const int lane = threadIdx.x % 32;
-    const int64_t blocks = (a.kept.cols + 31) / 32, n = a.kept.rows * blocks;
-    for (int64_t i = blockIdx.x * static_cast<int64_t>(kPackThreads / 32) + threadIdx.x / 32; i < n;
-         i += gridDim.x * static_cast<int64_t>(kPackThreads / 32)) {
-        const int64_t t = i / blocks, b = i % blocks, c = b * 32 + lane;
-        const bool in = c < a.kept.cols;
-        const float x = in ? load_value<G>(a.x, t * a.ld + c) : 0.0f;
-        const uint32_t largest = __reduce_max_sync(0xffffffffu, __float_as_uint(x) & 0x7fffffffu);
-        const int s = scale_byte(largest);
-        if (c < a.kept.pitch)
-            a.kept.codes[t * a.kept.pitch + c] = s == 255 ? 0 : static_cast<int8_t>(code_bits(x, scale_inverse(s)) & 0xffu);
-        if (lane == 0) a.kept.scales[scale_at(a.kept, t, b)] = static_cast<uint8_t>(s);
-        if (a.act_out && in) store_value<G>(a.act_out, t * a.ld_act + c, activation<ACT>(x));
+    const int64_t blocks = (a.kept.cols + 31) / 32, groups = (blocks + kLoose - 1) / kLoose, n = a.kept.rows * groups;
+    for (int64_t i = blockIdx.x * static_cast<int64_t>(kKeepThreads / 32) + threadIdx.x / 32; i < n;
+         i += gridDim.x * static_cast<int64_t>(kKeepThreads / 32)) {
+        const int64_t t = i / groups, b0 = i % groups * kLoose;
+        float x[kLoose];
+#pragma unroll
+        for (int q = 0; q < kLoose; ++q) {
+            const int64_t c = (b0 + q) * 32 + lane;
+            x[q] = c < a.kept.cols ? load_value<G>(a.x, t * a.ld + c) : 0.0f;
+        }
+#pragma unroll
+        for (int q = 0; q < kLoose; ++q) {
+            const int64_t b = b0 + q, c = b * 32 + lane;
+            if (b >= blocks) break;
+            const uint32_t largest = __reduce_max_sync(0xffffffffu, __float_as_uint(x[q]) & 0x7fffffffu);
+            const int s = scale_byte(largest);
+            if (c < a.kept.pitch)
+                a.kept.codes[t * a.kept.pitch + c] = s == 255 ? 0 : static_cast<int8_t>(code_bits(x[q], scale_inverse(s)) & 0xffu);
+            if (lane == 0) a.kept.scales[scale_at(a.kept, t, b)] = static_cast<uint8_t>(s);
+            if (a.act_out && c < a.kept.cols) store_value<G>(a.act_out, t * a.ld_act + c, activation<ACT>(x[q]));
+        }
     }
 }
 
@@ -130,29 +334,27 @@ __device__ __forceinline__ float kept_value(const Kept &k, int64_t t, int64_t c)
     return __fmul_rn(static_cast<float>(k.codes[t * k.pitch + c]), scale_value(k.scales[scale_at(k, t, c / 32)]));
 }
 
-struct UnpackArgs {
-    Kept kept;
-    void *out;
-    int64_t ld;
-    const void *dy;      // BACKWARD only
-    int64_t ld_dy;
-};
-
-// out = act(value), or dy * act'(value).
 template <typename G, int ACT, bool BACKWARD>
-__global__ void __launch_bounds__(kPackThreads) star_checkpoint_read_kernel(const __grid_constant__ UnpackArgs a)
+__global__ void __launch_bounds__(kKeepThreads) star_checkpoint_read_loose_kernel(const __grid_constant__ ReadArgs a)
 {
-    const int64_t n = a.kept.rows * a.kept.cols;
-    for (int64_t i = blockIdx.x * static_cast<int64_t>(kPackThreads) + threadIdx.x; i < n;
-         i += gridDim.x * static_cast<int64_t>(kPackThreads)) {
-        const int64_t t = i / a.kept.cols, c = i % a.kept.cols;
-        const float x = kept_value(a.kept, t, c);
-        float y;
-        if constexpr (BACKWARD)
-            y = __fmul_rn(load_value<G>(a.dy, t * a.ld_dy + c), activation_slope<ACT>(x));
-        else
-            y = activation<ACT>(x);
-        store_value<G>(a.out, t * a.ld + c, y);
+    const int lane = threadIdx.x % 32;
+    const int64_t blocks = (a.kept.cols + 31) / 32, groups = (blocks + kLoose - 1) / kLoose, n = a.kept.rows * groups;
+    for (int64_t i = blockIdx.x * static_cast<int64_t>(kKeepThreads / 32) + threadIdx.x / 32; i < n;
+         i += gridDim.x * static_cast<int64_t>(kKeepThreads / 32)) {
+        const int64_t t = i / groups, c0 = i % groups * kLoose * 32 + lane;
+        float x[kLoose], dy[kLoose];
+#pragma unroll
+        for (int q = 0; q < kLoose; ++q) {
+            const int64_t c = c0 + 32 * q;
+            x[q] = c < a.kept.cols ? kept_value(a.kept, t, c) : 0.0f;
+            dy[q] = BACKWARD && c < a.kept.cols ? load_value<G>(a.dy, t * a.ld_dy + c) : 0.0f;
+        }
+#pragma unroll
+        for (int q = 0; q < kLoose; ++q) {
+            const int64_t c = c0 + 32 * q;
+            if (c < a.kept.cols)
+                store_value<G>(a.out, t * a.ld + c, BACKWARD ? __fmul_rn(dy[q], activation_slope<ACT>(x[q])) : activation<ACT>(x[q]));
+        }
     }
 }
 
