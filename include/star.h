@@ -587,7 +587,10 @@ STAR_API star_status_t star_preference_loss(const void *logits, star_dtype_t dty
  *            then the next row: byte ((c / 128) * tall + t) * 4 + (c / 32) % 4 for
  *            element (t, c), tall = rows rounded up to a multiple of 64 (bytes of
  *            rows past `rows` and of blocks past cols are not used).  16-byte aligned
- * star_checkpoint_sizes gives pitch and the bytes of both (8.25 bits an element). */
+ * star_checkpoint_sizes gives pitch and the bytes of both (8.25 bits an element).
+ * The calls below take up to 2^31 - 1 rows and 2^32 columns (STAR_ERR_UNSUPPORTED
+ * beyond) and launch one kernel (pack, unpack and act_backward: one per 2^34
+ * elements). */
 STAR_API star_status_t star_checkpoint_sizes(int64_t rows, int64_t cols, int64_t *pitch_out,
                                              size_t *code_bytes_out, size_t *scale_bytes_out);
 
@@ -604,20 +607,19 @@ typedef enum {
 /* Forward pass: keeps x (rows x cols of dtype, stride ld) in codes and scales
  * and, where act_out is given, writes act(x) to it in the same pass over x
  * (rows x cols of dtype, stride ld_act; the activation of x itself, not of its
- * kept value; may be x: same pointer and stride).  One kernel launch. */
+ * kept value; may be x: same pointer and stride). */
 STAR_API star_status_t star_checkpoint_pack(int8_t *codes, uint8_t *scales, const void *x, star_dtype_t dtype,
                                             int64_t rows, int64_t cols, int64_t ld, star_activation_t act,
                                             void *act_out, int64_t ld_act, void *cuda_stream);
 
 /* out = act(value) for every kept value (STAR_ACT_NONE: the value itself,
- * exact).  out: rows x cols of dtype, stride ld.  One kernel launch. */
+ * exact).  out: rows x cols of dtype, stride ld. */
 STAR_API star_status_t star_checkpoint_unpack(void *out, star_dtype_t dtype, int64_t ld, const int8_t *codes,
                                               const uint8_t *scales, int64_t rows, int64_t cols,
                                               star_activation_t act, void *cuda_stream);
 
 /* Backward pass of an activation whose input was kept: dx = dy * act'(value).
- * dx, dy: rows x cols of dtype; dx may be dy (same pointer and stride).  One
- * kernel launch. */
+ * dx, dy: rows x cols of dtype; dx may be dy (same pointer and stride). */
 STAR_API star_status_t star_checkpoint_act_backward(void *dx, int64_t ld_dx, const void *dy, int64_t ld_dy,
                                                     star_dtype_t dtype, const int8_t *codes,
                                                     const uint8_t *scales, int64_t rows, int64_t cols,

@@ -27,30 +27,31 @@ Divisor make_divisor(uint32_t d)
     return r;
 }
 
-// Runs launch(halves, grid) on the rows in runs of less than 2^31 halves (one,
-// for all but checkpoints of 32 GB and more).
-template <typename F> star_status_t by_halves(int64_t rows, int64_t cols, F launch)
+// Runs launch(items, grid) on the rows in runs of at most 2^30 items, `per_row`
+// of them to a row (one run, for all but checkpoints of 16 GB and more).
+template <typename Items, typename F> star_status_t by_rows(int64_t rows, int64_t per_row, int items_per_block, F launch)
 {
-    const int64_t per_row = (cols + 31) / 32 * 2;
     const int64_t most = (int64_t{1} << 30) / per_row;
     for (int64_t first = 0; first < rows; first += most) {
         const int64_t n = std::min(most, rows - first) * per_row;
-        launch(Halves{make_divisor(static_cast<uint32_t>(per_row)), static_cast<uint32_t>(first), static_cast<uint32_t>(n)},
-               grid_for((n + kKeepThreads - 1) / kKeepThreads));
+        launch(Items{make_divisor(static_cast<uint32_t>(per_row)), static_cast<uint32_t>(first), static_cast<uint32_t>(n)},
+               grid_for((n + items_per_block - 1) / items_per_block));
         const star_status_t st = launched();
         if (st != STAR_OK) return st;
     }
     return STAR_OK;
 }
-
-// The 16-byte kernels number rows and halves of a row in 32 bits.
-bool countable(int64_t rows, int64_t cols) { return rows <= 0x7fffffff && cols <= (int64_t{1} << 32); }
-
-int loose_grid(int64_t rows, int64_t cols)
+template <typename F> star_status_t by_halves(int64_t rows, int64_t cols, F launch)
 {
-    const int64_t groups = ((cols + 31) / 32 + kLoose - 1) / kLoose, per_block = kKeepThreads / 32;
-    return grid_for(rows > (148 * 64 * per_block) / groups ? 148 * 64 : (rows * groups + per_block - 1) / per_block);
+    return by_rows<Halves>(rows, (cols + 31) / 32 * 2, kKeepThreads, launch);
 }
+template <typename F> star_status_t by_groups(int64_t rows, int64_t cols, F launch)
+{
+    return by_rows<Groups>(rows, ((cols + 31) / 32 + kLoose - 1) / kLoose, kKeepThreads / 32, launch);
+}
+
+// Rows and the items of a row are numbered in 32 bits.
+bool countable(int64_t rows, int64_t cols) { return rows <= 0x7fffffff && cols <= (int64_t{1} << 32); }
 
 // Calls f with the activation as a compile-time number.
 template <typename F> void with_act(int act, F f)
@@ -99,8 +100,9 @@ extern "C" star_status_t star_checkpoint_pack(int8_t *codes, uint8_t *scales, co
     a.act_out = act_out;
     a.ld_act = ld_act;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (!countable(rows, cols)) return STAR_ERR_UNSUPPORTED;
     const int size = dtype_size(dtype);
-    const bool vector = on_grid(x, ld, size) && (!act_out || on_grid(act_out, ld_act, size)) && countable(rows, cols);
+    const bool vector = on_grid(x, ld, size) && (!act_out || on_grid(act_out, ld_act, size));
     with_act(act, [&](auto k) {
         constexpr int ACT = decltype(k)::value;
         if (vector)
@@ -110,12 +112,15 @@ extern "C" star_status_t star_checkpoint_pack(int8_t *codes, uint8_t *scales, co
                 else
                     star_checkpoint_pack_kernel<GradF32, ACT><<<grid, kKeepThreads, 0, stream>>>(a, h);
             });
-        else if (dtype == STAR_DTYPE_BF16)
-            star_checkpoint_pack_loose_kernel<GradBF16, ACT><<<loose_grid(rows, cols), kKeepThreads, 0, stream>>>(a);
         else
-            star_checkpoint_pack_loose_kernel<GradF32, ACT><<<loose_grid(rows, cols), kKeepThreads, 0, stream>>>(a);
+            st = by_groups(rows, cols, [&](const Groups &h, int grid) {
+                if (dtype == STAR_DTYPE_BF16)
+                    star_checkpoint_pack_loose_kernel<GradBF16, ACT><<<grid, kKeepThreads, 0, stream>>>(a, h);
+                else
+                    star_checkpoint_pack_loose_kernel<GradF32, ACT><<<grid, kKeepThreads, 0, stream>>>(a, h);
+            });
     });
-    return vector ? st : launched();
+    return st;
 }
 
 namespace {
@@ -123,8 +128,9 @@ namespace {
 template <bool BACKWARD> star_status_t read_kept(const ReadArgs &a, star_dtype_t dtype, int act, void *cuda_stream)
 {
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (!countable(a.kept.rows, a.kept.cols)) return STAR_ERR_UNSUPPORTED;
     const int size = dtype_size(dtype);
-    const bool vector = on_grid(a.out, a.ld, size) && (!BACKWARD || on_grid(a.dy, a.ld_dy, size)) && countable(a.kept.rows, a.kept.cols);
+    const bool vector = on_grid(a.out, a.ld, size) && (!BACKWARD || on_grid(a.dy, a.ld_dy, size));
     star_status_t st = STAR_OK;
     with_act(act, [&](auto k) {
         constexpr int ACT = decltype(k)::value;
@@ -135,12 +141,15 @@ template <bool BACKWARD> star_status_t read_kept(const ReadArgs &a, star_dtype_t
                 else
                     star_checkpoint_read_kernel<GradF32, ACT, BACKWARD><<<grid, kKeepThreads, 0, stream>>>(a, h);
             });
-        else if (dtype == STAR_DTYPE_BF16)
-            star_checkpoint_read_loose_kernel<GradBF16, ACT, BACKWARD><<<loose_grid(a.kept.rows, a.kept.cols), kKeepThreads, 0, stream>>>(a);
         else
-            star_checkpoint_read_loose_kernel<GradF32, ACT, BACKWARD><<<loose_grid(a.kept.rows, a.kept.cols), kKeepThreads, 0, stream>>>(a);
+            st = by_groups(a.kept.rows, a.kept.cols, [&](const Groups &h, int grid) {
+                if (dtype == STAR_DTYPE_BF16)
+                    star_checkpoint_read_loose_kernel<GradBF16, ACT, BACKWARD><<<grid, kKeepThreads, 0, stream>>>(a, h);
+                else
+                    star_checkpoint_read_loose_kernel<GradF32, ACT, BACKWARD><<<grid, kKeepThreads, 0, stream>>>(a, h);
+            });
     });
-    return vector ? st : launched();
+    return st;
 }
 
 }  // namespace

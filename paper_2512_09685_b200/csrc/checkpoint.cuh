@@ -85,15 +85,29 @@ template <> __device__ __forceinline__ float activation_slope<STAR_ACT_SILU>(flo
     return __fmaf_rn(__fmul_rn(q, __fsub_rn(1.0f, q)), x, q);
 }
 
-template <> __device__ __forceinline__ float activation<STAR_ACT_GELU_ERF>(float x)
+// Phi(x) and exp(-x^2 / 2) by Abramowitz and Stegun 7.1.26 (Hastings): with
+// z = |x| / sqrt(2) and t = 1 / (1 + p z), erfc(z) = (a1 t + ... + a5 t^5)
+// exp(-z^2), off by at most 1.5e-7.  One exponential and one reciprocal, and the
+// slope needs the same exponential.
+struct NormalCdf {
+    float cdf, power;
+};
+__device__ __forceinline__ NormalCdf normal_cdf(float x)
 {
-    return __fmul_rn(__fmul_rn(0.5f, x), __fadd_rn(1.0f, erff(__fmul_rn(x, kSqrtHalf))));
+    const float t = __fdividef(1.0f, __fmaf_rn(0.3275911f * kSqrtHalf, fabsf(x), 1.0f));
+    const float power = exp2_fast(__fmul_rn(-0.5f * kLog2e, __fmul_rn(x, x)));
+    float q = __fmaf_rn(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+    q = __fmaf_rn(t, q, 0.5f * 1.421413741f);
+    q = __fmaf_rn(t, q, 0.5f * -0.284496736f);
+    q = __fmaf_rn(t, q, 0.5f * 0.254829592f);
+    q = __fmul_rn(__fmul_rn(t, q), power);               // erfc(z) / 2
+    return NormalCdf{x > 0.0f ? __fsub_rn(1.0f, q) : q, power};
 }
+template <> __device__ __forceinline__ float activation<STAR_ACT_GELU_ERF>(float x) { return __fmul_rn(x, normal_cdf(x).cdf); }
 template <> __device__ __forceinline__ float activation_slope<STAR_ACT_GELU_ERF>(float x)
 {
-    const float cdf = __fmaf_rn(0.5f, erff(__fmul_rn(x, kSqrtHalf)), 0.5f);
-    const float pdf = __fmul_rn(kInvSqrt2Pi, exp2_fast(__fmul_rn(-0.5f * kLog2e, __fmul_rn(x, x))));
-    return __fmaf_rn(x, pdf, cdf);
+    const NormalCdf n = normal_cdf(x);
+    return __fmaf_rn(x, __fmul_rn(kInvSqrt2Pi, n.power), n.cdf);
 }
 
 struct PackArgs {
@@ -140,26 +154,27 @@ struct Halves {
 
 template <typename G> struct Sixteen {
     static constexpr int kWords = G::kBytes * 4;
+    static constexpr int kEach = 16 / G::kBytes;         // values in 16 bytes
     // 16 values of a row from column c on; columns past the end read as 0.
     static __device__ __forceinline__ void load(const void *row, int64_t c, int64_t cols, uint32_t (&w)[kWords])
     {
         const char *p = static_cast<const char *>(row) + c * G::kBytes;
-        if (c + 16 <= cols) {
+        const int left = static_cast<int>(min(cols - c, int64_t{16}));
 #pragma unroll
-            for (int q = 0; q < kWords / 4; ++q) {
+        for (int q = 0; q < kWords / 4; ++q) {
+            if ((q + 1) * kEach <= left) {
                 const uint4 v = reinterpret_cast<const uint4 *>(p)[q];
                 w[4 * q] = v.x; w[4 * q + 1] = v.y; w[4 * q + 2] = v.z; w[4 * q + 3] = v.w;
-            }
-        } else {
+            } else {
+                w[4 * q] = w[4 * q + 1] = w[4 * q + 2] = w[4 * q + 3] = 0;
 #pragma unroll
-            for (int q = 0; q < kWords; ++q) w[q] = 0;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                if (c + e < cols) {
-                    if constexpr (G::kBytes == 2)
-                        w[e / 2] |= static_cast<uint32_t>(reinterpret_cast<const unsigned short *>(p)[e]) << (e % 2 * 16);
-                    else
-                        w[e] = reinterpret_cast<const uint32_t *>(p)[e];
+                for (int e = q * kEach; e < (q + 1) * kEach; ++e) {
+                    if (e < left) {
+                        if constexpr (G::kBytes == 2)
+                            w[e / 2] |= static_cast<uint32_t>(reinterpret_cast<const unsigned short *>(p)[e]) << (e % 2 * 16);
+                        else
+                            w[e] = reinterpret_cast<const uint32_t *>(p)[e];
+                    }
                 }
             }
         }
@@ -199,17 +214,20 @@ template <typename G> struct Sixteen {
             else
                 w[q] = __float_as_uint(f[q]);
         }
-        if (c + 16 <= cols) {
+        const int left = static_cast<int>(min(cols - c, int64_t{16}));
 #pragma unroll
-            for (int q = 0; q < kWords / 4; ++q) reinterpret_cast<uint4 *>(p)[q] = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
-        } else {
+        for (int q = 0; q < kWords / 4; ++q) {
+            if ((q + 1) * kEach <= left) {
+                reinterpret_cast<uint4 *>(p)[q] = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+            } else {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                if (c + e < cols) {
-                    if constexpr (G::kBytes == 2)
-                        reinterpret_cast<unsigned short *>(p)[e] = static_cast<unsigned short>(w[e / 2] >> (e % 2 * 16));
-                    else
-                        reinterpret_cast<uint32_t *>(p)[e] = w[e];
+                for (int e = q * kEach; e < (q + 1) * kEach; ++e) {
+                    if (e < left) {
+                        if constexpr (G::kBytes == 2)
+                            reinterpret_cast<unsigned short *>(p)[e] = static_cast<unsigned short>(w[e / 2] >> (e % 2 * 16));
+                        else
+                            reinterpret_cast<uint32_t *>(p)[e] = w[e];
+                    }
                 }
             }
         }
@@ -297,63 +315,71 @@ __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_read_kernel(cons
 }
 
 // ---------------------------------------------------------------------------
-// Any alignment: one warp per block, one lane per element, kLoose blocks of a
-// warp's in flight.
+// Any alignment: one lane per element, a warp on kLoose neighbouring blocks of a
+// row at a time.  Bound by instructions, two to three times slower.
 // ---------------------------------------------------------------------------
-constexpr int kLoose = 4;
+constexpr int kLoose = 8;
 
-template <typename G, int ACT> __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_pack_loose_kernel(const __grid_constant__ PackArgs a)
+struct Groups {
+    Divisor per_row;     // groups of kLoose blocks in a row
+    uint32_t first_row;
+    uint32_t n;          // groups of this launch
+};
+
+template <typename G, int ACT>
+__global__ void __launch_bounds__(kKeepThreads) star_checkpoint_pack_loose_kernel(const __grid_constant__ PackArgs a, const __grid_constant__ Groups h)
 {
     const int lane = threadIdx.x % 32;
-    const int64_t blocks = (a.kept.cols + 31) / 32, groups = (blocks + kLoose - 1) / kLoose, n = a.kept.rows * groups;
-    for (int64_t i = blockIdx.x * static_cast<int64_t>(kKeepThreads / 32) + threadIdx.x / 32; i < n;
-         i += gridDim.x * static_cast<int64_t>(kKeepThreads / 32)) {
-        const int64_t t = i / groups, b0 = i % groups * kLoose;
+    for (uint32_t i = blockIdx.x * (kKeepThreads / 32) + threadIdx.x / 32; i < h.n; i += gridDim.x * (kKeepThreads / 32)) {
+        const uint32_t row = divide(i, h.per_row), group = i - row * h.per_row.d;
+        const int64_t t = static_cast<int64_t>(h.first_row) + row, c0 = static_cast<int64_t>(group) * (kLoose * 32) + lane;
+        const char *src = static_cast<const char *>(a.x) + (t * a.ld + c0) * G::kBytes;
+        const int left = static_cast<int>(min(a.kept.cols - c0, static_cast<int64_t>(kLoose * 32)));       // this lane's elements lie below
+        const int left_code = static_cast<int>(min(a.kept.pitch - c0, static_cast<int64_t>(kLoose * 32)));
+        const int blocks = static_cast<int>(min((a.kept.cols - (c0 - lane) + 31) / 32, static_cast<int64_t>(kLoose)));
         float x[kLoose];
 #pragma unroll
-        for (int q = 0; q < kLoose; ++q) {
-            const int64_t c = (b0 + q) * 32 + lane;
-            x[q] = c < a.kept.cols ? load_value<G>(a.x, t * a.ld + c) : 0.0f;
-        }
+        for (int q = 0; q < kLoose; ++q) x[q] = 32 * q < left ? load_value<G>(src, 32 * q) : 0.0f;
+        int8_t *codes = a.kept.codes + t * a.kept.pitch + c0;
+        uint8_t *scales = a.kept.scales + scale_at(a.kept, t, static_cast<int64_t>(group) * kLoose);
+        char *out = static_cast<char *>(a.act_out) + (t * a.ld_act + c0) * G::kBytes;
 #pragma unroll
         for (int q = 0; q < kLoose; ++q) {
-            const int64_t b = b0 + q, c = b * 32 + lane;
-            if (b >= blocks) break;
+            if (q >= blocks) break;
             const uint32_t largest = __reduce_max_sync(0xffffffffu, __float_as_uint(x[q]) & 0x7fffffffu);
             const int s = scale_byte(largest);
-            if (c < a.kept.pitch)
-                a.kept.codes[t * a.kept.pitch + c] = s == 255 ? 0 : static_cast<int8_t>(code_bits(x[q], scale_inverse(s)) & 0xffu);
-            if (lane == 0) a.kept.scales[scale_at(a.kept, t, b)] = static_cast<uint8_t>(s);
-            if (a.act_out && c < a.kept.cols) store_value<G>(a.act_out, t * a.ld_act + c, activation<ACT>(x[q]));
+            if (32 * q < left_code) codes[32 * q] = s == 255 ? 0 : static_cast<int8_t>(code_bits(x[q], scale_inverse(s)) & 0xffu);
+            if (lane == 0) scales[q / 4 * 4 * a.kept.tall + q % 4] = static_cast<uint8_t>(s);
+            if (a.act_out && 32 * q < left) store_value<G>(out, 32 * q, activation<ACT>(x[q]));
         }
     }
 }
 
-__device__ __forceinline__ float kept_value(const Kept &k, int64_t t, int64_t c)
-{
-    return __fmul_rn(static_cast<float>(k.codes[t * k.pitch + c]), scale_value(k.scales[scale_at(k, t, c / 32)]));
-}
-
 template <typename G, int ACT, bool BACKWARD>
-__global__ void __launch_bounds__(kKeepThreads) star_checkpoint_read_loose_kernel(const __grid_constant__ ReadArgs a)
+__global__ void __launch_bounds__(kKeepThreads) star_checkpoint_read_loose_kernel(const __grid_constant__ ReadArgs a, const __grid_constant__ Groups h)
 {
     const int lane = threadIdx.x % 32;
-    const int64_t blocks = (a.kept.cols + 31) / 32, groups = (blocks + kLoose - 1) / kLoose, n = a.kept.rows * groups;
-    for (int64_t i = blockIdx.x * static_cast<int64_t>(kKeepThreads / 32) + threadIdx.x / 32; i < n;
-         i += gridDim.x * static_cast<int64_t>(kKeepThreads / 32)) {
-        const int64_t t = i / groups, c0 = i % groups * kLoose * 32 + lane;
-        float x[kLoose], dy[kLoose];
+    for (uint32_t i = blockIdx.x * (kKeepThreads / 32) + threadIdx.x / 32; i < h.n; i += gridDim.x * (kKeepThreads / 32)) {
+        const uint32_t row = divide(i, h.per_row), group = i - row * h.per_row.d;
+        const int64_t t = static_cast<int64_t>(h.first_row) + row, c0 = static_cast<int64_t>(group) * (kLoose * 32) + lane;
+        const int left = static_cast<int>(min(a.kept.cols - c0, static_cast<int64_t>(kLoose * 32)));
+        const int8_t *codes = a.kept.codes + t * a.kept.pitch + c0;
+        const uint8_t *scales = a.kept.scales + scale_at(a.kept, t, static_cast<int64_t>(group) * kLoose);
+        const char *src = static_cast<const char *>(a.dy) + (t * a.ld_dy + c0) * G::kBytes;
+        char *out = static_cast<char *>(a.out) + (t * a.ld + c0) * G::kBytes;
+        int code[kLoose];
+        float scale[kLoose], dy[kLoose];
 #pragma unroll
         for (int q = 0; q < kLoose; ++q) {
-            const int64_t c = c0 + 32 * q;
-            x[q] = c < a.kept.cols ? kept_value(a.kept, t, c) : 0.0f;
-            dy[q] = BACKWARD && c < a.kept.cols ? load_value<G>(a.dy, t * a.ld_dy + c) : 0.0f;
+            const bool in = 32 * q < left;
+            code[q] = in ? codes[32 * q] : 0;
+            scale[q] = in ? scale_value(scales[q / 4 * 4 * a.kept.tall + q % 4]) : 0.0f;
+            dy[q] = BACKWARD && in ? load_value<G>(src, 32 * q) : 0.0f;
         }
 #pragma unroll
         for (int q = 0; q < kLoose; ++q) {
-            const int64_t c = c0 + 32 * q;
-            if (c < a.kept.cols)
-                store_value<G>(a.out, t * a.ld + c, BACKWARD ? __fmul_rn(dy[q], activation_slope<ACT>(x[q])) : activation<ACT>(x[q]));
+            const float x = __fmul_rn(static_cast<float>(code[q]), scale[q]);
+            if (32 * q < left) store_value<G>(out, 32 * q, BACKWARD ? __fmul_rn(dy[q], activation_slope<ACT>(x)) : activation<ACT>(x));
         }
     }
 }
@@ -367,38 +393,5 @@ struct WeightGradArgs {
     int64_t outs;
     int accumulate;
 };
-
-// 32 x 32 outputs per block, 32 rows at a time.
-template <typename GY, typename GW> __global__ void __launch_bounds__(256) star_weight_grad_kernel(const __grid_constant__ WeightGradArgs a)
-{
-    __shared__ float xs[32][33], ys[32][33];
-    const int64_t c0 = static_cast<int64_t>(blockIdx.x) * 32, tiles = (a.outs + 31) / 32;
-    const int lane = threadIdx.x % 32, w = threadIdx.x / 32;
-    for (int64_t tile = blockIdx.y; tile < tiles; tile += gridDim.y) {
-        const int64_t o0 = tile * 32;
-        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int64_t t0 = 0; t0 < a.kept.rows; t0 += 32) {
-            for (int r = w; r < 32; r += 8) {
-                const int64_t t = t0 + r;
-                xs[r][lane] = t < a.kept.rows && c0 + lane < a.kept.cols ? kept_value(a.kept, t, c0 + lane) : 0.0f;
-                ys[r][lane] = t < a.kept.rows && o0 + lane < a.outs ? load_value<GY>(a.dy, t * a.ld_dy + o0 + lane) : 0.0f;
-            }
-            __syncthreads();
-            for (int r = 0; r < 32; ++r)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) sum[q] = __fmaf_rn(ys[r][w + 8 * q], xs[r][lane], sum[q]);
-            __syncthreads();
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int64_t o = o0 + w + 8 * q, c = c0 + lane;
-            if (o < a.outs && c < a.kept.cols) {
-                const int64_t at = o * a.stride_o + c * a.stride_c;
-                if (a.accumulate) sum[q] = __fadd_rn(sum[q], load_value<GW>(a.dw, at));
-                store_value<GW>(a.dw, at, sum[q]);
-            }
-        }
-    }
-}
 
 }  // namespace star

@@ -2,6 +2,7 @@
 // the launch, one kernel.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "checkpoint_host.h"
 #include "weight_grad.cuh"
@@ -46,31 +47,34 @@ bool make_map(CUtensorMap *map, CUtensorMapDataType type, const void *base, int6
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The kernel comes in three shapes.  Shared memory and TMEM hold one block on an
-// SM in all of them.
-//   kWide   a pair of blocks, 256 columns x 512 outputs: a widened code serves 512
-//           outputs, 0.73 us a step of 64 rows (1.47 PFLOP/s over 148 SMs)
-//   kNarrow a pair, 256 x 256: 0.56 us, bound by the widening
-//   kSingle a block, 128 x 256: 0.56 us
-enum Shape { kWide = 0, kNarrow = 1, kSingle = 2, kShapes = 3 };
+// The kernel's shapes.  Shared memory and TMEM hold one block on an SM in all of
+// them.
+//   kWide      a pair of blocks, 256 columns x 512 outputs: a widened code serves
+//              512 outputs, 0.73 us a step of 64 rows (1.47 PFLOP/s over 148 SMs)
+//   kNarrow    a pair, 256 x 256: 0.56 us, bound by the widening
+//   kSingle    a block, 128 x 256: 0.56 us
+//   kNarrowSum, kSingleSum      the same with a running sum, for a dw in fp32
+//   kLoosePair, kLooseSingle    dy in bf16 off the 16-byte grid: 256 x 256 by a
+//              pair, 128 x 128 by a block
+//   kCutPair, kCutSingle        dy in fp32, three terms
+enum Shape { kWide, kNarrow, kSingle, kNarrowSum, kSingleSum, kLoosePair, kLooseSingle, kCutPair, kCutSingle, kShapes };
 constexpr int kMostParts = 8;
 
 template <int SHAPE> struct ShapeOf;
-template <> struct ShapeOf<kWide> {
-    static constexpr int kOuts = 512, kBlocks = 2;
-    using Smem = GradSmem<512, 4, 3, true>;
-    static constexpr auto kernel() { return star_weight_grad_tensor_kernel<512, 4, 3, true>; }
+template <int BN, int LOADS, int WIDE, bool PAIR, int TERMS, bool FLUSH> struct ShapeBase {
+    static constexpr int kOuts = BN, kBlocks = PAIR ? 2 : 1;
+    using Smem = GradSmem<BN, LOADS, WIDE, PAIR, TERMS>;
+    static constexpr auto kernel() { return star_weight_grad_tensor_kernel<BN, LOADS, WIDE, PAIR, TERMS, FLUSH>; }
 };
-template <> struct ShapeOf<kNarrow> {
-    static constexpr int kOuts = 256, kBlocks = 2;
-    using Smem = GradSmem<256, 7, 3, true>;
-    static constexpr auto kernel() { return star_weight_grad_tensor_kernel<256, 7, 3, true>; }
-};
-template <> struct ShapeOf<kSingle> {
-    static constexpr int kOuts = 256, kBlocks = 1;
-    using Smem = GradSmem<256, 4, 3, false>;
-    static constexpr auto kernel() { return star_weight_grad_tensor_kernel<256, 4, 3, false>; }
-};
+template <> struct ShapeOf<kWide> : ShapeBase<512, 4, 3, true, 0, false> {};
+template <> struct ShapeOf<kNarrow> : ShapeBase<256, 7, 3, true, 0, false> {};
+template <> struct ShapeOf<kSingle> : ShapeBase<256, 4, 3, false, 0, false> {};
+template <> struct ShapeOf<kNarrowSum> : ShapeBase<256, 7, 3, true, 0, true> {};
+template <> struct ShapeOf<kSingleSum> : ShapeBase<256, 4, 3, false, 0, true> {};
+template <> struct ShapeOf<kLoosePair> : ShapeBase<256, 4, 4, true, 1, true> {};
+template <> struct ShapeOf<kLooseSingle> : ShapeBase<128, 4, 4, false, 1, true> {};
+template <> struct ShapeOf<kCutPair> : ShapeBase<256, 4, 3, true, 3, true> {};
+template <> struct ShapeOf<kCutSingle> : ShapeBase<128, 4, 3, false, 3, true> {};
 
 void fill_config(cudaLaunchConfig_t *config, cudaLaunchAttribute *attribute, int64_t columns, int64_t down, int blocks, int parts,
                  int smem, cudaStream_t stream)
@@ -125,6 +129,12 @@ cudaError_t prepared_device(Device **out)
         e = prepare_shape<kWide>(d);
         if (e == cudaSuccess) e = prepare_shape<kNarrow>(d);
         if (e == cudaSuccess) e = prepare_shape<kSingle>(d);
+        if (e == cudaSuccess) e = prepare_shape<kNarrowSum>(d);
+        if (e == cudaSuccess) e = prepare_shape<kSingleSum>(d);
+        if (e == cudaSuccess) e = prepare_shape<kLoosePair>(d);
+        if (e == cudaSuccess) e = prepare_shape<kLooseSingle>(d);
+        if (e == cudaSuccess) e = prepare_shape<kCutPair>(d);
+        if (e == cudaSuccess) e = prepare_shape<kCutSingle>(d);
         if (e != cudaSuccess) return e;
         d.ready.store(true, std::memory_order_release);
     }
@@ -148,36 +158,45 @@ star_status_t launch_shape(const WeightGradTile &tile, const CUtensorMap &codes,
 
 // Shape and number of parts with the least expected time: the waves of tiles the
 // device needs, each the steps of one part and what a tile costs beside them.
-// Measured (us; 8 to 256 steps, 128 to 4096 columns): a step takes 0.73 / 0.56 /
-// 0.56, the rest 5 and, split, 17 / 12 / 12 (accumulators through distributed
-// shared memory).  16384 rows, 1024 -> 4096: kWide in 2 parts 114 us, in 1 part
-// 191, kNarrow 150, kSingle 148.  8192 rows, 1024 -> 1024: kSingle in 4 parts 31
-// us, in 1 part 77, kWide in 4 parts 41.
+// Measured (us; 8 to 256 steps, 128 to 4096 columns): the rest beside the steps
+// takes 5 and, split, 17 with 512 outputs and 12 with 256 or fewer (accumulators
+// through distributed shared memory).  16384 rows, 1024 -> 4096: kWide in 2 parts
+// 114 us, in 1 part 191, kNarrow 150, kSingle 148.  8192 rows, 1024 -> 1024:
+// kSingle in 4 parts 31 us, in 1 part 77, kWide in 4 parts 41.
 struct Plan {
     Shape shape;
     int parts;
 };
 
-Plan choose(const Device &d, int64_t cols, int64_t outs, int64_t steps)
+struct Candidate {
+    Shape shape;
+    int blocks, outs;
+    double step_us, split_us;
+};
+
+template <size_t N> Plan choose(const Device &d, const Candidate (&candidates)[N], int64_t cols, int64_t outs, int64_t steps)
 {
-    constexpr double step_us[kShapes] = {0.73, 0.56, 0.56}, split_us[kShapes] = {17.0, 12.0, 12.0};
-    Plan best{kSingle, 1};
+    Plan best{candidates[0].shape, 1};
     double least = -1.0;
-    for (int shape = kWide; shape < kShapes; ++shape) {
-        const int blocks = shape == kSingle ? 1 : 2, outs_tile = shape == kWide ? 512 : 256;
-        const int64_t tiles = ((cols + blocks * kTileC - 1) / (blocks * kTileC)) * ((outs + outs_tile - 1) / outs_tile);
-        for (int parts = 1; parts * blocks <= 8 && parts <= steps; ++parts) {
-            const int held = std::max(d.clusters[shape][parts].load(std::memory_order_relaxed), 1);
+    for (const Candidate &c : candidates) {
+        const int64_t tiles = ((cols + c.blocks * kTileC - 1) / (c.blocks * kTileC)) * ((outs + c.outs - 1) / c.outs);
+        for (int parts = 1; parts * c.blocks <= 8 && parts <= steps; ++parts) {
+            const int held = std::max(d.clusters[c.shape][parts].load(std::memory_order_relaxed), 1);
             const double waves = static_cast<double>((tiles + held - 1) / held);
-            const double cost = waves * (static_cast<double>((steps + parts - 1) / parts) * step_us[shape] + (parts > 1 ? split_us[shape] : 5.0));
+            const double cost = waves * (static_cast<double>((steps + parts - 1) / parts) * c.step_us + (parts > 1 ? c.split_us : 5.0));
             if (least < 0.0 || cost < least) {
                 least = cost;
-                best = Plan{static_cast<Shape>(shape), parts};
+                best = Plan{c.shape, parts};
             }
         }
     }
     return best;
 }
+
+constexpr Candidate kPlain[3] = {{kWide, 2, 512, 0.73, 17.0}, {kNarrow, 2, 256, 0.56, 12.0}, {kSingle, 1, 256, 0.56, 12.0}};
+constexpr Candidate kSummed[2] = {{kNarrowSum, 2, 256, 0.60, 12.0}, {kSingleSum, 1, 256, 0.60, 12.0}};
+constexpr Candidate kLooseDy[2] = {{kLoosePair, 2, 256, 0.9, 12.0}, {kLooseSingle, 1, 128, 0.9, 12.0}};
+constexpr Candidate kCutDy[2] = {{kCutPair, 2, 256, 1.5, 12.0}, {kCutSingle, 1, 128, 1.2, 12.0}};
 
 }  // namespace
 
@@ -204,38 +223,35 @@ extern "C" star_status_t star_checkpoint_weight_grad(void *dw, star_dtype_t dw_d
     a.accumulate = accumulate;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const bool y16 = dy_dtype == STAR_DTYPE_BF16, w16 = dw_dtype == STAR_DTYPE_BF16;
-    // The TMA reads dy in place: 16-byte aligned rows, coordinates of 32 bits.
-    const bool tiled = y16 && rows > 0 && reinterpret_cast<uintptr_t>(dy) % 16 == 0 && ld_dy % 8 == 0 && rows < 0x7fffff00 &&
-                       cols < 0x7fffff00 && outs < 0x7fffff00 && (outs + kTileO - 1) / kTileO <= 65535;
-    if (tiled) {
-        CUtensorMap codes_map, dy_map;
-        if (!make_map(&codes_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, a.kept.pitch, rows, static_cast<uint64_t>(a.kept.pitch), kTileC,
-                      kTileT, CU_TENSOR_MAP_SWIZZLE_NONE) ||
-            !make_map(&dy_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dy, outs, rows, static_cast<uint64_t>(ld_dy) * 2, 64, kTileT,
-                      CU_TENSOR_MAP_SWIZZLE_128B))
-            return cuda_failed(cudaErrorInvalidValue);
-        const int64_t steps = (rows + kTileT - 1) / kTileT;
-        const WeightGradTile tile{a, static_cast<int>(steps)};
-        Device *device = nullptr;
-        const cudaError_t e = prepared_device(&device);
-        if (e != cudaSuccess) return cuda_failed(e);
-        const Plan plan = choose(*device, cols, outs, steps);
-        switch (plan.shape) {
-        case kWide: return launch_shape<kWide>(tile, codes_map, dy_map, w16, plan.parts, stream);
-        case kNarrow: return launch_shape<kNarrow>(tile, codes_map, dy_map, w16, plan.parts, stream);
-        default: return launch_shape<kSingle>(tile, codes_map, dy_map, w16, plan.parts, stream);
-        }
+    if (rows >= 0x7fffff00 || cols >= 0x7fffff00 || outs >= 0x7fffff00 || (outs + 127) / 128 > 65535) return STAR_ERR_UNSUPPORTED;
+    // Rows == 0 has no codes to describe: one tile walk of no steps writes the zeros.
+    const bool tiled = y16 && (rows == 0 || (reinterpret_cast<uintptr_t>(dy) % 16 == 0 && ld_dy % 8 == 0));
+    CUtensorMap codes_map{}, dy_map{};
+    if (rows > 0 && !make_map(&codes_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, a.kept.pitch, rows, static_cast<uint64_t>(a.kept.pitch), kTileC,
+                              kTileT, CU_TENSOR_MAP_SWIZZLE_NONE))
+        return cuda_failed(cudaErrorInvalidValue);
+    if (rows > 0 && tiled && !make_map(&dy_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dy, outs, rows, static_cast<uint64_t>(ld_dy) * 2, 64, kTileT,
+                                       CU_TENSOR_MAP_SWIZZLE_128B))
+        return cuda_failed(cudaErrorInvalidValue);
+    Device *device = nullptr;
+    const cudaError_t e = prepared_device(&device);
+    if (e != cudaSuccess) return cuda_failed(e);
+    const int64_t steps = (rows + kTileT - 1) / kTileT;
+    const WeightGradTile tile{a, static_cast<int>(steps)};
+    const Plan plan = !y16     ? choose(*device, kCutDy, cols, outs, steps)
+                      : !tiled ? choose(*device, kLooseDy, cols, outs, steps)
+                      : w16    ? choose(*device, kPlain, cols, outs, steps)
+                               : choose(*device, kSummed, cols, outs, steps);
+    const auto run = [&](auto shape) { return launch_shape<decltype(shape)::value>(tile, codes_map, dy_map, w16, plan.parts, stream); };
+    switch (plan.shape) {
+    case kWide: return run(std::integral_constant<int, kWide>());
+    case kNarrow: return run(std::integral_constant<int, kNarrow>());
+    case kNarrowSum: return run(std::integral_constant<int, kNarrowSum>());
+    case kSingleSum: return run(std::integral_constant<int, kSingleSum>());
+    case kLoosePair: return run(std::integral_constant<int, kLoosePair>());
+    case kLooseSingle: return run(std::integral_constant<int, kLooseSingle>());
+    case kCutPair: return run(std::integral_constant<int, kCutPair>());
+    case kCutSingle: return run(std::integral_constant<int, kCutSingle>());
+    default: return run(std::integral_constant<int, kSingle>());
     }
-    const int64_t across = (cols + 31) / 32, down = (outs + 31) / 32;
-    if (across > 0x7fffffff) return STAR_ERR_UNSUPPORTED;
-    const dim3 grid(static_cast<unsigned>(across), static_cast<unsigned>(down < 65535 ? down : 65535));
-    if (y16 && w16)
-        star_weight_grad_kernel<GradBF16, GradBF16><<<grid, 256, 0, stream>>>(a);
-    else if (y16)
-        star_weight_grad_kernel<GradBF16, GradF32><<<grid, 256, 0, stream>>>(a);
-    else if (w16)
-        star_weight_grad_kernel<GradF32, GradBF16><<<grid, 256, 0, stream>>>(a);
-    else
-        star_weight_grad_kernel<GradF32, GradF32><<<grid, 256, 0, stream>>>(a);
-    return launched();
 }

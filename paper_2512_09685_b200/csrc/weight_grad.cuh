@@ -5,18 +5,27 @@
 // of the step.  A block of threads owns 128 columns c (the accumulator's 128
 // lanes) and BN outputs o (its columns), and walks the rows in steps of 64:
 //   - one thread fetches the step's codes, scale bytes and dy tile by TMA;
-//   - eight warps widen the codes to bf16, which holds code * 2^e exactly, and
-//     write them as the A operand; the dy tile is the B operand as it lies in
-//     memory (both operands have the summed index t slowest: "MN-major");
+//   - two groups of eight warps, in turn, widen the codes to bf16, which holds
+//     code * 2^e exactly, and write them as the A operand; the dy tile is the B
+//     operand as it lies in memory (both operands have the summed index t slowest:
+//     "MN-major");
 //   - one thread issues the matrix instructions, which accumulate in TMEM.
-// Products are exact; the sums are binary32.  With few output tiles the rows are
-// split over the blocks of a cluster, which add their accumulators through
-// distributed shared memory in a fixed order.
+// With few output tiles the rows are split over the blocks of a cluster, which add
+// their accumulators through distributed shared memory in a fixed order.
+//
+// Precision.  Products are exact.  A dy in fp32 is cut into three bf16 terms of 8
+// bits each, which together are it, and multiplied three times.  The tensor
+// cores' binary32 additions cut instead of rounding: after n rows the sum is off
+// by about n 4e-10 of itself towards zero (16384 rows: 7e-6; measured).  For a dw
+// in bf16 that is far below its own rounding; for a dw in fp32 the accumulator is
+// added to a running sum, with rounding, every 2048 rows (FLUSH): 4e-7.
 #pragma once
 
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "checkpoint.cuh"
 
@@ -53,10 +62,10 @@ __device__ __forceinline__ uint64_t operand_descriptor(uint32_t address)
     return static_cast<uint64_t>((address >> 4) & 0x3fff) | leading << 16 | stride << 32 | uint64_t{1} << 46 | uint64_t{2} << 61;
 }
 
-// bf16 x bf16 -> fp32, both operands MN-major.  M = 128, or 256 over a pair of blocks.
-template <bool PAIR> __device__ __forceinline__ constexpr uint32_t instruction_descriptor()
+// bf16 x bf16 -> fp32, both operands MN-major, N columns.  M = 128, or 256 over a pair of blocks.
+template <int N, bool PAIR> __device__ __forceinline__ constexpr uint32_t instruction_descriptor()
 {
-    return 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | static_cast<uint32_t>(kTileO / 8) << 17 |
+    return 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | static_cast<uint32_t>(N / 8) << 17 |
            static_cast<uint32_t>((PAIR ? 2 : 1) * kTileC / 16) << 24;
 }
 
@@ -127,6 +136,22 @@ __device__ __forceinline__ void load_accumulator(uint32_t address, float (&out)[
     for (int i = 0; i < 32; ++i) out[i] = __uint_as_float(r[i]);
 }
 
+__device__ __forceinline__ void store_accumulator(uint32_t address, const float (&x)[32])
+{
+    uint32_t r[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(x[i]);
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+                 :: "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                    "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+                    "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+                    "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(address)
+                 : "memory");
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
 // ---------------------------------------------------------------------------
 // Widening.  With u = code + 128 in 0 .. 255, the float with bits 0x4b0000uu is
 // 2^23 + u; fma(that, 2^e, -(2^23 + 128) 2^e) = code * 2^e, exact, and exact in
@@ -150,26 +175,92 @@ __device__ __forceinline__ uint4 widen_codes(uint2 eight, float scale, float off
     return make_uint4(a.x, a.y, b.x, b.y);
 }
 
+// ---------------------------------------------------------------------------
+// A dy that the TMA does not read as it is: fp32 (three terms) or rows off the
+// 16-byte grid.  The widening warps fetch it themselves, eight neighbouring
+// outputs of a row a thread.
+// ---------------------------------------------------------------------------
+struct DyEight {
+    uint32_t w[8];       // fp32: the values; bf16: the first four words
+};
+
+template <int TERMS> __device__ __forceinline__ DyEight load_dy(const WeightGradArgs &a, int64_t t, int64_t o, bool vector)
+{
+    using G = std::conditional_t<TERMS == 3, GradF32, GradBF16>;
+    DyEight r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r.w[e] = 0;
+    if (t >= a.kept.rows || o >= a.outs) return r;
+    const char *p = static_cast<const char *>(a.dy) + (t * a.ld_dy + o) * G::kBytes;
+    if (vector && o + 8 <= a.outs) {
+#pragma unroll
+        for (int q = 0; q < G::kBytes / 2; ++q) {
+            const uint4 v = reinterpret_cast<const uint4 *>(p)[q];
+            r.w[4 * q] = v.x; r.w[4 * q + 1] = v.y; r.w[4 * q + 2] = v.z; r.w[4 * q + 3] = v.w;
+        }
+    } else {
+        const int left = static_cast<int>(min(a.outs - o, int64_t{8}));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (e < left) {
+                if constexpr (TERMS == 3)
+                    r.w[e] = reinterpret_cast<const uint32_t *>(p)[e];
+                else
+                    r.w[e / 2] |= static_cast<uint32_t>(reinterpret_cast<const unsigned short *>(p)[e]) << (e % 2 * 16);
+            }
+        }
+    }
+    return r;
+}
+
+// Cuts eight fp32 into three bf16 each: the upper half of the value, of what is
+// left, and of what is then left.  A value that is not finite is its first term
+// (a NaN stays one: its quiet bit lies in the upper half).
+__device__ __forceinline__ void cut_dy(const DyEight &v, uint4 (&term)[3])
+{
+    uint32_t first[8], second[8], third[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float x = __uint_as_float(v.w[e]);
+        const bool finite = fabsf(x) < INFINITY;
+        first[e] = x != x ? v.w[e] | 0x00400000u : v.w[e];
+        const float rest = finite ? __fsub_rn(x, __uint_as_float(v.w[e] & 0xffff0000u)) : 0.0f;
+        second[e] = __float_as_uint(rest);
+        third[e] = __float_as_uint(__fsub_rn(rest, __uint_as_float(second[e] & 0xffff0000u)));
+    }
+    const auto upper = [](const uint32_t (&w)[8]) {
+        return make_uint4(__byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632), __byte_perm(w[4], w[5], 0x7632),
+                          __byte_perm(w[6], w[7], 0x7632));
+    };
+    term[0] = upper(first);
+    term[1] = upper(second);
+    term[2] = upper(third);
+}
+
 // Shared memory of a block, from a 1024-byte aligned base: a ring of LOADS steps
 // as they are fetched (codes, scale bytes, dy), and a shorter one of WIDE steps
 // of the widened operand.  A step's copies take a microsecond or more under load
-// and its products a quarter of one, so the first ring has to be deep.
-template <int BN, int LOADS, int WIDE, bool PAIR> struct GradSmem {
-    static_assert(BN % kTileO == 0, "whole instructions");
+// and its products a quarter of one, so the first ring has to be deep.  TERMS = 0:
+// dy comes by TMA and is an operand as it lies; otherwise its TERMS terms are
+// written beside the widened operand.
+template <int BN, int LOADS, int WIDE, bool PAIR, int TERMS> struct GradSmem {
+    static constexpr int kN = BN < kTileO ? BN : kTileO;         // outputs of one matrix instruction
+    static_assert(BN % kN == 0, "whole instructions");
     static constexpr int kOuts = PAIR ? BN / 2 : BN;             // outputs whose dy this block holds
-    static constexpr int kRun = PAIR ? kTileO / 2 : kTileO;      // of them, side by side: this block's share of one instruction
+    static constexpr int kRun = PAIR ? kN / 2 : kN;              // of them, side by side: this block's share of one instruction
     static constexpr int kA = kTileC * kTileT * 2;
     static constexpr int kB = kOuts * kTileT * 2;
+    static constexpr int kBSlots = TERMS == 0 ? LOADS : WIDE * TERMS;
     static constexpr int kRaw = kTileC * kTileT;
     static constexpr int kScale = kTileT * 4;
     static constexpr int kOffB = WIDE * kA;
-    static constexpr int kOffRaw = kOffB + LOADS * kB;
+    static constexpr int kOffRaw = kOffB + kBSlots * kB;
     static constexpr int kOffScale = kOffRaw + LOADS * kRaw;
     static constexpr int kOffBarrier = kOffScale + LOADS * kScale;
     static constexpr int kBytes = kOffBarrier + 256;
     static constexpr int kDynamic = kBytes + 1024;               // room to align the base
-    static_assert(WIDE <= LOADS && 8 * (2 * LOADS + WIDE + 2) <= 256, "barriers");
-    static_assert(kTileC * kTileO * 4 <= kOffBarrier, "the accumulators of a split tile reuse the rings");
+    static_assert(WIDE <= LOADS && 8 * (2 * LOADS + WIDE + 4) <= 256, "barriers");
+    static_assert(kTileC * kN * 4 <= kOffBarrier, "the accumulators of a split tile reuse the rings");
     static_assert(kDynamic <= 232448, "more shared memory than a block may have");
 };
 
@@ -181,12 +272,12 @@ __device__ __forceinline__ float4 peer_load(uint32_t address)
 }
 
 // The sums of a split tile: part `part` adds its share of the columns over the
-// parts' accumulators (in their shared memory, [kTileO][kTileC]), in the order of
-// the parts, all loads of a sum in flight together.
-template <int PARTS, typename Store>
+// parts' accumulators (in their shared memory, [N][kTileC]), in the order of the
+// parts, all loads of a sum in flight together.
+template <int PARTS, int N, typename Store>
 __device__ __forceinline__ void join_parts(uint32_t sums, int part, uint32_t of_pair, uint32_t blocks, Store store)
 {
-    const int first = kTileO * part / PARTS, last = kTileO * (part + 1) / PARTS;
+    const int first = N * part / PARTS, last = N * (part + 1) / PARTS;
     for (int i = first * (kTileC / 4) + threadIdx.x; i < last * (kTileC / 4); i += kGradThreads) {
         float4 x[PARTS];
 #pragma unroll
@@ -223,12 +314,17 @@ __device__ __forceinline__ void store_weight(const WeightGradArgs &a, bool bf16,
 // the matrix instructions read 48 KB, the copies write 40 KB and the widening
 // moves 24 KB, 112 KB where 128 B a cycle give 64 KB in the 512 cycles of the
 // products.  In a pair that is 80 KB.
-template <int BN, int LOADS, int WIDE, bool PAIR>
+// FLUSH: the accumulator is added to a running sum beside it in TMEM every
+// kFlushSteps steps.
+constexpr int kFlushSteps = 32;
+
+template <int BN, int LOADS, int WIDE, bool PAIR, int TERMS, bool FLUSH>
 __global__ void __launch_bounds__(kGradThreads, 1)
 star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const __grid_constant__ CUtensorMap codes_map,
                                const __grid_constant__ CUtensorMap dy_map, int dw_bf16)
 {
-    using S = GradSmem<BN, LOADS, WIDE, PAIR>;
+    using S = GradSmem<BN, LOADS, WIDE, PAIR, TERMS>;
+    constexpr int kTmem = FLUSH ? 2 * BN : BN;                   // columns: the accumulator, then the running sum
     constexpr int kShare = BN / (kConvertWarps / 4);             // accumulator columns a converting warp reads at the end
     static_assert(kShare % 32 == 0, "whole loads");
     constexpr uint32_t kBlocks = PAIR ? 2 : 1;
@@ -242,7 +338,9 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
     const auto load_phase = [](int i) { return static_cast<uint32_t>(i / LOADS) & 1; };
     const auto wide_phase = [](int i) { return static_cast<uint32_t>(i / WIDE) & 1; };
     const uint32_t finished = bars + 8 * (2 * LOADS + WIDE);
-    uint32_t *tmem_at = reinterpret_cast<uint32_t *>(smem + S::kOffBarrier + 8 * (2 * LOADS + WIDE + 1));
+    const uint32_t summed = finished + 8;                        // FLUSH: a run's matrix instructions are done
+    const uint32_t drained = finished + 16;                      // and its accumulator is read (in both blocks)
+    uint32_t *tmem_at = reinterpret_cast<uint32_t *>(smem + S::kOffBarrier + 8 * (2 * LOADS + WIDE + 3));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = cluster_rank(), of_pair = rank % kBlocks, leader = rank - of_pair;
     const uint32_t mask = 3u << leader;
@@ -254,9 +352,11 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
         }
         for (int i = 0; i < WIDE; ++i) barrier_init(widened(i), kBlocks * kGroupWarps);
         barrier_init(finished, 1);
+        barrier_init(summed, 1);
+        barrier_init(drained, kBlocks * kConvertWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 2) tensor_alloc<BN, PAIR>(smem_address(tmem_at));
+    if (warp == 2) tensor_alloc<kTmem, PAIR>(smem_address(tmem_at));
     tensor_fence_before();
     __syncthreads();
     if constexpr (PAIR) cluster_sync();                          // the other block's barriers are ready
@@ -280,14 +380,16 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
             for (int k = first; k < last; ++k) {
                 const int i = k - first, s = i % LOADS;
                 if (i >= LOADS && !barrier_wait(used(i - LOADS), load_phase(i - LOADS))) break;
-                barrier_expect(loaded(i), S::kRaw + S::kScale + S::kB);
+                barrier_expect(loaded(i), S::kRaw + S::kScale + (TERMS == 0 ? S::kB : 0));
                 const int t = k * kTileT;
                 tma_load_2d(base + S::kOffRaw + s * S::kRaw, &codes_map, static_cast<int>(c0), t, loaded(i));
                 bulk_load(base + S::kOffScale + s * S::kScale, scales + static_cast<int64_t>(t) * 4, S::kScale, loaded(i));
+                if constexpr (TERMS == 0) {
 #pragma unroll
-                for (int q = 0; q < S::kOuts / 64; ++q)
-                    tma_load_2d(base + S::kOffB + s * S::kB + q * (kTileT * 128), &dy_map, outs0 + 64 * q / S::kRun * kTileO + 64 * q % S::kRun, t,
-                                loaded(i));
+                    for (int q = 0; q < S::kOuts / 64; ++q)
+                        tma_load_2d(base + S::kOffB + s * S::kB + q * (kTileT * 128), &dy_map,
+                                    outs0 + 64 * q / S::kRun * S::kN + 64 * q % S::kRun, t, loaded(i));
+                }
                 issued = i + 1;
             }
             // Copies still in flight land before the block goes on (they have, unless a wait ran out).
@@ -295,21 +397,27 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
         }
     } else if (warp == 1) {
         if (lane == 0 && of_pair == 0) {
-            constexpr uint32_t idesc = instruction_descriptor<PAIR>();
+            constexpr uint32_t idesc = instruction_descriptor<S::kN, PAIR>();
             for (int k = first; k < last && ok; ++k) {
-                const int i = k - first;
+                const int i = k - first, in_run = FLUSH ? i % kFlushSteps : i;
+                if (FLUSH && i > 0 && in_run == 0) ok = barrier_wait(drained, (i / kFlushSteps - 1) & 1);
                 // The widening warps of both blocks have seen their block's copies land.
-                ok = barrier_wait(loaded(i), load_phase(i)) && barrier_wait(widened(i), wide_phase(i));
+                ok = ok && barrier_wait(loaded(i), load_phase(i)) && barrier_wait(widened(i), wide_phase(i));
                 if (!ok) break;
                 tensor_fence_after();
-                const uint32_t as = base + (i % WIDE) * S::kA, bs = base + S::kOffB + (i % LOADS) * S::kB;
+                const uint32_t as = base + (i % WIDE) * S::kA;
+                const uint32_t bs = base + S::kOffB + (TERMS == 0 ? i % LOADS : i % WIDE * TERMS) * S::kB;
 #pragma unroll
                 for (int q = 0; q < kTileT / 16; ++q)                // 16 rows an instruction
 #pragma unroll
-                    for (int n = 0; n < BN / kTileO; ++n)
-                        matrix_multiply<PAIR>(tmem + n * kTileO, operand_descriptor(as + q * 2048),
-                                              operand_descriptor(bs + n * (S::kRun * kTileT * 2) + q * 2048), idesc, i > 0 || q > 0);
+                    for (int n = 0; n < BN / S::kN; ++n)
+#pragma unroll
+                        for (int term = 0; term < (TERMS == 0 ? 1 : TERMS); ++term)
+                            matrix_multiply<PAIR>(tmem + n * S::kN, operand_descriptor(as + q * 2048),
+                                                  operand_descriptor(bs + term * S::kB + n * (S::kRun * kTileT * 2) + q * 2048), idesc,
+                                                  in_run > 0 || q > 0 || term > 0);
                 matrix_commit<PAIR>(used(i), mask);
+                if (FLUSH && in_run == kFlushSteps - 1 && k + 1 < last) matrix_commit<PAIR>(summed, mask);
             }
             if (last > first) matrix_commit<PAIR>(finished, mask);
         }
@@ -323,8 +431,48 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
         static_assert(kRows % 8 == 0, "the swizzle depends on the row modulo 8");
         const int from = t0 * kTileC + j * 16, to = swap * (kTileT * 128) + t0 * 128;
         const int to0 = to + (((2 * (j % 4) + swap) ^ (t0 % 8)) << 4), to1 = to + (((2 * (j % 4) + 1 - swap) ^ (t0 % 8)) << 4);
+        // FLUSH: adds this warp's part of run `run`'s accumulator to the running sum.
+        const int quarter = warp % 4, share = (warp - kFirstConvert) / 4;
+        int run = 0;
+        const auto drain = [&] {
+            if (!barrier_wait(summed, run & 1)) return false;
+            tensor_fence_after();
+            for (int col = share * kShare; col < (share + 1) * kShare; col += 32) {
+                const uint32_t at = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + col;
+                float x[32];
+                load_accumulator(at, x);
+                if (run > 0) {
+                    float sum[32];
+                    load_accumulator(at + BN, sum);
+#pragma unroll
+                    for (int r = 0; r < 32; ++r) x[r] = __fadd_rn(x[r], sum[r]);
+                }
+                store_accumulator(at + BN, x);
+            }
+            tensor_fence_before();
+            __syncwarp();
+            if (lane == 0) barrier_arrive(peer_address(drained, leader));
+            ++run;
+            return true;
+        };
+        const int runs = FLUSH ? (last - first + kFlushSteps - 1) / kFlushSteps : 1;
+        const bool vector = TERMS == 0 || (reinterpret_cast<uintptr_t>(p.a.dy) % 16 == 0 && p.a.ld_dy * (TERMS == 3 ? 4 : 2) % 16 == 0);
         for (int k = first + (warp - kFirstConvert) / kGroupWarps; k < last; k += kGroups) {
             const int i = k - first, s = i % LOADS;
+            if constexpr (FLUSH) {
+                while (ok && run < i / kFlushSteps) ok = drain();
+                if (!ok) break;
+            }
+            // TERMS > 0: this block's dy of the step, four times eight outputs a thread, on its way while the codes are widened.
+            constexpr int kEights = TERMS == 0 ? 1 : S::kOuts * kTileT / 8 / (32 * kGroupWarps);
+            DyEight dy[kEights];
+            if constexpr (TERMS > 0) {
+#pragma unroll
+                for (int h = 0; h < kEights; ++h) {
+                    const int unit = w + h * 32 * kGroupWarps, t = unit / (S::kOuts / 8), j = unit % (S::kOuts / 8);
+                    dy[h] = load_dy<TERMS>(p.a, static_cast<int64_t>(k) * kTileT + t, o0 + of_pair * S::kRun + j * 8, vector);
+                }
+            }
             ok = (i < WIDE || barrier_wait(used(i - WIDE), load_phase(i - WIDE))) && barrier_wait(loaded(i), load_phase(i));
             if (!ok) break;
             const uint8_t *raw = smem + S::kOffRaw + s * S::kRaw + from, *scale = smem + S::kOffScale + s * S::kScale + t0 * 4 + j / 2;
@@ -339,10 +487,28 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
                 *reinterpret_cast<uint4 *>(as + h * kRows * 128 + to0) = widen_codes(c0, f, off);
                 *reinterpret_cast<uint4 *>(as + h * kRows * 128 + to1) = widen_codes(c1, f, off);
             }
+            if constexpr (TERMS > 0) {
+                uint8_t *bs = smem + S::kOffB + (i % WIDE) * TERMS * S::kB;
+#pragma unroll
+                for (int h = 0; h < kEights; ++h) {
+                    const int unit = w + h * 32 * kGroupWarps, t = unit / (S::kOuts / 8), j = unit % (S::kOuts / 8);
+                    uint4 *at = reinterpret_cast<uint4 *>(bs + j / 8 * (kTileT * 128) + t * 128 + ((j % 8) ^ (t % 8)) * 16);
+                    if constexpr (TERMS == 3) {
+                        uint4 term[3];
+                        cut_dy(dy[h], term);
+#pragma unroll
+                        for (int q = 0; q < 3; ++q) at[q * (S::kB / 16)] = term[q];
+                    } else {
+                        *at = make_uint4(dy[h].w[0], dy[h].w[1], dy[h].w[2], dy[h].w[3]);
+                    }
+                }
+            }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) barrier_arrive(peer_address(widened(i), leader));
         }
+        if constexpr (FLUSH)
+            while (ok && run + 1 < runs) ok = drain();
     }
 
     // The result: every warp waits for the last matrix instruction itself.
@@ -352,13 +518,24 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
     const bool whole = __syncthreads_and(ok);
     tensor_fence_after();
     const int quarter = warp % 4, share = (warp - kFirstConvert) / 4;            // of a converting warp
+    // 32 columns of the result in this warp's lanes, from column `col` on.
+    const auto result = [&](int col, float (&x)[32]) {
+        const uint32_t at = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + col;
+        load_accumulator(at, x);
+        if (FLUSH && last - first > kFlushSteps) {
+            float sum[32];
+            load_accumulator(at + BN, sum);
+#pragma unroll
+            for (int r = 0; r < 32; ++r) x[r] = __fadd_rn(x[r], sum[r]);
+        }
+    };
     if (parts == 1) {
         if (whole && warp >= kFirstConvert) {
             const int64_t c = c0 + quarter * 32 + lane;
             for (int col = share * kShare; col < (share + 1) * kShare; col += 32) {
                 float x[32];
                 if (any) {
-                    load_accumulator(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + col, x);
+                    result(col, x);
                 } else {
 #pragma unroll
                     for (int r = 0; r < 32; ++r) x[r] = 0.0f;
@@ -371,13 +548,13 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
             }
         }
     } else {
-        float *sums = reinterpret_cast<float *>(smem);               // [kTileO][kTileC]
-        constexpr int kPart = kTileO / (kConvertWarps / 4);
-        for (int n = 0; n < BN / kTileO; ++n) {
+        float *sums = reinterpret_cast<float *>(smem);               // [kN][kTileC]
+        constexpr int kPart = S::kN / (kConvertWarps / 4);
+        for (int n = 0; n < BN / S::kN; ++n) {
             if (warp >= kFirstConvert) {
                 for (int col = share * kPart; col < (share + 1) * kPart; col += 32) {
                     float x[32];
-                    load_accumulator(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + n * kTileO + col, x);
+                    result(n * S::kN + col, x);
 #pragma unroll
                     for (int r = 0; r < 32; ++r) sums[(col + r) * kTileC + quarter * 32 + lane] = x[r];
                 }
@@ -386,7 +563,7 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
             cluster_sync();
             if (whole) {
                 const auto store = [&](int col, int r, float4 x) {
-                    const int64_t o = o0 + n * kTileO + col;
+                    const int64_t o = o0 + n * S::kN + col;
                     if (o >= p.a.outs) return;
                     const float v[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
@@ -394,16 +571,16 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
                         if (c0 + r + e < p.a.kept.cols) store_weight(p.a, dw_bf16, o, c0 + r + e, v[e]);
                 };
                 switch (parts) {
-                case 2: join_parts<2>(base, part, of_pair, kBlocks, store); break;
-                case 3: join_parts<3>(base, part, of_pair, kBlocks, store); break;
-                case 4: join_parts<4>(base, part, of_pair, kBlocks, store); break;
-                case 5: join_parts<5>(base, part, of_pair, kBlocks, store); break;
-                case 6: join_parts<6>(base, part, of_pair, kBlocks, store); break;
-                case 7: join_parts<7>(base, part, of_pair, kBlocks, store); break;
-                default: join_parts<8>(base, part, of_pair, kBlocks, store); break;
+                case 2: join_parts<2, S::kN>(base, part, of_pair, kBlocks, store); break;
+                case 3: join_parts<3, S::kN>(base, part, of_pair, kBlocks, store); break;
+                case 4: join_parts<4, S::kN>(base, part, of_pair, kBlocks, store); break;
+                case 5: join_parts<5, S::kN>(base, part, of_pair, kBlocks, store); break;
+                case 6: join_parts<6, S::kN>(base, part, of_pair, kBlocks, store); break;
+                case 7: join_parts<7, S::kN>(base, part, of_pair, kBlocks, store); break;
+                default: join_parts<8, S::kN>(base, part, of_pair, kBlocks, store); break;
                 }
             }
-            if (n + 1 < BN / kTileO) {
+            if (n + 1 < BN / S::kN) {
                 __syncthreads();
                 cluster_sync();                                      // the sums are read before the next ones come
             }
@@ -412,7 +589,7 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
     tensor_fence_before();
     __syncthreads();
     if (PAIR || parts > 1) cluster_sync();                           // nobody leaves while a peer reads its memory or signals it
-    if (warp == 2) tensor_free<BN, PAIR>(tmem);
+    if (warp == 2) tensor_free<kTmem, PAIR>(tmem);
 }
 
 }  // namespace star
