@@ -631,7 +631,8 @@ STAR_API star_status_t star_checkpoint_act_backward(void *dx, int64_t ld_dx, con
  *   dw : dw_dtype, outs x cols with stride ld_dw; with transposed != 0 it is
  *        stored as cols x outs (the layout of a layer y = x W with W[in][out]).
  *        Usually the worker's gradient buffer that a round reads
- * rows == 0 gives zeros (or leaves dw, when accumulating). */
+ * rows == 0 gives zeros (or leaves dw, when accumulating).  cols and outs up to
+ * 4194240, rows below 2^31 - 256 (STAR_ERR_UNSUPPORTED beyond). */
 STAR_API star_status_t star_checkpoint_weight_grad(void *dw, star_dtype_t dw_dtype, int64_t ld_dw, int transposed,
                                                    const void *dy, star_dtype_t dy_dtype, int64_t ld_dy,
                                                    const int8_t *codes, const uint8_t *scales, int64_t rows,

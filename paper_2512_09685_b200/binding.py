@@ -342,9 +342,13 @@ def _state(t: torch.Tensor, what: str) -> int:
     return t.data_ptr()
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)        # absent in a torch without CUDA
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream(stream) -> int:
     if stream is None:                                  # the current stream's handle, without a Stream object around it
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return _raw_stream(_current_device())
     return stream.cuda_stream
 
 
@@ -810,13 +814,16 @@ _DTYPES = {torch.float32: STAR_DTYPE_F32, torch.bfloat16: STAR_DTYPE_BF16}
 
 def _matrix(t: torch.Tensor, what: str, shape=None, dtype=None) -> Tuple[int, int, int]:
     """(address, dtype code, row stride) of a CUDA matrix whose rows are contiguous."""
-    code = _DTYPES.get(t.dtype)
-    if code is None or t.dim() != 2 or not t.is_cuda or (dtype is not None and t.dtype != dtype):
+    kind, own = t.dtype, t.shape
+    code = _DTYPES.get(kind)
+    if code is None or len(own) != 2 or not t.is_cuda or (dtype is not None and kind is not dtype):
         raise TypeError("%s must be a 2-D %s CUDA tensor" % (what, "float32 or bfloat16" if dtype is None else dtype))
-    if shape is not None and tuple(t.shape) != shape:
-        raise ValueError("%s has shape %s, expected %s" % (what, tuple(t.shape), shape))
-    rows, cols = t.shape
+    rows, cols = own
+    if shape is not None and (rows, cols) != shape:
+        raise ValueError("%s has shape %s, expected %s" % (what, tuple(own), shape))
     ld, step = t.stride()
+    if step == 1 and ld >= cols:
+        return t.data_ptr(), code, ld
     if (step != 1 and cols > 1) or (ld < cols and rows > 1):
         raise TypeError("%s must have contiguous rows that do not overlap" % what)
     return t.data_ptr(), code, max(ld, cols)
@@ -825,7 +832,7 @@ def _matrix(t: torch.Tensor, what: str, shape=None, dtype=None) -> Tuple[int, in
 def _vector(t: Optional[torch.Tensor], n: int, what: str, dtype=torch.float32) -> Optional[int]:
     if t is None:
         return None
-    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
         raise TypeError("%s must be a contiguous %s CUDA tensor" % (what, dtype))
     if t.numel() != n:
         raise ValueError("%s has %d elements, expected %d" % (what, t.numel(), n))

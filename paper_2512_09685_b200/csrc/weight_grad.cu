@@ -53,11 +53,12 @@ bool make_map(CUtensorMap *map, CUtensorMapDataType type, const void *base, int6
 //              512 outputs, 0.73 us a step of 64 rows (1.47 PFLOP/s over 148 SMs)
 //   kNarrow    a pair, 256 x 256: 0.56 us, bound by the widening
 //   kSingle    a block, 128 x 256: 0.56 us
-//   kNarrowSum, kSingleSum      the same with a running sum, for a dw in fp32
-//   kLoosePair, kLooseSingle    dy in bf16 off the 16-byte grid: 256 x 256 by a
+//   kSmall     a block, 128 x 128, for few rows and few tiles
+//   kNarrowSum, kSingleSum      with a running sum, for a dw in fp32
+//   kLoosePair, kLooseSingle    dy in bf16 off the 16-byte grid: 256 x 128 by a
 //              pair, 128 x 128 by a block
-//   kCutPair, kCutSingle        dy in fp32, three terms
-enum Shape { kWide, kNarrow, kSingle, kNarrowSum, kSingleSum, kLoosePair, kLooseSingle, kCutPair, kCutSingle, kShapes };
+//   kCutPair, kCutSingle        dy in fp32, three terms: the same
+enum Shape { kWide, kNarrow, kSingle, kSmall, kNarrowSum, kSingleSum, kLoosePair, kLooseSingle, kCutPair, kCutSingle, kShapes };
 constexpr int kMostParts = 8;
 
 template <int SHAPE> struct ShapeOf;
@@ -69,11 +70,12 @@ template <int BN, int LOADS, int WIDE, bool PAIR, int TERMS, bool FLUSH> struct 
 template <> struct ShapeOf<kWide> : ShapeBase<512, 4, 3, true, 0, false> {};
 template <> struct ShapeOf<kNarrow> : ShapeBase<256, 7, 3, true, 0, false> {};
 template <> struct ShapeOf<kSingle> : ShapeBase<256, 4, 3, false, 0, false> {};
+template <> struct ShapeOf<kSmall> : ShapeBase<128, 6, 4, false, 0, false> {};
 template <> struct ShapeOf<kNarrowSum> : ShapeBase<256, 7, 3, true, 0, true> {};
 template <> struct ShapeOf<kSingleSum> : ShapeBase<256, 4, 3, false, 0, true> {};
-template <> struct ShapeOf<kLoosePair> : ShapeBase<256, 4, 4, true, 1, true> {};
+template <> struct ShapeOf<kLoosePair> : ShapeBase<128, 6, 5, true, 1, true> {};
 template <> struct ShapeOf<kLooseSingle> : ShapeBase<128, 4, 4, false, 1, true> {};
-template <> struct ShapeOf<kCutPair> : ShapeBase<256, 4, 3, true, 3, true> {};
+template <> struct ShapeOf<kCutPair> : ShapeBase<128, 5, 4, true, 3, true> {};
 template <> struct ShapeOf<kCutSingle> : ShapeBase<128, 4, 3, false, 3, true> {};
 
 void fill_config(cudaLaunchConfig_t *config, cudaLaunchAttribute *attribute, int64_t columns, int64_t down, int blocks, int parts,
@@ -129,6 +131,7 @@ cudaError_t prepared_device(Device **out)
         e = prepare_shape<kWide>(d);
         if (e == cudaSuccess) e = prepare_shape<kNarrow>(d);
         if (e == cudaSuccess) e = prepare_shape<kSingle>(d);
+        if (e == cudaSuccess) e = prepare_shape<kSmall>(d);
         if (e == cudaSuccess) e = prepare_shape<kNarrowSum>(d);
         if (e == cudaSuccess) e = prepare_shape<kSingleSum>(d);
         if (e == cudaSuccess) e = prepare_shape<kLoosePair>(d);
@@ -166,37 +169,63 @@ star_status_t launch_shape(const WeightGradTile &tile, const CUtensorMap &codes,
 struct Plan {
     Shape shape;
     int parts;
+    double us;
 };
 
 struct Candidate {
     Shape shape;
     int blocks, outs;
     double step_us, split_us;
+    int most_steps;              // in one part; 0: any number
 };
 
 template <size_t N> Plan choose(const Device &d, const Candidate (&candidates)[N], int64_t cols, int64_t outs, int64_t steps)
 {
-    Plan best{candidates[0].shape, 1};
-    double least = -1.0;
+    Plan best{candidates[0].shape, 1, -1.0};
     for (const Candidate &c : candidates) {
         const int64_t tiles = ((cols + c.blocks * kTileC - 1) / (c.blocks * kTileC)) * ((outs + c.outs - 1) / c.outs);
-        for (int parts = 1; parts * c.blocks <= 8 && parts <= steps; ++parts) {
+        for (int parts = 1; parts * c.blocks <= 8 && (parts <= steps || parts == 1); ++parts) {
+            if (c.most_steps > 0 && (steps + parts - 1) / parts > c.most_steps) continue;
             const int held = std::max(d.clusters[c.shape][parts].load(std::memory_order_relaxed), 1);
             const double waves = static_cast<double>((tiles + held - 1) / held);
             const double cost = waves * (static_cast<double>((steps + parts - 1) / parts) * c.step_us + (parts > 1 ? c.split_us : 5.0));
-            if (least < 0.0 || cost < least) {
-                least = cost;
-                best = Plan{c.shape, parts};
-            }
+            if (best.us < 0.0 || cost < best.us) best = Plan{c.shape, parts, cost};
         }
     }
     return best;
 }
 
-constexpr Candidate kPlain[3] = {{kWide, 2, 512, 0.73, 17.0}, {kNarrow, 2, 256, 0.56, 12.0}, {kSingle, 1, 256, 0.56, 12.0}};
-constexpr Candidate kSummed[2] = {{kNarrowSum, 2, 256, 0.60, 12.0}, {kSingleSum, 1, 256, 0.60, 12.0}};
-constexpr Candidate kLooseDy[2] = {{kLoosePair, 2, 256, 0.9, 12.0}, {kLooseSingle, 1, 128, 0.9, 12.0}};
-constexpr Candidate kCutDy[2] = {{kCutPair, 2, 256, 1.5, 12.0}, {kCutSingle, 1, 128, 1.2, 12.0}};
+constexpr Candidate kPlain[4] = {
+    {kWide, 2, 512, 0.73, 17.0, 0}, {kNarrow, 2, 256, 0.56, 12.0, 0}, {kSingle, 1, 256, 0.56, 12.0, 0}, {kSmall, 1, 128, 0.52, 10.0, 0}};
+// A dw in fp32 takes the same shapes as long as no part is longer than a run of the running sum.
+constexpr Candidate kSummed[6] = {{kNarrowSum, 2, 256, 0.76, 12.0, 0},          {kSingleSum, 1, 256, 0.76, 12.0, 0},
+                                  {kWide, 2, 512, 0.73, 17.0, kFlushSteps},     {kNarrow, 2, 256, 0.56, 12.0, kFlushSteps},
+                                  {kSingle, 1, 256, 0.56, 12.0, kFlushSteps},   {kSmall, 1, 128, 0.52, 10.0, kFlushSteps}};
+constexpr Candidate kLooseDy[2] = {{kLoosePair, 2, 128, 0.9, 10.0, 0}, {kLooseSingle, 1, 128, 0.9, 10.0, 0}};
+constexpr Candidate kCutDy[2] = {{kCutPair, 2, 128, 1.0, 10.0, 0}, {kCutSingle, 1, 128, 1.2, 10.0, 0}};
+
+// Few rows on the ordinary units, where that takes less than the tensor cores'
+// `us`: waves of tiles, two to an SM, each of 2 us and 0.25 us a row.  Measured at
+// 4096 x 4096, fp32: 1 row 15 us against 51, 16 rows 25 against 51.
+bool few_rows(int64_t rows, int64_t cols, int64_t outs, bool transposed, double us)
+{
+    const int64_t inner = transposed ? outs : cols, outer = transposed ? cols : outs;
+    const int64_t tiles = ((inner + kFewInner - 1) / kFewInner) * ((outer + kFewOuter - 1) / kFewOuter);
+    return 2.0 + static_cast<double>((tiles + 295) / 296) * (2.0 + 0.25 * static_cast<double>(rows)) < us;
+}
+
+template <typename GY, typename GW> star_status_t launch_few(const WeightGradArgs &a, bool transposed, cudaStream_t stream)
+{
+    const int64_t inner = transposed ? a.outs : a.kept.cols, outer = transposed ? a.kept.cols : a.outs;
+    const int64_t ld = transposed ? a.stride_c : a.stride_o;
+    const int vector = reinterpret_cast<uintptr_t>(a.dw) % (4 * GW::kBytes) == 0 && ld % 4 == 0;
+    const dim3 grid(static_cast<unsigned>((inner + kFewInner - 1) / kFewInner), static_cast<unsigned>((outer + kFewOuter - 1) / kFewOuter));
+    if (transposed)
+        star_weight_grad_few_kernel<GY, GW, true><<<grid, kFewThreads, 0, stream>>>(a, vector);
+    else
+        star_weight_grad_few_kernel<GY, GW, false><<<grid, kFewThreads, 0, stream>>>(a, vector);
+    return launched();
+}
 
 }  // namespace
 
@@ -223,29 +252,34 @@ extern "C" star_status_t star_checkpoint_weight_grad(void *dw, star_dtype_t dw_d
     a.accumulate = accumulate;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const bool y16 = dy_dtype == STAR_DTYPE_BF16, w16 = dw_dtype == STAR_DTYPE_BF16;
-    if (rows >= 0x7fffff00 || cols >= 0x7fffff00 || outs >= 0x7fffff00 || (outs + 127) / 128 > 65535) return STAR_ERR_UNSUPPORTED;
-    // Rows == 0 has no codes to describe: one tile walk of no steps writes the zeros.
-    const bool tiled = y16 && (rows == 0 || (reinterpret_cast<uintptr_t>(dy) % 16 == 0 && ld_dy % 8 == 0));
-    CUtensorMap codes_map{}, dy_map{};
-    if (rows > 0 && !make_map(&codes_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, a.kept.pitch, rows, static_cast<uint64_t>(a.kept.pitch), kTileC,
-                              kTileT, CU_TENSOR_MAP_SWIZZLE_NONE))
-        return cuda_failed(cudaErrorInvalidValue);
-    if (rows > 0 && tiled && !make_map(&dy_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dy, outs, rows, static_cast<uint64_t>(ld_dy) * 2, 64, kTileT,
-                                       CU_TENSOR_MAP_SWIZZLE_128B))
-        return cuda_failed(cudaErrorInvalidValue);
+    if (rows >= 0x7fffff00 || cols >= 0x7fffff00 || outs >= 0x7fffff00 || std::max(cols, outs) > int64_t{65535} * kFewOuter) return STAR_ERR_UNSUPPORTED;
+    // The TMA reads dy in place: rows on the 16-byte grid.
+    const bool tiled = y16 && reinterpret_cast<uintptr_t>(dy) % 16 == 0 && ld_dy % 8 == 0;
     Device *device = nullptr;
     const cudaError_t e = prepared_device(&device);
     if (e != cudaSuccess) return cuda_failed(e);
     const int64_t steps = (rows + kTileT - 1) / kTileT;
-    const WeightGradTile tile{a, static_cast<int>(steps)};
     const Plan plan = !y16     ? choose(*device, kCutDy, cols, outs, steps)
                       : !tiled ? choose(*device, kLooseDy, cols, outs, steps)
                       : w16    ? choose(*device, kPlain, cols, outs, steps)
                                : choose(*device, kSummed, cols, outs, steps);
+    if (rows == 0 || (few_rows(rows, cols, outs, transposed != 0, plan.us))) {
+        if (y16) return w16 ? launch_few<GradBF16, GradBF16>(a, transposed != 0, stream) : launch_few<GradBF16, GradF32>(a, transposed != 0, stream);
+        return w16 ? launch_few<GradF32, GradBF16>(a, transposed != 0, stream) : launch_few<GradF32, GradF32>(a, transposed != 0, stream);
+    }
+    CUtensorMap codes_map{}, dy_map{};
+    if (!make_map(&codes_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, a.kept.pitch, rows, static_cast<uint64_t>(a.kept.pitch), kTileC, kTileT,
+                  CU_TENSOR_MAP_SWIZZLE_NONE))
+        return cuda_failed(cudaErrorInvalidValue);
+    if (tiled && !make_map(&dy_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dy, outs, rows, static_cast<uint64_t>(ld_dy) * 2, 64, kTileT,
+                           CU_TENSOR_MAP_SWIZZLE_128B))
+        return cuda_failed(cudaErrorInvalidValue);
+    const WeightGradTile tile{a, static_cast<int>(steps)};
     const auto run = [&](auto shape) { return launch_shape<decltype(shape)::value>(tile, codes_map, dy_map, w16, plan.parts, stream); };
     switch (plan.shape) {
     case kWide: return run(std::integral_constant<int, kWide>());
     case kNarrow: return run(std::integral_constant<int, kNarrow>());
+    case kSmall: return run(std::integral_constant<int, kSmall>());
     case kNarrowSum: return run(std::integral_constant<int, kNarrowSum>());
     case kSingleSum: return run(std::integral_constant<int, kSingleSum>());
     case kLoosePair: return run(std::integral_constant<int, kLoosePair>());

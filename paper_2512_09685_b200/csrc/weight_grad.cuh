@@ -18,7 +18,9 @@
 // cores' binary32 additions cut instead of rounding: after n rows the sum is off
 // by about n 4e-10 of itself towards zero (16384 rows: 7e-6; measured).  For a dw
 // in bf16 that is far below its own rounding; for a dw in fp32 the accumulator is
-// added to a running sum, with rounding, every 2048 rows (FLUSH): 4e-7.
+// added to a running sum, with rounding, every 2048 rows (FLUSH): 4e-7.  The lower
+// terms of an fp32 dy have an accumulator of their own: beside sums 2^8 and 2^16
+// times their size most of their bits would be cut (6e-6 in one accumulator).
 #pragma once
 
 #include <cuda.h>
@@ -181,36 +183,71 @@ __device__ __forceinline__ uint4 widen_codes(uint2 eight, float scale, float off
 // outputs of a row a thread.
 // ---------------------------------------------------------------------------
 struct DyEight {
-    uint32_t w[8];       // fp32: the values; bf16: the first four words
+    uint32_t w[8];       // fp32: the values; bf16: the first four words, or two 16-byte loads around them
 };
 
-template <int TERMS> __device__ __forceinline__ DyEight load_dy(const WeightGradArgs &a, int64_t t, int64_t o, bool vector)
+// bf16 off the 16-byte grid: eight values lie within two aligned 16-byte pieces.
+// Where those are inside the matrix, *shift is the values' offset in them; -1 if not.
+__device__ __forceinline__ const uint4 *around_eight(const WeightGradArgs &a, int64_t t, int64_t o, int *shift)
+{
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a.dy) + static_cast<uintptr_t>((t * a.ld_dy + o) * 2), at = p & ~uintptr_t{15};
+    const uintptr_t from = reinterpret_cast<uintptr_t>(a.dy), to = from + static_cast<uintptr_t>(((a.kept.rows - 1) * a.ld_dy + a.outs) * 2);
+    const bool inside = t < a.kept.rows && o + 8 <= a.outs && at >= from && at + 32 <= to;
+    *shift = inside ? static_cast<int>(p & 15u) : -1;
+    return reinterpret_cast<const uint4 *>(at);
+}
+
+template <int TERMS> __device__ __forceinline__ void load_dy(const WeightGradArgs &a, int64_t t, int64_t o, bool vector, DyEight &r)
 {
     using G = std::conditional_t<TERMS == 3, GradF32, GradBF16>;
-    DyEight r;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) r.w[e] = 0;
-    if (t >= a.kept.rows || o >= a.outs) return r;
     const char *p = static_cast<const char *>(a.dy) + (t * a.ld_dy + o) * G::kBytes;
-    if (vector && o + 8 <= a.outs) {
+    if constexpr (TERMS == 1) {
+        int shift;
+        const uint4 *at = around_eight(a, t, o, &shift);
+        if (shift >= 0) {
 #pragma unroll
-        for (int q = 0; q < G::kBytes / 2; ++q) {
+            for (int q = 0; q < 2; ++q) {
+                const uint4 v = at[q];
+                r.w[4 * q] = v.x; r.w[4 * q + 1] = v.y; r.w[4 * q + 2] = v.z; r.w[4 * q + 3] = v.w;
+            }
+            return;
+        }
+    } else if (vector && t < a.kept.rows && o + 8 <= a.outs) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
             const uint4 v = reinterpret_cast<const uint4 *>(p)[q];
             r.w[4 * q] = v.x; r.w[4 * q + 1] = v.y; r.w[4 * q + 2] = v.z; r.w[4 * q + 3] = v.w;
         }
-    } else {
-        const int left = static_cast<int>(min(a.outs - o, int64_t{8}));
+        return;
+    }
+    const int left = t < a.kept.rows ? static_cast<int>(min(a.outs - o, int64_t{8})) : 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (e < left) {
-                if constexpr (TERMS == 3)
-                    r.w[e] = reinterpret_cast<const uint32_t *>(p)[e];
-                else
-                    r.w[e / 2] |= static_cast<uint32_t>(reinterpret_cast<const unsigned short *>(p)[e]) << (e % 2 * 16);
-            }
+    for (int e = 0; e < 8; ++e) r.w[e] = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if (e < left) {
+            if constexpr (TERMS == 3)
+                r.w[e] = reinterpret_cast<const uint32_t *>(p)[e];
+            else
+                r.w[e / 2] |= static_cast<uint32_t>(reinterpret_cast<const unsigned short *>(p)[e]) << (e % 2 * 16);
         }
     }
-    return r;
+}
+
+// The eight bf16 of what load_dy<1> fetched.
+__device__ __forceinline__ uint4 eight_bf16(const WeightGradArgs &a, int64_t t, int64_t o, DyEight r)
+{
+    int shift;
+    around_eight(a, t, o, &shift);
+    if (shift > 0) {
+#pragma unroll
+        for (int e = 0; e < 6; ++e) r.w[e] = shift & 8 ? r.w[e + 2] : r.w[e];
+#pragma unroll
+        for (int e = 0; e < 5; ++e) r.w[e] = shift & 4 ? r.w[e + 1] : r.w[e];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r.w[e] = __funnelshift_r(r.w[e], r.w[e + 1], (shift & 2) * 8);
+    }
+    return make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
 }
 
 // Cuts eight fp32 into three bf16 each: the upper half of the value, of what is
@@ -305,6 +342,82 @@ __device__ __forceinline__ void store_weight(const WeightGradArgs &a, bool bf16,
     }
 }
 
+// A warp's 32 columns c0 .. and 32 outputs o0 .. (x[r]: output o0 + r of this
+// lane's column).  `words`: pairs of bf16 at even columns lie on whole words.
+// Plain layout: neighbouring lanes trade halves, so that each stores two columns
+// of every other output; fp32 and transposed bf16 need no trade.
+__device__ __forceinline__ void store_block(const WeightGradArgs &a, bool bf16, bool words, int64_t o0, int64_t c0, int lane, const float (&x)[32])
+{
+    const int64_t c = c0 + lane;
+    if (bf16 && words && a.stride_c == 1 && o0 + 32 <= a.outs && c0 + 32 <= a.kept.cols) {
+        const int odd = lane & 1;
+        uint32_t *dst = reinterpret_cast<uint32_t *>(static_cast<unsigned short *>(a.dw) + (o0 + odd) * a.stride_o + (c - odd));
+        const int64_t two_rows = a.stride_o;                     // two outputs further, in words
+#pragma unroll
+        for (int r = 0; r < 32; r += 2, dst += two_rows) {
+            const float mine = odd ? x[r + 1] : x[r], theirs = __shfl_xor_sync(0xffffffffu, odd ? x[r] : x[r + 1], 1);
+            float lo = odd ? theirs : mine, hi = odd ? mine : theirs;
+            if (a.accumulate) {
+                const uint32_t before = *dst;
+                lo = __fadd_rn(lo, __uint_as_float(before << 16));
+                hi = __fadd_rn(hi, __uint_as_float(before & 0xffff0000u));
+            }
+            *dst = pack_bf16(lo, hi);
+        }
+        return;
+    }
+    if (bf16 && words && a.stride_o == 1 && o0 + 32 <= a.outs) {
+        if (c >= a.kept.cols) return;
+        uint32_t *dst = reinterpret_cast<uint32_t *>(static_cast<unsigned short *>(a.dw) + o0 + c * a.stride_c);
+#pragma unroll
+        for (int r = 0; r < 32; r += 2) {
+            float lo = x[r], hi = x[r + 1];
+            if (a.accumulate) {
+                const uint32_t before = dst[r / 2];
+                lo = __fadd_rn(lo, __uint_as_float(before << 16));
+                hi = __fadd_rn(hi, __uint_as_float(before & 0xffff0000u));
+            }
+            dst[r / 2] = pack_bf16(lo, hi);
+        }
+        return;
+    }
+    if (c >= a.kept.cols) return;
+    const int left = static_cast<int>(min(a.outs - o0, int64_t{32}));
+    if (!bf16) {
+        float *dst = static_cast<float *>(a.dw) + o0 * a.stride_o + c * a.stride_c;
+#pragma unroll
+        for (int r = 0; r < 32; ++r, dst += a.stride_o)
+            if (r < left) *dst = a.accumulate ? __fadd_rn(x[r], *dst) : x[r];
+        return;
+    }
+#pragma unroll
+    for (int r = 0; r < 32; ++r)
+        if (r < left) store_weight(a, true, o0 + r, c, x[r]);
+}
+
+// Four neighbouring columns of one output.
+__device__ __forceinline__ void store_four(const WeightGradArgs &a, bool bf16, bool words, int64_t o, int64_t c, float4 v)
+{
+    if (o >= a.outs) return;
+    if (bf16 && words && a.stride_c == 1 && c + 4 <= a.kept.cols) {
+        uint32_t *dst = reinterpret_cast<uint32_t *>(static_cast<unsigned short *>(a.dw) + o * a.stride_o + c);
+        if (a.accumulate) {
+            const uint32_t lo = dst[0], hi = dst[1];
+            v.x = __fadd_rn(v.x, __uint_as_float(lo << 16));
+            v.y = __fadd_rn(v.y, __uint_as_float(lo & 0xffff0000u));
+            v.z = __fadd_rn(v.z, __uint_as_float(hi << 16));
+            v.w = __fadd_rn(v.w, __uint_as_float(hi & 0xffff0000u));
+        }
+        dst[0] = pack_bf16(v.x, v.y);
+        dst[1] = pack_bf16(v.z, v.w);
+        return;
+    }
+    const float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (c + e < a.kept.cols) store_weight(a, bf16, o, c + e, x[e]);
+}
+
 // grid: (column tiles, output tiles, parts of the rows); cluster: (1 or 2, 1, parts).
 //
 // PAIR: two blocks with neighbouring column tiles work as one (cta_group::2).
@@ -324,7 +437,9 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
                                const __grid_constant__ CUtensorMap dy_map, int dw_bf16)
 {
     using S = GradSmem<BN, LOADS, WIDE, PAIR, TERMS>;
-    constexpr int kTmem = FLUSH ? 2 * BN : BN;                   // columns: the accumulator, then the running sum
+    // Columns of TMEM: the accumulator, the running sum, the lower terms' accumulator; a power of two.
+    constexpr int kTmem = TERMS == 3 ? 4 * BN : FLUSH ? 2 * BN : BN, kLower = 2 * BN;
+    static_assert(TERMS != 3 || (FLUSH && BN == S::kN), "one instruction's columns, summed");
     constexpr int kShare = BN / (kConvertWarps / 4);             // accumulator columns a converting warp reads at the end
     static_assert(kShare % 32 == 0, "whole loads");
     constexpr uint32_t kBlocks = PAIR ? 2 : 1;
@@ -413,9 +528,9 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
                     for (int n = 0; n < BN / S::kN; ++n)
 #pragma unroll
                         for (int term = 0; term < (TERMS == 0 ? 1 : TERMS); ++term)
-                            matrix_multiply<PAIR>(tmem + n * S::kN, operand_descriptor(as + q * 2048),
+                            matrix_multiply<PAIR>(tmem + n * S::kN + (term > 0 ? kLower : 0), operand_descriptor(as + q * 2048),
                                                   operand_descriptor(bs + term * S::kB + n * (S::kRun * kTileT * 2) + q * 2048), idesc,
-                                                  in_run > 0 || q > 0 || term > 0);
+                                                  (term > 0 ? i : in_run) > 0 || q > 0 || term > 1);
                 matrix_commit<PAIR>(used(i), mask);
                 if (FLUSH && in_run == kFlushSteps - 1 && k + 1 < last) matrix_commit<PAIR>(summed, mask);
             }
@@ -457,22 +572,23 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
         };
         const int runs = FLUSH ? (last - first + kFlushSteps - 1) / kFlushSteps : 1;
         const bool vector = TERMS == 0 || (reinterpret_cast<uintptr_t>(p.a.dy) % 16 == 0 && p.a.ld_dy * (TERMS == 3 ? 4 : 2) % 16 == 0);
+        constexpr int kEights = TERMS == 0 ? 1 : S::kOuts * kTileT / 8 / (32 * kGroupWarps);
+        DyEight dy[kEights];
+        const auto fetch_dy = [&](int k) {
+#pragma unroll
+            for (int h = 0; h < kEights; ++h) {
+                const int unit = w + h * 32 * kGroupWarps, t = unit / (S::kOuts / 8), j = unit % (S::kOuts / 8);
+                load_dy<TERMS>(p.a, static_cast<int64_t>(k) * kTileT + t, o0 + of_pair * S::kRun + j * 8, vector, dy[h]);
+            }
+        };
         for (int k = first + (warp - kFirstConvert) / kGroupWarps; k < last; k += kGroups) {
             const int i = k - first, s = i % LOADS;
             if constexpr (FLUSH) {
                 while (ok && run < i / kFlushSteps) ok = drain();
                 if (!ok) break;
             }
-            // TERMS > 0: this block's dy of the step, four times eight outputs a thread, on its way while the codes are widened.
-            constexpr int kEights = TERMS == 0 ? 1 : S::kOuts * kTileT / 8 / (32 * kGroupWarps);
-            DyEight dy[kEights];
-            if constexpr (TERMS > 0) {
-#pragma unroll
-                for (int h = 0; h < kEights; ++h) {
-                    const int unit = w + h * 32 * kGroupWarps, t = unit / (S::kOuts / 8), j = unit % (S::kOuts / 8);
-                    dy[h] = load_dy<TERMS>(p.a, static_cast<int64_t>(k) * kTileT + t, o0 + of_pair * S::kRun + j * 8, vector);
-                }
-            }
+            // TERMS > 0: the step's dy is on its way while the codes are widened.
+            if constexpr (TERMS > 0) fetch_dy(k);
             ok = (i < WIDE || barrier_wait(used(i - WIDE), load_phase(i - WIDE))) && barrier_wait(loaded(i), load_phase(i));
             if (!ok) break;
             const uint8_t *raw = smem + S::kOffRaw + s * S::kRaw + from, *scale = smem + S::kOffScale + s * S::kScale + t0 * 4 + j / 2;
@@ -499,7 +615,7 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
 #pragma unroll
                         for (int q = 0; q < 3; ++q) at[q * (S::kB / 16)] = term[q];
                     } else {
-                        *at = make_uint4(dy[h].w[0], dy[h].w[1], dy[h].w[2], dy[h].w[3]);
+                        *at = eight_bf16(p.a, static_cast<int64_t>(k) * kTileT + t, o0 + of_pair * S::kRun + j * 8, dy[h]);
                     }
                 }
             }
@@ -518,6 +634,7 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
     const bool whole = __syncthreads_and(ok);
     tensor_fence_after();
     const int quarter = warp % 4, share = (warp - kFirstConvert) / 4;            // of a converting warp
+    const bool words = reinterpret_cast<uintptr_t>(p.a.dw) % 4 == 0 && (p.a.stride_c == 1 ? p.a.stride_o : p.a.stride_c) % 2 == 0;
     // 32 columns of the result in this warp's lanes, from column `col` on.
     const auto result = [&](int col, float (&x)[32]) {
         const uint32_t at = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + col;
@@ -528,10 +645,15 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
 #pragma unroll
             for (int r = 0; r < 32; ++r) x[r] = __fadd_rn(x[r], sum[r]);
         }
+        if constexpr (TERMS == 3) {
+            float lower[32];
+            load_accumulator(at + kLower, lower);
+#pragma unroll
+            for (int r = 0; r < 32; ++r) x[r] = __fadd_rn(x[r], lower[r]);
+        }
     };
     if (parts == 1) {
         if (whole && warp >= kFirstConvert) {
-            const int64_t c = c0 + quarter * 32 + lane;
             for (int col = share * kShare; col < (share + 1) * kShare; col += 32) {
                 float x[32];
                 if (any) {
@@ -540,11 +662,7 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
 #pragma unroll
                     for (int r = 0; r < 32; ++r) x[r] = 0.0f;
                 }
-                if (c < p.a.kept.cols) {
-#pragma unroll
-                    for (int r = 0; r < 32; ++r)
-                        if (o0 + col + r < p.a.outs) store_weight(p.a, dw_bf16, o0 + col + r, c, x[r]);
-                }
+                store_block(p.a, dw_bf16, words, o0 + col, c0 + quarter * 32, lane, x);
             }
         }
     } else {
@@ -562,14 +680,7 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
             __syncthreads();
             cluster_sync();
             if (whole) {
-                const auto store = [&](int col, int r, float4 x) {
-                    const int64_t o = o0 + n * S::kN + col;
-                    if (o >= p.a.outs) return;
-                    const float v[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (c0 + r + e < p.a.kept.cols) store_weight(p.a, dw_bf16, o, c0 + r + e, v[e]);
-                };
+                const auto store = [&](int col, int r, float4 x) { store_four(p.a, dw_bf16, words, o0 + n * S::kN + col, c0 + r, x); };
                 switch (parts) {
                 case 2: join_parts<2, S::kN>(base, part, of_pair, kBlocks, store); break;
                 case 3: join_parts<3, S::kN>(base, part, of_pair, kBlocks, store); break;
@@ -590,6 +701,91 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
     __syncthreads();
     if (PAIR || parts > 1) cluster_sync();                           // nobody leaves while a peer reads its memory or signals it
     if (warp == 2) tensor_free<kTmem, PAIR>(tmem);
+}
+
+// ---------------------------------------------------------------------------
+// Few rows: the time goes into writing dw, and a tile of the tensor cores would
+// cost more in its preparation than in its products.  Outer products in binary32
+// on the ordinary units: a block makes 64 x 256 results, a thread 8 x 8 of them,
+// rows 32 at a time in shared memory.  The result's inner index, along which dw
+// is stored, runs over the lanes: columns, or outputs where dw is transposed.
+// 4096 x 4096 from 1 row: bf16 9 us, fp32 14 us (tensor cores 21 and 51).
+// ---------------------------------------------------------------------------
+constexpr int kFewRows = 32, kFewOuter = 64, kFewInner = 256, kFewThreads = 256;
+
+template <typename GY, typename GW, bool TRANSPOSED>
+__global__ void __launch_bounds__(kFewThreads, 2) star_weight_grad_few_kernel(const __grid_constant__ WeightGradArgs a, int vector)
+{
+    __shared__ alignas(16) float outer[kFewRows][kFewOuter], inner[kFewRows][kFewInner];
+    const int64_t n_outer = TRANSPOSED ? a.kept.cols : a.outs, n_inner = TRANSPOSED ? a.outs : a.kept.cols;
+    const int64_t i0 = static_cast<int64_t>(blockIdx.y) * kFewOuter, j0 = static_cast<int64_t>(blockIdx.x) * kFewInner;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const auto value = [&](int64_t t, int64_t c) {
+        return __fmul_rn(static_cast<float>(a.kept.codes[t * a.kept.pitch + c]), scale_value(a.kept.scales[scale_at(a.kept, t, c / 32)]));
+    };
+    const auto gradient = [&](int64_t t, int64_t o) { return load_value<GY>(a.dy, t * a.ld_dy + o); };
+    float sum[8][8];
+#pragma unroll
+    for (int p = 0; p < 8; ++p)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) sum[p][q] = 0.0f;
+    for (int64_t t0 = 0; t0 < a.kept.rows; t0 += kFewRows) {
+        const int rows = static_cast<int>(min(a.kept.rows - t0, static_cast<int64_t>(kFewRows)));
+        if (t0 > 0) __syncthreads();
+        static_assert(kFewThreads == kFewInner, "a thread fetches one inner index of every row");
+        const int64_t j = j0 + threadIdx.x;
+#pragma unroll 8
+        for (int t = 0; t < rows; ++t) {
+            float x = 0.0f;
+            if (j < n_inner) x = TRANSPOSED ? gradient(t0 + t, j) : value(t0 + t, j);
+            inner[t][threadIdx.x] = x;
+        }
+#pragma unroll 4
+        for (int e = threadIdx.x; e < rows * kFewOuter; e += kFewThreads) {
+            const int t = e / kFewOuter, i = e % kFewOuter;
+            float x = 0.0f;
+            if (i0 + i < n_outer) x = TRANSPOSED ? value(t0 + t, i0 + i) : gradient(t0 + t, i0 + i);
+            outer[t][i] = x;
+        }
+        __syncthreads();
+        for (int t = 0; t < rows; ++t) {
+            const float4 x0 = *reinterpret_cast<const float4 *>(&inner[t][4 * lane]), x1 = *reinterpret_cast<const float4 *>(&inner[t][128 + 4 * lane]);
+            const float4 y0 = *reinterpret_cast<const float4 *>(&outer[t][8 * warp]), y1 = *reinterpret_cast<const float4 *>(&outer[t][8 * warp + 4]);
+            const float x[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w}, y[8] = {y0.x, y0.y, y0.z, y0.w, y1.x, y1.y, y1.z, y1.w};
+#pragma unroll
+            for (int p = 0; p < 8; ++p)
+#pragma unroll
+                for (int q = 0; q < 8; ++q) sum[p][q] = __fmaf_rn(y[p], x[q], sum[p][q]);
+        }
+    }
+    // Columns 4 lane .. + 3 of each half of the 256.
+    const int64_t ld = TRANSPOSED ? a.stride_c : a.stride_o;
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+        const int64_t i = i0 + 8 * warp + p;
+        if (i >= n_outer) break;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int64_t j = j0 + half * 128 + 4 * lane, at = i * ld + j;
+            float v[4] = {sum[p][4 * half], sum[p][4 * half + 1], sum[p][4 * half + 2], sum[p][4 * half + 3]};
+            const int left = static_cast<int>(min(n_inner - j, int64_t{4}));
+            if (a.accumulate) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < left) v[e] = __fadd_rn(v[e], load_value<GW>(a.dw, at + e));
+            }
+            if (vector && left == 4) {
+                if constexpr (GW::kBytes == 2)
+                    *reinterpret_cast<uint2 *>(static_cast<unsigned short *>(a.dw) + at) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+                else
+                    *reinterpret_cast<float4 *>(static_cast<float *>(a.dw) + at) = make_float4(v[0], v[1], v[2], v[3]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < left) store_value<GW>(a.dw, at + e, v[e]);
+            }
+        }
+    }
 }
 
 }  // namespace star
