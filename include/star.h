@@ -76,7 +76,8 @@ typedef enum {
     STAR_ERR_BAD_SCHEDULE = 3,      /* empty group, duplicate or out-of-range member, bad offsets */
     STAR_ERR_UNSUPPORTED = 4,       /* W above STAR_MAX_WORKERS; a table-copying call inside a stream capture */
     STAR_ERR_WORKSPACE_TOO_SMALL = 5,
-    STAR_ERR_CUDA = 6               /* see star_last_cuda_error() */
+    STAR_ERR_CUDA = 6,              /* see star_last_cuda_error() */
+    STAR_ERR_TIMEOUT = 7            /* see star_check_waits() */
 } star_status_t;
 
 typedef enum { STAR_DTYPE_F32 = 0, STAR_DTYPE_BF16 = 1 } star_dtype_t;
@@ -638,6 +639,14 @@ STAR_API star_status_t star_checkpoint_weight_grad(void *dw, star_dtype_t dw_dty
                                                    const int8_t *codes, const uint8_t *scales, int64_t rows,
                                                    int64_t cols, int64_t outs, int accumulate,
                                                    void *cuda_stream);
+
+/* The policy loss and the weight gradient wait inside their kernels for copies
+ * that they have started.  Every such wait is bounded; one that runs out (some
+ * tenths of a second; a fault of the device or its memory) ends the kernel
+ * without a valid result.  star_check_waits waits for cuda_stream and says
+ * whether that has happened on the current device since the last check:
+ * STAR_ERR_TIMEOUT, or STAR_OK.  Not inside a stream capture. */
+STAR_API star_status_t star_check_waits(void *cuda_stream);
 
 /* ---------------------------------------------------------------------------
  * Tensor-list round for callers that cannot allocate device memory.

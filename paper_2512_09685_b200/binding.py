@@ -27,6 +27,7 @@ STAR_ERR_BAD_SCHEDULE = 3
 STAR_ERR_UNSUPPORTED = 4
 STAR_ERR_WORKSPACE_TOO_SMALL = 5
 STAR_ERR_CUDA = 6
+STAR_ERR_TIMEOUT = 7
 
 STAR_DTYPE_F32 = 0
 STAR_DTYPE_BF16 = 1
@@ -135,6 +136,8 @@ def _load() -> ctypes.CDLL:
     lib.star_multi_prepare_ex.restype = c_int
     lib.star_group_update_multi_ex.argtypes = [c_vp, c_vp, c_vp, c_int, c_vp, c_f, c_f, c_vp, c_int, c_vp]
     lib.star_group_update_multi_ex.restype = c_int
+    lib.star_check_waits.argtypes = [c_vp]
+    lib.star_check_waits.restype = c_int
     lib.star_token_logprobs.argtypes = [c_vp, c_int, c_i64, c_i64, c_i64, c_vp, c_f, c_vp, c_vp, c_vp]
     lib.star_token_logprobs.restype = c_int
     lib.star_loss_workspace_bytes.argtypes = [c_i64, c_i64, c_vp]
@@ -979,3 +982,8 @@ def star_checkpoint_weight_grad(dw: torch.Tensor, dy: torch.Tensor, codes: torch
     q, s = _kept(codes, scales, rows, cols)
     _check(_lib.star_checkpoint_weight_grad(w, w_dtype, ld_w, int(transposed), p, dtype, ld, q, s, rows, cols, outs,
                                             int(accumulate), _stream(stream)), "star_checkpoint_weight_grad")
+
+
+def star_check_waits(stream=None) -> None:
+    """Waits for the stream; raises if a wait inside a kernel ran out since the last check."""
+    _check(_lib.star_check_waits(_stream(stream)), "star_check_waits")

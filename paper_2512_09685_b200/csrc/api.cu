@@ -209,6 +209,7 @@ extern "C" const char *star_status_string(star_status_t status)
     case STAR_ERR_UNSUPPORTED: return "STAR_ERR_UNSUPPORTED";
     case STAR_ERR_WORKSPACE_TOO_SMALL: return "STAR_ERR_WORKSPACE_TOO_SMALL";
     case STAR_ERR_CUDA: return "STAR_ERR_CUDA";
+    case STAR_ERR_TIMEOUT: return "STAR_ERR_TIMEOUT";
     }
     return "STAR_ERR_UNKNOWN";
 }

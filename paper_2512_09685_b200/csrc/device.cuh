@@ -77,7 +77,7 @@ __device__ __forceinline__ uint32_t cluster_size()
 // ends after some tenths of a second at the earliest: waits for memory take
 // microseconds.
 constexpr int kWaitTries = 1 << 24;
-static __device__ int g_wait_expired;        // of this source file's kernels
+static __device__ int g_wait_expired;        // one of each source file that includes this
 
 __device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count)
 {
@@ -119,5 +119,16 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
 // complete and its writes are visible.  launch_dependents() lets it start.
 __device__ __forceinline__ void wait_for_primary() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// Reads and clears this source file's flag, after the work on `stream`.
+static inline cudaError_t take_expired(cudaStream_t stream, int *expired)
+{
+    const int none = 0;
+    cudaError_t e = cudaMemcpyFromSymbolAsync(expired, g_wait_expired, sizeof *expired, 0, cudaMemcpyDeviceToHost, stream);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
+    if (e == cudaSuccess && *expired) e = cudaMemcpyToSymbolAsync(g_wait_expired, &none, sizeof none, 0, cudaMemcpyHostToDevice, stream);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
+    return e;
+}
 
 }  // namespace star

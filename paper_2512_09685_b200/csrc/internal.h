@@ -16,6 +16,10 @@ star_status_t cuda_failed(cudaError_t e);
 // One more kernel launched (star_launch_count).
 void count_launch();
 
+// Whether a wait of the weight gradient's kernels has run out (and no longer
+// after this), once the work on `stream` is done.
+cudaError_t weight_grad_expired(cudaStream_t stream, int *expired);
+
 // The status of the launch just made.
 inline star_status_t launched()
 {

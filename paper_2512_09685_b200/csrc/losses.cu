@@ -381,3 +381,17 @@ extern "C" star_status_t star_preference_loss(const void *logits, star_dtype_t d
     g.loss = loss;
     return launch_gradient<false>(g, dtype, follows, stream);
 }
+
+extern "C" star_status_t star_check_waits(void *cuda_stream)
+{
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+    cudaError_t e = cudaStreamIsCapturing(stream, &capturing);
+    if (e != cudaSuccess) return cuda_failed(e);
+    if (capturing != cudaStreamCaptureStatusNone) return STAR_ERR_UNSUPPORTED;
+    int here = 0, there = 0;
+    e = take_expired(stream, &here);
+    if (e == cudaSuccess) e = weight_grad_expired(stream, &there);
+    if (e != cudaSuccess) return cuda_failed(e);
+    return here || there ? STAR_ERR_TIMEOUT : STAR_OK;
+}

@@ -229,6 +229,8 @@ template <typename GY, typename GW> star_status_t launch_few(const WeightGradArg
 
 }  // namespace
 
+cudaError_t star::weight_grad_expired(cudaStream_t stream, int *expired) { return take_expired(stream, expired); }
+
 extern "C" star_status_t star_checkpoint_weight_grad(void *dw, star_dtype_t dw_dtype, int64_t ld_dw, int transposed,
                                                      const void *dy, star_dtype_t dy_dtype, int64_t ld_dy,
                                                      const int8_t *codes, const uint8_t *scales, int64_t rows,
