@@ -48,66 +48,97 @@ __device__ __forceinline__ uint32_t code_bits(float x, float inverse)
     return __float_as_uint(__fmaf_rn(x, inverse, kRoundMagic));
 }
 
-template <int ACT> __device__ __forceinline__ float activation(float x);
-template <int ACT> __device__ __forceinline__ float activation_slope(float x);
-
-__device__ __forceinline__ float sigmoid(float x)
-{
-    return __fdividef(1.0f, __fadd_rn(1.0f, exp2_fast(__fmul_rn(-kLog2e, x))));
-}
-
-// 0.5 (1 + tanh(y)) = sigmoid(2 y).
+// ---------------------------------------------------------------------------
+// Activations and their slopes, two values at a time: an exponential and a
+// reciprocal each, the rest in packed binary32.
+// ---------------------------------------------------------------------------
 constexpr float kGeluB = 0.79788456080286536f * 2.0f;           // 2 sqrt(2 / pi)
 constexpr float kGeluC = kGeluB * 0.044715f;
 constexpr float kSqrtHalf = 0.70710678118654752f;
 constexpr float kInvSqrt2Pi = 0.39894228040143268f;
 
-template <> __device__ __forceinline__ float activation<STAR_ACT_NONE>(float x) { return x; }
-template <> __device__ __forceinline__ float activation_slope<STAR_ACT_NONE>(float) { return 1.0f; }
+// 1 / (1 + 2^y): the sigmoid of x for y = -log2(e) x.
+__device__ __forceinline__ Pair sigmoid_exp2(Pair y) { return pair_reciprocal(pair_add(pair_exp2(y), pair_of(1.0f))); }
 
-template <> __device__ __forceinline__ float activation<STAR_ACT_GELU_TANH>(float x)
+// x^2, at most 1e4: beyond |x| = 100 every sigmoid here is 0 or 1, and what
+// multiplies its slope of 0 must stay finite.
+__device__ __forceinline__ Pair bounded_square(Pair x)
 {
-    return __fmul_rn(x, sigmoid(__fmul_rn(x, __fmaf_rn(kGeluC, __fmul_rn(x, x), kGeluB))));
+    float lo, hi;
+    split_pair(pair_mul(x, x), &lo, &hi);
+    return make_pair(fminf(lo, 1e4f), fminf(hi, 1e4f));
 }
-template <> __device__ __forceinline__ float activation_slope<STAR_ACT_GELU_TANH>(float x)
-{
-    const float x2 = __fmul_rn(x, x);
-    const float q = sigmoid(__fmul_rn(x, __fmaf_rn(kGeluC, x2, kGeluB)));
-    const float inner = __fmul_rn(x, __fmaf_rn(3.0f * kGeluC, x2, kGeluB));      // x times the inner derivative
-    const float w = __fmul_rn(q, __fsub_rn(1.0f, q));
-    return w == 0.0f ? q : __fmaf_rn(w, inner, q);       // inner overflows where w is long 0
-}
+__device__ __forceinline__ Pair pair_negate(Pair x) { return x ^ 0x8000000080000000ull; }
 
-template <> __device__ __forceinline__ float activation<STAR_ACT_SILU>(float x) { return __fmul_rn(x, sigmoid(x)); }
-template <> __device__ __forceinline__ float activation_slope<STAR_ACT_SILU>(float x)
+// q + q (1 - q) inner: the slope of x sigmoid(g(x)), with inner = x g'(x).
+__device__ __forceinline__ Pair gated_slope(Pair q, Pair inner)
 {
-    const float q = sigmoid(x);
-    return __fmaf_rn(__fmul_rn(q, __fsub_rn(1.0f, q)), x, q);
+    return pair_fma(pair_mul(q, pair_add(pair_of(1.0f), pair_negate(q))), inner, q);
 }
 
-// Phi(x) and exp(-x^2 / 2) by Abramowitz and Stegun 7.1.26 (Hastings): with
-// z = |x| / sqrt(2) and t = 1 / (1 + p z), erfc(z) = (a1 t + ... + a5 t^5)
-// exp(-z^2), off by at most 1.5e-7.  One exponential and one reciprocal, and the
-// slope needs the same exponential.
-struct NormalCdf {
-    float cdf, power;
-};
-__device__ __forceinline__ NormalCdf normal_cdf(float x)
+// Phi(x) by Abramowitz and Stegun 7.1.26 (Hastings): with z = |x| / sqrt(2) and
+// t = 1 / (1 + p z), erfc(z) = (a1 t + ... + a5 t^5) exp(-z^2), off by at most
+// 1.5e-7.  *power = exp(-x^2 / 2), which the slope needs too.
+__device__ __forceinline__ Pair normal_cdf(Pair x, Pair *power)
 {
-    const float t = __fdividef(1.0f, __fmaf_rn(0.3275911f * kSqrtHalf, fabsf(x), 1.0f));
-    const float power = exp2_fast(__fmul_rn(-0.5f * kLog2e, __fmul_rn(x, x)));
-    float q = __fmaf_rn(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
-    q = __fmaf_rn(t, q, 0.5f * 1.421413741f);
-    q = __fmaf_rn(t, q, 0.5f * -0.284496736f);
-    q = __fmaf_rn(t, q, 0.5f * 0.254829592f);
-    q = __fmul_rn(__fmul_rn(t, q), power);               // erfc(z) / 2
-    return NormalCdf{x > 0.0f ? __fsub_rn(1.0f, q) : q, power};
+    const Pair size = x & 0x7fffffff7fffffffull;
+    const Pair t = pair_reciprocal(pair_fma(pair_of(0.3275911f * kSqrtHalf), size, pair_of(1.0f)));
+    *power = pair_exp2(pair_mul(pair_of(-0.5f * kLog2e), pair_mul(x, x)));
+    Pair q = pair_fma(t, pair_of(0.5f * 1.061405429f), pair_of(0.5f * -1.453152027f));
+    q = pair_fma(t, q, pair_of(0.5f * 1.421413741f));
+    q = pair_fma(t, q, pair_of(0.5f * -0.284496736f));
+    q = pair_fma(t, q, pair_of(0.5f * 0.254829592f));
+    q = pair_mul(pair_mul(t, q), *power);                // erfc(z) / 2
+    float x0, x1, q0, q1;
+    split_pair(x, &x0, &x1);
+    split_pair(q, &q0, &q1);
+    return make_pair(x0 > 0.0f ? __fsub_rn(1.0f, q0) : q0, x1 > 0.0f ? __fsub_rn(1.0f, q1) : q1);
 }
-template <> __device__ __forceinline__ float activation<STAR_ACT_GELU_ERF>(float x) { return __fmul_rn(x, normal_cdf(x).cdf); }
-template <> __device__ __forceinline__ float activation_slope<STAR_ACT_GELU_ERF>(float x)
+
+template <int ACT> __device__ __forceinline__ Pair activation(Pair x)
 {
-    const NormalCdf n = normal_cdf(x);
-    return __fmaf_rn(x, __fmul_rn(kInvSqrt2Pi, n.power), n.cdf);
+    if constexpr (ACT == STAR_ACT_GELU_TANH) {           // 0.5 (1 + tanh(y)) = sigmoid(2 y)
+        const Pair g = pair_fma(pair_of(-kLog2e * kGeluC), pair_mul(x, x), pair_of(-kLog2e * kGeluB));
+        return pair_mul(x, sigmoid_exp2(pair_mul(x, g)));
+    } else if constexpr (ACT == STAR_ACT_GELU_ERF) {
+        Pair power;
+        return pair_mul(x, normal_cdf(x, &power));
+    } else if constexpr (ACT == STAR_ACT_SILU) {
+        return pair_mul(x, sigmoid_exp2(pair_mul(x, pair_of(-kLog2e))));
+    } else {
+        return x;
+    }
+}
+
+template <int ACT> __device__ __forceinline__ Pair activation_slope(Pair x)
+{
+    if constexpr (ACT == STAR_ACT_GELU_TANH) {
+        const Pair x2 = bounded_square(x);
+        const Pair q = sigmoid_exp2(pair_mul(x, pair_fma(pair_of(-kLog2e * kGeluC), x2, pair_of(-kLog2e * kGeluB))));
+        return gated_slope(q, pair_mul(x, pair_fma(pair_of(3.0f * kGeluC), x2, pair_of(kGeluB))));
+    } else if constexpr (ACT == STAR_ACT_GELU_ERF) {
+        Pair power;
+        const Pair cdf = normal_cdf(x, &power);
+        return pair_fma(x, pair_mul(pair_of(kInvSqrt2Pi), power), cdf);
+    } else if constexpr (ACT == STAR_ACT_SILU) {
+        return gated_slope(sigmoid_exp2(pair_mul(x, pair_of(-kLog2e))), x);
+    } else {
+        return pair_of(1.0f);
+    }
+}
+
+// One value.
+template <int ACT> __device__ __forceinline__ float activation(float x)
+{
+    float lo, hi;
+    split_pair(activation<ACT>(make_pair(x, 0.0f)), &lo, &hi);
+    return lo;
+}
+template <int ACT> __device__ __forceinline__ float activation_slope(float x)
+{
+    float lo, hi;
+    split_pair(activation_slope<ACT>(make_pair(x, 0.0f)), &lo, &hi);
+    return lo;
 }
 
 struct PackArgs {
@@ -266,7 +297,7 @@ __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_pack_kernel(cons
         if (half % 2 == 0) a.kept.scales[scale_at(a.kept, t, half / 2)] = static_cast<uint8_t>(s);
         if (a.act_out) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) f[e] = activation<ACT>(f[e]);
+            for (int e = 0; e < 16; e += 2) split_pair(activation<ACT>(make_pair(f[e], f[e + 1])), &f[e], &f[e + 1]);
             Sixteen<G>::store(static_cast<char *>(a.act_out) + t * a.ld_act * G::kBytes, c, a.kept.cols, f);
         }
     }
@@ -276,14 +307,14 @@ __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_pack_kernel(cons
 __device__ __forceinline__ void widen_sixteen(const uint4 &codes, float scale, float (&f)[16])
 {
     const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
-    const float off = __fmul_rn(scale, -8388736.0f);
+    const Pair s = pair_of(scale), off = pair_of(__fmul_rn(scale, -8388736.0f));
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const uint32_t u = w[q] ^ 0x80808080u;
-        f[4 * q] = __fmaf_rn(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7650)), scale, off);
-        f[4 * q + 1] = __fmaf_rn(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7651)), scale, off);
-        f[4 * q + 2] = __fmaf_rn(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7652)), scale, off);
-        f[4 * q + 3] = __fmaf_rn(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7653)), scale, off);
+        const Pair lo = make_pair(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7650)), __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7651)));
+        const Pair hi = make_pair(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7652)), __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7653)));
+        split_pair(pair_fma(lo, s, off), &f[4 * q], &f[4 * q + 1]);
+        split_pair(pair_fma(hi, s, off), &f[4 * q + 2], &f[4 * q + 3]);
     }
 }
 
@@ -305,10 +336,11 @@ __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_read_kernel(cons
             float dy[16];
             Sixteen<G>::widen(w, dy);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) f[e] = __fmul_rn(dy[e], activation_slope<ACT>(f[e]));
+            for (int e = 0; e < 16; e += 2)
+                split_pair(pair_mul(make_pair(dy[e], dy[e + 1]), activation_slope<ACT>(make_pair(f[e], f[e + 1]))), &f[e], &f[e + 1]);
         } else {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) f[e] = activation<ACT>(f[e]);
+            for (int e = 0; e < 16; e += 2) split_pair(activation<ACT>(make_pair(f[e], f[e + 1])), &f[e], &f[e + 1]);
         }
         Sixteen<G>::store(static_cast<char *>(a.out) + t * a.ld * G::kBytes, c, a.kept.cols, f);
     }

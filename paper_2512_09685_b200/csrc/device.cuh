@@ -41,6 +41,55 @@ template <typename G> __device__ __forceinline__ void store_value(void *base, in
         static_cast<float *>(base)[i] = x;
 }
 
+// Two binary32 values worked on by one instruction.
+using Pair = unsigned long long;
+__device__ __forceinline__ Pair make_pair(float lo, float hi)
+{
+    Pair r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void split_pair(Pair p, float *lo, float *hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*lo), "=f"(*hi) : "l"(p)); }
+__device__ __forceinline__ Pair pair_add(Pair a, Pair b)
+{
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ Pair pair_mul(Pair a, Pair b)
+{
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ Pair pair_fma(Pair a, Pair b, Pair c)
+{
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+__device__ __forceinline__ Pair pair_of(float x) { return make_pair(x, x); }
+__device__ __forceinline__ Pair pair_exp2(Pair p)
+{
+    float lo, hi;
+    split_pair(p, &lo, &hi);
+    return make_pair(exp2_fast(lo), exp2_fast(hi));
+}
+// 1 / x, 1 ulp; 0 for an infinite x.
+__device__ __forceinline__ float reciprocal_fast(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ Pair pair_reciprocal(Pair p)
+{
+    float lo, hi;
+    split_pair(p, &lo, &hi);
+    return make_pair(reciprocal_fast(lo), reciprocal_fast(hi));
+}
+
 // ---------------------------------------------------------------------------
 // Shared memory, clusters, and launches that follow one another.
 // ---------------------------------------------------------------------------

@@ -231,34 +231,6 @@ __device__ __forceinline__ MaxSum warp_join(MaxSum x, float k)
     return MaxSum{m, warp_sum(__fmul_rn(x.s, rebase(x.m, m, k)))};
 }
 
-// Two binary32 values worked on by one instruction.
-using Pair = unsigned long long;
-__device__ __forceinline__ Pair make_pair(float lo, float hi)
-{
-    Pair r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ void split_pair(Pair p, float *lo, float *hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*lo), "=f"(*hi) : "l"(p)); }
-__device__ __forceinline__ Pair pair_add(Pair a, Pair b)
-{
-    Pair r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ Pair pair_mul(Pair a, Pair b)
-{
-    Pair r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ Pair pair_fma(Pair a, Pair b, Pair c)
-{
-    Pair r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-
 template <typename G> struct Granule {
     static constexpr int kCount = 16 / G::kBytes;                // elements
     static constexpr int kPairs = kCount / 2;
