@@ -14,8 +14,11 @@ bool is_act(int act) { return act >= STAR_ACT_NONE && act <= STAR_ACT_SILU; }
 
 int grid_for(int64_t blocks) { return static_cast<int>(blocks < 1 ? 1 : blocks < 148 * 64 ? blocks : 148 * 64); }
 
-// Whether every row of a matrix starts on a 16-byte boundary.
-bool on_grid(const void *p, int64_t ld, int size) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (ld * size) % 16 == 0; }
+// Whether every row of a matrix starts on a boundary of `bytes`.
+bool on_grid(const void *p, int64_t ld, int size, int bytes = 16)
+{
+    return reinterpret_cast<uintptr_t>(p) % static_cast<unsigned>(bytes) == 0 && (ld * size) % bytes == 0;
+}
 
 // i / d = (i * magic) >> (32 + shift) for all i < 2^31: magic = floor(2^(32 + shift) / d) + 1
 // with 2^shift the power of two at or below d - 1, so that it fits 32 bits.
@@ -34,16 +37,22 @@ template <typename Items, typename F> star_status_t by_rows(int64_t rows, int64_
     const int64_t most = (int64_t{1} << 30) / per_row;
     for (int64_t first = 0; first < rows; first += most) {
         const int64_t n = std::min(most, rows - first) * per_row;
-        launch(Items{make_divisor(static_cast<uint32_t>(per_row)), static_cast<uint32_t>(first), static_cast<uint32_t>(n)},
-               grid_for((n + items_per_block - 1) / items_per_block));
+        Items items{};
+        items.per_row = make_divisor(static_cast<uint32_t>(per_row));
+        items.first_row = static_cast<uint32_t>(first);
+        items.n = static_cast<uint32_t>(n);
+        launch(items, grid_for((n + items_per_block - 1) / items_per_block));
         const star_status_t st = launched();
         if (st != STAR_OK) return st;
     }
     return STAR_OK;
 }
-template <typename F> star_status_t by_halves(int64_t rows, int64_t cols, F launch)
+template <typename F> star_status_t by_halves(int64_t rows, int64_t cols, bool wide, F launch)
 {
-    return by_rows<Halves>(rows, (cols + 31) / 32 * 2, kKeepThreads, launch);
+    return by_rows<Halves>(rows, (cols + 31) / 32 * 2, kKeepThreads, [&](Halves h, int grid) {
+        h.wide = wide;
+        launch(h, grid);
+    });
 }
 template <typename F> star_status_t by_groups(int64_t rows, int64_t cols, F launch)
 {
@@ -103,10 +112,11 @@ extern "C" star_status_t star_checkpoint_pack(int8_t *codes, uint8_t *scales, co
     if (!countable(rows, cols)) return STAR_ERR_UNSUPPORTED;
     const int size = dtype_size(dtype);
     const bool vector = on_grid(x, ld, size) && (!act_out || on_grid(act_out, ld_act, size));
+    const bool wide = on_grid(x, ld, size, 32) && (!act_out || on_grid(act_out, ld_act, size, 32));
     with_act(act, [&](auto k) {
         constexpr int ACT = decltype(k)::value;
         if (vector)
-            st = by_halves(rows, cols, [&](const Halves &h, int grid) {
+            st = by_halves(rows, cols, wide, [&](const Halves &h, int grid) {
                 if (dtype == STAR_DTYPE_BF16)
                     star_checkpoint_pack_kernel<GradBF16, ACT><<<grid, kKeepThreads, 0, stream>>>(a, h);
                 else
@@ -131,11 +141,12 @@ template <bool BACKWARD> star_status_t read_kept(const ReadArgs &a, star_dtype_t
     if (!countable(a.kept.rows, a.kept.cols)) return STAR_ERR_UNSUPPORTED;
     const int size = dtype_size(dtype);
     const bool vector = on_grid(a.out, a.ld, size) && (!BACKWARD || on_grid(a.dy, a.ld_dy, size));
+    const bool wide = on_grid(a.out, a.ld, size, 32) && (!BACKWARD || on_grid(a.dy, a.ld_dy, size, 32));
     star_status_t st = STAR_OK;
     with_act(act, [&](auto k) {
         constexpr int ACT = decltype(k)::value;
         if (vector)
-            st = by_halves(a.kept.rows, a.kept.cols, [&](const Halves &h, int grid) {
+            st = by_halves(a.kept.rows, a.kept.cols, wide, [&](const Halves &h, int grid) {
                 if (dtype == STAR_DTYPE_BF16)
                     star_checkpoint_read_kernel<GradBF16, ACT, BACKWARD><<<grid, kKeepThreads, 0, stream>>>(a, h);
                 else

@@ -161,7 +161,7 @@ constexpr int kKeepThreads = 256;
 
 // ---------------------------------------------------------------------------
 // Rows whose values start on 16-byte boundaries: a thread takes half a block, 16
-// columns, and its neighbour the other half; all accesses are 16 bytes.  The
+// columns, and its neighbour the other half; all accesses are 16 or 32 bytes.  The
 // work is numbered row by row, an even number of halves to a row, so that two
 // neighbouring lanes always share a block.
 //
@@ -177,20 +177,44 @@ struct Divisor {
 };
 __device__ __forceinline__ uint32_t divide(uint32_t i, const Divisor &d) { return d.d == 1 ? i : __umulhi(i, d.magic) >> d.shift; }
 
+// 32 bytes by one access where the rows allow it (every row 32-byte aligned): a
+// whole sector, where two of 16 bytes would touch each sector twice.
+__device__ __forceinline__ void load_words(const void *p, uint32_t (&w)[8])
+{
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p) : "memory");
+}
+__device__ __forceinline__ void store_words(void *p, const uint32_t (&w)[8])
+{
+    asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                 :: "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "l"(p) : "memory");
+}
+
 struct Halves {
     Divisor per_row;     // halves of a row: an even number
     uint32_t first_row;  // rows in front of this launch
     uint32_t n;          // halves of this launch
+    int wide;            // rows are 32-byte aligned
 };
 
 template <typename G> struct Sixteen {
     static constexpr int kWords = G::kBytes * 4;
     static constexpr int kEach = 16 / G::kBytes;         // values in 16 bytes
     // 16 values of a row from column c on; columns past the end read as 0.
-    static __device__ __forceinline__ void load(const void *row, int64_t c, int64_t cols, uint32_t (&w)[kWords])
+    static __device__ __forceinline__ void load(const void *row, int64_t c, int64_t cols, int wide, uint32_t (&w)[kWords])
     {
         const char *p = static_cast<const char *>(row) + c * G::kBytes;
         const int left = static_cast<int>(min(cols - c, int64_t{16}));
+        if (wide && left == 16) {
+#pragma unroll
+            for (int q = 0; q < kWords / 8; ++q) {
+                uint32_t v[8];
+                load_words(p + 32 * q, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[8 * q + e] = v[e];
+            }
+            return;
+        }
 #pragma unroll
         for (int q = 0; q < kWords / 4; ++q) {
             if ((q + 1) * kEach <= left) {
@@ -234,7 +258,7 @@ template <typename G> struct Sixteen {
             return m;
         }
     }
-    static __device__ __forceinline__ void store(void *row, int64_t c, int64_t cols, const float (&f)[16])
+    static __device__ __forceinline__ void store(void *row, int64_t c, int64_t cols, int wide, const float (&f)[16])
     {
         char *p = static_cast<char *>(row) + c * G::kBytes;
         uint32_t w[kWords];
@@ -246,6 +270,16 @@ template <typename G> struct Sixteen {
                 w[q] = __float_as_uint(f[q]);
         }
         const int left = static_cast<int>(min(cols - c, int64_t{16}));
+        if (wide && left == 16) {
+#pragma unroll
+            for (int q = 0; q < kWords / 8; ++q) {
+                uint32_t v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = w[8 * q + e];
+                store_words(p + 32 * q, v);
+            }
+            return;
+        }
 #pragma unroll
         for (int q = 0; q < kWords / 4; ++q) {
             if ((q + 1) * kEach <= left) {
@@ -277,7 +311,7 @@ __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_pack_kernel(cons
         uint32_t w[Sixteen<G>::kWords];
         uint32_t largest = 0;
         if (in) {
-            Sixteen<G>::load(static_cast<const char *>(a.x) + t * a.ld * G::kBytes, c, a.kept.cols, w);
+            Sixteen<G>::load(static_cast<const char *>(a.x) + t * a.ld * G::kBytes, c, a.kept.cols, h.wide, w);
             largest = Sixteen<G>::largest(w);
         }
         largest = max(largest, __shfl_xor_sync(0xffffffffu, largest, 1));
@@ -298,7 +332,7 @@ __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_pack_kernel(cons
         if (a.act_out) {
 #pragma unroll
             for (int e = 0; e < 16; e += 2) split_pair(activation<ACT>(make_pair(f[e], f[e + 1])), &f[e], &f[e + 1]);
-            Sixteen<G>::store(static_cast<char *>(a.act_out) + t * a.ld_act * G::kBytes, c, a.kept.cols, f);
+            Sixteen<G>::store(static_cast<char *>(a.act_out) + t * a.ld_act * G::kBytes, c, a.kept.cols, h.wide, f);
         }
     }
 }
@@ -329,7 +363,7 @@ __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_read_kernel(cons
         const uint4 codes = *reinterpret_cast<const uint4 *>(a.kept.codes + t * a.kept.pitch + c);
         const float scale = scale_value(a.kept.scales[scale_at(a.kept, t, half / 2)]);
         uint32_t w[Sixteen<G>::kWords];
-        if constexpr (BACKWARD) Sixteen<G>::load(static_cast<const char *>(a.dy) + t * a.ld_dy * G::kBytes, c, a.kept.cols, w);
+        if constexpr (BACKWARD) Sixteen<G>::load(static_cast<const char *>(a.dy) + t * a.ld_dy * G::kBytes, c, a.kept.cols, h.wide, w);
         float f[16];
         widen_sixteen(codes, scale, f);
         if constexpr (BACKWARD) {
@@ -342,7 +376,7 @@ __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_read_kernel(cons
 #pragma unroll
             for (int e = 0; e < 16; e += 2) split_pair(activation<ACT>(make_pair(f[e], f[e + 1])), &f[e], &f[e + 1]);
         }
-        Sixteen<G>::store(static_cast<char *>(a.out) + t * a.ld * G::kBytes, c, a.kept.cols, f);
+        Sixteen<G>::store(static_cast<char *>(a.out) + t * a.ld * G::kBytes, c, a.kept.cols, h.wide, f);
     }
 }
 
