@@ -59,8 +59,8 @@ MAX_REPEATS = 50
 # capture was taken on: once the sources differ the figure is stale and
 # `traffic` is reported as null.
 NCU_TRAFFIC_PER_ELEMENT = {
-    "cfg4_gpt2_medium": (1644.47e6 / 34_631_680, "03e0fa45a87f327661444bc4c1aff616ef7e6deddd70b78ae0dd5d517a48867b"),
-    "cfg1_resnet50": (787.86e6 / 25_557_032, "03e0fa45a87f327661444bc4c1aff616ef7e6deddd70b78ae0dd5d517a48867b"),
+    "cfg4_gpt2_medium": (1644.19e6 / 34_631_680, "f02141dc889b0eb48a4d768c3881808302cc124fbc819b693cd40fc5c2a556ac"),
+    "cfg1_resnet50": (789.33e6 / 25_557_032, "f02141dc889b0eb48a4d768c3881808302cc124fbc819b693cd40fc5c2a556ac"),
 }
 
 

@@ -20,10 +20,11 @@ void count_launch();
 // after this), once the work on `stream` is done.
 cudaError_t weight_grad_expired(cudaStream_t stream, int *expired);
 
-// The status of the launch just made.
-inline star_status_t launched()
+// The status of the launch just made; `e` is what the launching call returned.
+inline star_status_t launched(cudaError_t e = cudaSuccess)
 {
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t noted = cudaGetLastError();
+    if (e == cudaSuccess) e = noted;
     if (e != cudaSuccess) return cuda_failed(e);
     count_launch();
     return STAR_OK;

@@ -40,8 +40,7 @@ star_status_t launch(void (*kernel)(Params...), int64_t grid, int threads, size_
     }
     config.attrs = attributes;
     config.numAttrs = static_cast<unsigned>(n);
-    const cudaError_t e = cudaLaunchKernelEx(&config, kernel, args...);
-    return e == cudaSuccess ? launched() : cuda_failed(e);
+    return launched(cudaLaunchKernelEx(&config, kernel, args...));
 }
 
 // Clusters of a kernel that the device holds at once, per device, cluster size

@@ -155,8 +155,7 @@ star_status_t launch_shape(const WeightGradTile &tile, const CUtensorMap &codes,
     constexpr int64_t columns = S::kBlocks * kTileC;
     fill_config(&config, &attribute, (tile.a.kept.cols + columns - 1) / columns, (tile.a.outs + S::kOuts - 1) / S::kOuts, S::kBlocks,
                 parts, S::Smem::kDynamic, stream);
-    const cudaError_t e = cudaLaunchKernelEx(&config, S::kernel(), tile, codes, dy, static_cast<int>(dw_bf16));
-    return e == cudaSuccess ? launched() : cuda_failed(e);
+    return launched(cudaLaunchKernelEx(&config, S::kernel(), tile, codes, dy, static_cast<int>(dw_bf16)));
 }
 
 // Shape and number of parts with the least expected time: the waves of tiles the
@@ -255,8 +254,8 @@ extern "C" star_status_t star_checkpoint_weight_grad(void *dw, star_dtype_t dw_d
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const bool y16 = dy_dtype == STAR_DTYPE_BF16, w16 = dw_dtype == STAR_DTYPE_BF16;
     if (rows >= 0x7fffff00 || cols >= 0x7fffff00 || outs >= 0x7fffff00 || std::max(cols, outs) > int64_t{65535} * kFewOuter) return STAR_ERR_UNSUPPORTED;
-    // The TMA reads dy in place: rows on the 16-byte grid.
-    const bool tiled = y16 && reinterpret_cast<uintptr_t>(dy) % 16 == 0 && ld_dy % 8 == 0;
+    // The TMA reads dy in place: rows on the 16-byte grid, strides of up to 40 bits.
+    const bool tiled = y16 && reinterpret_cast<uintptr_t>(dy) % 16 == 0 && ld_dy % 8 == 0 && ld_dy < (int64_t{1} << 38);
     Device *device = nullptr;
     const cudaError_t e = prepared_device(&device);
     if (e != cudaSuccess) return cuda_failed(e);
