@@ -87,9 +87,24 @@ template <typename Kernel> cudaError_t held_clusters(Kernel kernel, Held &known,
     return cudaSuccess;
 }
 
-// The rows' statistics: blocks of 32 to 256 threads with two batches of granules
-// or more for each thread, and a cluster of blocks per row where there are fewer
-// rows than half the SMs.
+// The rows' statistics.
+//
+// Threads to a row: as few as keep an SM busy, since a row's joins and the wait
+// for its first loads cost the same for any number; but 128 or 256 for rows of
+// more than 32 or 128 KB, whose last ones would otherwise be waited for.  More
+// for fewer rows, until there are about 900 threads to an SM.  bf16, us:
+//   rows x vocab      32 threads     64    128    256
+//   16384 x  4000           29.8   34.3   39.5   51.5
+//    4096 x 16000           26.1   28.9   27.0   30.8
+//    4096 x 50257           72.1   74.9   68.2   70.3
+//    4096 x 131072         177    184    165    161
+//    2048 x  8192           11.2    9.6   10.6   12.2
+//     512 x  8192            9.0    6.7    5.7    5.2
+// Few long rows: clusters of blocks, up to four blocks of 256 threads to an SM.
+// 1, 2, 4 and 8 blocks to a row:
+//      64 x 50257            9.7    8.0    6.5    6.7
+//     256 x 50257           11.0   10.2   12.6   17.5
+//      64 x  8192            3.0    3.6    3.6    3.8   (16 KB: one block)
 template <typename G, bool POLICY, int THREADS>
 star_status_t launch_rows(const RowWork &a, int cluster, int *parts_out, cudaStream_t stream)
 {
@@ -98,9 +113,11 @@ star_status_t launch_rows(const RowWork &a, int cluster, int *parts_out, cudaStr
     int held = 0;
     const cudaError_t e = held_clusters(kernel, known, THREADS, cluster, 0, &held);
     if (e != cudaSuccess) return cuda_failed(e);
-    // Short rows: as many blocks as the device holds, each with many rows.  Long
-    // rows: a block each, which evens out rows that are skipped.
-    const int64_t most = a.row.vocab * G::kBytes < 16384 ? held : int64_t{1} << 20, clusters = std::min(a.row.rows, most);
+    // Blocks of a warp: as many as the device holds, each with many rows (16384 x
+    // 200: 10.5 us, a block each 18.0).  Larger ones: a block each, which evens out
+    // their ends and rows that are skipped (16384 x 50257 with 128 threads: 252 us,
+    // as many as it holds 286).
+    const int64_t most = THREADS == 32 ? held : int64_t{1} << 20, clusters = std::min(a.row.rows, most);
     *parts_out = static_cast<int>(clusters);
     return launch(kernel, clusters * cluster, THREADS, 0, cluster, false, stream, a);
 }
@@ -108,9 +125,9 @@ star_status_t launch_rows(const RowWork &a, int cluster, int *parts_out, cudaStr
 template <typename G, bool POLICY> star_status_t walk_rows(const RowWork &a, int *parts_out, cudaStream_t stream)
 {
     const int64_t granules = a.row.vocab * G::kBytes / 16;
-    int cluster = 1, threads = 32;
-    while (cluster < 8 && a.row.rows * cluster * 2 <= 148 && granules / (cluster * 2) >= 512) cluster *= 2;
-    while (threads < 256 && granules / cluster > static_cast<int64_t>(threads) * 2 * kBatch) threads *= 2;
+    int cluster = 1, threads = granules <= 2048 ? 32 : granules <= 8192 ? 128 : 256;
+    while (threads < 256 && threads < granules && a.row.rows * threads < 148 * 800) threads *= 2;
+    while (granules > 2048 && cluster < 8 && a.row.rows * cluster * 2 <= 148 * 4 && granules / (cluster * 2) >= 448) cluster *= 2;
     switch (threads) {
     case 32: return launch_rows<G, POLICY, 32>(a, cluster, parts_out, stream);
     case 64: return launch_rows<G, POLICY, 64>(a, cluster, parts_out, stream);
@@ -134,14 +151,19 @@ template <typename G, int THREADS> star_status_t launch_policy(const RowWork &a,
 }
 
 // Whether the policy loss is made in one reading (and the smallest block whose
-// part of the SM's shared memory holds a row): rows of up to 224 KB, and enough
-// of them to fill half the SMs with a block each.  Fewer rows are shared by
-// clusters and read twice.  The same with and without a gradient, so that both
-// give the same bits.
+// part of the SM's shared memory holds a row): rows of up to 224 KB, and more
+// than three of them to an SM.  Fewer are shared by clusters and read twice, the
+// second time from L2.  The same with and without a gradient, so that both give
+// the same bits.  us, one reading / two:
+//   rows     8192 bf16   32000 bf16   50257 bf16    50257 fp32
+//    148     9.2 / 8.5  12.5 / 11.3  15.7 / 14.5   21.3 / 20.0
+//    444    11.6 / 10.5 22.6 / 19.1  30.0 / 28.6   46.6 / 51.7
+//    592    11.9 / 11.5 23.8 / 22.9  31.4 / 36.2   57.3 / 67.1
+//   1024    14.8 / 15.4 38.7 / 39.7  53.2 / 63.4   88.3 / 109.5
 bool one_reading(int64_t rows, int64_t vocab, int size, int *threads)
 {
     const int64_t bytes = vocab * size;
-    if (rows * 2 <= 148) return false;
+    if (rows <= 148 * 3) return false;
     for (int t : {32, 64, 128, 256, 512, 1024}) {
         *threads = t;
         if (bytes <= kKeepBytesPerThread * t) return true;

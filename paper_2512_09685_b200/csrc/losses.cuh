@@ -411,8 +411,8 @@ __device__ __forceinline__ int edge_element(const RowSplit &s, int i, int vocab)
 // few rows, owns a row; every thread keeps a running maximum and sum, which join
 // through warps, block and cluster, and one thread makes the row's results.
 // Nothing is shared between a row's elements until the join, so many small
-// blocks hide one another's loads: blocks of 256 threads, 1280 threads an SM,
-// read 4096 x 50257 bf16 in 72 us (5.7 TB/s), blocks of 512 and 1024 in 92.
+// blocks hide one another's loads: 4096 x 50257 bf16 in 68 us (6.0 TB/s; blocks
+// of 512 and 1024 threads took 92), 16384 x 16000 in 86 (6.1 TB/s).
 // ---------------------------------------------------------------------------
 template <typename G, bool POLICY, int THREADS>
 __global__ void __launch_bounds__(THREADS, row_blocks(THREADS)) star_row_kernel(const __grid_constant__ RowWork a)
