@@ -58,6 +58,17 @@ bool make_map(CUtensorMap *map, CUtensorMapDataType type, const void *base, int6
 //   kLoosePair, kLooseSingle    dy in bf16 off the 16-byte grid: 256 x 128 by a
 //              pair, 128 x 128 by a block
 //   kCutPair, kCutSingle        dy in fp32, three terms: the same
+// Each in its best number of parts, us (bf16; rows, columns -> outputs):
+//                          kWide  kNarrow  kSingle  kSmall
+//   16384, 1024 -> 4096    110    149      150      288
+//    8192, 4096 -> 4096    203    363      313      505
+//    8192, 1024 -> 1024     39     34       29       42
+//     515, 1024 -> 1024     14.7   11.8     11.1     10.1
+//     100,  256 ->  256     10.1    7.5      6.8      5.7
+// dw in fp32, kNarrowSum 193 and kSingleSum 193 for the first, kSingleSum 34 for
+// the third (kSingle in parts within a run of the sum: 29).  By pair / by block:
+// loose dy 395 / 514 for the first, 56 / 71 for the third, 14.0 / 12.0 for 2048,
+// 128 -> 1024; fp32 dy 567 / 684, 77 / 92 and 17.6 / 15.8.
 enum Shape { kWide, kNarrow, kSingle, kSmall, kNarrowSum, kSingleSum, kLoosePair, kLooseSingle, kCutPair, kCutSingle, kShapes };
 constexpr int kMostParts = 8;
 
@@ -163,8 +174,8 @@ star_status_t launch_shape(const WeightGradTile &tile, const CUtensorMap &codes,
 // Measured (us; 8 to 256 steps, 128 to 4096 columns): the rest beside the steps
 // takes 5 and, split, 17 with 512 outputs and 12 with 256 or fewer (accumulators
 // through distributed shared memory).  16384 rows, 1024 -> 4096: kWide in 2 parts
-// 114 us, in 1 part 191, kNarrow 150, kSingle 148.  8192 rows, 1024 -> 1024:
-// kSingle in 4 parts 31 us, in 1 part 77, kWide in 4 parts 41.
+// 110 us, in 1 part 185.  8192 rows, 1024 -> 1024: kSingle in 4 parts 29 us, in 1
+// part 75.
 struct Plan {
     Shape shape;
     int parts;
@@ -204,8 +215,9 @@ constexpr Candidate kLooseDy[2] = {{kLoosePair, 2, 128, 0.9, 10.0, 0}, {kLooseSi
 constexpr Candidate kCutDy[2] = {{kCutPair, 2, 128, 1.0, 10.0, 0}, {kCutSingle, 1, 128, 1.2, 10.0, 0}};
 
 // Few rows on the ordinary units, where that takes less than the tensor cores'
-// `us`: waves of tiles, two to an SM, each of 2 us and 0.25 us a row.  Measured at
-// 4096 x 4096, fp32: 1 row 15 us against 51, 16 rows 25 against 51.
+// `us`: waves of tiles, two to an SM, each of 2 us and 0.25 us a row.  4096 x 4096,
+// here / tensor cores: bf16 1 row 11.1 / 18.7 us, 8 rows 19.5 / 18.7, 16 rows 26 / 18;
+// dy and dw in fp32 1 row 15.8 / 50, 16 rows 31 / 50, 64 rows 88 / 50.
 bool few_rows(int64_t rows, int64_t cols, int64_t outs, bool transposed, double us)
 {
     const int64_t inner = transposed ? outs : cols, outer = transposed ? cols : outs;

@@ -709,7 +709,7 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
 // on the ordinary units: a block makes 64 x 256 results, a thread 8 x 8 of them,
 // rows 32 at a time in shared memory.  The result's inner index, along which dw
 // is stored, runs over the lanes: columns, or outputs where dw is transposed.
-// 4096 x 4096 from 1 row: bf16 9 us, fp32 14 us (tensor cores 21 and 51).
+// 4096 x 4096 from 1 row: bf16 11 us (3.0 TB/s), fp32 16 (4.2 TB/s).
 // ---------------------------------------------------------------------------
 constexpr int kFewRows = 32, kFewOuter = 64, kFewInner = 256, kFewThreads = 256;
 
