@@ -30,9 +30,9 @@ Divisor make_divisor(uint32_t d)
     return r;
 }
 
-// Runs launch(items, grid) on the rows in runs of at most 2^30 items, `per_row`
+// Runs launch_items(items, grid) on the rows in runs of at most 2^30 items, `per_row`
 // of them to a row (one run, for all but checkpoints of 16 GB and more).
-template <typename Items, typename F> star_status_t by_rows(int64_t rows, int64_t per_row, int items_per_block, F launch)
+template <typename Items, typename F> star_status_t by_rows(int64_t rows, int64_t per_row, int items_per_block, F launch_items)
 {
     const int64_t most = (int64_t{1} << 30) / per_row;
     for (int64_t first = 0; first < rows; first += most) {
@@ -41,22 +41,21 @@ template <typename Items, typename F> star_status_t by_rows(int64_t rows, int64_
         items.per_row = make_divisor(static_cast<uint32_t>(per_row));
         items.first_row = static_cast<uint32_t>(first);
         items.n = static_cast<uint32_t>(n);
-        launch(items, grid_for((n + items_per_block - 1) / items_per_block));
-        const star_status_t st = launched();
+        const star_status_t st = launch_items(items, grid_for((n + items_per_block - 1) / items_per_block));
         if (st != STAR_OK) return st;
     }
     return STAR_OK;
 }
-template <typename F> star_status_t by_halves(int64_t rows, int64_t cols, bool wide, F launch)
+template <typename F> star_status_t by_halves(int64_t rows, int64_t cols, bool wide, F launch_items)
 {
     return by_rows<Halves>(rows, (cols + 31) / 32 * 2, kKeepThreads, [&](Halves h, int grid) {
         h.wide = wide;
-        launch(h, grid);
+        return launch_items(h, grid);
     });
 }
-template <typename F> star_status_t by_groups(int64_t rows, int64_t cols, F launch)
+template <typename F> star_status_t by_groups(int64_t rows, int64_t cols, F launch_items)
 {
-    return by_rows<Groups>(rows, ((cols + 31) / 32 + kLoose - 1) / kLoose, kKeepThreads / 32, launch);
+    return by_rows<Groups>(rows, ((cols + 31) / 32 + kLoose - 1) / kLoose, kKeepThreads / 32, launch_items);
 }
 
 // Rows and the items of a row are numbered in 32 bits.
@@ -118,16 +117,14 @@ extern "C" star_status_t star_checkpoint_pack(int8_t *codes, uint8_t *scales, co
         if (vector)
             st = by_halves(rows, cols, wide, [&](const Halves &h, int grid) {
                 if (dtype == STAR_DTYPE_BF16)
-                    star_checkpoint_pack_kernel<GradBF16, ACT><<<grid, kKeepThreads, 0, stream>>>(a, h);
-                else
-                    star_checkpoint_pack_kernel<GradF32, ACT><<<grid, kKeepThreads, 0, stream>>>(a, h);
+                    return launch(star_checkpoint_pack_kernel<GradBF16, ACT>, dim3(static_cast<unsigned>(grid)), kKeepThreads, 0, dim3(1), stream, a, h);
+                return launch(star_checkpoint_pack_kernel<GradF32, ACT>, dim3(static_cast<unsigned>(grid)), kKeepThreads, 0, dim3(1), stream, a, h);
             });
         else
             st = by_groups(rows, cols, [&](const Groups &h, int grid) {
                 if (dtype == STAR_DTYPE_BF16)
-                    star_checkpoint_pack_loose_kernel<GradBF16, ACT><<<grid, kKeepThreads, 0, stream>>>(a, h);
-                else
-                    star_checkpoint_pack_loose_kernel<GradF32, ACT><<<grid, kKeepThreads, 0, stream>>>(a, h);
+                    return launch(star_checkpoint_pack_loose_kernel<GradBF16, ACT>, dim3(static_cast<unsigned>(grid)), kKeepThreads, 0, dim3(1), stream, a, h);
+                return launch(star_checkpoint_pack_loose_kernel<GradF32, ACT>, dim3(static_cast<unsigned>(grid)), kKeepThreads, 0, dim3(1), stream, a, h);
             });
     });
     return st;
@@ -148,16 +145,14 @@ template <bool BACKWARD> star_status_t read_kept(const ReadArgs &a, star_dtype_t
         if (vector)
             st = by_halves(a.kept.rows, a.kept.cols, wide, [&](const Halves &h, int grid) {
                 if (dtype == STAR_DTYPE_BF16)
-                    star_checkpoint_read_kernel<GradBF16, ACT, BACKWARD><<<grid, kKeepThreads, 0, stream>>>(a, h);
-                else
-                    star_checkpoint_read_kernel<GradF32, ACT, BACKWARD><<<grid, kKeepThreads, 0, stream>>>(a, h);
+                    return launch(star_checkpoint_read_kernel<GradBF16, ACT, BACKWARD>, dim3(static_cast<unsigned>(grid)), kKeepThreads, 0, dim3(1), stream, a, h);
+                return launch(star_checkpoint_read_kernel<GradF32, ACT, BACKWARD>, dim3(static_cast<unsigned>(grid)), kKeepThreads, 0, dim3(1), stream, a, h);
             });
         else
             st = by_groups(a.kept.rows, a.kept.cols, [&](const Groups &h, int grid) {
                 if (dtype == STAR_DTYPE_BF16)
-                    star_checkpoint_read_loose_kernel<GradBF16, ACT, BACKWARD><<<grid, kKeepThreads, 0, stream>>>(a, h);
-                else
-                    star_checkpoint_read_loose_kernel<GradF32, ACT, BACKWARD><<<grid, kKeepThreads, 0, stream>>>(a, h);
+                    return launch(star_checkpoint_read_loose_kernel<GradBF16, ACT, BACKWARD>, dim3(static_cast<unsigned>(grid)), kKeepThreads, 0, dim3(1), stream, a, h);
+                return launch(star_checkpoint_read_loose_kernel<GradF32, ACT, BACKWARD>, dim3(static_cast<unsigned>(grid)), kKeepThreads, 0, dim3(1), stream, a, h);
             });
     });
     return st;

@@ -302,6 +302,7 @@ template <typename G> struct Sixteen {
 template <typename G, int ACT>
 __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_pack_kernel(const __grid_constant__ PackArgs a, const __grid_constant__ Halves h)
 {
+    wait_for_primary();
     // Whole warps go round the loop: neighbours exchange their magnitudes.
     for (uint32_t base = blockIdx.x * kKeepThreads; base < h.n; base += gridDim.x * kKeepThreads) {
         const uint32_t i = base + threadIdx.x;
@@ -356,6 +357,7 @@ __device__ __forceinline__ void widen_sixteen(const uint4 &codes, float scale, f
 template <typename G, int ACT, bool BACKWARD>
 __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_read_kernel(const __grid_constant__ ReadArgs a, const __grid_constant__ Halves h)
 {
+    wait_for_primary();
     for (uint32_t i = blockIdx.x * kKeepThreads + threadIdx.x; i < h.n; i += gridDim.x * kKeepThreads) {
         const uint32_t row = divide(i, h.per_row), half = i - row * h.per_row.d;
         const int64_t t = static_cast<int64_t>(h.first_row) + row, c = static_cast<int64_t>(half) * 16;
@@ -395,6 +397,7 @@ struct Groups {
 template <typename G, int ACT>
 __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_pack_loose_kernel(const __grid_constant__ PackArgs a, const __grid_constant__ Groups h)
 {
+    wait_for_primary();
     const int lane = threadIdx.x % 32;
     for (uint32_t i = blockIdx.x * (kKeepThreads / 32) + threadIdx.x / 32; i < h.n; i += gridDim.x * (kKeepThreads / 32)) {
         const uint32_t row = divide(i, h.per_row), group = i - row * h.per_row.d;
@@ -424,6 +427,7 @@ __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_pack_loose_kerne
 template <typename G, int ACT, bool BACKWARD>
 __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_read_loose_kernel(const __grid_constant__ ReadArgs a, const __grid_constant__ Groups h)
 {
+    wait_for_primary();
     const int lane = threadIdx.x % 32;
     for (uint32_t i = blockIdx.x * (kKeepThreads / 32) + threadIdx.x / 32; i < h.n; i += gridDim.x * (kKeepThreads / 32)) {
         const uint32_t row = divide(i, h.per_row), group = i - row * h.per_row.d;

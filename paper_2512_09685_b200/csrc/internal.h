@@ -30,6 +30,30 @@ inline star_status_t launched(cudaError_t e = cudaSuccess)
     return STAR_OK;
 }
 
+// Launches `kernel` as a programmatic dependent of the kernel in front of it in
+// the stream: its blocks may be set up before that one is done, and wait by
+// themselves before they touch memory.  Also the cheaper launch for the host, by
+// 1 to 2 us.  `cluster` of one block: none.
+template <typename... Params, typename... Args>
+star_status_t launch(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, dim3 cluster, cudaStream_t stream, const Args &...args)
+{
+    cudaLaunchConfig_t config{};
+    config.gridDim = grid;
+    config.blockDim = dim3(static_cast<unsigned>(threads));
+    config.dynamicSmemBytes = smem;
+    config.stream = stream;
+    cudaLaunchAttribute attributes[2] = {};
+    attributes[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attributes[0].val.programmaticStreamSerializationAllowed = 1;
+    attributes[1].id = cudaLaunchAttributeClusterDimension;
+    attributes[1].val.clusterDim.x = cluster.x;
+    attributes[1].val.clusterDim.y = cluster.y;
+    attributes[1].val.clusterDim.z = cluster.z;
+    config.attrs = attributes;
+    config.numAttrs = cluster.x * cluster.y * cluster.z > 1 ? 2 : 1;
+    return launched(cudaLaunchKernelEx(&config, kernel, args...));
+}
+
 inline bool is_dtype(int dt) { return dt == STAR_DTYPE_F32 || dt == STAR_DTYPE_BF16; }
 inline int dtype_size(int dt) { return dt == STAR_DTYPE_BF16 ? 2 : 4; }
 

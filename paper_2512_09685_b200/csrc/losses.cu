@@ -13,36 +13,6 @@ using namespace star;
 
 constexpr int kMaxDevices = 64;
 
-// Launches `kernel` as the dependent of the kernel in front of it in the stream
-// (programmatic: it may start early and waits by itself) or in order.
-template <typename... Params, typename... Args>
-star_status_t launch(void (*kernel)(Params...), int64_t grid, int threads, size_t smem, int cluster, bool dependent, cudaStream_t stream,
-                     const Args &...args)
-{
-    cudaLaunchConfig_t config{};
-    config.gridDim = dim3(static_cast<unsigned>(grid));
-    config.blockDim = dim3(static_cast<unsigned>(threads));
-    config.dynamicSmemBytes = smem;
-    config.stream = stream;
-    cudaLaunchAttribute attributes[2] = {};
-    int n = 0;
-    if (cluster > 1) {
-        attributes[n].id = cudaLaunchAttributeClusterDimension;
-        attributes[n].val.clusterDim.x = static_cast<unsigned>(cluster);
-        attributes[n].val.clusterDim.y = 1;
-        attributes[n].val.clusterDim.z = 1;
-        ++n;
-    }
-    if (dependent) {
-        attributes[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attributes[n].val.programmaticStreamSerializationAllowed = 1;
-        ++n;
-    }
-    config.attrs = attributes;
-    config.numAttrs = static_cast<unsigned>(n);
-    return launched(cudaLaunchKernelEx(&config, kernel, args...));
-}
-
 // Clusters of a kernel that the device holds at once, per device, cluster size
 // and shared memory (in KiB), asked once: the question takes longer than a small
 // launch.
@@ -119,7 +89,7 @@ star_status_t launch_rows(const RowWork &a, int cluster, int *parts_out, cudaStr
     // as many as it holds 286).
     const int64_t most = THREADS == 32 ? held : int64_t{1} << 20, clusters = std::min(a.row.rows, most);
     *parts_out = static_cast<int>(clusters);
-    return launch(kernel, clusters * cluster, THREADS, 0, cluster, false, stream, a);
+    return launch(kernel, dim3(static_cast<unsigned>(clusters * cluster)), THREADS, 0, dim3(static_cast<unsigned>(cluster)), stream, a);
 }
 
 template <typename G, bool POLICY> star_status_t walk_rows(const RowWork &a, int *parts_out, cudaStream_t stream)
@@ -147,7 +117,7 @@ template <typename G, int THREADS> star_status_t launch_policy(const RowWork &a,
     if (e != cudaSuccess) return cuda_failed(e);
     const int64_t blocks = std::min<int64_t>(a.row.rows, held);
     *parts_out = static_cast<int>(blocks);
-    return launch(kernel, blocks, THREADS, static_cast<size_t>(kib) * 1024, 1, false, stream, a);
+    return launch(kernel, dim3(static_cast<unsigned>(blocks)), THREADS, static_cast<size_t>(kib) * 1024, dim3(1), stream, a);
 }
 
 // Whether the policy loss is made in one reading (and the smallest block whose
@@ -184,12 +154,13 @@ template <typename G> star_status_t run_policy(const RowWork &a, int threads, in
 }
 
 // The gradient from what was kept of the rows.
-template <bool POLICY> star_status_t launch_gradient(const GradArgs &g, star_dtype_t dtype, bool follows, cudaStream_t stream)
+template <bool POLICY> star_status_t launch_gradient(const GradArgs &g, star_dtype_t dtype, cudaStream_t stream)
 {
     const int64_t per_row = g.row.vocab * dtype_size(dtype) / 16 / kGradGranules + 1;
-    const int64_t most = 148 * 64, grid = g.row.rows > most / per_row ? most : g.row.rows * per_row;
-    return dtype == STAR_DTYPE_BF16 ? launch(star_row_gradient_kernel<GradBF16, POLICY>, grid, kRowThreads, 0, 1, follows, stream, g)
-                                    : launch(star_row_gradient_kernel<GradF32, POLICY>, grid, kRowThreads, 0, 1, follows, stream, g);
+    const int64_t most = 148 * 64;
+    const dim3 grid(static_cast<unsigned>(g.row.rows > most / per_row ? most : g.row.rows * per_row));
+    return dtype == STAR_DTYPE_BF16 ? launch(star_row_gradient_kernel<GradBF16, POLICY>, grid, kRowThreads, 0, dim3(1), stream, g)
+                                    : launch(star_row_gradient_kernel<GradF32, POLICY>, grid, kRowThreads, 0, dim3(1), stream, g);
 }
 
 // The checks that the three operators share.  read[0] is the logits' extent.
@@ -329,9 +300,9 @@ extern "C" star_status_t star_policy_loss(const void *logits, star_dtype_t dtype
         g.partial = a.partial;
         g.parts = parts;
         g.sums = sums;
-        return launch_gradient<true>(g, dtype, true, stream);
+        return launch_gradient<true>(g, dtype, stream);
     }
-    return launch(star_policy_sums_kernel, 1, kSumThreads, 0, 1, rows > 0, stream, static_cast<const float4 *>(a.partial),
+    return launch(star_policy_sums_kernel, dim3(1), kSumThreads, 0, dim3(1), stream, static_cast<const float4 *>(a.partial),
                   static_cast<int64_t>(parts), sums);
 }
 
@@ -386,11 +357,10 @@ extern "C" star_status_t star_preference_loss(const void *logits, star_dtype_t d
         if (st != STAR_OK) return st;
     }
     if (pairs > 0) {
-        st = launch(star_preference_pair_kernel, std::min<int64_t>(pairs, 65536), kPairThreads, 0, 1, rows > 0, stream, a);
+        st = launch(star_preference_pair_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(pairs, 65536))), kPairThreads, 0, dim3(1), stream, a);
         if (st != STAR_OK) return st;
     }
-    const bool follows = rows > 0 || pairs > 0;
-    if (!dlogits || rows == 0) return launch(star_preference_total_kernel, 1, kPairThreads, 0, 1, follows, stream, a);
+    if (!dlogits || rows == 0) return launch(star_preference_total_kernel, dim3(1), kPairThreads, 0, dim3(1), stream, a);
     GradArgs g{};
     g.row = a.row;
     g.kept = a.kept;
@@ -400,7 +370,7 @@ extern "C" star_status_t star_preference_loss(const void *logits, star_dtype_t d
     g.pairs = pairs;
     g.loss_scale = loss_scale;
     g.loss = loss;
-    return launch_gradient<false>(g, dtype, follows, stream);
+    return launch_gradient<false>(g, dtype, stream);
 }
 
 extern "C" star_status_t star_check_waits(void *cuda_stream)

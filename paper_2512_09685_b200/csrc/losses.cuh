@@ -430,6 +430,7 @@ __global__ void __launch_bounds__(THREADS, row_blocks(THREADS)) star_row_kernel(
     const int vocab = static_cast<int>(a.row.vocab);
     launch_dependents();
     if (threadIdx.x == 0) sums = RowSums{0.0, 0.0, 0.0, 0.0};
+    wait_for_primary();
 
     int parity = 0;
     for (int64_t t = first; t < a.row.rows; t += step, parity ^= 1) {
@@ -520,6 +521,7 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_policy_k
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
+    wait_for_primary();
 
     const auto row_base = [&](int64_t t) { return static_cast<const char *>(a.row.logits) + t * a.row.ld * G::kBytes; };
     // Thread 0: fetches row t.

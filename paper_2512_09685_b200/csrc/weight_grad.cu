@@ -89,23 +89,6 @@ template <> struct ShapeOf<kLooseSingle> : ShapeBase<128, 4, 4, false, 1, true> 
 template <> struct ShapeOf<kCutPair> : ShapeBase<128, 5, 4, true, 3, true> {};
 template <> struct ShapeOf<kCutSingle> : ShapeBase<128, 4, 3, false, 3, true> {};
 
-void fill_config(cudaLaunchConfig_t *config, cudaLaunchAttribute *attribute, int64_t columns, int64_t down, int blocks, int parts,
-                 int smem, cudaStream_t stream)
-{
-    *config = cudaLaunchConfig_t{};
-    config->gridDim = dim3(static_cast<unsigned>(columns * blocks), static_cast<unsigned>(down), static_cast<unsigned>(parts));
-    config->blockDim = dim3(kGradThreads);
-    config->dynamicSmemBytes = static_cast<size_t>(smem);
-    config->stream = stream;
-    *attribute = cudaLaunchAttribute{};
-    attribute->id = cudaLaunchAttributeClusterDimension;
-    attribute->val.clusterDim.x = static_cast<unsigned>(blocks);
-    attribute->val.clusterDim.y = 1;
-    attribute->val.clusterDim.z = static_cast<unsigned>(parts);
-    config->attrs = attribute;
-    config->numAttrs = 1;
-}
-
 // Per device and shape: how many clusters of `parts` tiles the device holds at
 // once (GPUs of one kind differ: their SMs come in groups of uneven size, and a
 // cluster stays within a group).  0: not asked yet.
@@ -121,9 +104,17 @@ template <int SHAPE> cudaError_t prepare_shape(Device &d)
     const auto kernel = S::kernel();
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::Smem::kDynamic);
     for (int parts = 1; e == cudaSuccess && parts * S::kBlocks <= 8; ++parts) {
-        cudaLaunchConfig_t config;
-        cudaLaunchAttribute attribute;
-        fill_config(&config, &attribute, 64, 1, S::kBlocks, parts, S::Smem::kDynamic, nullptr);
+        cudaLaunchConfig_t config{};
+        cudaLaunchAttribute attribute{};
+        config.gridDim = dim3(static_cast<unsigned>(64 * S::kBlocks), 1, static_cast<unsigned>(parts));
+        config.blockDim = dim3(kGradThreads);
+        config.dynamicSmemBytes = S::Smem::kDynamic;
+        attribute.id = cudaLaunchAttributeClusterDimension;
+        attribute.val.clusterDim.x = S::kBlocks;
+        attribute.val.clusterDim.y = 1;
+        attribute.val.clusterDim.z = static_cast<unsigned>(parts);
+        config.attrs = &attribute;
+        config.numAttrs = 1;
         int n = 0;
         e = cudaOccupancyMaxActiveClusters(&n, kernel, &config);
         d.clusters[SHAPE][parts].store(n, std::memory_order_relaxed);
@@ -161,12 +152,11 @@ star_status_t launch_shape(const WeightGradTile &tile, const CUtensorMap &codes,
                            cudaStream_t stream)
 {
     using S = ShapeOf<SHAPE>;
-    cudaLaunchConfig_t config;
-    cudaLaunchAttribute attribute;
     constexpr int64_t columns = S::kBlocks * kTileC;
-    fill_config(&config, &attribute, (tile.a.kept.cols + columns - 1) / columns, (tile.a.outs + S::kOuts - 1) / S::kOuts, S::kBlocks,
-                parts, S::Smem::kDynamic, stream);
-    return launched(cudaLaunchKernelEx(&config, S::kernel(), tile, codes, dy, static_cast<int>(dw_bf16)));
+    const dim3 grid(static_cast<unsigned>((tile.a.kept.cols + columns - 1) / columns * S::kBlocks),
+                    static_cast<unsigned>((tile.a.outs + S::kOuts - 1) / S::kOuts), static_cast<unsigned>(parts));
+    return launch(S::kernel(), grid, kGradThreads, S::Smem::kDynamic, dim3(S::kBlocks, 1, static_cast<unsigned>(parts)), stream, tile,
+                  codes, dy, static_cast<int>(dw_bf16));
 }
 
 // Shape and number of parts with the least expected time: the waves of tiles the
@@ -232,10 +222,8 @@ template <typename GY, typename GW> star_status_t launch_few(const WeightGradArg
     const int vector = reinterpret_cast<uintptr_t>(a.dw) % (4 * GW::kBytes) == 0 && ld % 4 == 0;
     const dim3 grid(static_cast<unsigned>((inner + kFewInner - 1) / kFewInner), static_cast<unsigned>((outer + kFewOuter - 1) / kFewOuter));
     if (transposed)
-        star_weight_grad_few_kernel<GY, GW, true><<<grid, kFewThreads, 0, stream>>>(a, vector);
-    else
-        star_weight_grad_few_kernel<GY, GW, false><<<grid, kFewThreads, 0, stream>>>(a, vector);
-    return launched();
+        return launch(star_weight_grad_few_kernel<GY, GW, true>, grid, kFewThreads, 0, dim3(1), stream, a, vector);
+    return launch(star_weight_grad_few_kernel<GY, GW, false>, grid, kFewThreads, 0, dim3(1), stream, a, vector);
 }
 
 }  // namespace

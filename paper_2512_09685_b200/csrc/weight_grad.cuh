@@ -477,6 +477,7 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
     if constexpr (PAIR) cluster_sync();                          // the other block's barriers are ready
     tensor_fence_after();
     const uint32_t tmem = *tmem_at;
+    wait_for_primary();
 
     const int64_t c0 = static_cast<int64_t>(blockIdx.x) * kTileC, o0 = static_cast<int64_t>(blockIdx.y) * BN;
     const int parts = static_cast<int>(gridDim.z), part = static_cast<int>(blockIdx.z);
@@ -729,6 +730,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) star_weight_grad_few_kernel(co
     for (int p = 0; p < 8; ++p)
 #pragma unroll
         for (int q = 0; q < 8; ++q) sum[p][q] = 0.0f;
+    wait_for_primary();
     for (int64_t t0 = 0; t0 < a.kept.rows; t0 += kFewRows) {
         const int rows = static_cast<int>(min(a.kept.rows - t0, static_cast<int64_t>(kFewRows)));
         if (t0 > 0) __syncthreads();
