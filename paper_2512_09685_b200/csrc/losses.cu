@@ -40,6 +40,7 @@ template <typename Kernel> cudaError_t held_clusters(Kernel kernel, Held &known,
             cudaLaunchConfig_t config{};
             config.gridDim = dim3(static_cast<unsigned>(cluster) * 64);
             config.blockDim = dim3(static_cast<unsigned>(threads));
+            config.dynamicSmemBytes = static_cast<size_t>(kib) * 1024;
             cudaLaunchAttribute attribute{};
             attribute.id = cudaLaunchAttributeClusterDimension;
             attribute.val.clusterDim.x = static_cast<unsigned>(cluster);
@@ -107,49 +108,62 @@ template <typename G, bool POLICY> star_status_t walk_rows(const RowWork &a, int
 }
 
 // The policy loss in one reading of the rows.
-template <typename G, int THREADS> star_status_t launch_policy(const RowWork &a, int *parts_out, cudaStream_t stream)
+template <typename G, int THREADS> star_status_t launch_policy(const RowWork &a, int cluster, int *parts_out, cudaStream_t stream)
 {
     static Held known;
     constexpr auto kernel = star_policy_kernel<G, THREADS>;
-    const int kib = static_cast<int>((a.row.vocab * G::kBytes / 16 * 16 + 1023) / 1024);
+    const int64_t granules = a.row.vocab * G::kBytes / 16;
+    const int kib = static_cast<int>(((granules + cluster - 1) / cluster * 16 + 1023) / 1024);
     int held = 0;
-    const cudaError_t e = held_clusters(kernel, known, THREADS, 1, kib, &held);
+    const cudaError_t e = held_clusters(kernel, known, THREADS, cluster, kib, &held);
     if (e != cudaSuccess) return cuda_failed(e);
-    const int64_t blocks = std::min<int64_t>(a.row.rows, held);
-    *parts_out = static_cast<int>(blocks);
-    return launch(kernel, dim3(static_cast<unsigned>(blocks)), THREADS, static_cast<size_t>(kib) * 1024, dim3(1), stream, a);
+    const int64_t clusters = std::min<int64_t>(a.row.rows, held);
+    *parts_out = static_cast<int>(clusters);
+    return launch(kernel, dim3(static_cast<unsigned>(clusters * cluster)), THREADS, static_cast<size_t>(kib) * 1024, dim3(static_cast<unsigned>(cluster)), stream, a);
 }
 
-// Whether the policy loss is made in one reading (and the smallest block whose
-// part of the SM's shared memory holds a row): rows of up to 224 KB, and more
-// than three of them to an SM.  Fewer are shared by clusters and read twice, the
-// second time from L2.  The same with and without a gradient, so that both give
-// the same bits.  us, one reading / two:
-//   rows     8192 bf16   32000 bf16   50257 bf16    50257 fp32
-//    148     9.2 / 8.5  12.5 / 11.3  15.7 / 14.5   21.3 / 20.0
-//    444    11.6 / 10.5 22.6 / 19.1  30.0 / 28.6   46.6 / 51.7
-//    592    11.9 / 11.5 23.8 / 22.9  31.4 / 36.2   57.3 / 67.1
-//   1024    14.8 / 15.4 38.7 / 39.7  53.2 / 63.4   88.3 / 109.5
-bool one_reading(int64_t rows, int64_t vocab, int size, int *threads)
+// Whether the policy loss is made in one reading, and the smallest block whose
+// part of the SM's shared memory holds a row; rows of more than 112 KB are shared
+// by a cluster of blocks.  Two readings where the second finds the logits in L2,
+// up to 45 MB of them, and rows are too few to hide one another's waits.  The same
+// with and without a gradient, so that both give the same bits.  us:
+//     rows x vocab         one   two         rows x vocab            one   two
+//      148 x 50257 bf16   15.7  14.5           600 x 32000 bf16     26.7  23.3
+//      444 x 50257 bf16   30.0  28.6          1024 x 16000 bf16     23.5  22.0
+//      600 x 50257 bf16   35.8  36.5          4096 x  1000 fp32     14.0  20.2
+//     2048 x 50257 bf16   89.0   116           300 x 131072 bf16    43.6  48.9
+//      200 x 50257 fp32   30.9  25.0          1024 x 131072 bf16     130   143
+//      444 x 50257 fp32   44.3  52.2          1024 x 200000 fp32     318   385
+// Clusters for rows that a block of 1024 threads could hold, 57500 bf16: 1024 rows
+// 66.5 us against 71.4, 4096 rows 247 against 250.  And of 2 x 256 threads instead
+// of a block of 512, 50257 bf16: 50.1 against 54.1 and 170 against 165: not taken.
+bool one_reading(int64_t rows, int64_t vocab, int size, int *threads, int *cluster)
 {
     const int64_t bytes = vocab * size;
-    if (rows <= 148 * 3) return false;
-    for (int t : {32, 64, 128, 256, 512, 1024}) {
+    if (rows <= 1024 && bytes * rows <= 45'000'000) return false;
+    *cluster = 1;
+    for (int t : {32, 64, 128, 256, 512}) {
         *threads = t;
         if (bytes <= kKeepBytesPerThread * t) return true;
+    }
+    for (int t : {256, 512}) {
+        *threads = t;
+        for (int c : {4, 8}) {
+            *cluster = c;
+            if (bytes <= int64_t{kKeepBytesPerThread} * t * c) return true;
+        }
     }
     return false;
 }
 
-template <typename G> star_status_t run_policy(const RowWork &a, int threads, int *parts_out, cudaStream_t stream)
+template <typename G> star_status_t run_policy(const RowWork &a, int threads, int cluster, int *parts_out, cudaStream_t stream)
 {
     switch (threads) {
-    case 32: return launch_policy<G, 32>(a, parts_out, stream);
-    case 64: return launch_policy<G, 64>(a, parts_out, stream);
-    case 128: return launch_policy<G, 128>(a, parts_out, stream);
-    case 256: return launch_policy<G, 256>(a, parts_out, stream);
-    case 512: return launch_policy<G, 512>(a, parts_out, stream);
-    default: return launch_policy<G, 1024>(a, parts_out, stream);
+    case 32: return launch_policy<G, 32>(a, cluster, parts_out, stream);
+    case 64: return launch_policy<G, 64>(a, cluster, parts_out, stream);
+    case 128: return launch_policy<G, 128>(a, cluster, parts_out, stream);
+    case 256: return launch_policy<G, 256>(a, cluster, parts_out, stream);
+    default: return launch_policy<G, 512>(a, cluster, parts_out, stream);
     }
 }
 
@@ -282,10 +296,10 @@ extern "C" star_status_t star_policy_loss(const void *logits, star_dtype_t dtype
     a.ld_dlogits = ld_dlogits;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const bool bf16 = dtype == STAR_DTYPE_BF16;
-    int parts = 0, threads = 0;
-    const bool once = one_reading(rows, vocab, dtype_size(dtype), &threads);
+    int parts = 0, threads = 0, cluster = 1;
+    const bool once = one_reading(rows, vocab, dtype_size(dtype), &threads, &cluster);
     if (once) {
-        st = bf16 ? run_policy<GradBF16>(a, threads, &parts, stream) : run_policy<GradF32>(a, threads, &parts, stream);
+        st = bf16 ? run_policy<GradBF16>(a, threads, cluster, &parts, stream) : run_policy<GradF32>(a, threads, cluster, &parts, stream);
     } else if (rows > 0) {
         if (dlogits) a.kept = reinterpret_cast<RowKept *>(a.partial + rows);
         st = bf16 ? walk_rows<GradBF16, true>(a, &parts, stream) : walk_rows<GradF32, true>(a, &parts, stream);

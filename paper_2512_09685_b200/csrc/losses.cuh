@@ -317,6 +317,16 @@ template <typename G> __device__ __forceinline__ RowSplit split_row(const void *
     return RowSplit{static_cast<int>(head), static_cast<int>(rest / E), static_cast<int>(rest % E)};
 }
 
+// The granules [begin, begin + count) of a row that a block of a cluster takes.
+struct RowShare {
+    int begin, count;
+};
+__device__ __forceinline__ RowShare row_share(int granules, uint32_t rank, int log_blocks)
+{
+    const int each = (granules + (1 << log_blocks) - 1) >> log_blocks, begin = min(each * static_cast<int>(rank), granules);
+    return RowShare{begin, min(each, granules - begin)};
+}
+
 constexpr int kBatch = 4;            // granules that a thread loads at once
 // Blocks of an SM that the kernels are compiled for: the statistics alone in 1280
 // threads of 48 registers, with the gradient 1024 of 64.
@@ -399,6 +409,19 @@ template <int WARPS, typename Sync> __device__ __forceinline__ MaxSum block_join
     return x;
 }
 
+// Joins the blocks' parts; meaningful in warp 0 of every block.
+__device__ __forceinline__ MaxSum cluster_join(MaxSum x, MaxSum (&part)[8], uint32_t blocks, uint32_t rank, float k)
+{
+    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    if (warp == 0 && lane < blocks) {
+        const uint32_t at = peer_address(smem_address(&part[rank]), lane);
+        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" :: "r"(at), "f"(x.m), "f"(x.s) : "memory");
+    }
+    cluster_sync();
+    if (warp == 0) x = warp_join(lane < blocks ? part[lane] : MaxSum{-INFINITY, 0.0f}, k);
+    return x;
+}
+
 // The element beside the granules that thread i takes, or -1.
 __device__ __forceinline__ int edge_element(const RowSplit &s, int i, int vocab)
 {
@@ -430,6 +453,7 @@ __global__ void __launch_bounds__(THREADS, row_blocks(THREADS)) star_row_kernel(
     const int vocab = static_cast<int>(a.row.vocab);
     launch_dependents();
     if (threadIdx.x == 0) sums = RowSums{0.0, 0.0, 0.0, 0.0};
+    if (blocks > 1) cluster_sync();                              // the others have started
     wait_for_primary();
 
     int parity = 0;
@@ -441,8 +465,7 @@ __global__ void __launch_bounds__(THREADS, row_blocks(THREADS)) star_row_kernel(
         if (wanted) {
             const char *base = static_cast<const char *>(a.row.logits) + t * a.row.ld * G::kBytes;
             const RowSplit s = split_row<G>(base, vocab);
-            const int each = (s.granules + static_cast<int>(blocks) - 1) >> log_blocks;
-            const int begin = min(each * static_cast<int>(rank), s.granules);
+            const RowShare own = row_share(s.granules, rank, log_blocks);
             const int edge_at = rank == 0 ? edge_element(s, threadIdx.x, vocab) : -1;
             float edge = 0.0f;
             if (edge_at >= 0) edge = load_value<G>(base, edge_at);
@@ -456,21 +479,14 @@ __global__ void __launch_bounds__(THREADS, row_blocks(THREADS)) star_row_kernel(
                 }
                 row_in[threadIdx.x] = in;
             }
-            int left = min(each, s.granules - begin) - static_cast<int>(threadIdx.x);
-            const uint4 *from = reinterpret_cast<const uint4 *>(base + s.head * G::kBytes) + begin + threadIdx.x;
+            int left = own.count - static_cast<int>(threadIdx.x);
+            const uint4 *from = reinterpret_cast<const uint4 *>(base + s.head * G::kBytes) + own.begin + threadIdx.x;
             for (; left > kStep - THREADS; left -= kStep, from += kStep) take_batch<G, kBatch, THREADS, true>(&x, from, left, k);
             if (left > 0) take_batch<G, kBatch, THREADS, false>(&x, from, left, k);
             if (edge_at >= 0) x = join(x, MaxSum{edge, exp2_fast(exponent(edge, edge, k))}, k);
         }
         x = block_join<kWarps>(x, warp_part[parity], k, [] { __syncthreads(); });
-        if (blocks > 1) {
-            if (warp == 0 && lane < static_cast<int>(blocks)) {
-                const uint32_t at = peer_address(smem_address(&block_part[parity][rank]), lane);
-                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" :: "r"(at), "f"(x.m), "f"(x.s) : "memory");
-            }
-            cluster_sync();
-            if (warp == 0) x = warp_join(lane < static_cast<int>(blocks) ? block_part[parity][lane] : MaxSum{-INFINITY, 0.0f}, k);
-        }
+        if (blocks > 1) x = cluster_join(x, block_part[parity], blocks, rank, k);
         if (warp == 0 && rank == 0) {
             __syncwarp();                                        // row_in is written
             if (lane == 0) {
@@ -490,13 +506,16 @@ __global__ void __launch_bounds__(THREADS, row_blocks(THREADS)) star_row_kernel(
 // The policy loss with its gradient in one reading: a row comes by one bulk copy
 // and stays in shared memory from its statistics to its gradient.  Blocks of
 // THREADS, as many on an SM as make 1024 threads, so that one block's copy, joins
-// and waits run under another's arithmetic.  The thread that finishes a row makes
-// its factors first and lets the others go before it writes results and sums.
+// and waits run under another's arithmetic.  Longer rows lie in the shared memory
+// of a cluster's blocks, which join their parts and each make all factors.  The
+// thread that finishes a row makes its factors first and lets the others go before
+// it writes results and sums.
 //
-// 4096 x 50257 bf16, no row masked: 163 us, 5.05 TB/s of reading and writing.
-// Other arrangements of the same arithmetic: two rows in shared memory and one
-// block of 1024 threads 190 us (its warps all join at once); no shared memory and
-// a second reading from L1 and L2 186; the copy in 2 or 4 parts, the next row's
+// 4096 x 50257 bf16, no row masked: 164 us, 5.0 TB/s of reading and writing;
+// 4096 x 131072 480 us, 4.5 TB/s.  Other arrangements of the same arithmetic, at
+// 50257: two rows in shared memory and one block of 1024 threads 190 us (its warps
+// all join at once); four blocks an SM, two to a row, 170; no shared memory and a
+// second reading from L1 and L2 186; the copy in 2 or 4 parts, the next row's
 // following the second walk part by part, 166 to 212.
 // ---------------------------------------------------------------------------
 constexpr int kKeepBytesPerThread = 224;     // shared memory for the row: 224 KB an SM
@@ -507,6 +526,7 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_policy_k
     constexpr int E = Granule<G>::kCount, kWarps = THREADS / 32, kStep = kBatch * THREADS;
     extern __shared__ uint4 kept_row[];
     __shared__ MaxSum warp_part[2][kWarps];
+    __shared__ alignas(8) MaxSum block_part[2][8];
     __shared__ RowFactors factors;
     __shared__ RowSums sums;
     __shared__ RowIn row_in;
@@ -514,6 +534,9 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_policy_k
     const float k = __fmul_rn(a.row.inv_temperature, kLog2e);
     const int vocab = static_cast<int>(a.row.vocab);
     const bool writes = a.dlogits != nullptr;
+    const uint32_t blocks = cluster_size(), rank = cluster_rank();
+    const int log_blocks = 31 - __clz(static_cast<int>(blocks));
+    const int64_t first = blockIdx.x >> log_blocks, step = gridDim.x >> log_blocks;
     launch_dependents();
     if (threadIdx.x == 0) {
         sums = RowSums{0.0, 0.0, 0.0, 0.0};
@@ -521,35 +544,38 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_policy_k
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
+    if (blocks > 1) cluster_sync();                              // the others have started
     wait_for_primary();
 
     const auto row_base = [&](int64_t t) { return static_cast<const char *>(a.row.logits) + t * a.row.ld * G::kBytes; };
-    // Thread 0: fetches row t.
+    // Thread 0: fetches the block's share of row t.
     const auto fetch = [&](int64_t t) {
         const char *base = row_base(t);
         const RowSplit s = split_row<G>(base, vocab);
-        if (s.granules == 0) return;
-        const uint32_t bytes = static_cast<uint32_t>(s.granules) * 16, bar = smem_address(&landed);
+        const RowShare own = row_share(s.granules, rank, log_blocks);
+        if (own.count == 0) return;
+        const uint32_t bytes = static_cast<uint32_t>(own.count) * 16, bar = smem_address(&landed);
         barrier_expect(bar, bytes);
-        bulk_load(smem_address(kept_row), base + s.head * G::kBytes, bytes, bar);
+        bulk_load(smem_address(kept_row), base + s.head * G::kBytes + static_cast<int64_t>(own.begin) * 16, bytes, bar);
     };
 
     uint32_t phase = 0;
     int parity = 0;
     int64_t label = -1;
     float weight = 0.0f;
-    bool wanted = row_wanted(a.row, blockIdx.x, &label, &weight);
-    if (wanted && threadIdx.x == 0) fetch(blockIdx.x);
-    for (int64_t t = blockIdx.x; t < a.row.rows; t += gridDim.x, parity ^= 1) {
+    bool wanted = row_wanted(a.row, first, &label, &weight);
+    if (wanted && threadIdx.x == 0) fetch(first);
+    for (int64_t t = first; t < a.row.rows; t += step, parity ^= 1) {
         const RowSplit s = split_row<G>(row_base(t), vocab);
+        const RowShare own = row_share(s.granules, rank, log_blocks);
         // The next row's label and weight are on their way.
         int64_t next_label = -1;
         float next_weight = 0.0f;
-        if (t + gridDim.x < a.row.rows) {
-            next_label = a.row.labels[t + gridDim.x];
-            next_weight = a.row.weights ? a.row.weights[t + gridDim.x] : 1.0f;
+        if (t + step < a.row.rows) {
+            next_label = a.row.labels[t + step];
+            next_weight = a.row.weights ? a.row.weights[t + step] : 1.0f;
         }
-        const int edge_at = edge_element(s, threadIdx.x, vocab);
+        const int edge_at = rank == 0 ? edge_element(s, threadIdx.x, vocab) : -1;
         float edge = 0.0f;
         MaxSum x{-INFINITY, 0.0f};
         if (wanted) {
@@ -560,30 +586,31 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_policy_k
                 row_in.old_lp = a.old_logp ? a.old_logp[t] : 0.0f;
                 row_in.ref_lp = a.ref_logp ? a.ref_logp[t] : 0.0f;
             }
-            if (s.granules > 0) {
+            if (own.count > 0) {
                 barrier_wait(smem_address(&landed), phase);
                 phase ^= 1;
             }
             const uint4 *from = kept_row + threadIdx.x;
-            int left = s.granules - static_cast<int>(threadIdx.x);
+            int left = own.count - static_cast<int>(threadIdx.x);
             for (; left > kStep - THREADS; left -= kStep, from += kStep) take_batch<G, kBatch, THREADS, true>(&x, from, left, k);
             if (left > 0) take_batch<G, kBatch, THREADS, false>(&x, from, left, k);
             if (edge_at >= 0) x = join(x, MaxSum{edge, exp2_fast(exponent(edge, edge, k))}, k);
         }
         x = block_join<kWarps>(x, warp_part[parity], k, [] { __syncthreads(); });
+        if (blocks > 1) x = cluster_join(x, block_part[parity], blocks, rank, k);
         float lp;
         PolicyRow r;
         if (threadIdx.x == 0) factors = make_factors<true>(a, wanted, x, weight, row_in, &lp, &r);
         const bool next_wanted = next_label >= 0 && next_label < vocab && next_weight != 0.0f;
         __syncthreads();                                         // the factors; and the first walk is over
-        if (threadIdx.x == 0) finish_row<true>(a, t, factors, x, weight, lp, r, &sums);
+        if (threadIdx.x == 0 && rank == 0) finish_row<true>(a, t, factors, x, weight, lp, r, &sums);
         if (writes) {
             const RowFactors f = factors;
             char *out = static_cast<char *>(a.dlogits) + t * a.ld_dlogits * G::kBytes;
             const bool same_phase = (reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(row_base(t))) % 16 == 0;
             if (same_phase) {
-                uint4 *to = reinterpret_cast<uint4 *>(out + s.head * G::kBytes) + threadIdx.x;
-                int left = s.granules - static_cast<int>(threadIdx.x);
+                uint4 *to = reinterpret_cast<uint4 *>(out + s.head * G::kBytes) + own.begin + threadIdx.x;
+                int left = own.count - static_cast<int>(threadIdx.x);
                 if (f.active) {
                     const Power power(f.m, k);
                     const uint4 *from = kept_row + threadIdx.x;
@@ -594,21 +621,24 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_policy_k
                     for (; left > 0; left -= THREADS, to += THREADS) *to = make_uint4(0, 0, 0, 0);
                 }
             } else {
-                for (int e = threadIdx.x; e < s.granules * E; e += THREADS)
-                    store_value<G>(out, s.head + e, f.active ? __fmul_rn(f.scale, exp2_fast(exponent(load_value<G>(kept_row, e), f.m, k))) : 0.0f);
+                for (int e = threadIdx.x; e < own.count * E; e += THREADS)
+                    store_value<G>(out, s.head + own.begin * E + e, f.active ? __fmul_rn(f.scale, exp2_fast(exponent(load_value<G>(kept_row, e), f.m, k))) : 0.0f);
             }
             if (edge_at >= 0)
                 store_value<G>(out, edge_at, f.active ? __fmul_rn(f.scale, exp2_fast(exponent(edge, f.m, k))) : 0.0f);
             __syncthreads();                                     // the row is read and written
-            // The label's element again.
-            if (threadIdx.x == 0 && f.active) store_value<G>(out, label, __fmaf_rn(f.scale, f.label_power, f.coef));
+            // The label's element again, by the block that has it.
+            const int at = static_cast<int>(label) - s.head;
+            const bool in_granules = at >= 0 && at < s.granules * E;
+            const bool has_label = in_granules ? at / E >= own.begin && at / E < own.begin + own.count : rank == 0;
+            if (threadIdx.x == 0 && f.active && has_label) store_value<G>(out, label, __fmaf_rn(f.scale, f.label_power, f.coef));
         }
-        if (next_wanted && threadIdx.x == 0) fetch(t + gridDim.x);
+        if (next_wanted && threadIdx.x == 0) fetch(t + step);
         label = next_label;
         weight = next_weight;
         wanted = next_wanted;
     }
-    if (threadIdx.x == 0) store_partial<true>(a, blockIdx.x, sums);
+    if (threadIdx.x == 0 && rank == 0) store_partial<true>(a, first, sums);
 }
 
 constexpr int kSumThreads = 1024;
