@@ -108,10 +108,10 @@ template <typename G, bool POLICY> star_status_t walk_rows(const RowWork &a, int
 }
 
 // The policy loss in one reading of the rows.
-template <typename G, int THREADS> star_status_t launch_policy(const RowWork &a, int cluster, int *parts_out, cudaStream_t stream)
+template <typename G, int THREADS, bool CLUSTER> star_status_t launch_policy(const RowWork &a, int cluster, int *parts_out, cudaStream_t stream)
 {
     static Held known;
-    constexpr auto kernel = star_policy_kernel<G, THREADS>;
+    constexpr auto kernel = star_policy_kernel<G, THREADS, CLUSTER>;
     const int64_t granules = a.row.vocab * G::kBytes / 16;
     const int kib = static_cast<int>(((granules + cluster - 1) / cluster * 16 + 1023) / 1024);
     int held = 0;
@@ -158,12 +158,14 @@ bool one_reading(int64_t rows, int64_t vocab, int size, int *threads, int *clust
 
 template <typename G> star_status_t run_policy(const RowWork &a, int threads, int cluster, int *parts_out, cudaStream_t stream)
 {
+    if (cluster > 1)
+        return threads == 256 ? launch_policy<G, 256, true>(a, cluster, parts_out, stream) : launch_policy<G, 512, true>(a, cluster, parts_out, stream);
     switch (threads) {
-    case 32: return launch_policy<G, 32>(a, cluster, parts_out, stream);
-    case 64: return launch_policy<G, 64>(a, cluster, parts_out, stream);
-    case 128: return launch_policy<G, 128>(a, cluster, parts_out, stream);
-    case 256: return launch_policy<G, 256>(a, cluster, parts_out, stream);
-    default: return launch_policy<G, 512>(a, cluster, parts_out, stream);
+    case 32: return launch_policy<G, 32, false>(a, 1, parts_out, stream);
+    case 64: return launch_policy<G, 64, false>(a, 1, parts_out, stream);
+    case 128: return launch_policy<G, 128, false>(a, 1, parts_out, stream);
+    case 256: return launch_policy<G, 256, false>(a, 1, parts_out, stream);
+    default: return launch_policy<G, 512, false>(a, 1, parts_out, stream);
     }
 }
 

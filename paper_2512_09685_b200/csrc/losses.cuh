@@ -511,7 +511,7 @@ __global__ void __launch_bounds__(THREADS, row_blocks(THREADS)) star_row_kernel(
 // thread that finishes a row makes its factors first and lets the others go before
 // it writes results and sums.
 //
-// 4096 x 50257 bf16, no row masked: 164 us, 5.0 TB/s of reading and writing;
+// 4096 x 50257 bf16, no row masked: 161 us, 5.1 TB/s of reading and writing;
 // 4096 x 131072 480 us, 4.5 TB/s.  Other arrangements of the same arithmetic, at
 // 50257: two rows in shared memory and one block of 1024 threads 190 us (its warps
 // all join at once); four blocks an SM, two to a row, 170; no shared memory and a
@@ -520,7 +520,7 @@ __global__ void __launch_bounds__(THREADS, row_blocks(THREADS)) star_row_kernel(
 // ---------------------------------------------------------------------------
 constexpr int kKeepBytesPerThread = 224;     // shared memory for the row: 224 KB an SM
 
-template <typename G, int THREADS>
+template <typename G, int THREADS, bool CLUSTER>
 __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_policy_kernel(const __grid_constant__ RowWork a)
 {
     constexpr int E = Granule<G>::kCount, kWarps = THREADS / 32, kStep = kBatch * THREADS;
@@ -534,8 +534,8 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_policy_k
     const float k = __fmul_rn(a.row.inv_temperature, kLog2e);
     const int vocab = static_cast<int>(a.row.vocab);
     const bool writes = a.dlogits != nullptr;
-    const uint32_t blocks = cluster_size(), rank = cluster_rank();
-    const int log_blocks = 31 - __clz(static_cast<int>(blocks));
+    const uint32_t blocks = CLUSTER ? cluster_size() : 1, rank = CLUSTER ? cluster_rank() : 0;
+    const int log_blocks = CLUSTER ? 31 - __clz(static_cast<int>(blocks)) : 0;
     const int64_t first = blockIdx.x >> log_blocks, step = gridDim.x >> log_blocks;
     launch_dependents();
     if (threadIdx.x == 0) {
