@@ -172,9 +172,9 @@ template <typename G> star_status_t run_policy(const RowWork &a, int threads, in
 // The gradient from what was kept of the rows.
 template <bool POLICY> star_status_t launch_gradient(const GradArgs &g, star_dtype_t dtype, cudaStream_t stream)
 {
-    const int64_t per_row = g.row.vocab * dtype_size(dtype) / 16 / kGradGranules + 1;
-    const int64_t most = 148 * 64;
-    const dim3 grid(static_cast<unsigned>(g.row.rows > most / per_row ? most : g.row.rows * per_row));
+    const int64_t per_row = g.row.vocab * dtype_size(dtype) / 16 / kGradGranules + 1;        // of a warp
+    const int64_t most = 148 * 64, warps = kRowThreads / 32;
+    const dim3 grid(static_cast<unsigned>(g.row.rows > most * warps / per_row ? most : (g.row.rows * per_row + warps - 1) / warps));
     return dtype == STAR_DTYPE_BF16 ? launch(star_row_gradient_kernel<GradBF16, POLICY>, grid, kRowThreads, 0, dim3(1), stream, g)
                                     : launch(star_row_gradient_kernel<GradF32, POLICY>, grid, kRowThreads, 0, dim3(1), stream, g);
 }

@@ -768,12 +768,14 @@ __global__ void __launch_bounds__(kPairThreads) star_preference_total_kernel(con
 // ---------------------------------------------------------------------------
 // The gradient from what was kept of the rows, in a second reading of the logits:
 // for the preference loss, because a row's factor needs every row of its pair;
-// for the policy loss where rows are few or too long for shared memory.  Rows are taken from the
-// last to the first, so that those read last by the first step are still in L2.
-// An item is a run of kGradGranules granules of a row.
+// for the policy loss where rows are few or too long for shared memory.  Rows are
+// taken from the last to the first, so that those read last by the first step are
+// still in L2.  A warp takes a run of kGradGranules granules of a row at a time:
+// nothing is shared between warps, and short rows fill the blocks as long ones do.
+// ---------------------------------------------------------------------------
 constexpr int kRowThreads = 256;
 constexpr int kGradPerThread = 4;
-constexpr int kGradGranules = kRowThreads * kGradPerThread;
+constexpr int kGradGranules = 32 * kGradPerThread;
 
 struct GradArgs {
     RowArgs row;
@@ -804,8 +806,11 @@ template <typename G, bool POLICY> __global__ void __launch_bounds__(kRowThreads
     const float k = __fmul_rn(a.row.inv_temperature, kLog2e);
     const int64_t per_row = (a.row.vocab / E + kGradGranules) / kGradGranules;           // the last run may be empty
     const int64_t items = a.row.rows * per_row;
-    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const int64_t t = a.row.rows - 1 - item / per_row, run = item % per_row;
+    const int lane = threadIdx.x % 32, warps = kRowThreads / 32;
+    for (int64_t item = static_cast<int64_t>(blockIdx.x) * warps + threadIdx.x / 32; item < items; item += static_cast<int64_t>(gridDim.x) * warps) {
+        // A division in 32 bits, five times cheaper, for all but the largest.
+        const int64_t row = items <= 0xffffffff ? static_cast<uint32_t>(item) / static_cast<uint32_t>(per_row) : item / per_row;
+        const int64_t t = a.row.rows - 1 - row, run = item - row * per_row;
         const RowKept r = a.kept[t];
         const bool active = r.inv_s != 0.0f && r.coef != 0.0f;
         const char *base = static_cast<const char *>(a.row.logits) + t * a.row.ld * G::kBytes;
@@ -825,26 +830,25 @@ template <typename G, bool POLICY> __global__ void __launch_bounds__(kRowThreads
             if (active) {
                 const int64_t at_label = label - s.head;
                 const bool label_here = at_label >= static_cast<int64_t>(begin) * E && at_label < static_cast<int64_t>(end) * E &&
-                                        (at_label / E - begin) % kRowThreads == threadIdx.x;
+                                        (at_label / E - begin) % 32 == lane;
                 const float label_logit = label_here ? load_value<G>(src, at_label) : 0.0f;      // before an in-place store
-                const int at = begin + static_cast<int>(threadIdx.x), left = end - at;
+                const int at = begin + lane, left = end - at;
                 const Power power(r.m, k);
-                if (left > (kGradPerThread - 1) * kRowThreads)
-                    store_batch<G, kGradPerThread, kRowThreads, true>(dst + at, src + at, left, power, scale);
+                if (left > (kGradPerThread - 1) * 32)
+                    store_batch<G, kGradPerThread, 32, true>(dst + at, src + at, left, power, scale);
                 else if (left > 0)
-                    store_batch<G, kGradPerThread, kRowThreads, false>(dst + at, src + at, left, power, scale);
+                    store_batch<G, kGradPerThread, 32, false>(dst + at, src + at, left, power, scale);
                 if (label_here) store_value<G>(dst, at_label, grad(label_logit, label));         // by the thread that stored its granule
             } else {
-                for (int i = begin + threadIdx.x; i < end; i += kRowThreads) dst[i] = make_uint4(0, 0, 0, 0);
+                for (int i = begin + lane; i < end; i += 32) dst[i] = make_uint4(0, 0, 0, 0);
             }
         } else {
             const int64_t last = s.head + static_cast<int64_t>(end) * E;
-            for (int64_t at = s.head + static_cast<int64_t>(begin) * E + threadIdx.x; at < last; at += kRowThreads)
+            for (int64_t at = s.head + static_cast<int64_t>(begin) * E + lane; at < last; at += 32)
                 store_value<G>(out, at, active ? grad(load_value<G>(base, at), at) : 0.0f);
         }
-        if (run == 0 && static_cast<int>(threadIdx.x) < s.head + s.tail) {
-            const int i = threadIdx.x;
-            const int64_t at = i < s.head ? i : a.row.vocab - s.tail + (i - s.head);
+        if (run == 0 && lane < s.head + s.tail) {
+            const int64_t at = lane < s.head ? lane : a.row.vocab - s.tail + (lane - s.head);
             store_value<G>(out, at, active ? grad(load_value<G>(base, at), at) : 0.0f);
         }
     }
