@@ -345,7 +345,9 @@ __device__ __forceinline__ void store_weight(const WeightGradArgs &a, bool bf16,
 // A warp's 32 columns c0 .. and 32 outputs o0 .. (x[r]: output o0 + r of this
 // lane's column).  `words`: pairs of bf16 at even columns lie on whole words.
 // Plain layout: neighbouring lanes trade halves, so that each stores two columns
-// of every other output; fp32 and transposed bf16 need no trade.
+// of every other output; fp32 and transposed bf16 need no trade.  What is added to
+// is loaded ahead of the stores, 16 words at a time: the compiler cannot move a load
+// over a store that might change it.
 __device__ __forceinline__ void store_block(const WeightGradArgs &a, bool bf16, bool words, int64_t o0, int64_t c0, int lane, const float (&x)[32])
 {
     const int64_t c = c0 + lane;
@@ -353,14 +355,16 @@ __device__ __forceinline__ void store_block(const WeightGradArgs &a, bool bf16, 
         const int odd = lane & 1;
         uint32_t *dst = reinterpret_cast<uint32_t *>(static_cast<unsigned short *>(a.dw) + (o0 + odd) * a.stride_o + (c - odd));
         const int64_t two_rows = a.stride_o;                     // two outputs further, in words
+        uint32_t before[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) before[r] = a.accumulate ? dst[r * two_rows] : 0u;
 #pragma unroll
         for (int r = 0; r < 32; r += 2, dst += two_rows) {
             const float mine = odd ? x[r + 1] : x[r], theirs = __shfl_xor_sync(0xffffffffu, odd ? x[r] : x[r + 1], 1);
             float lo = odd ? theirs : mine, hi = odd ? mine : theirs;
             if (a.accumulate) {
-                const uint32_t before = *dst;
-                lo = __fadd_rn(lo, __uint_as_float(before << 16));
-                hi = __fadd_rn(hi, __uint_as_float(before & 0xffff0000u));
+                lo = __fadd_rn(lo, __uint_as_float(before[r / 2] << 16));
+                hi = __fadd_rn(hi, __uint_as_float(before[r / 2] & 0xffff0000u));
             }
             *dst = pack_bf16(lo, hi);
         }
@@ -369,13 +373,15 @@ __device__ __forceinline__ void store_block(const WeightGradArgs &a, bool bf16, 
     if (bf16 && words && a.stride_o == 1 && o0 + 32 <= a.outs) {
         if (c >= a.kept.cols) return;
         uint32_t *dst = reinterpret_cast<uint32_t *>(static_cast<unsigned short *>(a.dw) + o0 + c * a.stride_c);
+        uint32_t before[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) before[r] = a.accumulate ? dst[r] : 0u;
 #pragma unroll
         for (int r = 0; r < 32; r += 2) {
             float lo = x[r], hi = x[r + 1];
             if (a.accumulate) {
-                const uint32_t before = dst[r / 2];
-                lo = __fadd_rn(lo, __uint_as_float(before << 16));
-                hi = __fadd_rn(hi, __uint_as_float(before & 0xffff0000u));
+                lo = __fadd_rn(lo, __uint_as_float(before[r / 2] << 16));
+                hi = __fadd_rn(hi, __uint_as_float(before[r / 2] & 0xffff0000u));
             }
             dst[r / 2] = pack_bf16(lo, hi);
         }
@@ -386,8 +392,14 @@ __device__ __forceinline__ void store_block(const WeightGradArgs &a, bool bf16, 
     if (!bf16) {
         float *dst = static_cast<float *>(a.dw) + o0 * a.stride_o + c * a.stride_c;
 #pragma unroll
-        for (int r = 0; r < 32; ++r, dst += a.stride_o)
-            if (r < left) *dst = a.accumulate ? __fadd_rn(x[r], *dst) : x[r];
+        for (int r0 = 0; r0 < 32; r0 += 16, dst += 16 * a.stride_o) {
+            float before[16];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) before[r] = a.accumulate && r0 + r < left ? dst[r * a.stride_o] : 0.0f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (r0 + r < left) dst[r * a.stride_o] = a.accumulate ? __fadd_rn(x[r0 + r], before[r]) : x[r0 + r];
+        }
         return;
     }
 #pragma unroll
@@ -411,6 +423,17 @@ __device__ __forceinline__ void store_four(const WeightGradArgs &a, bool bf16, b
         dst[0] = pack_bf16(v.x, v.y);
         dst[1] = pack_bf16(v.z, v.w);
         return;
+    }
+    if (!bf16 && a.stride_c == 1 && c + 4 <= a.kept.cols) {
+        float *dst = static_cast<float *>(a.dw) + o * a.stride_o + c;
+        if (reinterpret_cast<uintptr_t>(dst) % 16 == 0) {
+            if (a.accumulate) {
+                const float4 before = *reinterpret_cast<const float4 *>(dst);
+                v = make_float4(__fadd_rn(v.x, before.x), __fadd_rn(v.y, before.y), __fadd_rn(v.z, before.z), __fadd_rn(v.w, before.w));
+            }
+            *reinterpret_cast<float4 *>(dst) = v;
+            return;
+        }
     }
     const float x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
