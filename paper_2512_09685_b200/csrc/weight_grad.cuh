@@ -309,8 +309,8 @@ __device__ __forceinline__ float4 peer_load(uint32_t address)
 }
 
 // The sums of a split tile: part `part` adds its share of the columns over the
-// parts' accumulators (in their shared memory, [N][kTileC]), in the order of the
-// parts, all loads of a sum in flight together.
+// parts' accumulators (in their shared memory, N * kTileC values), in the order of
+// the parts, all loads of a sum in flight together.  store(i, x): the i-th four.
 template <int PARTS, int N, typename Store>
 __device__ __forceinline__ void join_parts(uint32_t sums, int part, uint32_t of_pair, uint32_t blocks, Store store)
 {
@@ -326,7 +326,7 @@ __device__ __forceinline__ void join_parts(uint32_t sums, int part, uint32_t of_
             x[0].z = __fadd_rn(x[0].z, x[q].z);
             x[0].w = __fadd_rn(x[0].w, x[q].w);
         }
-        store(i / (kTileC / 4), i % (kTileC / 4) * 4, x[0]);
+        store(i, x[0]);
     }
 }
 
@@ -342,11 +342,44 @@ __device__ __forceinline__ void store_weight(const WeightGradArgs &a, bool bf16,
     }
 }
 
+// dst[0 .. 32) = x, or += x, in 32-byte accesses; values of BYTES each.
+template <int BYTES> __device__ __forceinline__ void add_and_store(char *dst, const float (&x)[32], bool accumulate)
+{
+#pragma unroll
+    for (int half = 0; half < BYTES / 2; ++half, dst += 64) {            // two accesses at a time
+        uint32_t before[2][8];
+        if (accumulate) {
+            load_words(dst, before[0]);
+            load_words(dst + 32, before[1]);
+        }
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            uint32_t w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if constexpr (BYTES == 4) {
+                    const float v = x[16 * half + 8 * q + e];
+                    w[e] = __float_as_uint(accumulate ? __fadd_rn(v, __uint_as_float(before[q][e])) : v);
+                } else {
+                    float lo = x[16 * q + 2 * e], hi = x[16 * q + 2 * e + 1];
+                    if (accumulate) {
+                        lo = __fadd_rn(lo, __uint_as_float(before[q][e] << 16));
+                        hi = __fadd_rn(hi, __uint_as_float(before[q][e] & 0xffff0000u));
+                    }
+                    w[e] = pack_bf16(lo, hi);
+                }
+            }
+            store_words(dst + 32 * q, w);
+        }
+    }
+}
+
 // A warp's 32 columns c0 .. and 32 outputs o0 .. (x[r]: output o0 + r of this
 // lane's column).  `words`: pairs of bf16 at even columns lie on whole words.
 // Plain layout: neighbouring lanes trade halves, so that each stores two columns
-// of every other output; fp32 and transposed bf16 need no trade.  What is added to
-// is loaded ahead of the stores, 16 words at a time: the compiler cannot move a load
+// of every other output; fp32 needs no trade.  Transposed, a lane's outputs are
+// neighbours in memory (2048 rows, 4096 -> 4096, fp32: 32-byte accesses 73 us, words
+// 161).  What is added to is loaded ahead of the stores, 16 words at a time: the compiler cannot move a load
 // over a store that might change it.
 __device__ __forceinline__ void store_block(const WeightGradArgs &a, bool bf16, bool words, int64_t o0, int64_t c0, int lane, const float (&x)[32])
 {
@@ -370,22 +403,16 @@ __device__ __forceinline__ void store_block(const WeightGradArgs &a, bool bf16, 
         }
         return;
     }
-    if (bf16 && words && a.stride_o == 1 && o0 + 32 <= a.outs) {
+    if (a.stride_o == 1 && o0 + 32 <= a.outs) {
         if (c >= a.kept.cols) return;
-        uint32_t *dst = reinterpret_cast<uint32_t *>(static_cast<unsigned short *>(a.dw) + o0 + c * a.stride_c);
-        uint32_t before[16];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) before[r] = a.accumulate ? dst[r] : 0u;
-#pragma unroll
-        for (int r = 0; r < 32; r += 2) {
-            float lo = x[r], hi = x[r + 1];
-            if (a.accumulate) {
-                lo = __fadd_rn(lo, __uint_as_float(before[r / 2] << 16));
-                hi = __fadd_rn(hi, __uint_as_float(before[r / 2] & 0xffff0000u));
-            }
-            dst[r / 2] = pack_bf16(lo, hi);
+        char *dst = static_cast<char *>(a.dw) + (o0 + c * a.stride_c) * (bf16 ? 2 : 4);
+        if (reinterpret_cast<uintptr_t>(dst) % 32 == 0) {        // whole sectors: a lane's outputs are neighbours
+            if (bf16)
+                add_and_store<2>(dst, x, a.accumulate);
+            else
+                add_and_store<4>(dst, x, a.accumulate);
+            return;
         }
-        return;
     }
     if (c >= a.kept.cols) return;
     const int left = static_cast<int>(min(a.outs - o0, int64_t{32}));
@@ -407,12 +434,15 @@ __device__ __forceinline__ void store_block(const WeightGradArgs &a, bool bf16, 
         if (r < left) store_weight(a, true, o0 + r, c, x[r]);
 }
 
-// Four neighbouring columns of one output.
-__device__ __forceinline__ void store_four(const WeightGradArgs &a, bool bf16, bool words, int64_t o, int64_t c, float4 v)
+// Four neighbours along dw's rows: columns c .. of an output or, `swapped`, outputs
+// o .. of a column.
+__device__ __forceinline__ void store_four(const WeightGradArgs &a, bool bf16, bool words, bool swapped, int64_t o, int64_t c, float4 v)
 {
-    if (o >= a.outs) return;
-    if (bf16 && words && a.stride_c == 1 && c + 4 <= a.kept.cols) {
-        uint32_t *dst = reinterpret_cast<uint32_t *>(static_cast<unsigned short *>(a.dw) + o * a.stride_o + c);
+    const int64_t left = swapped ? a.outs - o : a.kept.cols - c;
+    if (left <= 0 || (swapped ? c >= a.kept.cols : o >= a.outs)) return;
+    const int64_t at = o * a.stride_o + c * a.stride_c;
+    if (bf16 && words && left >= 4) {
+        uint32_t *dst = reinterpret_cast<uint32_t *>(static_cast<unsigned short *>(a.dw) + at);
         if (a.accumulate) {
             const uint32_t lo = dst[0], hi = dst[1];
             v.x = __fadd_rn(v.x, __uint_as_float(lo << 16));
@@ -424,8 +454,8 @@ __device__ __forceinline__ void store_four(const WeightGradArgs &a, bool bf16, b
         dst[1] = pack_bf16(v.z, v.w);
         return;
     }
-    if (!bf16 && a.stride_c == 1 && c + 4 <= a.kept.cols) {
-        float *dst = static_cast<float *>(a.dw) + o * a.stride_o + c;
+    if (!bf16 && left >= 4) {
+        float *dst = static_cast<float *>(a.dw) + at;
         if (reinterpret_cast<uintptr_t>(dst) % 16 == 0) {
             if (a.accumulate) {
                 const float4 before = *reinterpret_cast<const float4 *>(dst);
@@ -438,7 +468,7 @@ __device__ __forceinline__ void store_four(const WeightGradArgs &a, bool bf16, b
     const float x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-        if (c + e < a.kept.cols) store_weight(a, bf16, o, c + e, x[e]);
+        if (e < left) store_weight(a, bf16, swapped ? o + e : o, swapped ? c : c + e, x[e]);
 }
 
 // grid: (column tiles, output tiles, parts of the rows); cluster: (1 or 2, 1, parts).
@@ -690,21 +720,35 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
             }
         }
     } else {
-        float *sums = reinterpret_cast<float *>(smem);               // [kN][kTileC]
+        // [kN][kTileC], or [kTileC][kN] in fours that trade places within eight, so
+        // that neither these stores nor the loads of the join collide in the banks.
+        float *sums = reinterpret_cast<float *>(smem);
+        const bool swapped = p.a.stride_o == 1 && p.a.stride_c != 1;
         constexpr int kPart = S::kN / (kConvertWarps / 4);
         for (int n = 0; n < BN / S::kN; ++n) {
             if (warp >= kFirstConvert) {
                 for (int col = share * kPart; col < (share + 1) * kPart; col += 32) {
                     float x[32];
                     result(n * S::kN + col, x);
+                    const int c = quarter * 32 + lane;
+                    if (swapped) {
+                        float4 *row = reinterpret_cast<float4 *>(sums + c * S::kN);
 #pragma unroll
-                    for (int r = 0; r < 32; ++r) sums[(col + r) * kTileC + quarter * 32 + lane] = x[r];
+                        for (int r = 0; r < 8; ++r) row[(col / 4 + r) ^ (c & 7)] = make_float4(x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]);
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 32; ++r) sums[(col + r) * kTileC + c] = x[r];
+                    }
                 }
             }
             __syncthreads();
             cluster_sync();
             if (whole) {
-                const auto store = [&](int col, int r, float4 x) { store_four(p.a, dw_bf16, words, o0 + n * S::kN + col, c0 + r, x); };
+                const auto store = [&](int i, float4 x) {
+                    const int c = swapped ? i / (S::kN / 4) : i % (kTileC / 4) * 4;
+                    const int o = swapped ? (i % (S::kN / 4) ^ (c & 7)) * 4 : i / (kTileC / 4);
+                    store_four(p.a, dw_bf16, words, swapped, o0 + n * S::kN + o, c0 + c, x);
+                };
                 switch (parts) {
                 case 2: join_parts<2, S::kN>(base, part, of_pair, kBlocks, store); break;
                 case 3: join_parts<3, S::kN>(base, part, of_pair, kBlocks, store); break;
