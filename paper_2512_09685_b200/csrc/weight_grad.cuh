@@ -777,9 +777,32 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
 // on the ordinary units: a block makes 64 x 256 results, a thread 8 x 8 of them,
 // rows 32 at a time in shared memory.  The result's inner index, along which dw
 // is stored, runs over the lanes: columns, or outputs where dw is transposed.
-// 4096 x 4096 from 1 row: bf16 11 us (3.0 TB/s), fp32 16 (4.2 TB/s).
+// 4096 x 4096 from 1 row: bf16 10 us (3.4 TB/s), fp32 13 (5.0 TB/s); added to 12.7 and 16.1.
 // ---------------------------------------------------------------------------
 constexpr int kFewRows = 32, kFewOuter = 64, kFewInner = 256, kFewThreads = 256;
+
+// dw[at .. at + left) as four values, 0 beyond.
+template <typename GW> __device__ __forceinline__ void load_four(const void *dw, int64_t at, bool whole, int left, float (&x)[4])
+{
+    if (whole) {
+        if constexpr (GW::kBytes == 2) {
+            const uint2 w = *reinterpret_cast<const uint2 *>(static_cast<const unsigned short *>(dw) + at);
+            x[0] = __uint_as_float(w.x << 16);
+            x[1] = __uint_as_float(w.x & 0xffff0000u);
+            x[2] = __uint_as_float(w.y << 16);
+            x[3] = __uint_as_float(w.y & 0xffff0000u);
+        } else {
+            const float4 w = *reinterpret_cast<const float4 *>(static_cast<const float *>(dw) + at);
+            x[0] = w.x;
+            x[1] = w.y;
+            x[2] = w.z;
+            x[3] = w.w;
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x[q] = q < left ? load_value<GW>(dw, at + q) : 0.0f;
+    }
+}
 
 template <typename GY, typename GW, bool TRANSPOSED>
 __global__ void __launch_bounds__(kFewThreads, 2) star_weight_grad_few_kernel(const __grid_constant__ WeightGradArgs a, int vector)
@@ -827,34 +850,48 @@ __global__ void __launch_bounds__(kFewThreads, 2) star_weight_grad_few_kernel(co
                 for (int q = 0; q < 8; ++q) sum[p][q] = __fmaf_rn(y[p], x[q], sum[p][q]);
         }
     }
-    // Columns 4 lane .. + 3 of each half of the 256.
+    // Columns 4 lane .. + 3 of each half of the 256, four rows of them at a time: what
+    // they are added to is loaded ahead of the stores.  Whole tiles without branches.
     const int64_t ld = TRANSPOSED ? a.stride_c : a.stride_o;
+    const auto results = [&](auto whole) {
 #pragma unroll
-    for (int p = 0; p < 8; ++p) {
-        const int64_t i = i0 + 8 * warp + p;
-        if (i >= n_outer) break;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int64_t j = j0 + half * 128 + 4 * lane, at = i * ld + j;
-            float v[4] = {sum[p][4 * half], sum[p][4 * half + 1], sum[p][4 * half + 2], sum[p][4 * half + 3]};
-            const int left = static_cast<int>(min(n_inner - j, int64_t{4}));
+        for (int p0 = 0; p0 < 8; p0 += 4) {
+            float before[8][4];
             if (a.accumulate) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (e < left) v[e] = __fadd_rn(v[e], load_value<GW>(a.dw, at + e));
+                for (int e = 0; e < 8; ++e) {
+                    const int64_t i = i0 + 8 * warp + p0 + e / 2, j = j0 + e % 2 * 128 + 4 * lane, at = i * ld + j;
+                    const int left = whole.value ? 4 : i < n_outer ? static_cast<int>(min(n_inner - j, int64_t{4})) : 0;
+                    load_four<GW>(a.dw, at, whole.value, left, before[e]);
+                }
             }
-            if (vector && left == 4) {
-                if constexpr (GW::kBytes == 2)
-                    *reinterpret_cast<uint2 *>(static_cast<unsigned short *>(a.dw) + at) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-                else
-                    *reinterpret_cast<float4 *>(static_cast<float *>(a.dw) + at) = make_float4(v[0], v[1], v[2], v[3]);
-            } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (e < left) store_value<GW>(a.dw, at + e, v[e]);
+            for (int e = 0; e < 8; ++e) {
+                const int p = p0 + e / 2, half = e % 2;
+                const int64_t i = i0 + 8 * warp + p, j = j0 + half * 128 + 4 * lane, at = i * ld + j;
+                const int left = whole.value ? 4 : i < n_outer ? static_cast<int>(min(n_inner - j, int64_t{4})) : 0;
+                float v[4] = {sum[p][4 * half], sum[p][4 * half + 1], sum[p][4 * half + 2], sum[p][4 * half + 3]};
+                if (a.accumulate) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) v[q] = __fadd_rn(v[q], before[e][q]);
+                }
+                if constexpr (whole.value) {
+                    if constexpr (GW::kBytes == 2)
+                        *reinterpret_cast<uint2 *>(static_cast<unsigned short *>(a.dw) + at) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+                    else
+                        *reinterpret_cast<float4 *>(static_cast<float *>(a.dw) + at) = make_float4(v[0], v[1], v[2], v[3]);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (q < left) store_value<GW>(a.dw, at + q, v[q]);
+                }
             }
         }
-    }
+    };
+    if (vector && i0 + kFewOuter <= n_outer && j0 + kFewInner <= n_inner)
+        results(std::true_type());
+    else
+        results(std::false_type());
 }
 
 }  // namespace star
