@@ -472,6 +472,7 @@ __device__ __forceinline__ void store_four(const WeightGradArgs &a, bool bf16, b
 }
 
 // grid: (column tiles, output tiles, parts of the rows); cluster: (1 or 2, 1, parts).
+// Every part has a step at least.
 //
 // PAIR: two blocks with neighbouring column tiles work as one (cta_group::2).
 // Each widens its own 128 columns and fetches half of the dy tile; the matrix
@@ -588,7 +589,7 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
                 matrix_commit<PAIR>(used(i), mask);
                 if (FLUSH && in_run == kFlushSteps - 1 && k + 1 < last) matrix_commit<PAIR>(summed, mask);
             }
-            if (last > first) matrix_commit<PAIR>(finished, mask);
+            matrix_commit<PAIR>(finished, mask);
         }
     } else if (warp >= kFirstConvert) {
         // Thread w of a group widens 16 codes of rows w / 8 + 32 h: their place is the
@@ -682,9 +683,8 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
     }
 
     // The result: every warp waits for the last matrix instruction itself.
-    const bool any = last > first;
     __syncwarp();                        // the idle lanes of a role do not spin beside it
-    if (any) ok = barrier_wait(finished, 0) && ok;
+    ok = barrier_wait(finished, 0) && ok;
     const bool whole = __syncthreads_and(ok);
     tensor_fence_after();
     const int quarter = warp % 4, share = (warp - kFirstConvert) / 4;            // of a converting warp
@@ -710,12 +710,7 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
         if (whole && warp >= kFirstConvert) {
             for (int col = share * kShare; col < (share + 1) * kShare; col += 32) {
                 float x[32];
-                if (any) {
-                    result(col, x);
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 32; ++r) x[r] = 0.0f;
-                }
+                result(col, x);
                 store_block(p.a, dw_bf16, words, o0 + col, c0 + quarter * 32, lane, x);
             }
         }
