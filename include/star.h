@@ -641,12 +641,20 @@ STAR_API star_status_t star_checkpoint_weight_grad(void *dw, star_dtype_t dw_dty
                                                    void *cuda_stream);
 
 /* The policy loss and the weight gradient wait inside their kernels for copies
- * that they have started.  Every such wait is bounded; one that runs out (some
- * tenths of a second; a fault of the device or its memory) ends the kernel
- * without a valid result.  star_check_waits waits for cuda_stream and says
- * whether that has happened on the current device since the last check:
+ * that they have started.  Every such wait is bounded; one that runs out (a third
+ * of a second at the earliest, as long as the hardware holds its attempts at the
+ * latest; a fault of the device or its memory) ends the kernel without a valid
+ * result: the policy loss's sums are NaN.  star_check_waits waits for cuda_stream
+ * and says whether that has happened on the current device since the last check:
  * STAR_ERR_TIMEOUT, or STAR_OK.  Not inside a stream capture. */
 STAR_API star_status_t star_check_waits(void *cuda_stream);
+
+/* The attempts of every such wait in launches made after this call, by any thread:
+ * 2^24 (what more is taken for) unless set, not negative.  With 0 each wait has run
+ * out at once and a call whose kernel waits ends without a result, which is how a
+ * program's answer to STAR_ERR_TIMEOUT is tried out; what a kernel has in flight it
+ * waits for all the same. */
+STAR_API star_status_t star_set_wait_attempts(int attempts);
 
 /* ---------------------------------------------------------------------------
  * Tensor-list round for callers that cannot allocate device memory.

@@ -138,6 +138,8 @@ def _load() -> ctypes.CDLL:
     lib.star_group_update_multi_ex.restype = c_int
     lib.star_check_waits.argtypes = [c_vp]
     lib.star_check_waits.restype = c_int
+    lib.star_set_wait_attempts.argtypes = [c_int]
+    lib.star_set_wait_attempts.restype = c_int
     lib.star_token_logprobs.argtypes = [c_vp, c_int, c_i64, c_i64, c_i64, c_vp, c_f, c_vp, c_vp, c_vp]
     lib.star_token_logprobs.restype = c_int
     lib.star_loss_workspace_bytes.argtypes = [c_i64, c_i64, c_vp]
@@ -987,3 +989,11 @@ def star_checkpoint_weight_grad(dw: torch.Tensor, dy: torch.Tensor, codes: torch
 def star_check_waits(stream=None) -> None:
     """Waits for the stream; raises if a wait inside a kernel ran out since the last check."""
     _check(_lib.star_check_waits(_stream(stream)), "star_check_waits")
+
+
+STAR_WAIT_ATTEMPTS = 1 << 24
+
+
+def star_set_wait_attempts(attempts: int = STAR_WAIT_ATTEMPTS) -> None:
+    """Attempts of a wait inside a kernel, for launches from now on; 0: every wait has run out at once."""
+    _check(_lib.star_set_wait_attempts(attempts), "star_set_wait_attempts")

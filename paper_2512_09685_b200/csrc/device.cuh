@@ -118,13 +118,15 @@ __device__ __forceinline__ uint32_t cluster_size()
 }
 
 // ---------------------------------------------------------------------------
-// Barriers in shared memory.  Every wait ends: after kWaitTries attempts it reports failure,
-// sets a flag that star_check_waits reads, and the kernel ends without a valid
-// result, its copies drained.
+// Barriers in shared memory.  Every wait ends: after `tries` attempts it sets a
+// flag that star_check_waits reads and reports failure, upon which the kernel takes
+// up no further work, waits for its copies and matrix instructions in flight
+// (kWaitTries attempts at most, whatever `tries` is) and ends without a valid result.
 // ---------------------------------------------------------------------------
-// An attempt takes 20 ns or more (the hardware holds it for a while), so a wait
-// ends after some tenths of a second at the earliest: waits for memory take
-// microseconds.
+// An attempt takes 20 ns or more, and the hardware may hold it for longer, so this
+// many end after a third of a second at the earliest; waits for memory take
+// microseconds.  Attempts are counted, not time: a kernel that is taken off the
+// device for a while is not late when it comes back.
 constexpr int kWaitTries = 1 << 24;
 static __device__ int g_wait_expired;        // one of each source file that includes this
 
@@ -149,9 +151,9 @@ __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity)
                  "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
-__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity)
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, int tries)
 {
-    for (int i = 0; i < kWaitTries; ++i)
+    for (int left = tries; left > 0; --left)
         if (barrier_try(bar, parity)) return true;
     atomicExch(&g_wait_expired, 1);
     return false;

@@ -16,6 +16,9 @@ star_status_t cuda_failed(cudaError_t e);
 // One more kernel launched (star_launch_count).
 void count_launch();
 
+// Attempts of a wait inside a kernel (star_set_wait_attempts).
+int wait_attempts();
+
 // Whether a wait of the weight gradient's kernels has run out (and no longer
 // after this), once the work on `stream` is done.
 cudaError_t weight_grad_expired(cudaStream_t stream, int *expired);

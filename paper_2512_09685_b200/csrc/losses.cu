@@ -7,6 +7,13 @@
 #include "internal.h"
 #include "losses.cuh"
 
+namespace star {
+
+static std::atomic<int> g_wait_attempts{kWaitTries};
+int wait_attempts() { return g_wait_attempts.load(std::memory_order_relaxed); }
+
+}  // namespace star
+
 namespace {
 
 using namespace star;
@@ -296,6 +303,7 @@ extern "C" star_status_t star_policy_loss(const void *logits, star_dtype_t dtype
     a.partial = static_cast<float4 *>(workspace);
     a.dlogits = dlogits;
     a.ld_dlogits = ld_dlogits;
+    a.tries = wait_attempts();
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const bool bf16 = dtype == STAR_DTYPE_BF16;
     int parts = 0, threads = 0, cluster = 1;
@@ -387,6 +395,13 @@ extern "C" star_status_t star_preference_loss(const void *logits, star_dtype_t d
     g.loss_scale = loss_scale;
     g.loss = loss;
     return launch_gradient<false>(g, dtype, stream);
+}
+
+extern "C" star_status_t star_set_wait_attempts(int attempts)
+{
+    if (attempts < 0) return STAR_ERR_INVALID_ARG;
+    g_wait_attempts.store(std::min(attempts, kWaitTries), std::memory_order_relaxed);
+    return STAR_OK;
 }
 
 extern "C" star_status_t star_check_waits(void *cuda_stream)

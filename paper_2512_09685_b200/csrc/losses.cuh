@@ -43,6 +43,7 @@ struct RowWork {
     float4 *partial;             // the four sums of each block's (cluster's) rows
     void *dlogits;               // may be null
     int64_t ld_dlogits;
+    int tries;                   // of a wait
 };
 
 constexpr float kLn2 = 0.69314718055994531f;
@@ -143,6 +144,7 @@ struct alignas(16) RowFactors {
     float coef;
     float label_power;           // 2^exponent(label's logit, m)
     int active;
+    int late;                    // a wait for the row ran out: nothing of it holds
 };
 
 // What belongs to a row beside its logits, for the thread that finishes it.
@@ -159,7 +161,7 @@ template <bool POLICY>
 __device__ __forceinline__ RowFactors make_factors(const RowWork &a, bool wanted, MaxSum row, float weight, const RowIn &in, float *lp, PolicyRow *r)
 {
     const float inv_t = a.row.inv_temperature, k = __fmul_rn(inv_t, kLog2e);
-    RowFactors f{row.m, 0.0f, 0.0f, 0.0f, wanted && !(row.s == 0.0f) ? 1 : 0};
+    RowFactors f{row.m, 0.0f, 0.0f, 0.0f, wanted && !(row.s == 0.0f) ? 1 : 0, 0};
     *lp = 0.0f;
     *r = PolicyRow{0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     if (f.active) {
@@ -175,7 +177,7 @@ __device__ __forceinline__ RowFactors make_factors(const RowWork &a, bool wanted
     return f;
 }
 // The rest: results and sums.
-template <bool POLICY>
+template <bool POLICY, bool KEEPS>
 __device__ __forceinline__ void finish_row(const RowWork &a, int64_t t, const RowFactors &f, MaxSum row, float weight, float lp,
                                            const PolicyRow &r, RowSums *sums)
 {
@@ -191,7 +193,7 @@ __device__ __forceinline__ void finish_row(const RowWork &a, int64_t t, const Ro
     } else {
         if (a.lse) a.lse[t] = f.active ? log_sum_exp(row, a.row.inv_temperature) : 0.0f;
     }
-    if (a.kept) a.kept[t] = RowKept{row.m, f.active ? __fdiv_rn(1.0f, row.s) : 0.0f, lp, r.coef};
+    if (KEEPS && a.kept) a.kept[t] = RowKept{row.m, f.active ? __fdiv_rn(1.0f, row.s) : 0.0f, lp, r.coef};
 }
 
 template <bool POLICY> __device__ __forceinline__ void store_partial(const RowWork &a, int64_t at, const RowSums &sums)
@@ -493,7 +495,7 @@ __global__ void __launch_bounds__(THREADS, row_blocks(THREADS)) star_row_kernel(
                 float lp;
                 PolicyRow r;
                 const RowFactors f = make_factors<POLICY>(a, wanted, x, weight, RowIn{row_in[0], row_in[1], row_in[2], row_in[3]}, &lp, &r);
-                finish_row<POLICY>(a, t, f, x, weight, lp, r, &sums);
+                finish_row<POLICY, true>(a, t, f, x, weight, lp, r, &sums);
             }
             __syncwarp();                                        // and read, before the next row's
         }
@@ -510,6 +512,9 @@ __global__ void __launch_bounds__(THREADS, row_blocks(THREADS)) star_row_kernel(
 // of a cluster's blocks, which join their parts and each make all factors.  The
 // thread that finishes a row makes its factors first and lets the others go before
 // it writes results and sums.
+//
+// A wait that runs out ends all blocks of the row's cluster after that row's joins,
+// without results from this row on and with sums of NaN.
 //
 // 4096 x 50257 bf16, no row masked: 161 us, 5.1 TB/s of reading and writing;
 // 4096 x 131072 480 us, 4.5 TB/s.  Other arrangements of the same arithmetic, at
@@ -529,7 +534,12 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_policy_k
     __shared__ alignas(8) MaxSum block_part[2][8];
     __shared__ RowFactors factors;
     __shared__ RowSums sums;
-    __shared__ RowIn row_in;
+    __shared__ RowIn row_in;                                     // and the row's weight and label: thread 0's alone
+    __shared__ float row_weight;
+    __shared__ int row_label;
+    // A wait for the row ran out, in any block of the cluster.  One for every other row: a block
+    // may tell of the next row while another has yet to read this row's.
+    __shared__ int late[2];
     __shared__ alignas(8) uint64_t landed;                       // the row's copy is in place
     const float k = __fmul_rn(a.row.inv_temperature, kLog2e);
     const int vocab = static_cast<int>(a.row.vocab);
@@ -540,6 +550,7 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_policy_k
     launch_dependents();
     if (threadIdx.x == 0) {
         sums = RowSums{0.0, 0.0, 0.0, 0.0};
+        late[0] = late[1] = factors.late = 0;
         barrier_init(smem_address(&landed), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -561,11 +572,18 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_policy_k
 
     uint32_t phase = 0;
     int parity = 0;
-    int64_t label = -1;
-    float weight = 0.0f;
-    bool wanted = row_wanted(a.row, first, &label, &weight);
-    if (wanted && threadIdx.x == 0) fetch(first);
-    for (int64_t t = first; t < a.row.rows; t += step, parity ^= 1) {
+    bool wanted;
+    {
+        int64_t label;
+        float weight;
+        wanted = row_wanted(a.row, first, &label, &weight);
+        if (wanted && threadIdx.x == 0) {
+            fetch(first);
+            row_label = static_cast<int>(label);
+            row_weight = weight;
+        }
+    }
+    for (int64_t t = first; t < a.row.rows && !factors.late; t += step, parity ^= 1) {
         const RowSplit s = split_row<G>(row_base(t), vocab);
         const RowShare own = row_share(s.granules, rank, log_blocks);
         // The next row's label and weight are on their way.
@@ -581,13 +599,17 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_policy_k
         if (wanted) {
             if (edge_at >= 0) edge = load_value<G>(row_base(t), edge_at);
             if (threadIdx.x == 0) {
-                row_in.label_logit = load_value<G>(row_base(t), label);
+                row_in.label_logit = load_value<G>(row_base(t), row_label);
                 row_in.advantage = a.advantages[t];
                 row_in.old_lp = a.old_logp ? a.old_logp[t] : 0.0f;
                 row_in.ref_lp = a.ref_logp ? a.ref_logp[t] : 0.0f;
             }
             if (own.count > 0) {
-                barrier_wait(smem_address(&landed), phase);
+                if (!barrier_wait(smem_address(&landed), phase, a.tries)) {
+                    late[parity] = 1;                            // what the walk below finds is not used
+                    for (uint32_t q = 0; CLUSTER && q < blocks; ++q)
+                        asm volatile("st.shared::cluster.s32 [%0], 1;" :: "r"(peer_address(smem_address(&late[parity]), q)) : "memory");
+                }
                 phase ^= 1;
             }
             const uint4 *from = kept_row + threadIdx.x;
@@ -600,11 +622,16 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_policy_k
         if (blocks > 1) x = cluster_join(x, block_part[parity], blocks, rank, k);
         float lp;
         PolicyRow r;
-        if (threadIdx.x == 0) factors = make_factors<true>(a, wanted, x, weight, row_in, &lp, &r);
-        const bool next_wanted = next_label >= 0 && next_label < vocab && next_weight != 0.0f;
+        if (kWarps == 1) __syncwarp();                           // `late` is written, the last row's factors are read
+        if (threadIdx.x == 0) {
+            factors = make_factors<true>(a, wanted, x, row_weight, row_in, &lp, &r);
+            factors.late = late[parity];
+        }
         __syncthreads();                                         // the factors; and the first walk is over
-        if (threadIdx.x == 0 && rank == 0) finish_row<true>(a, t, factors, x, weight, lp, r, &sums);
-        if (writes) {
+        const bool ended = factors.late != 0;
+        const bool next_wanted = next_label >= 0 && next_label < vocab && next_weight != 0.0f && !ended;
+        if (threadIdx.x == 0 && rank == 0 && !ended) finish_row<true, false>(a, t, factors, x, row_weight, lp, r, &sums);
+        if (writes && !ended) {
             const RowFactors f = factors;
             char *out = static_cast<char *>(a.dlogits) + t * a.ld_dlogits * G::kBytes;
             const bool same_phase = (reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(row_base(t))) % 16 == 0;
@@ -628,17 +655,25 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_policy_k
                 store_value<G>(out, edge_at, f.active ? __fmul_rn(f.scale, exp2_fast(exponent(edge, f.m, k))) : 0.0f);
             __syncthreads();                                     // the row is read and written
             // The label's element again, by the block that has it.
-            const int at = static_cast<int>(label) - s.head;
-            const bool in_granules = at >= 0 && at < s.granules * E;
-            const bool has_label = in_granules ? at / E >= own.begin && at / E < own.begin + own.count : rank == 0;
-            if (threadIdx.x == 0 && f.active && has_label) store_value<G>(out, label, __fmaf_rn(f.scale, f.label_power, f.coef));
+            if (threadIdx.x == 0 && f.active) {
+                const int at = row_label - s.head;
+                const bool in_granules = at >= 0 && at < s.granules * E;
+                const bool has_label = in_granules ? at / E >= own.begin && at / E < own.begin + own.count : rank == 0;
+                if (has_label) store_value<G>(out, row_label, __fmaf_rn(f.scale, f.label_power, f.coef));
+            }
         }
-        if (next_wanted && threadIdx.x == 0) fetch(t + step);
-        label = next_label;
-        weight = next_weight;
+        if (next_wanted && threadIdx.x == 0) {
+            fetch(t + step);
+            row_label = static_cast<int>(next_label);
+            row_weight = next_weight;
+        }
         wanted = next_wanted;
     }
-    if (threadIdx.x == 0 && rank == 0) store_partial<true>(a, first, sums);
+    if (threadIdx.x == 0 && factors.late) {
+        barrier_wait(smem_address(&landed), phase ^ 1, kWaitTries);      // the copy in flight, if any
+        sums.loss = sums.gain = sums.kl = sums.clipped = NAN;
+    }
+    if (threadIdx.x == 0 && rank == 0) store_partial<true>(a, blockIdx.x >> log_blocks, sums);
 }
 
 constexpr int kSumThreads = 1024;

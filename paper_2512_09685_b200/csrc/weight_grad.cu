@@ -275,7 +275,7 @@ extern "C" star_status_t star_checkpoint_weight_grad(void *dw, star_dtype_t dw_d
     if (tiled && !make_map(&dy_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dy, outs, rows, static_cast<uint64_t>(ld_dy) * 2, 64, kTileT,
                            CU_TENSOR_MAP_SWIZZLE_128B))
         return cuda_failed(cudaErrorInvalidValue);
-    const WeightGradTile tile{a, static_cast<int>(steps)};
+    const WeightGradTile tile{a, static_cast<int>(steps), wait_attempts()};
     const auto run = [&](auto shape) { return launch_shape<decltype(shape)::value>(tile, codes_map, dy_map, w16, plan.parts, stream); };
     switch (plan.shape) {
     case kWide: return run(std::integral_constant<int, kWide>());

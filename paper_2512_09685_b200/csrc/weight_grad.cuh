@@ -45,6 +45,7 @@ constexpr int kGradThreads = 32 * (kFirstConvert + kConvertWarps);
 struct WeightGradTile {
     WeightGradArgs a;
     int steps;                       // of kTileT rows
+    int tries;                       // of a wait
 };
 
 // ---------------------------------------------------------------------------
@@ -549,7 +550,7 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
             int issued = 0;
             for (int k = first; k < last; ++k) {
                 const int i = k - first, s = i % LOADS;
-                if (i >= LOADS && !barrier_wait(used(i - LOADS), load_phase(i - LOADS))) break;
+                if (i >= LOADS && !barrier_wait(used(i - LOADS), load_phase(i - LOADS), p.tries)) break;
                 barrier_expect(loaded(i), S::kRaw + S::kScale + (TERMS == 0 ? S::kB : 0));
                 const int t = k * kTileT;
                 tma_load_2d(base + S::kOffRaw + s * S::kRaw, &codes_map, static_cast<int>(c0), t, loaded(i));
@@ -563,16 +564,16 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
                 issued = i + 1;
             }
             // Copies still in flight land before the block goes on (they have, unless a wait ran out).
-            for (int i = issued > LOADS ? issued - LOADS : 0; i < issued; ++i) barrier_wait(loaded(i), load_phase(i));
+            for (int i = issued > LOADS ? issued - LOADS : 0; i < issued; ++i) barrier_wait(loaded(i), load_phase(i), kWaitTries);
         }
     } else if (warp == 1) {
         if (lane == 0 && of_pair == 0) {
             constexpr uint32_t idesc = instruction_descriptor<S::kN, PAIR>();
             for (int k = first; k < last && ok; ++k) {
                 const int i = k - first, in_run = FLUSH ? i % kFlushSteps : i;
-                if (FLUSH && i > 0 && in_run == 0) ok = barrier_wait(drained, (i / kFlushSteps - 1) & 1);
+                if (FLUSH && i > 0 && in_run == 0) ok = barrier_wait(drained, (i / kFlushSteps - 1) & 1, p.tries);
                 // The widening warps of both blocks have seen their block's copies land.
-                ok = ok && barrier_wait(loaded(i), load_phase(i)) && barrier_wait(widened(i), wide_phase(i));
+                ok = ok && barrier_wait(loaded(i), load_phase(i), p.tries) && barrier_wait(widened(i), wide_phase(i), p.tries);
                 if (!ok) break;
                 tensor_fence_after();
                 const uint32_t as = base + (i % WIDE) * S::kA;
@@ -605,7 +606,7 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
         const int quarter = warp % 4, share = (warp - kFirstConvert) / 4;
         int run = 0;
         const auto drain = [&] {
-            if (!barrier_wait(summed, run & 1)) return false;
+            if (!barrier_wait(summed, run & 1, p.tries)) return false;
             tensor_fence_after();
             for (int col = share * kShare; col < (share + 1) * kShare; col += 32) {
                 const uint32_t at = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + col;
@@ -644,7 +645,7 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
             }
             // TERMS > 0: the step's dy is on its way while the codes are widened.
             if constexpr (TERMS > 0) fetch_dy(k);
-            ok = (i < WIDE || barrier_wait(used(i - WIDE), load_phase(i - WIDE))) && barrier_wait(loaded(i), load_phase(i));
+            ok = (i < WIDE || barrier_wait(used(i - WIDE), load_phase(i - WIDE), p.tries)) && barrier_wait(loaded(i), load_phase(i), p.tries);
             if (!ok) break;
             const uint8_t *raw = smem + S::kOffRaw + s * S::kRaw + from, *scale = smem + S::kOffScale + s * S::kScale + t0 * 4 + j / 2;
             uint8_t *as = smem + (i % WIDE) * S::kA;
@@ -682,9 +683,10 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
             while (ok && run + 1 < runs) ok = drain();
     }
 
-    // The result: every warp waits for the last matrix instruction itself.
+    // The result: every warp waits for the last matrix instruction itself, also where
+    // other waits ran out.
     __syncwarp();                        // the idle lanes of a role do not spin beside it
-    ok = barrier_wait(finished, 0) && ok;
+    ok = barrier_wait(finished, 0, kWaitTries) && ok;
     const bool whole = __syncthreads_and(ok);
     tensor_fence_after();
     const int quarter = warp % 4, share = (warp - kFirstConvert) / 4;            // of a converting warp
