@@ -80,7 +80,7 @@ __device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float k)
 // part so that the large terms cancel: the error stays near the result's own ulp
 // instead of that of the log-sum-exp (ten times larger at a vocabulary of 50
 // thousand).
-__device__ __forceinline__ float log_prob(float x, MaxSum row, float k)
+__device__ __forceinline__ float log_prob(float x, MaxSum row, float k, float inv_temperature)
 {
     const int bits = __float_as_int(row.s);
     const int e = (bits >> 23) - 127;                    // s is near 1 or more (the largest logit's own term), or NaN
@@ -88,7 +88,9 @@ __device__ __forceinline__ float log_prob(float x, MaxSum row, float k)
     const float d = exponent(x, row.m, k);               // log2 of p s
     if (!(row.s < INFINITY)) return __fadd_rn(d, row.s); // NaN
     const float whole = __fsub_rn(d, static_cast<float>(e));
-    return __fsub_rn(__fmul_rn(whole, kLn2), logf(f));
+    // A label masked by the type's lowest value: its exponent does not fit, its log p does.
+    const float far = __fmul_rn(__fsub_rn(x, pivot(row.m)), inv_temperature);
+    return __fsub_rn(d == -INFINITY ? far : __fmul_rn(whole, kLn2), logf(f));
 }
 
 __device__ __forceinline__ float log_sum_exp(MaxSum row, float inv_temperature)
@@ -165,7 +167,7 @@ __device__ __forceinline__ RowFactors make_factors(const RowWork &a, bool wanted
     *lp = 0.0f;
     *r = PolicyRow{0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     if (f.active) {
-        *lp = log_prob(in.label_logit, row, k);
+        *lp = log_prob(in.label_logit, row, k, inv_t);
         if constexpr (POLICY) {
             *r = policy_row(*lp, in.advantage, a.old_logp != nullptr, in.old_lp, a.ref_logp != nullptr, in.ref_lp, a.clip_low,
                             a.clip_high, a.kl_coef, weight, inv_t);
