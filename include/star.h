@@ -526,6 +526,7 @@ STAR_API star_status_t star_loss_workspace_bytes(int64_t rows, int64_t sequences
  *     dlogits[t][j] = w / temperature * ((j == label) - p[j]) *
  *                     (-(u <= c) r A + kl_coef (1 - exp(ref_logp[t] - logp)))
  *     sums = { sum w token_loss, sum w (-min(u, c)), sum w kl, sum w (c < u) }
+ * A factor of exactly 0 (A, kl_coef) takes its term out, however large the other one.
  * dlogits is the gradient of sums[0]; the caller puts the mean's 1 / n (per
  * token or per sequence) and any loss scale into weights.
  *   old_logp NULL differentiates the ratio as if old_logp were logp itself.

@@ -109,8 +109,10 @@ __device__ __forceinline__ PolicyRow policy_row(float lp, float advantage, bool 
                                                 float weight, float inv_temperature)
 {
     const float r = has_old ? expf(__fsub_rn(lp, old_lp)) : lp != lp ? lp : 1.0f;    // a NaN row shows in the totals
-    const float u = __fmul_rn(r, advantage);
-    const float c = __fmul_rn(fminf(fmaxf(r, __fsub_rn(1.0f, clip_low)), __fadd_rn(1.0f, clip_high)), advantage);
+    // A factor of exactly 0 takes its term out, also where the other one is beyond binary32.
+    const bool out_of_it = advantage == 0.0f && r == INFINITY;
+    const float u = out_of_it ? 0.0f : __fmul_rn(r, advantage);
+    const float c = out_of_it ? 0.0f : __fmul_rn(fminf(fmaxf(r, __fsub_rn(1.0f, clip_low)), __fadd_rn(1.0f, clip_high)), advantage);
     PolicyRow out;
     out.clipped = u > c ? 1.0f : 0.0f;
     const float gain = u > c ? c : u;                    // a NaN in u stays
@@ -122,8 +124,10 @@ __device__ __forceinline__ PolicyRow policy_row(float lp, float advantage, bool 
         // exp(d) - d - 1 without the cancellation at small d.
         const float em1 = expm1f(d);
         out.kl = __fsub_rn(em1, d);
-        loss = __fmaf_rn(kl_coef, out.kl, loss);
-        slope = __fmaf_rn(kl_coef, -em1, slope);
+        if (kl_coef != 0.0f) {
+            loss = __fmaf_rn(kl_coef, out.kl, loss);
+            slope = __fmaf_rn(kl_coef, -em1, slope);
+        }
     }
     out.loss = loss;
     out.gain = gain;
