@@ -54,7 +54,6 @@ __device__ __forceinline__ uint32_t code_bits(float x, float inverse)
 // ---------------------------------------------------------------------------
 constexpr float kGeluB = 0.79788456080286536f * 2.0f;           // 2 sqrt(2 / pi)
 constexpr float kGeluC = kGeluB * 0.044715f;
-constexpr float kSqrtHalf = 0.70710678118654752f;
 constexpr float kInvSqrt2Pi = 0.39894228040143268f;
 
 // 1 / (1 + 2^y): the sigmoid of x for y = -log2(e) x.
@@ -76,33 +75,57 @@ __device__ __forceinline__ Pair gated_slope(Pair q, Pair inner)
     return pair_fma(pair_mul(q, pair_add(pair_of(1.0f), pair_negate(q))), inner, q);
 }
 
-// Phi(x) by Abramowitz and Stegun 7.1.26 (Hastings): with z = |x| / sqrt(2) and
-// t = 1 / (1 + p z), erfc(z) = (a1 t + ... + a5 t^5) exp(-z^2), off by at most
-// 1.5e-7.  *power = exp(-x^2 / 2), which the slope needs too.
-__device__ __forceinline__ Pair normal_cdf(Pair x, Pair *power)
+template <int N> __device__ __forceinline__ Pair polynomial(const float (&c)[N], Pair x)
 {
-    const Pair size = x & 0x7fffffff7fffffffull;
-    const Pair t = pair_reciprocal(pair_fma(pair_of(0.3275911f * kSqrtHalf), size, pair_of(1.0f)));
-    *power = pair_exp2(pair_mul(pair_of(-0.5f * kLog2e), pair_mul(x, x)));
-    Pair q = pair_fma(t, pair_of(0.5f * 1.061405429f), pair_of(0.5f * -1.453152027f));
-    q = pair_fma(t, q, pair_of(0.5f * 1.421413741f));
-    q = pair_fma(t, q, pair_of(0.5f * -0.284496736f));
-    q = pair_fma(t, q, pair_of(0.5f * 0.254829592f));
-    q = pair_mul(pair_mul(t, q), *power);                // erfc(z) / 2
-    float x0, x1, q0, q1;
-    split_pair(x, &x0, &x1);
-    split_pair(q, &q0, &q1);
-    return make_pair(x0 > 0.0f ? __fsub_rn(1.0f, q0) : q0, x1 > 0.0f ? __fsub_rn(1.0f, q1) : q1);
+    Pair y = pair_of(c[N - 1]);
+#pragma unroll
+    for (int i = N - 2; i >= 0; --i) y = pair_fma(x, y, pair_of(c[i]));
+    return y;
 }
 
-template <int ACT> __device__ __forceinline__ Pair activation(Pair x)
+// Phi(x), with a bound on its error relative to itself: x Phi(x) and its slope live in
+// the tail too.  The tail is Phi(-|x|) = t P(t) exp(-x^2 / 2) with t = 1 / (1 + p |x|)
+// and P of degree 6, a minimax fit of the relative error for |x| <= 14.
+//   not FINE, for bf16 results: one P for all x, off by 9e-7, a 2000th of their rounding.
+//   FINE, for fp32: P for |x| >= 1, off by 9e-8, and below 1/2 + x S(x^2) with S of degree
+//   5, fitted to (Phi(x) - 1/2) / x, 3e-8.  In norm, on Gaussian values, 3.6e-8 for x Phi(x)
+//   and 4.9e-8 for the slope, as of binary32's erf and exp.
+// Both for both, us, with GELU forward / backward: 16384 x 4096 bf16 60 / 56 not FINE, 73 / 70
+// FINE (issue-bound); 8192 x 4096 fp32 46 / 45 FINE, bound by memory either way.
+// *power = exp(-x^2 / 2), which the slope needs too.
+template <bool FINE> __device__ __forceinline__ Pair normal_cdf(Pair x, Pair *power)
+{
+    constexpr float kNear[6] = {0.3989422917366028f, -0.06649035960435867f, 0.009973322972655296f, -0.0011863299878314137f,
+                                0.00011348637053743005f, -7.65420827519847e-06f};
+    constexpr float kTail[7] = {0.159595787525177f, 0.1590999811887741f, 0.13900233805179596f, 0.055540427565574646f,
+                                0.10536342114210129f, -0.1864282488822937f, 0.06812146306037903f};
+    constexpr float kWhole[7] = {0.1437130570411682f, 0.14177247881889343f, 0.13971911370754242f, 0.026549765840172768f,
+                                 0.18095333874225616f, -0.17976419627666473f, 0.04705614596605301f};
+    const Pair size = x & 0x7fffffff7fffffffull, x2 = pair_mul(x, x);
+    const Pair t = pair_reciprocal(pair_fma(pair_of(FINE ? 0.4f : 0.36f), size, pair_of(1.0f)));
+    *power = pair_exp2(pair_mul(pair_of(-0.5f * kLog2e), x2));
+    const Pair tail = pair_mul(pair_mul(t, polynomial(FINE ? kTail : kWhole, t)), *power);
+    float x0, x1, q0, q1, n0 = 0.0f, n1 = 0.0f;
+    split_pair(x, &x0, &x1);
+    split_pair(tail, &q0, &q1);
+    q0 = x0 > 0.0f ? __fsub_rn(1.0f, q0) : q0;
+    q1 = x1 > 0.0f ? __fsub_rn(1.0f, q1) : q1;
+    if constexpr (FINE) {
+        split_pair(pair_fma(x, polynomial(kNear, x2), pair_of(0.5f)), &n0, &n1);
+        q0 = fabsf(x0) < 1.0f ? n0 : q0;
+        q1 = fabsf(x1) < 1.0f ? n1 : q1;
+    }
+    return make_pair(q0, q1);
+}
+
+template <int ACT, bool FINE> __device__ __forceinline__ Pair activation(Pair x)
 {
     if constexpr (ACT == STAR_ACT_GELU_TANH) {           // 0.5 (1 + tanh(y)) = sigmoid(2 y)
         const Pair g = pair_fma(pair_of(-kLog2e * kGeluC), pair_mul(x, x), pair_of(-kLog2e * kGeluB));
         return pair_mul(x, sigmoid_exp2(pair_mul(x, g)));
     } else if constexpr (ACT == STAR_ACT_GELU_ERF) {
         Pair power;
-        return pair_mul(x, normal_cdf(x, &power));
+        return pair_mul(x, normal_cdf<FINE>(x, &power));
     } else if constexpr (ACT == STAR_ACT_SILU) {
         return pair_mul(x, sigmoid_exp2(pair_mul(x, pair_of(-kLog2e))));
     } else {
@@ -110,7 +133,7 @@ template <int ACT> __device__ __forceinline__ Pair activation(Pair x)
     }
 }
 
-template <int ACT> __device__ __forceinline__ Pair activation_slope(Pair x)
+template <int ACT, bool FINE> __device__ __forceinline__ Pair activation_slope(Pair x)
 {
     if constexpr (ACT == STAR_ACT_GELU_TANH) {
         const Pair x2 = bounded_square(x);
@@ -118,7 +141,7 @@ template <int ACT> __device__ __forceinline__ Pair activation_slope(Pair x)
         return gated_slope(q, pair_mul(x, pair_fma(pair_of(3.0f * kGeluC), x2, pair_of(kGeluB))));
     } else if constexpr (ACT == STAR_ACT_GELU_ERF) {
         Pair power;
-        const Pair cdf = normal_cdf(x, &power);
+        const Pair cdf = normal_cdf<FINE>(x, &power);
         return pair_fma(x, pair_mul(pair_of(kInvSqrt2Pi), power), cdf);
     } else if constexpr (ACT == STAR_ACT_SILU) {
         return gated_slope(sigmoid_exp2(pair_mul(x, pair_of(-kLog2e))), x);
@@ -128,16 +151,16 @@ template <int ACT> __device__ __forceinline__ Pair activation_slope(Pair x)
 }
 
 // One value.
-template <int ACT> __device__ __forceinline__ float activation(float x)
+template <int ACT, bool FINE> __device__ __forceinline__ float activation(float x)
 {
     float lo, hi;
-    split_pair(activation<ACT>(make_pair(x, 0.0f)), &lo, &hi);
+    split_pair(activation<ACT, FINE>(make_pair(x, 0.0f)), &lo, &hi);
     return lo;
 }
-template <int ACT> __device__ __forceinline__ float activation_slope(float x)
+template <int ACT, bool FINE> __device__ __forceinline__ float activation_slope(float x)
 {
     float lo, hi;
-    split_pair(activation_slope<ACT>(make_pair(x, 0.0f)), &lo, &hi);
+    split_pair(activation_slope<ACT, FINE>(make_pair(x, 0.0f)), &lo, &hi);
     return lo;
 }
 
@@ -332,7 +355,7 @@ __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_pack_kernel(cons
         if (half % 2 == 0) a.kept.scales[scale_at(a.kept, t, half / 2)] = static_cast<uint8_t>(s);
         if (a.act_out) {
 #pragma unroll
-            for (int e = 0; e < 16; e += 2) split_pair(activation<ACT>(make_pair(f[e], f[e + 1])), &f[e], &f[e + 1]);
+            for (int e = 0; e < 16; e += 2) split_pair(activation<ACT, G::kBytes == 4>(make_pair(f[e], f[e + 1])), &f[e], &f[e + 1]);
             Sixteen<G>::store(static_cast<char *>(a.act_out) + t * a.ld_act * G::kBytes, c, a.kept.cols, h.wide, f);
         }
     }
@@ -373,10 +396,10 @@ __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_read_kernel(cons
             Sixteen<G>::widen(w, dy);
 #pragma unroll
             for (int e = 0; e < 16; e += 2)
-                split_pair(pair_mul(make_pair(dy[e], dy[e + 1]), activation_slope<ACT>(make_pair(f[e], f[e + 1]))), &f[e], &f[e + 1]);
+                split_pair(pair_mul(make_pair(dy[e], dy[e + 1]), activation_slope<ACT, G::kBytes == 4>(make_pair(f[e], f[e + 1]))), &f[e], &f[e + 1]);
         } else {
 #pragma unroll
-            for (int e = 0; e < 16; e += 2) split_pair(activation<ACT>(make_pair(f[e], f[e + 1])), &f[e], &f[e + 1]);
+            for (int e = 0; e < 16; e += 2) split_pair(activation<ACT, G::kBytes == 4>(make_pair(f[e], f[e + 1])), &f[e], &f[e + 1]);
         }
         Sixteen<G>::store(static_cast<char *>(a.out) + t * a.ld * G::kBytes, c, a.kept.cols, h.wide, f);
     }
@@ -419,7 +442,7 @@ __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_pack_loose_kerne
             const int s = scale_byte(largest);
             if (32 * q < left_code) codes[32 * q] = s == 255 ? 0 : static_cast<int8_t>(code_bits(x[q], scale_inverse(s)) & 0xffu);
             if (lane == 0) scales[q / 4 * 4 * a.kept.tall + q % 4] = static_cast<uint8_t>(s);
-            if (a.act_out && 32 * q < left) store_value<G>(out, 32 * q, activation<ACT>(x[q]));
+            if (a.act_out && 32 * q < left) store_value<G>(out, 32 * q, activation<ACT, G::kBytes == 4>(x[q]));
         }
     }
 }
@@ -449,7 +472,7 @@ __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_read_loose_kerne
 #pragma unroll
         for (int q = 0; q < kLoose; ++q) {
             const float x = __fmul_rn(static_cast<float>(code[q]), scale[q]);
-            if (32 * q < left) store_value<G>(out, 32 * q, BACKWARD ? __fmul_rn(dy[q], activation_slope<ACT>(x)) : activation<ACT>(x));
+            if (32 * q < left) store_value<G>(out, 32 * q, BACKWARD ? __fmul_rn(dy[q], activation_slope<ACT, G::kBytes == 4>(x)) : activation<ACT, G::kBytes == 4>(x));
         }
     }
 }
