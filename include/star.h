@@ -490,7 +490,9 @@ STAR_API star_status_t star_group_update_host_ex(float *h_params, float *h_momen
  * that share one phase modulo 16 bytes and whose stride keeps it are the fast
  * case.  Sizes of zero are successful no-ops (sums and losses are still
  * written: zero).  Written buffers must not overlap any other buffer of the
- * call, except where an in-place form is named.  All sums, softmax statistics
+ * call, except where an in-place form is named; matrices with one stride may lie
+ * side by side in the rows of one buffer, those with different strides may not.
+ * All sums, softmax statistics
  * and activation values are held in binary32; results are rounded once.  The
  * same call on the same inputs gives the same bits.
  * ------------------------------------------------------------------------- */

@@ -61,20 +61,30 @@ inline bool is_dtype(int dt) { return dt == STAR_DTYPE_F32 || dt == STAR_DTYPE_B
 inline int dtype_size(int dt) { return dt == STAR_DTYPE_BF16 ? 2 : 4; }
 
 // A device buffer of an argument list: where it starts and how many bytes of
-// address space it spans.
+// address space it spans; of a matrix of several rows, also how far apart they
+// are and how many bytes of each are its own.
 struct Extent {
     uintptr_t begin = 0;
     uint64_t bytes = 0;
+    uint64_t pitch = 0, width = 0;       // 0: one run of bytes
 };
 
+// Whether two buffers share memory.  Matrices with the same stride may lie side by
+// side in the rows of one buffer: then their columns decide.  With different strides
+// their address ranges do.
 inline bool overlap(const Extent &a, const Extent &b)
 {
-    return a.bytes && b.bytes && a.begin < b.begin + b.bytes && b.begin < a.begin + a.bytes;
+    if (!a.bytes || !b.bytes || a.begin >= b.begin + b.bytes || b.begin >= a.begin + a.bytes) return false;
+    const uint64_t pitch = a.pitch ? a.pitch : b.pitch;
+    if (!pitch || (a.pitch && b.pitch && a.pitch != b.pitch)) return true;
+    // Where b's rows start in a's, going round from row to row.
+    const uint64_t at = b.begin >= a.begin ? (b.begin - a.begin) % pitch : (pitch - (a.begin - b.begin) % pitch) % pitch;
+    return at < (a.pitch ? a.width : a.bytes) || at + (b.pitch ? b.width : b.bytes) > pitch;
 }
 
 inline Extent extent(const void *p, uint64_t bytes)
 {
-    return p ? Extent{reinterpret_cast<uintptr_t>(p), bytes} : Extent{};
+    return p ? Extent{reinterpret_cast<uintptr_t>(p), bytes, 0, 0} : Extent{};
 }
 
 // Largest byte count a matrix argument may span: far beyond any device's
@@ -95,6 +105,10 @@ inline star_status_t check_matrix(const void *p, int64_t rows, int64_t cols, int
         return STAR_ERR_INVALID_ARG;
     *out = extent(p, (static_cast<uint64_t>(rows - 1) * static_cast<uint64_t>(ld) + static_cast<uint64_t>(cols)) *
                          static_cast<unsigned>(size));
+    if (rows > 1) {
+        out->pitch = static_cast<uint64_t>(ld) * static_cast<unsigned>(size);
+        out->width = static_cast<uint64_t>(cols) * static_cast<unsigned>(size);
+    }
     return STAR_OK;
 }
 
