@@ -51,21 +51,36 @@ class Worker:
     def __init__(self, rows: int, d: int, f: int, vocab: int, device="cuda"):
         self.rows, self.d, self.f, self.vocab = rows, d, f, vocab
         self.grad = HeadWeights(torch.zeros(HeadWeights.size(d, f, vocab), dtype=torch.bfloat16, device=device), d, f, vocab)
-        self.kept = {name: B.star_checkpoint_empty(rows, width, device)
-                     for name, width in (("x", d), ("u", f), ("h", f), ("y", d))}
+        self.widths = {"x": d, "u": f, "h": f, "y": d}
+        self.store = {name: B.star_checkpoint_empty(rows, width, device) for name, width in self.widths.items()}
+        self.kept = self.checkpoints(rows)
         self.h = torch.empty((rows, f), dtype=torch.bfloat16, device=device)
         self.logp = torch.empty(rows, device=device)
         self.token_loss = torch.empty(rows, device=device)
         self.sums = torch.empty(4, device=device)
         self.workspace = torch.empty(B.star_loss_workspace_bytes(rows, rows), dtype=torch.uint8, device=device)
 
+    def checkpoints(self, rows: int) -> Dict[str, Tuple[torch.Tensor, torch.Tensor]]:
+        """Codes and scales of a step of ``rows`` tokens: the front of the buffers, laid out for that number."""
+        kept = {}
+        for name, (codes, scales) in self.store.items():
+            pitch, code_bytes, scale_bytes = B.star_checkpoint_sizes(rows, self.widths[name])
+            kept[name] = (codes.view(-1)[:code_bytes].view(rows, pitch),
+                          scales.view(-1)[:scale_bytes].view(scales.shape[0], -1, 4))
+        return kept
+
     def forward(self, x: torch.Tensor, weights: HeadWeights) -> torch.Tensor:
-        """Logits of the embeddings x (rows x d, bf16); what the backward pass needs is kept in 8 bits."""
+        """Logits of the embeddings x (up to rows x d, bf16); what the backward pass needs is kept in 8 bits."""
+        rows = x.shape[0]
+        if rows > self.rows:
+            raise ValueError("a step of %d tokens, the worker's buffers hold %d" % (rows, self.rows))
+        self.kept = self.checkpoints(rows)
+        h = self.h[:rows]
         B.star_checkpoint_pack(*self.kept["x"], x)
         u = x @ weights.w1.t()
-        B.star_checkpoint_pack(*self.kept["u"], u, act="gelu_tanh", act_out=self.h)
-        B.star_checkpoint_pack(*self.kept["h"], self.h)
-        y = torch.addmm(x, self.h, weights.w2.t())
+        B.star_checkpoint_pack(*self.kept["u"], u, act="gelu_tanh", act_out=h)
+        B.star_checkpoint_pack(*self.kept["h"], h)
+        y = torch.addmm(x, h, weights.w2.t())
         B.star_checkpoint_pack(*self.kept["y"], y)
         return y @ weights.w3.t()
 
@@ -83,7 +98,8 @@ class Worker:
                     token_weights: Optional[torch.Tensor] = None, kl_coef: float = 0.0) -> torch.Tensor:
         """One step of the policy loss; returns its four sums."""
         logits = self.forward(x, weights)
-        B.star_policy_loss(logits, labels, advantages, self.logp, self.token_loss, self.sums, self.workspace,
+        rows = x.shape[0]
+        B.star_policy_loss(logits, labels, advantages, self.logp[:rows], self.token_loss[:rows], self.sums, self.workspace,
                            dlogits=logits, weights=token_weights, old_logp=old_logp, ref_logp=ref_logp, kl_coef=kl_coef)
         self.backward(logits, weights)
         return self.sums
@@ -96,7 +112,7 @@ class Worker:
                "margin": torch.empty(pairs, device=x.device), "loss": torch.empty(1, device=x.device)}
         logits = self.forward(x, weights)
         B.star_preference_loss(logits, labels, seq_offsets, out["seq_logp"], out["pair_loss"], out["margin"], out["loss"],
-                               self.workspace, dlogits=logits, ref_logp=ref_seq_logp, beta=beta, loss_scale=1.0 / pairs)
+                               self.workspace, dlogits=logits, ref_logp=ref_seq_logp, beta=beta, loss_scale=1.0 / max(pairs, 1))
         self.backward(logits, weights)
         return out
 
