@@ -526,13 +526,15 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
         barrier_init(drained, kBlocks * kConvertWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    // Taking TMEM waits without limit for whoever holds it, so a block that waits for the
+    // kernel in front must not hold any that that kernel may still ask for.
+    wait_for_primary();
     if (warp == 2) tensor_alloc<kTmem, PAIR>(smem_address(tmem_at));
     tensor_fence_before();
     __syncthreads();
     if constexpr (PAIR) cluster_sync();                          // the other block's barriers are ready
     tensor_fence_after();
     const uint32_t tmem = *tmem_at;
-    wait_for_primary();
 
     const int64_t c0 = static_cast<int64_t>(blockIdx.x) * kTileC, o0 = static_cast<int64_t>(blockIdx.y) * BN;
     const int parts = static_cast<int>(gridDim.z), part = static_cast<int>(blockIdx.z);
