@@ -195,8 +195,12 @@ template <size_t N> Plan choose(const Device &d, const Candidate (&candidates)[N
     return best;
 }
 
-constexpr Candidate kPlain[4] = {
-    {kWide, 2, 512, 0.73, 17.0, 0}, {kNarrow, 2, 256, 0.56, 12.0, 0}, {kSingle, 1, 256, 0.56, 12.0, 0}, {kSmall, 1, 128, 0.52, 10.0, 0}};
+// One accumulator over at most 16384 rows: it cuts 4.1e-5 of a sum of one sign, a hundredth of what
+// a bf16 result is rounded by (65536 rows 2.7e-4).  More go by a running sum.
+constexpr int kLongSteps = 16384 / kTileT;
+constexpr Candidate kPlain[6] = {{kWide, 2, 512, 0.73, 17.0, kLongSteps},   {kNarrow, 2, 256, 0.56, 12.0, kLongSteps},
+                                 {kSingle, 1, 256, 0.56, 12.0, kLongSteps}, {kSmall, 1, 128, 0.52, 10.0, kLongSteps},
+                                 {kNarrowSum, 2, 256, 0.76, 12.0, 0},       {kSingleSum, 1, 256, 0.76, 12.0, 0}};
 // A dw in fp32 takes the same shapes as long as no part is longer than a run of the running sum.
 constexpr Candidate kSummed[6] = {{kNarrowSum, 2, 256, 0.76, 12.0, 0},          {kSingleSum, 1, 256, 0.76, 12.0, 0},
                                   {kWide, 2, 512, 0.73, 17.0, kFlushSteps},     {kNarrow, 2, 256, 0.56, 12.0, kFlushSteps},
