@@ -15,12 +15,16 @@
 //
 // Precision.  Products are exact.  A dy in fp32 is cut into three bf16 terms of 8
 // bits each, which together are it, and multiplied three times.  The tensor
-// cores' binary32 additions cut instead of rounding: after n rows the sum is off
-// by about n 4e-10 of itself towards zero (16384 rows: 7e-6; measured).  For a dw
-// in bf16 that is far below its own rounding; for a dw in fp32 the accumulator is
-// added to a running sum, with rounding, every 2048 rows (FLUSH): 4e-7.  The lower
-// terms of an fp32 dy have an accumulator of their own: beside sums 2^8 and 2^16
-// times their size most of their bits would be cut (6e-6 in one accumulator).
+// cores' binary32 additions cut instead of rounding: a sum of one sign in one
+// accumulator is off towards zero by 2.3e-6 of itself after 2048 rows, 1.7e-5 after 8192,
+// 4.1e-5 after 16384 and 2.7e-4 after 65536, one of random signs by 4.8e-7 after 2048
+// (measured).  For a dw in bf16 that stays far below its own rounding up to the 16384
+// rows that go into one; for a dw in fp32 the accumulator is added to a running sum, with
+// rounding, every 1280 rows (FLUSH): 1.2e-6 and 2.8e-7 for any number of rows, where a binary32
+// product on the ordinary units has 1.9e-6 and 5.4e-7 after 16384.  Every 2048 rows would be
+// 2.3e-6 and 4.8e-7 and 0 to 5 % faster.  The lower terms of an fp32 dy have an accumulator of
+// their own, beside sums 2^8 and 2^16 times their size most of their bits would be cut: 1.5e-6 and
+// 3.6e-7.
 #pragma once
 
 #include <cuda.h>
@@ -484,7 +488,7 @@ __device__ __forceinline__ void store_four(const WeightGradArgs &a, bool bf16, b
 // products.  In a pair that is 80 KB.
 // FLUSH: the accumulator is added to a running sum beside it in TMEM every
 // kFlushSteps steps.
-constexpr int kFlushSteps = 32;
+constexpr int kFlushSteps = 20;
 
 template <int BN, int LOADS, int WIDE, bool PAIR, int TERMS, bool FLUSH>
 __global__ void __launch_bounds__(kGradThreads, 1)
