@@ -486,8 +486,8 @@ __device__ __forceinline__ void store_four(const WeightGradArgs &a, bool bf16, b
 // the matrix instructions read 48 KB, the copies write 40 KB and the widening
 // moves 24 KB, 112 KB where 128 B a cycle give 64 KB in the 512 cycles of the
 // products.  In a pair that is 80 KB.
-// FLUSH: the accumulator is added to a running sum beside it in TMEM every
-// kFlushSteps steps.
+// FLUSH: the accumulator, and that of the lower terms, is added to a running sum beside
+// it in TMEM every kFlushSteps steps.
 constexpr int kFlushSteps = 20;
 
 template <int BN, int LOADS, int WIDE, bool PAIR, int TERMS, bool FLUSH>
@@ -592,7 +592,7 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
                         for (int term = 0; term < (TERMS == 0 ? 1 : TERMS); ++term)
                             matrix_multiply<PAIR>(tmem + n * S::kN + (term > 0 ? kLower : 0), operand_descriptor(as + q * 2048),
                                                   operand_descriptor(bs + term * S::kB + n * (S::kRun * kTileT * 2) + q * 2048), idesc,
-                                                  (term > 0 ? i : in_run) > 0 || q > 0 || term > 1);
+                                                  in_run > 0 || q > 0 || term > 1);
                 matrix_commit<PAIR>(used(i), mask);
                 if (FLUSH && in_run == kFlushSteps - 1 && k + 1 < last) matrix_commit<PAIR>(summed, mask);
             }
@@ -618,6 +618,12 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
                 const uint32_t at = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + col;
                 float x[32];
                 load_accumulator(at, x);
+                if constexpr (TERMS == 3) {
+                    float lower[32];
+                    load_accumulator(at + kLower, lower);
+#pragma unroll
+                    for (int r = 0; r < 32; ++r) x[r] = __fadd_rn(x[r], lower[r]);
+                }
                 if (run > 0) {
                     float sum[32];
                     load_accumulator(at + BN, sum);

@@ -1,6 +1,8 @@
-"""A weight gradient in bf16 over more rows than one accumulator may take."""
+"""Weight gradients over more rows than one accumulator may take."""
 import pytest
 import torch
+
+from tests import worker_step_reference as R
 
 pytestmark = pytest.mark.gpu
 
@@ -34,3 +36,22 @@ def test_a_bf16_result_over_a_million_rows_is_not_biased(B):
     error = (dw.double() - want) / want
     assert float(error.abs().max()) <= 2.0 ** -8
     assert abs(float(error.mean())) <= 3e-5
+
+
+def test_the_lower_terms_of_an_fp32_gradient_over_millions_of_rows(B):
+    """The bound of some thousands of rows, 2e-6 (test_gpu_weight_grad_long_sums.py): the 240 runs of a part are
+    added with rounding, 2e-7 as they come.  One accumulator for the lower terms of all 300000 rows of a part
+    loses about 2e-3 of sums that are 2^-9 of the whole, 4e-6."""
+    T, C, O = 2_400_000, 128, 128
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn((T, C), generator=g, device="cuda").abs_()
+    dy = torch.randn((T, O), generator=g, device="cuda").abs_()
+    codes, scales = B.star_checkpoint_empty(T, C)
+    B.star_checkpoint_pack(codes, scales, x)
+    B.star_checkpoint_unpack(x, codes, scales)
+    want = torch.zeros((O, C), dtype=torch.float64, device="cuda")
+    for a in range(0, T, 100_000):
+        want += dy[a: a + 100_000].double().t() @ x[a: a + 100_000].double()
+    dw = torch.empty((O, C), device="cuda")
+    B.star_checkpoint_weight_grad(dw, dy, codes, scales)
+    assert R.rel(dw, want) <= 2e-6
