@@ -211,15 +211,24 @@ constexpr Candidate kSummed[6] = {{kNarrowSum, 2, 256, 0.76, 12.0, 0},          
 constexpr Candidate kLooseDy[2] = {{kLoosePair, 2, 128, 0.9, 10.0, 0}, {kLooseSingle, 1, 128, 0.9, 10.0, 0}};
 constexpr Candidate kCutDy[2] = {{kCutPair, 2, 128, 1.0, 10.0, 0}, {kCutSingle, 1, 128, 1.2, 10.0, 0}};
 
-// Few rows on the ordinary units, where that takes less than the tensor cores'
-// `us`: waves of tiles, two to an SM, each of 2 us and 0.25 us a row.  4096 x 4096,
-// here / tensor cores: bf16 1 row 11.1 / 18.7 us, 8 rows 19.5 / 18.7, 16 rows 26 / 18;
-// dy and dw in fp32 1 row 15.8 / 50, 16 rows 31 / 50, 64 rows 88 / 50.
-bool few_rows(int64_t rows, int64_t cols, int64_t outs, bool transposed, double us)
+// Few rows on the ordinary units, where that takes less than the tensor cores.  Here: waves
+// of tiles, two to an SM, each of 2 us and 0.25 us a row (0.3 transposed).  There: `us`, as chosen
+// above, or, where few steps leave the time to the stores, 5 us and 0.8 us a million results in
+// bf16 (0.9), 1.1 in fp32 (1.3), 2.9 from a dy in fp32 (narrower tiles).  Here / tensor cores, us:
+//                        1 row         2         4         8        16        32
+//   bf16 4096 x 4096  10.2/18.7 12.2/19.0 15.4/18.7 18.1/18.6 22.5/18.2 38.3/18.1
+//   bf16 1024 x 4096   4.4/7.9   4.9/8.1   6.2/8.0   6.3/8.0   8.1/7.9  12.8/7.9
+//   bf16 1024 x 1024   2.6/5.1   3.1/5.3   3.6/5.1   3.7/5.1   4.7/5.1   7.3/5.0
+//   dw in fp32, 4096 x 4096      14.7/24.2 16.3/24.0 19.7/24.1 22.1/24.0 27.4/23.6 42.6/23.6
+//   dy and dw in fp32, the same  14.5/52.3 16.2/52.4 19.5/52.5 21.8/52.6 27.2/52.8 42.4/53.9
+bool few_rows(int64_t rows, int64_t cols, int64_t outs, bool transposed, bool y16, bool w16, double us)
 {
     const int64_t inner = transposed ? outs : cols, outer = transposed ? cols : outs;
     const int64_t tiles = ((inner + kFewInner - 1) / kFewInner) * ((outer + kFewOuter - 1) / kFewOuter);
-    return 2.0 + static_cast<double>((tiles + 295) / 296) * (2.0 + 0.25 * static_cast<double>(rows)) < us;
+    const double millions = static_cast<double>(cols) * static_cast<double>(outs) * 1e-6;
+    const double stores = 5.0 + millions * (!y16 ? 2.9 : w16 ? (transposed ? 0.9 : 0.8) : (transposed ? 1.3 : 1.1));
+    const double row = transposed ? 0.3 : 0.25;
+    return 2.0 + static_cast<double>((tiles + 295) / 296) * (2.0 + row * static_cast<double>(rows)) < std::max(us, stores);
 }
 
 template <typename GY, typename GW> star_status_t launch_few(const WeightGradArgs &a, bool transposed, cudaStream_t stream)
@@ -271,7 +280,7 @@ extern "C" star_status_t star_checkpoint_weight_grad(void *dw, star_dtype_t dw_d
                       : !tiled ? choose(*device, kLooseDy, cols, outs, steps)
                       : w16    ? choose(*device, kPlain, cols, outs, steps)
                                : choose(*device, kSummed, cols, outs, steps);
-    if (rows == 0 || (few_rows(rows, cols, outs, transposed != 0, plan.us))) {
+    if (rows == 0 || few_rows(rows, cols, outs, transposed != 0, y16, w16, plan.us)) {
         if (y16) return w16 ? launch_few<GradBF16, GradBF16>(a, transposed != 0, stream) : launch_few<GradBF16, GradF32>(a, transposed != 0, stream);
         return w16 ? launch_few<GradF32, GradBF16>(a, transposed != 0, stream) : launch_few<GradF32, GradF32>(a, transposed != 0, stream);
     }
