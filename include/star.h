@@ -531,7 +531,9 @@ STAR_API star_status_t star_loss_workspace_bytes(int64_t rows, int64_t sequences
  * A factor of exactly 0 (A, kl_coef) takes its term out, however large the other one.
  * dlogits is the gradient of sums[0]; the caller puts the mean's 1 / n (per
  * token or per sequence) and any loss scale into weights.
- *   old_logp NULL differentiates the ratio as if old_logp were logp itself.
+ *   old_logp NULL differentiates the ratio as if old_logp were logp itself.  So with
+ *               advantages of 1 and no ref_logp dlogits is the gradient of the weighted
+ *               cross-entropy, -sum w logp, whose terms are in logp
  *   dlogits   : rows x vocab of dtype with stride ld_dlogits, or NULL for the
  *               forward pass alone; may be the logits themselves (same pointer
  *               and stride), which are then replaced by their gradient

@@ -202,6 +202,7 @@ __device__ __forceinline__ void finish_row(const RowWork &a, int64_t t, const Ro
     if (KEEPS && a.kept) a.kept[t] = RowKept{row.m, f.active ? __fdiv_rn(1.0f, row.s) : 0.0f, lp, r.coef};
 }
 
+// A block's sums, rounded to binary32 once; they are added in binary64 again.
 template <bool POLICY> __device__ __forceinline__ void store_partial(const RowWork &a, int64_t at, const RowSums &sums)
 {
     if constexpr (POLICY)

@@ -50,25 +50,26 @@ bool make_map(CUtensorMap *map, CUtensorMapDataType type, const void *base, int6
 // The kernel's shapes.  Shared memory and TMEM hold one block on an SM in all of
 // them.
 //   kWide      a pair of blocks, 256 columns x 512 outputs: a widened code serves
-//              512 outputs, 0.73 us a step of 64 rows (1.47 PFLOP/s over 148 SMs)
+//              512 outputs, 0.73 us a step of 64 rows (23 TFLOP/s a pair)
 //   kNarrow    a pair, 256 x 256: 0.56 us, bound by the widening
 //   kSingle    a block, 128 x 256: 0.56 us
 //   kSmall     a block, 128 x 128, for few rows and few tiles
-//   kNarrowSum, kSingleSum      with a running sum, for a dw in fp32
+//   kNarrowSum, kSingleSum      with a running sum, for a dw in fp32 and for many rows
 //   kLoosePair, kLooseSingle    dy in bf16 off the 16-byte grid: 256 x 128 by a
 //              pair, 128 x 128 by a block
 //   kCutPair, kCutSingle        dy in fp32, three terms: the same
-// Each in its best number of parts, us (bf16; rows, columns -> outputs):
+// Each in its best number of parts, us, in bursts of 20 launches (bf16; rows, columns ->
+// outputs; launched without a pause the first takes 128, under the power cap):
 //                          kWide  kNarrow  kSingle  kSmall
-//   16384, 1024 -> 4096    110    149      150      288
-//    8192, 4096 -> 4096    203    363      313      505
-//    8192, 1024 -> 1024     39     34       29       42
-//     515, 1024 -> 1024     14.7   11.8     11.1     10.1
-//     100,  256 ->  256     10.1    7.5      6.8      5.7
-// dw in fp32, kNarrowSum 193 and kSingleSum 193 for the first, kSingleSum 34 for
-// the third (kSingle in parts within a run of the sum: 29).  By pair / by block:
-// loose dy 395 / 514 for the first, 56 / 71 for the third, 14.0 / 12.0 for 2048,
-// 128 -> 1024; fp32 dy 567 / 684, 77 / 92 and 17.6 / 15.8.
+//   16384, 1024 -> 4096    107    148      142      273
+//    8192, 4096 -> 4096    199    302      292      490
+//    8192, 1024 -> 1024     38     34       28       41
+//     515, 1024 -> 1024     14.8   11.9     10.7      9.7
+//     100,  256 ->  256     10.3    7.5      6.5      5.5
+// dw in fp32, kNarrowSum 202 and kSingleSum 203 for the first, 43 and 35 for the
+// third (kSingle in parts of 2048 rows: 28.5).  By pair / by block: loose dy 407 / 539
+// for the first, 58 / 75 for the third, 13.9 / 12.1 for 2048, 128 -> 1024; fp32 dy 580 / 731,
+// 80 / 99 and 17.3 / 15.7.
 enum Shape { kWide, kNarrow, kSingle, kSmall, kNarrowSum, kSingleSum, kLoosePair, kLooseSingle, kCutPair, kCutSingle, kShapes };
 constexpr int kMostParts = 8;
 
@@ -164,7 +165,7 @@ star_status_t launch_shape(const WeightGradTile &tile, const CUtensorMap &codes,
 // Measured (us; 8 to 256 steps, 128 to 4096 columns): the rest beside the steps
 // takes 5 and, split, 17 with 512 outputs and 12 with 256 or fewer (accumulators
 // through distributed shared memory).  16384 rows, 1024 -> 4096: kWide in 2 parts
-// 110 us, in 1 part 185.  8192 rows, 1024 -> 1024: kSingle in 4 parts 29 us, in 1
+// 107 us, in 1 part 185.  8192 rows, 1024 -> 1024: kSingle in 4 parts 29 us, in 1
 // part 75.
 struct Plan {
     Shape shape;

@@ -786,7 +786,7 @@ star_weight_grad_tensor_kernel(const __grid_constant__ WeightGradTile p, const _
 // on the ordinary units: a block makes 64 x 256 results, a thread 8 x 8 of them,
 // rows 32 at a time in shared memory.  The result's inner index, along which dw
 // is stored, runs over the lanes: columns, or outputs where dw is transposed.
-// 4096 x 4096 from 1 row: bf16 10 us (3.4 TB/s), fp32 13 (5.0 TB/s); added to 12.7 and 16.1.
+// 4096 x 4096 from 1 row: bf16 10 us (3.3 TB/s), fp32 14.5 (4.6 TB/s); added to 12.7 and 16.1.
 // ---------------------------------------------------------------------------
 constexpr int kFewRows = 32, kFewOuter = 64, kFewInner = 256, kFewThreads = 256;
 
