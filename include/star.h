@@ -575,6 +575,88 @@ STAR_API star_status_t star_preference_loss(const void *logits, star_dtype_t dty
                                             void *dlogits, int64_t ld_dlogits, void *workspace,
                                             size_t workspace_bytes, void *cuda_stream);
 
+/* Log-probabilities with entropy and the k largest logits of every row: what a
+ * teacher's record holds, and what a server answers with.
+ *     logp    = z[label] - lse                        (labels given)
+ *     entropy = lse - sum_j p[j] z[j]
+ *     top_ids[t][0 .. k), top_logp[t][0 .. k) : the k largest logits' ids and their
+ *               log-probabilities, descending; equal logits by ascending id (+0 and -0
+ *               are equal).  A logit of -inf is none of them: where a row has fewer,
+ *               the remaining entries have id -1 and log-probability -inf
+ *   labels  : as above, or NULL: every row takes part, and logp is NULL too
+ *   logp, lse, entropy : rows entries each, or NULL
+ *   top_ids, top_logp  : rows x k with row stride ld_top; may be NULL where k is 0
+ * A row whose label is outside [0, vocab), or whose logits are all -inf, is inactive:
+ * lse = -inf (unlike star_token_logprobs; the backward pass goes by it), logp =
+ * entropy = 0, no alternatives.  A row with a NaN or +inf logit has ids of -1, the
+ * rest is NaN.  k from 0 to STAR_MAX_ALTERNATIVES (STAR_ERR_UNSUPPORTED beyond).
+ * One kernel launch. */
+#define STAR_MAX_ALTERNATIVES 128
+STAR_API star_status_t star_token_alternatives(const void *logits, star_dtype_t dtype, int64_t rows,
+                                               int64_t vocab, int64_t ld, const int64_t *labels,
+                                               float temperature, int k, int32_t *top_ids, float *top_logp,
+                                               int64_t ld_top, float *logp, float *lse, float *entropy,
+                                               void *cuda_stream);
+
+/* Its backward pass: the gradient of the logits from the gradients of its results
+ * (an entropy bonus, a loss on the alternatives), with the results' lse and entropy:
+ *     dlogits[t][j] = 1 / temperature * (d_logp (j == label) + sum_i d_top[i] (j == top_ids[i])
+ *                     - p[j] (d_logp + sum_i d_top[i] + d_entropy (log p[j] + entropy)))
+ *   lse     : rows entries; a row of -inf (and, with labels, one whose label is out
+ *             of range) has a zero gradient, and its logits are not read
+ *   entropy : rows entries; NULL only without d_entropy
+ *   d_logp  : or NULL; needs labels.   d_entropy : or NULL
+ *   top_ids, d_top_logp : rows x k, strides ld_top and ld_d_top; ids outside [0, vocab)
+ *             are passed over with their gradients; an id may come twice
+ *   dlogits : rows x vocab of dtype, stride ld_dlogits; may be the logits themselves
+ * One kernel launch. */
+STAR_API star_status_t star_token_alternatives_backward(void *dlogits, int64_t ld_dlogits, const void *logits,
+                                                        star_dtype_t dtype, int64_t rows, int64_t vocab,
+                                                        int64_t ld, const int64_t *labels, float temperature,
+                                                        const float *lse, const float *entropy,
+                                                        const float *d_logp, const float *d_entropy, int k,
+                                                        const int32_t *top_ids, int64_t ld_top,
+                                                        const float *d_top_logp, int64_t ld_d_top,
+                                                        void *cuda_stream);
+
+/* Distillation from a teacher's top logits, forward and backward in one pass over
+ * the student's logits.  The teacher is k ids and values a row.  With
+ * v = values / teacher_temperature, p the student's softmax at `temperature` over the
+ * whole vocabulary:
+ *     rest == 0:  q[i] = exp(v[i]) / sum_i exp(v[i])           the list is all there is
+ *     rest != 0:  q[i] = exp(v[i]),  q0 = max(0, 1 - sum_i q[i])   the values are
+ *                 log-probabilities (star_token_alternatives' at the same temperature);
+ *                 what they leave is held against p0, the student's probability of
+ *                 everything that is not listed
+ *     kl = sum_i q[i] log(q[i] / p[ids[i]])  (+ q0 log(q0 / p0))
+ *     ce = -log softmax(x)[label]            at temperature 1; 0 where label_coef is 0
+ *     token_loss[t] = soft_coef kl + label_coef ce
+ *     sums = { sum w token_loss, sum w kl, sum w ce, sum w }      over the active rows
+ * and dlogits is the gradient of sums[0] (no factor of temperature^2 is put in).
+ * Ids outside [0, vocab) are entries that are not there (a record's -1); a value of
+ * -inf is a probability of 0; an id that is listed twice has the sum of its q.  Where
+ * the student's rest has no logit but -inf, the term in q0 is left out.  A coefficient
+ * of exactly 0 takes its term out.
+ *   labels  : NULL only where label_coef is 0.  A row is active iff its label, where
+ *             labels are given, lies in [0, vocab), its weight is not 0 (1 without
+ *             weights) and not every logit is -inf; the others have token_loss 0 and a
+ *             zero gradient, and their logits and lists are not read
+ *   teacher_ids, teacher_values : rows x k, strides ld_ids and ld_values
+ *   dlogits : as for the policy loss (NULL: forward alone; may be the logits)
+ *   token_loss : rows entries;  sums : 4 entries
+ *   workspace : device, 16-byte aligned, star_loss_workspace_bytes(rows, 0) bytes
+ * Coefficients and temperatures finite, the latter > 0.  k up to STAR_MAX_ALTERNATIVES,
+ * rows of logits up to 1.6 MiB (851968 of bf16, 425984 of fp32): STAR_ERR_UNSUPPORTED
+ * beyond.  Two kernel launches.  It waits inside its kernel as the policy loss does. */
+STAR_API star_status_t star_distillation_loss(const void *logits, star_dtype_t dtype, int64_t rows,
+                                              int64_t vocab, int64_t ld, const int32_t *teacher_ids,
+                                              int64_t ld_ids, const float *teacher_values, int64_t ld_values,
+                                              int k, int rest, float teacher_temperature,
+                                              const int64_t *labels, const float *weights, float temperature,
+                                              float soft_coef, float label_coef, float *token_loss, float *sums,
+                                              void *dlogits, int64_t ld_dlogits, void *workspace,
+                                              size_t workspace_bytes, void *cuda_stream);
+
 /* Activations kept in 8 bits.  A checkpoint of x (rows x cols) holds, for every
  * block of 32 consecutive columns of a row (the last block of a row may be
  * shorter), a scale 2^e and a code per element,
@@ -645,11 +727,55 @@ STAR_API star_status_t star_checkpoint_weight_grad(void *dw, star_dtype_t dw_dty
                                                    int64_t cols, int64_t outs, int accumulate,
                                                    void *cuda_stream);
 
-/* The policy loss and the weight gradient wait inside their kernels for copies
- * that they have started.  Every such wait is bounded; one that runs out (a third
+/* Root-mean-square norm of a residual stream, with the residual's addition, and its
+ * result kept in 8 bits in the same pass.  Per row
+ *     total = x + residual            rounded to dtype (x itself without residual)
+ *     rstd  = 1 / sqrt(mean(total^2) + eps)
+ *     y     = total * rstd * gain     rounded to dtype (gain NULL: 1)
+ *     codes, scales : the checkpoint that star_checkpoint_pack makes of y
+ *   total  : rows x cols, or NULL; may be x or the residual (same pointer and stride)
+ *   rstd   : rows entries, or NULL;  codes, scales : both or neither (NULL)
+ *   gain   : cols entries of gain_dtype
+ * Sums and rstd are binary32.  A row whose squares' sum is not finite in binary32 is
+ * NaN throughout.  eps finite, > 0.  One kernel launch. */
+STAR_API star_status_t star_rms_norm(void *y, int64_t ld_y, const void *x, int64_t ld_x, const void *residual,
+                                     int64_t ld_residual, void *total, int64_t ld_total, star_dtype_t dtype,
+                                     int64_t rows, int64_t cols, const void *gain, star_dtype_t gain_dtype,
+                                     float eps, float *rstd, int8_t *codes, uint8_t *scales,
+                                     void *cuda_stream);
+
+/* Device workspace of the backward pass, where the gain's gradient is wanted.  Need
+ * not be initialized. */
+STAR_API star_status_t star_rms_norm_workspace_bytes(int64_t rows, int64_t cols, size_t *bytes_out);
+
+/* Its backward pass.  With n = total * rstd:
+ *     dx = d_total + rstd (gain dy - n mean(gain dy n))
+ *     dgain[c] = sum_t dy n           (+ dgain[c] before, if accumulate != 0)
+ *   total  : the stream as star_rms_norm normalized it (rows x cols of dtype), or NULL
+ *            and codes, scales instead: a checkpoint of it (star_checkpoint_pack)
+ *   rstd   : of the forward pass
+ *   d_total: what reaches the stream past the norm, or NULL
+ *   dx     : the gradient of x and of the residual; may be dy or d_total (same pointer
+ *            and stride)
+ *   dgain  : cols entries of dgain_dtype, or NULL; usually in the worker's gradient
+ *            buffer.  rows == 0 gives zeros (or leaves it, when accumulating)
+ *   workspace : star_rms_norm_workspace_bytes(rows, cols) bytes, 16-byte aligned; may be
+ *            NULL without dgain
+ * Both calls take up to 2^31 - 65 columns and 2^31 - 1 rows (STAR_ERR_UNSUPPORTED
+ * beyond).  Two kernel launches, one without dgain. */
+STAR_API star_status_t star_rms_norm_backward(void *dx, int64_t ld_dx, void *dgain, star_dtype_t dgain_dtype,
+                                              int accumulate, const void *dy, int64_t ld_dy, const void *total,
+                                              int64_t ld_total, const int8_t *codes, const uint8_t *scales,
+                                              const void *d_total, int64_t ld_d_total, star_dtype_t dtype,
+                                              int64_t rows, int64_t cols, const void *gain,
+                                              star_dtype_t gain_dtype, const float *rstd, void *workspace,
+                                              size_t workspace_bytes, void *cuda_stream);
+
+/* The policy loss, the distillation loss and the weight gradient wait inside their
+ * kernels for copies that they have started.  Every such wait is bounded; one that runs out (a third
  * of a second at the earliest, as long as the hardware holds its attempts at the
  * latest; a fault of the device or its memory) ends the kernel without a valid
- * result: the policy loss's sums are NaN.  star_check_waits waits for cuda_stream
+ * result: the sums of the policy and the distillation loss are NaN.  star_check_waits waits for cuda_stream
  * and says whether that has happened on the current device since the last check:
  * STAR_ERR_TIMEOUT, or STAR_OK.  Not inside a stream capture. */
 STAR_API star_status_t star_check_waits(void *cuda_stream);

@@ -150,6 +150,22 @@ def _load() -> ctypes.CDLL:
     lib.star_preference_loss.argtypes = ([c_vp, c_int, c_i64, c_i64, c_i64, c_vp, c_vp, c_i64, c_vp, c_f, c_f, c_f, c_int,
                                           c_f] + [c_vp] * 5 + [c_i64, c_vp, ctypes.c_size_t, c_vp])
     lib.star_preference_loss.restype = c_int
+    lib.star_token_alternatives.argtypes = [c_vp, c_int, c_i64, c_i64, c_i64, c_vp, c_f, c_int, c_vp, c_vp, c_i64, c_vp, c_vp, c_vp,
+                                            c_vp]
+    lib.star_token_alternatives.restype = c_int
+    lib.star_token_alternatives_backward.argtypes = ([c_vp, c_i64, c_vp, c_int, c_i64, c_i64, c_i64, c_vp, c_f] + [c_vp] * 4
+                                                     + [c_int, c_vp, c_i64, c_vp, c_i64, c_vp])
+    lib.star_token_alternatives_backward.restype = c_int
+    lib.star_distillation_loss.argtypes = ([c_vp, c_int, c_i64, c_i64, c_i64, c_vp, c_i64, c_vp, c_i64, c_int, c_int, c_f, c_vp, c_vp,
+                                            c_f, c_f, c_f, c_vp, c_vp, c_vp, c_i64, c_vp, ctypes.c_size_t, c_vp])
+    lib.star_distillation_loss.restype = c_int
+    lib.star_rms_norm.argtypes = ([c_vp, c_i64] * 4 + [c_int, c_i64, c_i64, c_vp, c_int, c_f] + [c_vp] * 4)
+    lib.star_rms_norm.restype = c_int
+    lib.star_rms_norm_workspace_bytes.argtypes = [c_i64, c_i64, c_vp]
+    lib.star_rms_norm_workspace_bytes.restype = c_int
+    lib.star_rms_norm_backward.argtypes = [c_vp, c_i64, c_vp, c_int, c_int, c_vp, c_i64, c_vp, c_i64, c_vp, c_vp, c_vp, c_i64, c_int,
+                                           c_i64, c_i64, c_vp, c_int, c_vp, c_vp, ctypes.c_size_t, c_vp]
+    lib.star_rms_norm_backward.restype = c_int
     lib.star_checkpoint_sizes.argtypes = [c_i64, c_i64, c_vp, c_vp, c_vp]
     lib.star_checkpoint_sizes.restype = c_int
     lib.star_checkpoint_pack.argtypes = [c_vp, c_vp, c_vp, c_int, c_i64, c_i64, c_i64, c_int, c_vp, c_i64, c_vp]
@@ -914,6 +930,85 @@ def star_preference_loss(logits: torch.Tensor, labels: torch.Tensor, seq_offsets
            "star_preference_loss")
 
 
+STAR_MAX_ALTERNATIVES = 128
+
+
+def _listed(t: Optional[torch.Tensor], rows: int, k: int, what: str, dtype) -> Tuple[Optional[int], int]:
+    """(address, row stride) of a rows x k matrix of a teacher's or of top entries."""
+    if t is None:
+        return None, k
+    if t.dtype is not dtype or t.dim() != 2 or not t.is_cuda:
+        raise TypeError("%s must be a 2-D %s CUDA tensor" % (what, dtype))
+    if tuple(t.shape) != (rows, k):
+        raise ValueError("%s has shape %s, expected %s" % (what, tuple(t.shape), (rows, k)))
+    ld, step = t.stride()
+    if (step != 1 and k > 1) or (ld < k and rows > 1):
+        raise TypeError("%s must have contiguous rows that do not overlap" % what)
+    return t.data_ptr(), max(ld, k)
+
+
+def star_token_alternatives(logits: torch.Tensor, top_ids: Optional[torch.Tensor] = None,
+                            top_logp: Optional[torch.Tensor] = None, labels: Optional[torch.Tensor] = None,
+                            logp: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                            entropy: Optional[torch.Tensor] = None, temperature: float = 1.0, stream=None) -> None:
+    """The largest logits' ids (int32, rows x k) and log-probabilities, with lse,
+    entropy and the labels' logp where asked for; without labels every row takes part."""
+    rows, vocab = logits.shape
+    x, dtype, ld = _matrix(logits, "logits")
+    if (top_ids is None) != (top_logp is None):
+        raise ValueError("top_ids and top_logp come together")
+    k = 0 if top_ids is None else top_ids.shape[-1]
+    ids, ld_ids = _listed(top_ids, rows, k, "top_ids", torch.int32)
+    top, ld_top = _listed(top_logp, rows, k, "top_logp", torch.float32)
+    if ld_ids != ld_top and rows > 1:
+        raise ValueError("top_ids and top_logp must have one row stride")
+    _check(_lib.star_token_alternatives(x, dtype, rows, vocab, ld, _vector(labels, rows, "labels", torch.int64), temperature, k,
+                                        ids, top, max(ld_ids, ld_top), _vector(logp, rows, "logp"), _vector(lse, rows, "lse"),
+                                        _vector(entropy, rows, "entropy"), _stream(stream)), "star_token_alternatives")
+
+
+def star_token_alternatives_backward(dlogits: torch.Tensor, logits: torch.Tensor, lse: torch.Tensor,
+                                     labels: Optional[torch.Tensor] = None, d_logp: Optional[torch.Tensor] = None,
+                                     entropy: Optional[torch.Tensor] = None, d_entropy: Optional[torch.Tensor] = None,
+                                     top_ids: Optional[torch.Tensor] = None, d_top_logp: Optional[torch.Tensor] = None,
+                                     temperature: float = 1.0, stream=None) -> None:
+    """The gradient of the logits (which it may replace) from those of
+    star_token_alternatives' results, with that call's lse and entropy."""
+    rows, vocab = logits.shape
+    x, dtype, ld = _matrix(logits, "logits")
+    d, _, ld_d = _matrix(dlogits, "dlogits", (rows, vocab), logits.dtype)
+    if (top_ids is None) != (d_top_logp is None):
+        raise ValueError("top_ids and d_top_logp come together")
+    k = 0 if top_ids is None else top_ids.shape[-1]
+    ids, ld_ids = _listed(top_ids, rows, k, "top_ids", torch.int32)
+    top, ld_top = _listed(d_top_logp, rows, k, "d_top_logp", torch.float32)
+    _check(_lib.star_token_alternatives_backward(d, ld_d, x, dtype, rows, vocab, ld, _vector(labels, rows, "labels", torch.int64),
+                                                 temperature, _vector(lse, rows, "lse"), _vector(entropy, rows, "entropy"),
+                                                 _vector(d_logp, rows, "d_logp"), _vector(d_entropy, rows, "d_entropy"), k, ids,
+                                                 ld_ids, top, ld_top, _stream(stream)), "star_token_alternatives_backward")
+
+
+def star_distillation_loss(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_values: torch.Tensor,
+                           token_loss: torch.Tensor, sums: torch.Tensor, workspace: torch.Tensor,
+                           dlogits: Optional[torch.Tensor] = None, labels: Optional[torch.Tensor] = None,
+                           weights: Optional[torch.Tensor] = None, temperature: float = 1.0, teacher_temperature: float = 1.0,
+                           rest: bool = False, soft_coef: float = 1.0, label_coef: float = 0.0, stream=None) -> None:
+    """Distillation from a teacher's k ids and values a row (logits, or with
+    ``rest`` log-probabilities whose remainder counts too): token_loss, the four
+    sums and, unless None, the gradient of the logits (which may be the logits)."""
+    rows, vocab = logits.shape
+    x, dtype, ld = _matrix(logits, "logits")
+    d, _, ld_d = (None, dtype, vocab) if dlogits is None else _matrix(dlogits, "dlogits", (rows, vocab), logits.dtype)
+    k = teacher_ids.shape[-1]
+    ids, ld_ids = _listed(teacher_ids, rows, k, "teacher_ids", torch.int32)
+    values, ld_values = _listed(teacher_values, rows, k, "teacher_values", torch.float32)
+    ws, ws_bytes = _workspace(workspace)
+    _check(_lib.star_distillation_loss(x, dtype, rows, vocab, ld, ids, ld_ids, values, ld_values, k, int(rest), teacher_temperature,
+                                       _vector(labels, rows, "labels", torch.int64), _vector(weights, rows, "weights"), temperature,
+                                       soft_coef, label_coef, _vector(token_loss, rows, "token_loss"), _vector(sums, 4, "sums"), d,
+                                       ld_d, ws, ws_bytes, _stream(stream)), "star_distillation_loss")
+
+
 def star_checkpoint_sizes(rows: int, cols: int) -> Tuple[int, int, int]:
     """(pitch, bytes of codes, bytes of scales) of a checkpoint of rows x cols values."""
     pitch, code_bytes, scale_bytes = ctypes.c_int64(0), ctypes.c_size_t(0), ctypes.c_size_t(0)
@@ -984,6 +1079,71 @@ def star_checkpoint_weight_grad(dw: torch.Tensor, dy: torch.Tensor, codes: torch
     q, s = _kept(codes, scales, rows, cols)
     _check(_lib.star_checkpoint_weight_grad(w, w_dtype, ld_w, int(transposed), p, dtype, ld, q, s, rows, cols, outs,
                                             int(accumulate), _stream(stream)), "star_checkpoint_weight_grad")
+
+
+def _gain(t: Optional[torch.Tensor], cols: int, what: str) -> Tuple[Optional[int], int]:
+    """(address, dtype code) of a vector of float32 or bfloat16."""
+    if t is None:
+        return None, STAR_DTYPE_F32
+    if t.dtype not in _DTYPES:
+        raise TypeError("%s must be a contiguous float32 or bfloat16 CUDA tensor" % what)
+    return _vector(t, cols, what, t.dtype), _DTYPES[t.dtype]
+
+
+def _optional_matrix(t: Optional[torch.Tensor], what: str, shape, dtype) -> Tuple[Optional[int], int]:
+    if t is None:
+        return None, shape[1]
+    p, _, ld = _matrix(t, what, shape, dtype)
+    return p, ld
+
+
+def _optional_kept(codes, scales, rows: int, cols: int) -> Tuple[Optional[int], Optional[int]]:
+    if (codes is None) != (scales is None):
+        raise ValueError("codes and scales come together")
+    return (None, None) if codes is None else _kept(codes, scales, rows, cols)
+
+
+def star_rms_norm(y: torch.Tensor, x: torch.Tensor, gain: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+                  total: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
+                  codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                  stream=None) -> None:
+    """y = the root-mean-square norm of x + residual; the sum goes to total (which may
+    be x or the residual), and y is kept in 8 bits in codes and scales, where given."""
+    rows, cols = x.shape
+    p, dtype, ld = _matrix(x, "x")
+    o, _, ld_o = _matrix(y, "y", (rows, cols), x.dtype)
+    r, ld_r = _optional_matrix(residual, "residual", (rows, cols), x.dtype)
+    s, ld_s = _optional_matrix(total, "total", (rows, cols), x.dtype)
+    g, g_dtype = _gain(gain, cols, "gain")
+    q, b = _optional_kept(codes, scales, rows, cols)
+    _check(_lib.star_rms_norm(o, ld_o, p, ld, r, ld_r, s, ld_s, dtype, rows, cols, g, g_dtype, eps, _vector(rstd, rows, "rstd"),
+                              q, b, _stream(stream)), "star_rms_norm")
+
+
+def star_rms_norm_workspace_bytes(rows: int, cols: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.star_rms_norm_workspace_bytes(rows, cols, ctypes.byref(out)), "star_rms_norm_workspace_bytes")
+    return out.value
+
+
+def star_rms_norm_backward(dx: torch.Tensor, dgain: Optional[torch.Tensor], dy: torch.Tensor, gain: Optional[torch.Tensor],
+                           rstd: torch.Tensor, workspace: Optional[torch.Tensor] = None, total: Optional[torch.Tensor] = None,
+                           codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                           d_total: Optional[torch.Tensor] = None, accumulate: bool = False, stream=None) -> None:
+    """dx (which may be dy or d_total) and, unless None, dgain = or += its sums, from
+    the normalized stream: total, or a checkpoint of it in codes and scales."""
+    rows, cols = dy.shape
+    p, dtype, ld = _matrix(dy, "dy")
+    d, _, ld_d = _matrix(dx, "dx", (rows, cols), dy.dtype)
+    s, ld_s = _optional_matrix(total, "total", (rows, cols), dy.dtype)
+    e, ld_e = _optional_matrix(d_total, "d_total", (rows, cols), dy.dtype)
+    g, g_dtype = _gain(gain, cols, "gain")
+    dg, dg_dtype = _gain(dgain, cols, "dgain")
+    q, b = _optional_kept(codes, scales, rows, cols)
+    ws, ws_bytes = (None, 0) if workspace is None else _workspace(workspace)
+    _check(_lib.star_rms_norm_backward(d, ld_d, dg, dg_dtype, int(accumulate), p, ld, s, ld_s, q, b, e, ld_e, dtype, rows, cols, g,
+                                       g_dtype, _vector(rstd, rows, "rstd"), ws, ws_bytes, _stream(stream)),
+           "star_rms_norm_backward")
 
 
 def star_check_waits(stream=None) -> None:

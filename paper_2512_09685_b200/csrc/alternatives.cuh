@@ -1,0 +1,461 @@
+// Device code of log-probabilities with entropy and top alternatives, and of their
+// backward pass (sm_100a).
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "rows.cuh"
+
+namespace star {
+
+constexpr int kMostAlternatives = 128;       // STAR_MAX_ALTERNATIVES
+
+struct AlternativesArgs {
+    RowArgs row;                 // labels may be null
+    int k;
+    int32_t *top_ids;
+    float *top_logp;
+    int64_t ld_top;
+    float *logp, *lse, *entropy; // each may be null
+};
+
+// Largest logit m, the sum s of 2^exponent(x, m), and t = the sum of
+// 2^exponent(x, m) exponent(x, m): the entropy is log s - t log(2) / s, both terms
+// of one sign.
+struct MaxSums {
+    float m, s, t;
+};
+// A power below the smallest binary32 adds nothing, whatever its exponent.
+__device__ __forceinline__ float bounded(float d) { return fmaxf(d, -150.0f); }
+__device__ __forceinline__ MaxSums move_to(MaxSums x, float m, float k)
+{
+    const float d = bounded(exponent(x.m, m, k)), r = exp2_fast(d);
+    return MaxSums{m, __fmul_rn(x.s, r), __fmul_rn(r, __fmaf_rn(d, x.s, x.t))};
+}
+__device__ __forceinline__ MaxSums add(MaxSums a, MaxSums b) { return MaxSums{a.m, __fadd_rn(a.s, b.s), __fadd_rn(a.t, b.t)}; }
+__device__ __forceinline__ MaxSums take_one(MaxSums x, float v, float k)
+{
+    const float m = fmaxf(x.m, v), d = exponent(v, m, k), e = exp2_fast(d);
+    return add(move_to(x, m, k), MaxSums{m, e, __fmul_rn(e, bounded(d))});
+}
+__device__ __forceinline__ MaxSums warp_join(MaxSums x, float k)
+{
+    x = move_to(x, warp_max(x.m), k);
+    return MaxSums{x.m, warp_sum(x.s), warp_sum(x.t)};
+}
+
+// As take_batch, with t.  Returns the batch's largest logit.
+template <typename G, int N, int THREADS, bool FULL>
+__device__ __forceinline__ float take_batch_with_entropy(MaxSums *x, const uint4 *from, int left, float k)
+{
+    constexpr int P = Granule<G>::kPairs;
+    uint4 v[N];
+#pragma unroll
+    for (int q = 0; q < N; ++q)
+        if (FULL || q * THREADS < left) v[q] = from[q * THREADS];
+    RunningMax<G> most;
+#pragma unroll
+    for (int q = 0; q < N; ++q)
+        if (FULL || q * THREADS < left) most.take(v[q]);
+    const float m = most.value();
+    if (m > x->m) *x = move_to(*x, m, k);
+    const Pair minus_m = pair_of(-pivot(x->m)), kk = pair_of(k);
+    Pair s = pair_of(0.0f), t = pair_of(0.0f);
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+        if (FULL || q * THREADS < left) {
+            Pair f[P];
+            Granule<G>::widen(v[q], f);
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+                float lo, hi;
+                split_pair(pair_mul(pair_add(f[e], minus_m), kk), &lo, &hi);
+                const Pair p = make_pair(exp2_fast(lo), exp2_fast(hi));
+                s = pair_add(s, p);
+                t = pair_fma(p, make_pair(bounded(lo), bounded(hi)), t);
+            }
+        }
+    }
+    float lo, hi;
+    split_pair(s, &lo, &hi);
+    x->s = __fadd_rn(x->s, __fadd_rn(lo, hi));
+    split_pair(t, &lo, &hi);
+    x->t = __fadd_rn(x->t, __fadd_rn(lo, hi));
+    return m;
+}
+
+// A logit's place in the order: larger for larger logits, one for both zeros.
+// -inf has kLowest; a NaN's is beyond +inf or below it.
+__device__ __forceinline__ uint32_t order_of(float x)
+{
+    const uint32_t bits = __float_as_uint(__fadd_rn(x, 0.0f));
+    return bits & 0x80000000u ? ~bits : bits | 0x80000000u;
+}
+constexpr uint32_t kLowest = 0x007fffffu;    // order_of(-inf)
+
+// ---------------------------------------------------------------------------
+// Statistics and the k largest logits of a row, in one reading of it from memory.
+//
+// A row is split among the threads, and every thread knows the largest logit of
+// its part when the statistics are done.  The k-th largest of these is at most the
+// k-th largest logit, so no logit below it is wanted, and in a row whose large
+// logits lie anywhere little more than k are not: those are gathered by a second
+// look at the parts that hold one (from L2), and each finds its rank by comparing
+// itself with the others.  Rows that leave too many (many equal logits, or the
+// large ones side by side) are searched for the k-th largest by counting.
+// ---------------------------------------------------------------------------
+constexpr int kMostCandidates = 1088;        // k groups of a thread's one granule, and the edges
+
+struct Candidates {
+    uint64_t key[kMostCandidates];           // order in the upper half, 2^31 - 1 - index below
+    int count;
+};
+__device__ __forceinline__ void put_candidate(Candidates &c, uint32_t order, int index)
+{
+    const int at = atomicAdd(&c.count, 1);
+    if (at < kMostCandidates) c.key[at] = static_cast<uint64_t>(order) << 32 | static_cast<uint32_t>(0x7fffffff - index);
+}
+
+// The largest bound that at least k of the values (`EACH` to a lane) reach, or one
+// that few more reach.
+template <int EACH> __device__ __forceinline__ uint32_t bound_of(const uint32_t (&x)[EACH], int k)
+{
+    uint32_t low = 0xffffffffu, high = 0;
+#pragma unroll
+    for (int q = 0; q < EACH; ++q) {
+        low = min(low, x[q]);
+        high = max(high, x[q]);
+    }
+    low = __reduce_min_sync(0xffffffffu, low);
+    high = __reduce_max_sync(0xffffffffu, high);
+    uint32_t width = high - low;             // the bound lies in [low, low + width]
+    while (width > 0) {
+        const uint32_t mid = low + (width - width / 2);
+        int n = 0;
+#pragma unroll
+        for (int q = 0; q < EACH; ++q) n += x[q] >= mid ? 1 : 0;
+        n = __reduce_add_sync(0xffffffffu, n);
+        if (n >= k) {
+            width -= mid - low;
+            low = mid;
+            if (n <= k + k / 8) break;
+        } else {
+            width = mid - low - 1;
+        }
+    }
+    return low;
+}
+
+// How many logits of a row reach `bound`, by a block of THREADS; every thread gets it.
+template <typename G, int THREADS> __device__ int count_row(const void *base, int vocab, uint32_t bound, int *total)
+{
+    int n = 0;
+    for (int i = threadIdx.x; i < vocab; i += THREADS) n += order_of(load_value<G>(base, i)) >= bound ? 1 : 0;
+    n = __reduce_add_sync(0xffffffffu, n);
+    __syncthreads();
+    if (threadIdx.x == 0) *total = 0;
+    __syncthreads();
+    if (threadIdx.x % 32 == 0) atomicAdd(total, n);
+    __syncthreads();
+    return *total;
+}
+
+// The candidates of a row that `low` leaves too many of (but at least k): counting
+// finds a bound that leaves few enough, or the k-th largest logit itself, whose
+// equals are then taken by ascending index.
+template <typename G, int THREADS>
+__device__ void search_row(const void *base, int vocab, int k, uint32_t low, Candidates &found, int *scratch)
+{
+    uint32_t width = 0xffffffffu - low;
+    int reach = kMostCandidates + 1;         // logits at or above low
+    while (width > 0 && reach > kMostCandidates) {
+        const uint32_t mid = low + (width - width / 2);
+        const int n = count_row<G, THREADS>(base, vocab, mid, scratch);
+        if (n >= k) {
+            width -= mid - low;
+            low = mid;
+            reach = n;
+        } else {
+            width = mid - low - 1;
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) found.count = 0;
+    __syncthreads();
+    const bool ties = reach > kMostCandidates;               // low is the k-th largest, and many equal it
+    for (int i = threadIdx.x; i < vocab; i += THREADS) {
+        const uint32_t order = order_of(load_value<G>(base, i));
+        if (ties ? order > low : order >= low) put_candidate(found, order, i);
+    }
+    __syncthreads();
+    if (!ties) return;
+    // One warp, in the order of the indexes.
+    if (threadIdx.x < 32) {
+        int have = found.count;
+        for (int i = threadIdx.x; i - static_cast<int>(threadIdx.x) < vocab && have < k; i += 32) {
+            const bool equal = i < vocab && order_of(load_value<G>(base, i)) == low;
+            const uint32_t who = __ballot_sync(0xffffffffu, equal);
+            const int at = have + __popc(who & ((1u << threadIdx.x) - 1));
+            if (equal && at < k) found.key[at] = static_cast<uint64_t>(low) << 32 | static_cast<uint32_t>(0x7fffffff - i);
+            have += __popc(who);
+        }
+        __syncwarp();
+        if (threadIdx.x == 0) found.count = min(have, k);
+    }
+    __syncthreads();
+}
+
+template <typename G, int THREADS>
+__global__ void __launch_bounds__(THREADS, row_blocks(THREADS)) star_alternatives_kernel(const __grid_constant__ AlternativesArgs a)
+{
+    constexpr int E = Granule<G>::kCount, kWarps = THREADS / 32, kStep = kBatch * THREADS;
+    __shared__ MaxSums warp_part[kWarps];
+    __shared__ MaxSums row_sums;
+    __shared__ uint32_t group_order[THREADS];
+    __shared__ Candidates found;
+    __shared__ uint32_t row_bound;
+    __shared__ int scratch;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const float k = __fmul_rn(a.row.inv_temperature, kLog2e);
+    const int vocab = static_cast<int>(a.row.vocab);
+    launch_dependents();
+    wait_for_primary();
+
+    for (int64_t t = blockIdx.x; t < a.row.rows; t += gridDim.x) {
+        const char *base = static_cast<const char *>(a.row.logits) + t * a.row.ld * G::kBytes;
+        const int64_t label = a.row.labels ? a.row.labels[t] : 0;
+        const bool wanted = label >= 0 && label < vocab;     // vocab of 0: none
+        const RowSplit s = split_row<G>(base, vocab);
+        const uint4 *granules = reinterpret_cast<const uint4 *>(base + s.head * G::kBytes);
+        MaxSums x{-INFINITY, 0.0f, 0.0f};
+        float edge = -INFINITY;
+        if (wanted) {
+            int left = s.granules - static_cast<int>(threadIdx.x);
+            const uint4 *from = granules + threadIdx.x;
+            for (; left > kStep - THREADS; left -= kStep, from += kStep) take_batch_with_entropy<G, kBatch, THREADS, true>(&x, from, left, k);
+            if (left > 0) take_batch_with_entropy<G, kBatch, THREADS, false>(&x, from, left, k);
+            const int edge_at = edge_element(s, threadIdx.x, vocab);
+            if (edge_at >= 0) {
+                edge = load_value<G>(base, edge_at);
+                x = take_one(x, edge, k);
+            }
+            if (a.k > 0) group_order[threadIdx.x] = order_of(x.m);
+            const float own = x.m;
+            x = warp_join(x, k);
+            if (lane == 0) warp_part[warp] = x;
+            if (threadIdx.x == 0) found.count = 0;
+            __syncthreads();
+            if (warp == 0) {
+                x = warp_join(lane < kWarps ? warp_part[lane] : MaxSums{-INFINITY, 0.0f, 0.0f}, k);
+                if (lane == 0) row_sums = x;
+                if (a.k > 0) {
+                    uint32_t most[THREADS / 32];
+#pragma unroll
+                    for (int q = 0; q < THREADS / 32; ++q) most[q] = group_order[q * 32 + lane];
+                    // No bound where there are fewer parts than alternatives.
+                    const uint32_t bound = a.k <= THREADS ? bound_of(most, a.k) : 0;
+                    if (lane == 0) row_bound = max(bound, kLowest + 1);
+                }
+            }
+            __syncthreads();
+            x = row_sums;
+            // A second look at the parts that reach the bound.
+            if (a.k > 0 && x.s > 0.0f) {
+                const uint32_t bound = row_bound;
+                if (order_of(own) >= bound) {
+                    if (edge_at >= 0 && order_of(edge) >= bound) put_candidate(found, order_of(edge), edge_at);
+                    for (int g = threadIdx.x; g < s.granules; g += THREADS) {
+                        const uint4 v = granules[g];
+                        RunningMax<G> most;
+                        most.take(v);
+                        if (order_of(most.value()) < bound) continue;
+                        for (int e = 0; e < E; ++e) {
+                            const float f = load_value<G>(granules, static_cast<int64_t>(g) * E + e);
+                            if (order_of(f) >= bound) put_candidate(found, order_of(f), s.head + g * E + e);
+                        }
+                    }
+                }
+                __syncthreads();
+                if (found.count > kMostCandidates) search_row<G, THREADS>(base, vocab, a.k, bound, found, &scratch);
+            }
+        }
+        const bool active = wanted && !(x.s == 0.0f), whole = active && x.s < INFINITY;
+        if (threadIdx.x == 0) {
+            const float nan = x.s;                           // where the row has no sum
+            if (a.logp) a.logp[t] = active ? log_prob(load_value<G>(base, label), MaxSum{x.m, x.s}, k, a.row.inv_temperature) : 0.0f;
+            if (a.lse) a.lse[t] = active ? log_sum_exp(MaxSum{x.m, x.s}, a.row.inv_temperature) : -INFINITY;
+            if (a.entropy) a.entropy[t] = whole ? __fsub_rn(logf(x.s), __fmul_rn(kLn2, __fdiv_rn(x.t, x.s))) : active ? nan : 0.0f;
+        }
+        if (a.k > 0) {
+            const int n = whole ? found.count : 0, have = min(n, a.k);
+            int32_t *ids = a.top_ids + t * a.ld_top;
+            float *top = a.top_logp + t * a.ld_top;
+            for (int i = threadIdx.x; i < n; i += THREADS) {
+                const uint64_t key = found.key[i];
+                int rank = 0;
+                for (int j = 0; j < n; ++j) rank += found.key[j] > key ? 1 : 0;
+                if (rank < a.k) {
+                    const uint32_t order = static_cast<uint32_t>(key >> 32);
+                    const float f = __uint_as_float(order & 0x80000000u ? order & 0x7fffffffu : ~order);
+                    ids[rank] = 0x7fffffff - static_cast<int32_t>(key & 0xffffffffu);
+                    top[rank] = log_prob(f, MaxSum{x.m, x.s}, k, a.row.inv_temperature);
+                }
+            }
+            for (int i = have + threadIdx.x; i < a.k; i += THREADS) {
+                ids[i] = -1;
+                top[i] = active && !whole ? x.s : -INFINITY;
+            }
+        }
+        __syncthreads();                                     // the candidates are read
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The backward pass.  With u = z - lse and p = exp(u),
+//     dlogits[j] = (sum of the gradients of what names j - p (G + h (u + H))) / temperature,
+// G the sum of the gradients of a row's log-probabilities, h that of its entropy H.
+// A warp takes a run of granules of a row at a time, as for the losses' gradients;
+// elements that the label or an alternative names are made by the same warp.
+// ---------------------------------------------------------------------------
+struct AlternativesGradArgs {
+    RowArgs row;                 // labels may be null
+    const float *lse, *entropy, *d_logp, *d_entropy;     // entropy and the gradients may be null
+    int k;
+    const int32_t *top_ids;
+    const float *d_top;
+    int64_t ld_top, ld_d_top;
+    void *dlogits;
+    int64_t ld_dlogits;
+};
+
+// What a row's dense part is made with.
+struct AlternativesRow {
+    float lse, inv_temperature;
+    float plain, slope;          // -p (plain + slope u) / temperature
+};
+__device__ __forceinline__ float dense_gradient(float x, const AlternativesRow &r)
+{
+    const float u = fmaxf(__fmaf_rn(x, r.inv_temperature, -r.lse), -200.0f);
+    return __fmul_rn(exp2_fast(__fmul_rn(u, kLog2e)), __fmaf_rn(r.slope, u, r.plain));
+}
+
+constexpr int kAltThreads = 256;
+constexpr int kAltPerThread = 4;
+constexpr int kAltGranules = 32 * kAltPerThread;
+constexpr int kAltSlots = kMostAlternatives / 32 + 1;        // what names an element, to a lane
+
+template <typename G> __global__ void __launch_bounds__(kAltThreads, 4) star_alternatives_backward_kernel(const __grid_constant__ AlternativesGradArgs a)
+{
+    constexpr int E = Granule<G>::kCount, P = Granule<G>::kPairs;
+    launch_dependents();
+    wait_for_primary();
+    const int vocab = static_cast<int>(a.row.vocab);
+    const int64_t per_row = (a.row.vocab / E + kAltGranules) / kAltGranules;             // the last run may be empty
+    const int64_t items = a.row.rows * per_row;
+    const int lane = threadIdx.x % 32, warps = kAltThreads / 32;
+    for (int64_t item = static_cast<int64_t>(blockIdx.x) * warps + threadIdx.x / 32; item < items; item += static_cast<int64_t>(gridDim.x) * warps) {
+        const int64_t t = items <= 0xffffffff ? static_cast<uint32_t>(item) / static_cast<uint32_t>(per_row) : item / per_row;
+        const int64_t run = item - t * per_row;
+        const char *base = static_cast<const char *>(a.row.logits) + t * a.row.ld * G::kBytes;
+        char *out = static_cast<char *>(a.dlogits) + t * a.ld_dlogits * G::kBytes;
+        const RowSplit s = split_row<G>(base, vocab);
+        const int begin = static_cast<int>(run) * kAltGranules, end = min(begin + kAltGranules, s.granules);
+        const int first = s.head + begin * E, last = s.head + end * E;                   // the run's elements; run 0 has the edges too
+        const int edge_at = run == 0 ? edge_element(s, lane, vocab) : -1;
+        const float lse = a.lse[t];
+        const int64_t label = a.row.labels ? a.row.labels[t] : 0;
+        const bool active = lse != -INFINITY && label >= 0 && label < vocab;
+        // What names an element, and its gradient: the alternatives, then the label.
+        int named[kAltSlots];
+        float grad[kAltSlots], each = 0.0f;
+        AlternativesRow r{lse, a.row.inv_temperature, 0.0f, 0.0f};
+        if (active) {
+#pragma unroll
+            for (int q = 0; q < kAltSlots; ++q) {
+                const int i = q * 32 + lane;
+                named[q] = -1;
+                grad[q] = 0.0f;
+                if (i < a.k) {
+                    const int id = a.top_ids[t * a.ld_top + i];
+                    if (id >= 0 && id < vocab) {
+                        named[q] = id;
+                        grad[q] = a.d_top[t * a.ld_d_top + i];
+                    }
+                } else if (i == a.k && a.d_logp) {
+                    named[q] = static_cast<int>(label);
+                    grad[q] = a.d_logp[t];
+                }
+                each = __fadd_rn(each, grad[q]);
+            }
+            each = warp_sum(each);
+            const float h = a.d_entropy ? a.d_entropy[t] : 0.0f;
+            float plain = h == 0.0f ? each : __fmaf_rn(h, a.entropy[t], each);
+            if (lse != lse) plain = lse;                     // a NaN row's gradient is NaN
+            r.plain = -__fmul_rn(plain, r.inv_temperature);
+            r.slope = -__fmul_rn(h, r.inv_temperature);
+        }
+        // The named elements' logits, before anything is stored in place.
+        float at_named[kAltSlots];
+        uint32_t here[kAltSlots];
+        if (active) {
+#pragma unroll
+            for (int q = 0; q < kAltSlots; ++q) {
+                const bool in = named[q] >= 0 && ((named[q] >= first && named[q] < last) || (run == 0 && (named[q] < s.head || named[q] >= vocab - s.tail)));
+                here[q] = __ballot_sync(0xffffffffu, in);
+                at_named[q] = in ? load_value<G>(base, named[q]) : 0.0f;
+            }
+            __syncwarp();
+        }
+        const float edge = active && edge_at >= 0 ? load_value<G>(base, edge_at) : 0.0f;
+        const bool same_phase = (reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(base)) % 16 == 0;
+        if (same_phase) {
+            const uint4 *src = reinterpret_cast<const uint4 *>(base + s.head * G::kBytes) + begin + lane;
+            uint4 *dst = reinterpret_cast<uint4 *>(out + s.head * G::kBytes) + begin + lane;
+            const int left = end - begin - lane;
+            if (active) {
+                uint4 v[kAltPerThread];
+#pragma unroll
+                for (int q = 0; q < kAltPerThread; ++q)
+                    if (q * 32 < left) v[q] = src[q * 32];
+#pragma unroll
+                for (int q = 0; q < kAltPerThread; ++q) {
+                    if (q * 32 < left) {
+                        Pair g[P];
+                        Granule<G>::widen(v[q], g);
+#pragma unroll
+                        for (int e = 0; e < P; ++e) {
+                            float lo, hi;
+                            split_pair(g[e], &lo, &hi);
+                            g[e] = make_pair(dense_gradient(lo, r), dense_gradient(hi, r));
+                        }
+                        dst[q * 32] = Granule<G>::narrow(g);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < kAltPerThread; ++q)
+                    if (q * 32 < left) dst[q * 32] = make_uint4(0, 0, 0, 0);
+            }
+        } else {
+            for (int at = first + lane; at < last; at += 32) store_value<G>(out, at, active ? dense_gradient(load_value<G>(base, at), r) : 0.0f);
+        }
+        if (edge_at >= 0) store_value<G>(out, edge_at, active ? dense_gradient(edge, r) : 0.0f);
+        if (!active) continue;
+        __syncwarp();                                        // the run is stored
+#pragma unroll
+        for (int q = 0; q < kAltSlots; ++q) {
+            for (uint32_t rest = here[q]; rest; rest &= rest - 1) {
+                const int who = __ffs(rest) - 1;
+                const int id = __shfl_sync(0xffffffffu, named[q], who);
+                float sum = 0.0f;                            // of all that name it
+#pragma unroll
+                for (int p = 0; p < kAltSlots; ++p) sum = __fadd_rn(sum, named[p] == id ? grad[p] : 0.0f);
+                sum = warp_sum(sum);
+                if (lane == who) store_value<G>(out, id, __fmaf_rn(sum, r.inv_temperature, dense_gradient(at_named[q], r)));
+            }
+        }
+    }
+}
+
+}  // namespace star

@@ -1,0 +1,114 @@
+// Entry point of the distillation loss: argument checks on the host, then the
+// launches.
+#include <algorithm>
+#include <cmath>
+
+#include "distillation.cuh"
+#include "rows_host.h"
+
+namespace star {
+
+cudaError_t distillation_expired(cudaStream_t stream, int *expired) { return take_expired(stream, expired); }
+
+}  // namespace star
+
+namespace {
+
+using namespace star;
+
+static_assert(kMostListed == STAR_MAX_ALTERNATIVES, "the kernels' and the interface's limit");
+
+template <typename G, int THREADS, bool TWO>
+star_status_t launch_loss(const DistillArgs &a, int cluster, int *parts_out, cudaStream_t stream)
+{
+    static Held known;
+    constexpr auto kernel = star_distillation_kernel<G, THREADS, TWO>;
+    const int64_t granules = a.row.vocab * G::kBytes / 16;
+    const int kib = static_cast<int>(((granules + cluster - 1) / cluster * 16 + 1023) / 1024);
+    int held = 0;
+    const cudaError_t e = held_clusters(kernel, known, THREADS, cluster, kib, &held);
+    if (e != cudaSuccess) return cuda_failed(e);
+    const int64_t clusters = std::min<int64_t>(a.row.rows, held);
+    *parts_out = static_cast<int>(clusters);
+    return launch(kernel, dim3(static_cast<unsigned>(clusters * cluster)), THREADS, static_cast<size_t>(kib) * 1024, dim3(static_cast<unsigned>(cluster)), stream, a);
+}
+
+template <typename G, bool TWO> star_status_t run_threads(const DistillArgs &a, int threads, int cluster, int *parts_out, cudaStream_t stream)
+{
+    switch (threads) {
+    case 128: return launch_loss<G, 128, TWO>(a, cluster, parts_out, stream);
+    case 256: return launch_loss<G, 256, TWO>(a, cluster, parts_out, stream);
+    default: return launch_loss<G, 512, TWO>(a, cluster, parts_out, stream);
+    }
+}
+
+// The smallest block whose part of the SM's shared memory holds a row, or a cluster
+// of them; the cluster's blocks may take an SM's shared memory each.  More blocks to
+// a row where there are few.
+bool shape(int64_t rows, int64_t vocab, int size, int *threads, int *cluster)
+{
+    const int64_t bytes = vocab * size;
+    *cluster = 1;
+    *threads = 512;
+    for (int t : {512, 256, 128})
+        if (bytes <= int64_t{kDistillBytesPerThread} * t) *threads = t;
+    while (*cluster < 8 && bytes > int64_t{kDistillBytesPerThread} * *threads * *cluster) *cluster *= 2;
+    while (*cluster < 8 && rows * *cluster * 2 <= 148 * 2 && bytes / (*cluster * 2) >= 448 * 16) *cluster *= 2;
+    return bytes <= int64_t{kDistillBytesPerThread} * 1024 * *cluster;
+}
+
+}  // namespace
+
+extern "C" star_status_t star_distillation_loss(const void *logits, star_dtype_t dtype, int64_t rows, int64_t vocab, int64_t ld,
+                                                const int32_t *teacher_ids, int64_t ld_ids, const float *teacher_values,
+                                                int64_t ld_values, int k, int rest, float teacher_temperature,
+                                                const int64_t *labels, const float *weights, float temperature, float soft_coef,
+                                                float label_coef, float *token_loss, float *sums, void *dlogits,
+                                                int64_t ld_dlogits, void *workspace, size_t workspace_bytes, void *cuda_stream)
+{
+    if (k < 0 || !std::isfinite(soft_coef) || !std::isfinite(label_coef) || !(teacher_temperature > 0.0f) ||
+        !std::isfinite(teacher_temperature) || !std::isfinite(1.0f / teacher_temperature))
+        return STAR_ERR_INVALID_ARG;
+    if (k > kMostListed) return STAR_ERR_UNSUPPORTED;
+    DistillArgs a{};
+    Extent read[5], written[4];
+    star_status_t st = check_rows(logits, dtype, rows, vocab, ld, labels, temperature, &a.row, read, label_coef == 0.0f);
+    if (st == STAR_OK) st = check_vector(weights, rows, 4, true, &read[2]);
+    if (st == STAR_OK && k > 0) st = check_matrix(teacher_ids, rows, k, ld_ids, 4, &read[3]);
+    if (st == STAR_OK && k > 0) st = check_matrix(teacher_values, rows, k, ld_values, 4, &read[4]);
+    if (st == STAR_OK) st = check_vector(token_loss, rows, 4, false, &written[0]);
+    if (st == STAR_OK) st = check_vector(sums, 4, 4, false, &written[1]);
+    if (st == STAR_OK) st = check_workspace(workspace, workspace_bytes, rows, 0, &written[2]);
+    if (st == STAR_OK) st = check_disjoint(written, 3, read, 5);
+    if (st == STAR_OK) st = check_gradient(dlogits, ld_dlogits, dtype, a.row, read[0], &written[3]);
+    if (st == STAR_OK && (overlaps_any(written[3], read + 1, 4) || overlaps_any(written[3], written, 3))) st = STAR_ERR_INVALID_ARG;
+    if (st != STAR_OK) return st;
+    int threads = 0, cluster = 0, parts = 0;
+    if (!shape(rows, vocab, dtype_size(dtype), &threads, &cluster)) return STAR_ERR_UNSUPPORTED;
+    a.row.weights = weights;
+    a.ids = teacher_ids;
+    a.values = teacher_values;
+    a.ld_ids = ld_ids;
+    a.ld_values = ld_values;
+    a.k = k;
+    a.rest = rest != 0;
+    a.inv_teacher_temperature = 1.0f / teacher_temperature;
+    a.soft = soft_coef;
+    a.hard = label_coef;
+    a.token_loss = token_loss;
+    a.partial = static_cast<float4 *>(workspace);
+    a.dlogits = dlogits;
+    a.ld_dlogits = ld_dlogits;
+    a.tries = wait_attempts();
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (rows > 0) {
+        const bool two = label_coef != 0.0f && a.row.inv_temperature != 1.0f;
+        if (dtype == STAR_DTYPE_BF16)
+            st = two ? run_threads<GradBF16, true>(a, threads, cluster, &parts, stream) : run_threads<GradBF16, false>(a, threads, cluster, &parts, stream);
+        else
+            st = two ? run_threads<GradF32, true>(a, threads, cluster, &parts, stream) : run_threads<GradF32, false>(a, threads, cluster, &parts, stream);
+        if (st != STAR_OK) return st;
+    }
+    return launch(star_distillation_sums_kernel, dim3(1), kDistillSumThreads, 0, dim3(1), stream, static_cast<const float4 *>(a.partial),
+                  static_cast<int64_t>(parts), sums);
+}

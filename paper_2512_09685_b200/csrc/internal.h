@@ -19,9 +19,10 @@ void count_launch();
 // Attempts of a wait inside a kernel (star_set_wait_attempts).
 int wait_attempts();
 
-// Whether a wait of the weight gradient's kernels has run out (and no longer
-// after this), once the work on `stream` is done.
+// Whether a wait of the weight gradient's or of the distillation loss's kernels has
+// run out (and no longer after this), once the work on `stream` is done.
 cudaError_t weight_grad_expired(cudaStream_t stream, int *expired);
+cudaError_t distillation_expired(cudaStream_t stream, int *expired);
 
 // The status of the launch just made; `e` is what the launching call returned.
 inline star_status_t launched(cudaError_t e = cudaSuccess)
