@@ -282,10 +282,8 @@ template <typename G> struct Sixteen {
             return m;
         }
     }
-    static __device__ __forceinline__ void store(void *row, int64_t c, int64_t cols, int wide, const float (&f)[16])
+    static __device__ __forceinline__ void narrow(const float (&f)[16], uint32_t (&w)[kWords])
     {
-        char *p = static_cast<char *>(row) + c * G::kBytes;
-        uint32_t w[kWords];
 #pragma unroll
         for (int q = 0; q < kWords; ++q) {
             if constexpr (G::kBytes == 2)
@@ -293,6 +291,16 @@ template <typename G> struct Sixteen {
             else
                 w[q] = __float_as_uint(f[q]);
         }
+    }
+    static __device__ __forceinline__ void store(void *row, int64_t c, int64_t cols, int wide, const float (&f)[16])
+    {
+        uint32_t w[kWords];
+        narrow(f, w);
+        store(row, c, cols, wide, w);
+    }
+    static __device__ __forceinline__ void store(void *row, int64_t c, int64_t cols, int wide, const uint32_t (&w)[kWords])
+    {
+        char *p = static_cast<char *>(row) + c * G::kBytes;
         const int left = static_cast<int>(min(cols - c, int64_t{16}));
         if (wide && left == 16) {
 #pragma unroll
@@ -323,6 +331,20 @@ template <typename G> struct Sixteen {
     }
 };
 
+// The codes of 16 values of a block with scale byte s.
+__device__ __forceinline__ uint4 codes_of(const float (&f)[16], int s)
+{
+    const float inverse = scale_inverse(s);
+    uint32_t codes[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const uint32_t lo = __byte_perm(code_bits(f[4 * q], inverse), code_bits(f[4 * q + 1], inverse), 0x0040);
+        const uint32_t hi = __byte_perm(code_bits(f[4 * q + 2], inverse), code_bits(f[4 * q + 3], inverse), 0x0040);
+        codes[q] = s == 255 ? 0u : __byte_perm(lo, hi, 0x5410);
+    }
+    return make_uint4(codes[0], codes[1], codes[2], codes[3]);
+}
+
 template <typename G, int ACT>
 __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_pack_kernel(const __grid_constant__ PackArgs a, const __grid_constant__ Halves h)
 {
@@ -342,17 +364,9 @@ __global__ void __launch_bounds__(kKeepThreads) star_checkpoint_pack_kernel(cons
         largest = max(largest, __shfl_xor_sync(0xffffffffu, largest, 1));
         if (!in) continue;
         const int s = scale_byte(largest);
-        const float inverse = scale_inverse(s);
         float f[16];
         Sixteen<G>::widen(w, f);
-        uint32_t codes[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const uint32_t lo = __byte_perm(code_bits(f[4 * q], inverse), code_bits(f[4 * q + 1], inverse), 0x0040);
-            const uint32_t hi = __byte_perm(code_bits(f[4 * q + 2], inverse), code_bits(f[4 * q + 3], inverse), 0x0040);
-            codes[q] = s == 255 ? 0u : __byte_perm(lo, hi, 0x5410);
-        }
-        *reinterpret_cast<uint4 *>(a.kept.codes + t * a.kept.pitch + c) = make_uint4(codes[0], codes[1], codes[2], codes[3]);
+        *reinterpret_cast<uint4 *>(a.kept.codes + t * a.kept.pitch + c) = codes_of(f, s);
         if (half % 2 == 0) a.kept.scales[scale_at(a.kept, t, half / 2)] = static_cast<uint8_t>(s);
         if (a.act_out) {
 #pragma unroll

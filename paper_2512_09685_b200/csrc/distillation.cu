@@ -18,28 +18,37 @@ using namespace star;
 
 static_assert(kMostListed == STAR_MAX_ALTERNATIVES, "the kernels' and the interface's limit");
 
-template <typename G, int THREADS, bool TWO>
+template <typename G, int THREADS, int MODE>
 star_status_t launch_loss(const DistillArgs &a, int cluster, int *parts_out, cudaStream_t stream)
 {
     static Held known;
-    constexpr auto kernel = star_distillation_kernel<G, THREADS, TWO>;
+    constexpr auto kernel = star_distillation_kernel<G, THREADS, MODE>;
     const int64_t granules = a.row.vocab * G::kBytes / 16;
     const int kib = static_cast<int>(((granules + cluster - 1) / cluster * 16 + 1023) / 1024);
     int held = 0;
-    const cudaError_t e = held_clusters(kernel, known, THREADS, cluster, kib, &held);
+    const cudaError_t e = held_clusters(kernel, known, THREADS, cluster, kib, &held, kDistillBytesPerThread);
     if (e != cudaSuccess) return cuda_failed(e);
     const int64_t clusters = std::min<int64_t>(a.row.rows, held);
     *parts_out = static_cast<int>(clusters);
     return launch(kernel, dim3(static_cast<unsigned>(clusters * cluster)), THREADS, static_cast<size_t>(kib) * 1024, dim3(static_cast<unsigned>(cluster)), stream, a);
 }
 
-template <typename G, bool TWO> star_status_t run_threads(const DistillArgs &a, int threads, int cluster, int *parts_out, cudaStream_t stream)
+template <typename G, int MODE> star_status_t run_threads(const DistillArgs &a, int threads, int cluster, int *parts_out, cudaStream_t stream)
 {
     switch (threads) {
-    case 128: return launch_loss<G, 128, TWO>(a, cluster, parts_out, stream);
-    case 256: return launch_loss<G, 256, TWO>(a, cluster, parts_out, stream);
-    default: return launch_loss<G, 512, TWO>(a, cluster, parts_out, stream);
+    case 128: return launch_loss<G, 128, MODE>(a, cluster, parts_out, stream);
+    case 256: return launch_loss<G, 256, MODE>(a, cluster, parts_out, stream);
+    default: return launch_loss<G, 512, MODE>(a, cluster, parts_out, stream);
     }
+}
+
+template <typename G> star_status_t run_mode(const DistillArgs &a, int threads, int cluster, int *parts_out, cudaStream_t stream)
+{
+    const float inv_t = a.row.inv_temperature;
+    if (a.hard == 0.0f || inv_t == 1.0f) return run_threads<G, kOne>(a, threads, cluster, parts_out, stream);
+    if (inv_t == 0.5f) return run_threads<G, kSquare>(a, threads, cluster, parts_out, stream);
+    if (inv_t == 0.25f) return run_threads<G, kFourth>(a, threads, cluster, parts_out, stream);
+    return run_threads<G, kTwo>(a, threads, cluster, parts_out, stream);
 }
 
 // The smallest block whose part of the SM's shared memory holds a row, or a cluster
@@ -102,11 +111,7 @@ extern "C" star_status_t star_distillation_loss(const void *logits, star_dtype_t
     a.tries = wait_attempts();
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (rows > 0) {
-        const bool two = label_coef != 0.0f && a.row.inv_temperature != 1.0f;
-        if (dtype == STAR_DTYPE_BF16)
-            st = two ? run_threads<GradBF16, true>(a, threads, cluster, &parts, stream) : run_threads<GradBF16, false>(a, threads, cluster, &parts, stream);
-        else
-            st = two ? run_threads<GradF32, true>(a, threads, cluster, &parts, stream) : run_threads<GradF32, false>(a, threads, cluster, &parts, stream);
+        st = dtype == STAR_DTYPE_BF16 ? run_mode<GradBF16>(a, threads, cluster, &parts, stream) : run_mode<GradF32>(a, threads, cluster, &parts, stream);
         if (st != STAR_OK) return st;
     }
     return launch(star_distillation_sums_kernel, dim3(1), kDistillSumThreads, 0, dim3(1), stream, static_cast<const float4 *>(a.partial),

@@ -37,12 +37,19 @@ struct alignas(16) DistillFactors {
     float m_rest;        // the largest element that is not listed
     float rest, rest1;   // dlogits[j] = rest 2^exponent(x, m_rest) + rest1 2^exponent1(x, m_rest)
     float m, s, s1;      // of the whole row
-    float shift, log_sum;        // of the teacher's list
+    float inv_s, log_s;
+    float rest_s;        // of what is not listed, at m_rest
+    float p0, q0;        // the probabilities of what is not listed, the student's and the teacher's; q0 of 0: no such term
     float mass;          // what the teacher's probabilities that count add up to
     float soft, hard;    // weight and coefficients in front of the gradient's parts
     int active;
     int late;            // a wait for the row ran out: nothing of it holds
 };
+
+// How the sum at temperature 1 is had: kOne, not at all (no label term, or temperature 1
+// itself); kTwo, by a power of its own; kSquare and kFourth, for temperatures of 2 and 4,
+// as the second and fourth power of the other one.
+enum Mode { kOne, kTwo, kSquare, kFourth };
 
 struct DistillSums {
     double loss, kl, ce, weight;
@@ -57,14 +64,6 @@ __device__ __forceinline__ float divergence(float q, float p, float d)
     return __fsub_rn(__fsub_rn(p, q), __fmul_rn(q, d));
 }
 
-// A teacher's list of one row, in shared memory.
-struct Listed {
-    int id[kMostListed];         // -1: absent
-    float value[kMostListed];
-    float x[kMostListed];        // the student's logit
-    int first[kMostListed];      // no entry in front has this id
-};
-
 // The same sum in every thread of a warp; NaNs stay.
 __device__ __forceinline__ double warp_sum_wide(double x)
 {
@@ -73,140 +72,151 @@ __device__ __forceinline__ double warp_sum_wide(double x)
     return x;
 }
 
-// What makes log-probabilities of the teacher's values v: (v - shift) / temperature -
-// log_sum, the difference first, as for the student's.  By a warp.  log_sum = -inf:
-// nothing is listed.
-struct Normalizer {
+// What a teacher's list says by itself.  (v - shift) / temperature - log_sum is the
+// log-probability of a value v, the difference first, as for the student's; log_sum =
+// -inf: nothing is listed.
+struct Teacher {
     float shift, log_sum;
+    float mass;          // of the listed
+    float missing;       // 1 - mass where the rest counts, else 0
 };
-__device__ __forceinline__ Normalizer list_normalizer(const DistillArgs &a, const Listed &list)
+__device__ __forceinline__ float listed_log(const DistillArgs &a, float v, const Teacher &t)
 {
-    if (a.rest) return Normalizer{0.0f, 0.0f};                   // log-probabilities already
-    const int lane = threadIdx.x % 32;
-    float v[kMostListed / 32], most = -INFINITY;
-    bool bad = false;
-#pragma unroll
-    for (int q = 0; q < kMostListed / 32; ++q) {
-        const int i = q * 32 + lane;
-        v[q] = i < a.k && list.id[i] >= 0 ? list.value[i] : -INFINITY;
-        bad |= v[q] != v[q];
-        most = fmaxf(most, v[q]);
-    }
-    most = warp_max(most);
-    if (__any_sync(0xffffffffu, bad) || most == INFINITY) return Normalizer{0.0f, NAN};
-    if (most == -INFINITY) return Normalizer{0.0f, -INFINITY};
-    float s = 0.0f;
-#pragma unroll
-    for (int q = 0; q < kMostListed / 32; ++q) s = __fadd_rn(s, expf(__fmul_rn(__fsub_rn(v[q], most), a.inv_teacher_temperature)));
-    return Normalizer{most, logf(warp_sum(s))};
-}
-__device__ __forceinline__ float listed_log(const DistillArgs &a, float v, float shift, float log_sum)
-{
-    return log_sum == -INFINITY ? -INFINITY : __fsub_rn(__fmul_rn(__fsub_rn(v, shift), a.inv_teacher_temperature), log_sum);
+    return t.log_sum == -INFINITY ? -INFINITY : __fsub_rn(__fmul_rn(__fsub_rn(v, t.shift), a.inv_teacher_temperature), t.log_sum);
 }
 
-// A row's factors and results from its statistics and its list, by a warp.
-__device__ __forceinline__ DistillFactors distill_row(const DistillArgs &a, const Listed &list, RestSums rest, bool wanted, float weight,
-                                                      float label_logit, Normalizer teacher, float *kl_out, float *ce_out)
+// A row's list, with a thread for each entry, and what else there is to know of a row
+// before its logits are there.
+constexpr int kListWarps = kMostListed / 32;
+struct Listed {
+    int4 id4[kMostListed / 4];   // -1 or less: absent
+    float value[kMostListed];    // the teacher's
+    int64_t asked_label;         // as given
+    float weight;
+    int label;                   // -1: none
+    float label_logit;
+    int wanted;                  // the label and the weight let the row take part
+    RestSums part[kListWarps];   // the student's statistics of the first entries of each id
+    float most[kListWarps];      // of the teacher's values: the largest, -inf, or NaN
+    double sum[kListWarps];      // of exp((value - most) / temperature)
+    float terms[kListWarps];     // of the loss
+    Teacher teacher;
+    int edge[32];                // who lists the elements beside the whole pieces; -1: nobody
+    int twice, has_label;        // an id is listed twice; the label is listed
+    __device__ __forceinline__ const int *ids() const { return reinterpret_cast<const int *>(id4); }
+};
+template <typename G> __device__ __forceinline__ void mark(void *row, int at, int n)
 {
-    const int lane = threadIdx.x % 32;
+    if constexpr (G::kBytes == 2)
+        static_cast<unsigned short *>(row)[at] = static_cast<unsigned short>(n);
+    else
+        static_cast<int *>(row)[at] = n;
+}
+template <typename G> __device__ __forceinline__ bool marked(const void *row, int at, int n)
+{
+    if constexpr (G::kBytes == 2)
+        return static_cast<const volatile unsigned short *>(row)[at] == n;
+    else
+        return static_cast<const volatile int *>(row)[at] == n;
+}
+// 4 or 8 bytes, asynchronously.
+template <int SIZE> __device__ __forceinline__ void copy_word(void *to, const void *from)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" :: "r"(smem_address(to)), "l"(from), "n"(SIZE) : "memory");
+}
+__device__ __forceinline__ void list_sync() { asm volatile("bar.sync 1, %0;" :: "n"(kMostListed) : "memory"); }
+
+// From the warps' parts.
+__device__ __forceinline__ Teacher make_teacher(const DistillArgs &a, const Listed &list)
+{
+    const int warps = (a.k + 31) / 32;
+    float shift = -INFINITY;
+    bool bad = false;
+    for (int w = 0; w < warps; ++w) {
+        bad |= list.most[w] != list.most[w];
+        shift = fmaxf(shift, list.most[w]);
+    }
+    if (bad || shift == INFINITY) return Teacher{0.0f, NAN, NAN, NAN};
+    if (shift == -INFINITY) return a.rest ? Teacher{0.0f, 0.0f, 0.0f, 1.0f} : Teacher{0.0f, -INFINITY, 0.0f, 0.0f};
+    double sum = 0.0;
+    for (int w = 0; w < warps; ++w)
+        if (list.most[w] > -INFINITY) sum += list.sum[w] * static_cast<double>(a.rest ? 1.0f : expf(__fmul_rn(__fsub_rn(list.most[w], shift), a.inv_teacher_temperature)));
+    if (a.rest) return Teacher{0.0f, 0.0f, static_cast<float>(sum), static_cast<float>(1.0 - sum)};      // log-probabilities already
+    return Teacher{shift, logf(static_cast<float>(sum)), 1.0f, 0.0f};
+}
+
+// A row's factors from its statistics without and of the listed elements, by a warp: what
+// the gradient waits for.
+template <int MODE>
+__device__ __forceinline__ DistillFactors make_factors(const DistillArgs &a, const Teacher &teacher, RestSums rest, RestSums listed, float weight)
+{
     const float inv_t = a.row.inv_temperature, k = __fmul_rn(inv_t, kLog2e);
-    const bool two = a.hard != 0.0f && inv_t != 1.0f;
     DistillFactors f{};
-    f.shift = teacher.shift;
-    f.log_sum = teacher.log_sum;
     f.m_rest = rest.m;
-    // The listed elements join the rest: an element once, however often it is listed.
-    float x[kMostListed / 32], most = rest.m;
-    bool present[kMostListed / 32], first[kMostListed / 32];
-#pragma unroll
-    for (int q = 0; q < kMostListed / 32; ++q) {
-        const int i = q * 32 + lane;
-        present[q] = i < a.k && list.id[i] >= 0;
-        first[q] = present[q] && list.first[i];
-        x[q] = present[q] ? list.x[i] : -INFINITY;
-        most = fmaxf(most, x[q]);
-    }
-    f.m = warp_max(most);
-    float s = 0.0f, s1 = 0.0f;
-#pragma unroll
-    for (int q = 0; q < kMostListed / 32; ++q) {
-        if (first[q]) {
-            s = __fadd_rn(s, exp2_fast(exponent(x[q], f.m, k)));
-            if (two) s1 = __fadd_rn(s1, exp2_fast(exponent(x[q], f.m, kLog2e)));
-        }
-    }
+    f.rest_s = rest.s;
+    f.m = fmaxf(rest.m, listed.m);
     const float down = rest.s == 0.0f ? 0.0f : rebase(rest.m, f.m, k);
     const float rest_s = __fmul_rn(rest.s, down);                // what is not listed, at the row's reference
-    f.s = __fadd_rn(warp_sum(s), rest_s);
-    float down1 = 0.0f;
-    if (two) {
-        down1 = rest.s == 0.0f ? 0.0f : rebase(rest.m, f.m, kLog2e);
-        f.s1 = __fadd_rn(warp_sum(s1), __fmul_rn(rest.s1, down1));
-    }
-    f.active = wanted && !(f.s == 0.0f) ? 1 : 0;
-    *kl_out = *ce_out = 0.0f;
-    if (!f.active) return f;
-    const MaxSum row{f.m, f.s};
-    // sum q log(q / p) as a sum of terms of one sign.  They add up to it if both
-    // distributions add up to 1; what they do not is put right at the end.
-    float terms = 0.0f, again = 0.0f;
-    double mass = 0.0;
-#pragma unroll
-    for (int q = 0; q < kMostListed / 32; ++q) {
-        if (present[q]) {
-            const float log_q = listed_log(a, list.value[q * 32 + lane], f.shift, f.log_sum), prob = expf(log_q);
-            const float log_p = log_prob(x[q], row, k, inv_t), p = expf(log_p);
-            mass += prob;
-            terms = __fadd_rn(terms, divergence(prob, p, __fsub_rn(log_p, log_q)));
-            if (!first[q]) again = __fadd_rn(again, p);
-        }
-    }
-    terms = warp_sum(terms);
-    again = warp_sum(again);
-    mass = warp_sum_wide(mass);
-    const float p0 = __fdiv_rn(rest_s, f.s);
-    float q0 = 0.0f, off;                                        // off: by how much the teacher's probabilities miss 1
-    if (a.rest) {
-        const double left = 1.0 - mass;
-        q0 = left > 0.0 && rest.s > 0.0f ? static_cast<float>(left) : 0.0f;
-        off = q0 > 0.0f ? 0.0f : static_cast<float>(-left);
-        f.mass = q0 > 0.0f ? 1.0f : static_cast<float>(mass);
-        if (mass != mass) f.mass = off = NAN;
-    } else {
-        f.mass = f.log_sum == -INFINITY ? 0.0f : f.log_sum != f.log_sum ? f.log_sum : 1.0f;
-        off = __fsub_rn(f.mass, 1.0f);
-    }
-    // log p0 by its parts: it exists where p0 itself is below binary32.
-    const float log_p0 = __fadd_rn(log_prob(rest.m, row, k, inv_t), logf(rest.s));
-    terms = __fadd_rn(terms, divergence(q0, p0, q0 > 0.0f ? __fsub_rn(log_p0, logf(q0)) : 0.0f));
-    const float kl = __fadd_rn(__fsub_rn(terms, again), off);
-    *kl_out = kl;
-    if (a.hard != 0.0f) *ce_out = -(two ? log_prob(label_logit, MaxSum{f.m, f.s1}, kLog2e, 1.0f) : log_prob(label_logit, row, k, inv_t));
-    // The gradient's factors.
+    f.s = __fadd_rn(__fmul_rn(listed.s, rebase(listed.m, f.m, k)), rest_s);
+    f.active = !(f.s == 0.0f);
+    f.inv_s = reciprocal_fast(f.s);                              // sums are near 1 or more
+    f.p0 = __fmul_rn(rest_s, f.inv_s);
+    f.q0 = teacher.missing > 0.0f && rest.s > 0.0f ? teacher.missing : 0.0f;
+    f.mass = f.q0 > 0.0f ? 1.0f : teacher.mass;
     f.soft = __fmul_rn(__fmul_rn(weight, a.soft), inv_t);
     f.hard = __fmul_rn(weight, a.hard);
-    float scale = 0.0f;
-    if (a.soft != 0.0f) {
-        scale = __fdiv_rn(__fmul_rn(f.mass, down), f.s);
-        if (q0 > 0.0f) scale = __fdiv_rn(__fsub_rn(__fmul_rn(f.mass, p0), q0), rest.s);
-        scale = __fmul_rn(f.soft, scale);
+    f.s1 = f.s;
+    if (a.soft != 0.0f)
+        f.rest = __fmul_rn(f.soft, f.q0 > 0.0f ? __fmul_rn(__fsub_rn(f.p0, f.q0), reciprocal_fast(rest.s)) : __fmul_rn(__fmul_rn(f.mass, down), f.inv_s));
+    if constexpr (MODE != kOne) {
+        const float down1 = rest.s == 0.0f ? 0.0f : rebase(rest.m, f.m, kLog2e);
+        f.s1 = __fadd_rn(__fmul_rn(listed.s1, rebase(listed.m, f.m, kLog2e)), __fmul_rn(rest.s1, down1));
+        f.rest1 = __fmul_rn(f.hard, __fmul_rn(down1, reciprocal_fast(f.s1)));
+    } else {
+        f.rest = __fmaf_rn(f.hard, __fmul_rn(down, f.inv_s), f.rest);
     }
-    if (a.hard != 0.0f) {
-        if (two)
-            f.rest1 = __fmul_rn(f.hard, __fdiv_rn(down1, f.s1));
-        else
-            scale = __fmaf_rn(f.hard, __fdiv_rn(down, f.s), scale);
-    }
-    f.rest = scale;
+    f.log_s = logf(f.s);
     return f;
 }
 
-// As take_batch, with the sum at temperature 1 where TWO.
-template <typename G, int N, int THREADS, bool FULL, bool TWO>
+// The two parts of an active row's loss, given the sum of the listed entries' terms.
+//
+// sum q log(q / p) is made of terms of one sign (divergence above).  They add up to it
+// if both distributions add up to 1; what they do not is put right at the end.
+__device__ __forceinline__ void row_loss(const DistillArgs &a, const Teacher &teacher, const DistillFactors &f, float terms, float label_logit, float *kl_out,
+                                         float *ce_out)
+{
+    const float inv_t = a.row.inv_temperature, k = __fmul_rn(inv_t, kLog2e);
+    const MaxSum row{f.m, f.s};
+    // log p0 by its parts: it exists where p0 itself is below binary32.
+    float d = 0.0f;
+    if (f.q0 > 0.0f) d = __fsub_rn(__fadd_rn(log_prob(f.m_rest, row, k, inv_t), logf(f.rest_s)), logf(f.q0));
+    const float off = f.q0 > 0.0f ? 0.0f : a.rest ? -teacher.missing : __fsub_rn(f.mass, 1.0f);      // the teacher's sum - 1
+    *kl_out = __fadd_rn(__fadd_rn(terms, divergence(f.q0, f.p0, d)), off);
+    *ce_out = 0.0f;
+    if (a.hard != 0.0f) {
+        const bool one = inv_t == 1.0f;
+        *ce_out = -log_prob(label_logit, MaxSum{f.m, one ? f.s : f.s1}, one ? k : kLog2e, 1.0f);
+    }
+}
+
+// The powers at both temperatures.
+template <int MODE> __device__ __forceinline__ void two_powers(Pair d, Pair k, Pair k1, Pair *p, Pair *p1)
+{
+    *p = pair_exp2(pair_mul(d, k));
+    if constexpr (MODE == kTwo) {
+        *p1 = pair_exp2(pair_mul(d, k1));
+    } else {
+        *p1 = pair_mul(*p, *p);
+        if constexpr (MODE == kFourth) *p1 = pair_mul(*p1, *p1);
+    }
+}
+
+// As take_batch, with the sum at temperature 1 where it is another.
+template <typename G, int N, int THREADS, bool FULL, int MODE>
 __device__ __forceinline__ void take_rest(RestSums *x, const uint4 *from, int left, float k)
 {
-    if constexpr (!TWO) {
+    if constexpr (MODE == kOne) {
         MaxSum y{x->m, x->s};
         take_batch<G, N, THREADS, FULL>(&y, from, left, k);
         x->m = y.m;
@@ -236,9 +246,10 @@ __device__ __forceinline__ void take_rest(RestSums *x, const uint4 *from, int le
                 Granule<G>::widen(v[q], f);
 #pragma unroll
                 for (int e = 0; e < P; ++e) {
-                    const Pair d = pair_add(f[e], minus_m);
-                    s = pair_add(s, pair_exp2(pair_mul(d, kk)));
-                    s1 = pair_add(s1, pair_exp2(pair_mul(d, k1)));
+                    Pair p, p1;
+                    two_powers<MODE>(pair_add(f[e], minus_m), kk, k1, &p, &p1);
+                    s = pair_add(s, p);
+                    s1 = pair_add(s1, p1);
                 }
             }
         }
@@ -253,10 +264,10 @@ __device__ __forceinline__ RestSums rest_move(RestSums x, float m, float k)
 {
     return RestSums{m, __fmul_rn(x.s, rebase(x.m, m, k)), __fmul_rn(x.s1, rebase(x.m, m, kLog2e))};
 }
-__device__ __forceinline__ RestSums warp_join(RestSums x, float k)
+template <int MODE> __device__ __forceinline__ RestSums warp_join(RestSums x, float k)
 {
-    x = rest_move(x, warp_max(x.m), k);
-    return RestSums{x.m, warp_sum(x.s), warp_sum(x.s1)};
+    const float m = warp_max(x.m);
+    return RestSums{m, warp_sum(__fmul_rn(x.s, rebase(x.m, m, k))), MODE == kOne ? 0.0f : warp_sum(__fmul_rn(x.s1, rebase(x.m, m, kLog2e)))};
 }
 __device__ __forceinline__ RestSums take_one(RestSums x, float v, float k)
 {
@@ -265,28 +276,36 @@ __device__ __forceinline__ RestSums take_one(RestSums x, float v, float k)
     return RestSums{m, __fadd_rn(x.s, exp2_fast(exponent(v, m, k))), __fadd_rn(x.s1, exp2_fast(exponent(v, m, kLog2e)))};
 }
 
-// The gradient of an element that is not listed.
-template <bool TWO> __device__ __forceinline__ float rest_gradient(float x, const DistillFactors &f, float k)
+// The gradient of an element that is not listed, from the factors that it takes.
+struct RestFactors {
+    float m, rest, rest1;
+};
+template <int MODE> __device__ __forceinline__ float rest_gradient(float x, const RestFactors &f, float k)
 {
-    const float g = __fmul_rn(f.rest, exp2_fast(exponent(x, f.m_rest, k)));
-    return TWO ? __fmaf_rn(f.rest1, exp2_fast(exponent(x, f.m_rest, kLog2e)), g) : g;
+    const float g = __fmul_rn(f.rest, exp2_fast(exponent(x, f.m, k)));
+    return MODE != kOne ? __fmaf_rn(f.rest1, exp2_fast(exponent(x, f.m, kLog2e)), g) : g;
 }
-template <typename G, int N, int THREADS, bool FULL>
-__device__ __forceinline__ void store_two(uint4 *to, const uint4 *from, int left, const DistillFactors &f, float k)
+template <typename G, int N, int THREADS, bool FULL, int MODE>
+__device__ __forceinline__ void store_rest(uint4 *to, const uint4 *from, int left, const RestFactors &f, float k)
 {
-    constexpr int P = Granule<G>::kPairs;
-    const Pair minus_m = pair_of(-pivot(f.m_rest)), kk = pair_of(k), k1 = pair_of(kLog2e), a = pair_of(f.rest), b = pair_of(f.rest1);
+    if constexpr (MODE == kOne) {
+        store_batch<G, N, THREADS, FULL>(to, from, left, Power(f.m, k), f.rest);
+    } else {
+        constexpr int P = Granule<G>::kPairs;
+        const Pair minus_m = pair_of(-pivot(f.m)), kk = pair_of(k), k1 = pair_of(kLog2e), a = pair_of(f.rest), b = pair_of(f.rest1);
 #pragma unroll
-    for (int q = 0; q < N; ++q) {
-        if (FULL || q * THREADS < left) {
-            Pair g[P];
-            Granule<G>::widen(from[q * THREADS], g);
+        for (int q = 0; q < N; ++q) {
+            if (FULL || q * THREADS < left) {
+                Pair g[P];
+                Granule<G>::widen(from[q * THREADS], g);
 #pragma unroll
-            for (int e = 0; e < P; ++e) {
-                const Pair d = pair_add(g[e], minus_m);
-                g[e] = pair_fma(b, pair_exp2(pair_mul(d, k1)), pair_mul(a, pair_exp2(pair_mul(d, kk))));
+                for (int e = 0; e < P; ++e) {
+                    Pair p, p1;
+                    two_powers<MODE>(pair_add(g[e], minus_m), kk, k1, &p, &p1);
+                    g[e] = pair_fma(b, p1, pair_mul(a, p));
+                }
+                to[q * THREADS] = Granule<G>::narrow(g);
             }
-            to[q * THREADS] = Granule<G>::narrow(g);
         }
     }
 }
@@ -304,23 +323,25 @@ __device__ __forceinline__ void store_two(uint4 *to, const uint4 *from, int left
 // ---------------------------------------------------------------------------
 constexpr int kDistillBytesPerThread = 208;  // shared memory for the row: 208 KB an SM
 
-template <typename G, int THREADS, bool TWO>
+template <typename G, int THREADS, int MODE>
 __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distillation_kernel(const __grid_constant__ DistillArgs a)
 {
     constexpr int E = Granule<G>::kCount, kWarps = THREADS / 32, kStep = kBatch * THREADS;
+    // The list's threads: not the first warp's, where there are others.
+    constexpr int kListFirst = THREADS > kMostListed ? 128 : 0;
     static_assert(THREADS >= kMostListed, "a thread to a listed element");
     extern __shared__ uint4 kept_row[];
     __shared__ RestSums warp_part[kWarps];
     __shared__ RestSums block_part[2][8];
     __shared__ DistillFactors factors;
     __shared__ DistillSums sums;
-    __shared__ Listed list;
-    __shared__ Normalizer teacher;
-    __shared__ float row_label_logit;
-    __shared__ int edge_listed[32];
+    __shared__ Listed lists[2];                                  // of every other row
     __shared__ int late[2];                                      // of every other row, as in the policy loss
     __shared__ alignas(8) uint64_t landed;                       // the row's copy is in place
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int at_list = static_cast<int>(threadIdx.x) - kListFirst, list_warp = at_list / 32;
+    const bool lists_it = at_list >= 0 && at_list < kMostListed;
+    const bool works = lists_it && list_warp * 32 < a.k;         // this warp has entries
     const float k = __fmul_rn(a.row.inv_temperature, kLog2e);
     const int vocab = static_cast<int>(a.row.vocab);
     const uint32_t blocks = cluster_size(), rank = cluster_rank();
@@ -329,21 +350,28 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
     launch_dependents();
     if (threadIdx.x == 0) {
         sums = DistillSums{0.0, 0.0, 0.0, 0.0};
-        late[0] = late[1] = factors.late = 0;
+        late[0] = late[1] = 0;
         barrier_init(smem_address(&landed), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (lists_it) {
+        for (Listed &list : lists) {                             // what no record brings
+            reinterpret_cast<int *>(list.id4)[at_list] = -1;
+            list.value[at_list] = -INFINITY;
+        }
+        if (at_list == 0) {
+            for (Listed &list : lists) {
+                list.asked_label = -1;
+                list.weight = 1.0f;
+                list.label_logit = 0.0f;
+            }
+        }
     }
     __syncthreads();
     if (blocks > 1) cluster_sync();                              // the others have started
     wait_for_primary();
 
     const auto row_base = [&](int64_t t) { return static_cast<const char *>(a.row.logits) + t * a.row.ld * G::kBytes; };
-    // Whether a row takes part, as far as its label and weight say.
-    const auto row_in = [&](int64_t t, int64_t *label, float *weight) {
-        *label = a.row.labels ? a.row.labels[t] : 0;
-        *weight = a.row.weights ? a.row.weights[t] : 1.0f;
-        return *label >= 0 && *label < vocab && *weight != 0.0f;
-    };
     // Thread 0: fetches the block's share of row t.
     const auto fetch = [&](int64_t t) {
         const char *base = row_base(t);
@@ -354,59 +382,99 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
         barrier_expect(bar, bytes);
         bulk_load(smem_address(kept_row), base + s.head * G::kBytes + static_cast<int64_t>(own.begin) * 16, bytes, bar);
     };
-    // A thread's entry of row t's list.
-    const auto entry = [&](int64_t t, int *id, float *value) {
-        *id = -1;
-        *value = 0.0f;
-        if (static_cast<int>(threadIdx.x) < a.k) {
-            const int given = a.ids[t * a.ld_ids + threadIdx.x];
-            if (given >= 0 && given < vocab) *id = given;
-            *value = a.values[t * a.ld_values + threadIdx.x];
+    // Row t's list, label and weight, into shared memory by the list's threads: under way ...
+    const auto ask = [&](int64_t t, Listed &list) {
+        if (!lists_it || t >= a.row.rows) return;
+        if (at_list < a.k) {
+            copy_word<4>(reinterpret_cast<int *>(list.id4) + at_list, a.ids + t * a.ld_ids + at_list);
+            copy_word<4>(list.value + at_list, a.values + t * a.ld_values + at_list);
+        }
+        if (at_list == 0) {
+            if (a.row.labels) copy_word<8>(&list.asked_label, a.row.labels + t);
+            if (a.row.weights) copy_word<4>(&list.weight, a.row.weights + t);
+        }
+    };
+    // No entry in front has its id.
+    const auto is_first = [&](const Listed &list, int id) {
+        bool first = true;
+        for (int i = 0; i < at_list; i += 4) {
+            const int4 other = list.id4[i / 4];
+            first &= other.x != id && (other.y != id || i + 1 >= at_list) && (other.z != id || i + 2 >= at_list) && (other.w != id || i + 3 >= at_list);
+        }
+        return first;
+    };
+    // ... and there: what the teacher's list says by itself, and a thread's entry's logit (or the label's, by
+    // the thread behind the list's last), which are then on their way.
+    const auto take_list = [&](int64_t t, Listed &list, float *x, float *label_logit) {
+        if (t >= a.row.rows) {
+            if (lists_it && at_list == 0) list.wanted = 0;
+            return;
+        }
+        if (!lists_it) return;
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        const char *base = row_base(t);
+        int id = list.ids()[at_list];
+        if (id >= vocab) {
+            id = -1;
+            reinterpret_cast<int *>(list.id4)[at_list] = -1;
+        }
+        if (id >= 0) *x = load_value<G>(base, id);
+        if (at_list < 32) list.edge[at_list] = -1;
+        if (at_list == 0) {
+            const int64_t asked = list.asked_label;
+            const int label = asked >= 0 && asked < vocab ? static_cast<int>(asked) : -1;
+            list.label = label;
+            list.wanted = (label >= 0 || !a.row.labels) && list.weight != 0.0f;
+            list.twice = list.has_label = 0;
+            if (label >= 0 && a.hard != 0.0f) *label_logit = load_value<G>(base, label);
+        }
+        if (works) {
+            const float v = id >= 0 ? list.value[at_list] : -INFINITY, most = warp_max(v);
+            const bool bad = __any_sync(0xffffffffu, v != v);
+            const float p = v > -INFINITY ? expf(__fmul_rn(a.rest ? v : __fsub_rn(v, most), a.inv_teacher_temperature)) : 0.0f;
+            const double sum = a.rest ? warp_sum_wide(p) : warp_sum(p);          // 1 - the sum cancels
+            if (lane == 0) {
+                list.most[list_warp] = bad ? NAN : most;
+                list.sum[list_warp] = sum;
+            }
+        }
+        list_sync();
+        if (id >= 0 && id == list.label) list.has_label = 1;
+        if (list_warp == 0) {
+            const Teacher teacher = make_teacher(a, list);
+            if (lane == 0) list.teacher = teacher;
+        }
+        if (blocks > 1 && id >= 0) {
+            const RowSplit s = split_row<G>(base, vocab);
+            if (id < s.head) list.edge[id] = at_list;
+            if (id >= vocab - s.tail) list.edge[s.head + id - (vocab - s.tail)] = at_list;
+            if (!is_first(list, id)) list.twice = 1;
         }
     };
 
     uint32_t phase = 0;
     int parity = 0;
-    for (int64_t t = first_row; t < a.row.rows; t += step, parity ^= 1) {
-        const char *base = row_base(t);
-        const RowSplit s = split_row<G>(base, vocab);
+    float x_own = 0.0f, label_logit = 0.0f;
+    ask(first_row, lists[0]);
+    take_list(first_row, lists[0], &x_own, &label_logit);
+    __syncthreads();
+    if (lists[0].wanted && threadIdx.x == 0) fetch(first_row);
+    int64_t t = first_row;
+    for (; t < a.row.rows; t += step, parity ^= 1) {
+        Listed &list = lists[parity], &next = lists[parity ^ 1];
+        const bool writes = a.dlogits != nullptr;
+        const auto out_of = [&] { return static_cast<char *>(a.dlogits) + t * a.ld_dlogits * G::kBytes; };
+        const auto same_phase = [&] { return (reinterpret_cast<uintptr_t>(out_of()) - reinterpret_cast<uintptr_t>(row_base(t))) % 16 == 0; };
+        const RowSplit s = split_row<G>(row_base(t), vocab);
         const RowShare own = row_share(s.granules, rank, log_blocks);
-        int64_t label;
-        float weight;
-        const bool wanted = row_in(t, &label, &weight);
-        if (wanted && threadIdx.x == 0) fetch(t);
         const int edge_at = rank == 0 ? edge_element(s, threadIdx.x, vocab) : -1;
-        float edge = 0.0f, x_own = 0.0f, value_own = 0.0f;
-        int id_own = -1;
-        bool first_own = false;
-        RestSums x{-INFINITY, 0.0f, 0.0f};
-        if (wanted) {
-            entry(t, &id_own, &value_own);
-            if (id_own >= 0) x_own = load_value<G>(base, id_own);
-            if (threadIdx.x < kMostListed) {
-                list.id[threadIdx.x] = id_own;
-                list.value[threadIdx.x] = value_own;
-                list.x[threadIdx.x] = x_own;
-            }
-            if (edge_at >= 0) edge = load_value<G>(base, edge_at);
-            if (threadIdx.x < 32) edge_listed[threadIdx.x] = 0;
-            if (threadIdx.x == 0) row_label_logit = a.row.labels ? load_value<G>(base, label) : 0.0f;
-        }
-        __syncthreads();                                         // the list
-        const int in_own = id_own - s.head - own.begin * E;      // where an id lies in this block's share
-        const bool in_share = id_own >= s.head && in_own >= 0 && in_own < own.count * E;
-        if (wanted) {
-            if (id_own >= 0) {
-                first_own = true;
-                for (int i = 0; i < static_cast<int>(threadIdx.x); ++i) first_own &= list.id[i] != id_own;
-                if (id_own < s.head) edge_listed[id_own] = 1;
-                if (id_own >= vocab - s.tail) edge_listed[s.head + id_own - (vocab - s.tail)] = 1;
-            }
-            if (threadIdx.x < kMostListed) list.first[threadIdx.x] = first_own;
-            if (warp == kWarps - 1) {
-                const Normalizer n = list_normalizer(a, list);
-                if (lane == 0) teacher = n;
-            }
+        bool active = false;
+        if (list.wanted) {
+            const float edge = edge_at >= 0 ? load_value<G>(row_base(t), edge_at) : 0.0f;
+            if (lists_it && at_list == 0) list.label_logit = label_logit;
+            // This thread's entry, and where it lies in the block's share.
+            const int id = lists_it ? list.ids()[at_list] : -1, in_own = id - s.head - own.begin * E;
+            const bool in_share = id >= s.head && in_own >= 0 && in_own < own.count * E;
             if (own.count > 0) {
                 if (!barrier_wait(smem_address(&landed), phase, a.tries)) {
                     late[parity] = 1;                            // what the walk below finds is not used
@@ -415,117 +483,159 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
                 }
                 phase ^= 1;
             }
-            if (in_share) store_value<G>(kept_row, in_own, -INFINITY);
-        }
-        __syncthreads();                                         // the listed elements are out of the row
-        if (wanted) {
-            const uint4 *from = kept_row + threadIdx.x;
-            int left = own.count - static_cast<int>(threadIdx.x);
-            for (; left > kStep - THREADS; left -= kStep, from += kStep) take_rest<G, kBatch, THREADS, true, TWO>(&x, from, left, k);
-            if (left > 0) take_rest<G, kBatch, THREADS, false, TWO>(&x, from, left, k);
-            if (edge_at >= 0 && !edge_listed[threadIdx.x]) x = take_one(x, edge, k);
-        }
-        x = warp_join(x, k);
-        if (lane == 0) warp_part[warp] = x;
-        __syncthreads();
-        if (warp == 0) x = warp_join(lane < kWarps ? warp_part[lane] : RestSums{-INFINITY, 0.0f, 0.0f}, k);
-        if (blocks > 1) {
-            if (warp == 0 && lane < static_cast<int>(blocks)) {
-                const uint32_t at = peer_address(smem_address(&block_part[parity][rank]), lane);
-                asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0 + 4], %2;\n\tst.shared::cluster.f32 [%0 + 8], %3;"
-                             :: "r"(at), "f"(x.m), "f"(x.s), "f"(x.s1) : "memory");
+            if (blocks == 1 && lists_it) {
+                // Whether an id is listed twice: each entry leaves its number in its element's place and looks who was last.
+                const int edge_of = id < 0 || in_share ? -1 : id < s.head ? id : s.head + id - (vocab - s.tail);
+                if (in_share) mark<G>(kept_row, in_own, at_list);
+                if (edge_of >= 0) list.edge[edge_of] = at_list;
+                list_sync();
+                if (in_share ? !marked<G>(kept_row, in_own, at_list) : edge_of >= 0 && list.edge[edge_of] != at_list) list.twice = 1;
             }
-            cluster_sync();
-            if (warp == 0) x = warp_join(lane < static_cast<int>(blocks) ? block_part[parity][lane] : RestSums{-INFINITY, 0.0f, 0.0f}, k);
-        }
-        if (warp == 0) {
-            float kl = 0.0f, ce = 0.0f;
-            DistillFactors f = distill_row(a, list, x, wanted, weight, wanted ? row_label_logit : 0.0f, wanted ? teacher : Normalizer{0.0f, 0.0f}, &kl, &ce);
-            f.late = late[parity];
-            if (lane == 0) {
-                factors = f;
-                if (rank == 0 && !f.late) {
-                    // A coefficient of exactly 0 takes its term out.
-                    const float soft = a.soft == 0.0f ? 0.0f : __fmul_rn(a.soft, kl), hard = a.hard == 0.0f ? 0.0f : __fmul_rn(a.hard, ce);
-                    const float loss = __fadd_rn(soft, hard);
-                    a.token_loss[t] = loss;
-                    if (f.active) {
-                        const double w = weight;
-                        sums.loss += w * loss;
-                        sums.kl += w * kl;
-                        sums.ce += w * ce;
-                        sums.weight += w;
-                    }
-                }
+            if (in_share) {
+                store_value<G>(kept_row, in_own, -INFINITY);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // before the next copy into its place
             }
-        }
-        __syncthreads();                                         // the factors
-        const DistillFactors f = factors;
-        if (f.late) break;
-        if (a.dlogits) {
-            char *out = static_cast<char *>(a.dlogits) + t * a.ld_dlogits * G::kBytes;
-            const bool same_phase = (reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(base)) % 16 == 0;
-            if (same_phase) {
-                uint4 *to = reinterpret_cast<uint4 *>(out + s.head * G::kBytes) + own.begin + threadIdx.x;
+            __syncthreads();                                     // the listed elements are out of the row
+            bool first = id >= 0;
+            if (works) {
+                if (list.twice && first) first = is_first(list, id);
+                const float one = first ? exp2_fast(exponent(x_own, x_own, k)) : 0.0f;           // 0 for -inf, NaN for a NaN
+                const RestSums part = warp_join<MODE>(RestSums{first ? x_own : -INFINITY, one, one}, k);
+                if (lane == 0) list.part[list_warp] = part;
+            }
+            ask(t + step, next);                                 // while the walk goes on
+            RestSums x{-INFINITY, 0.0f, 0.0f};
+            {
+                const uint4 *from = kept_row + threadIdx.x;
                 int left = own.count - static_cast<int>(threadIdx.x);
-                if (f.active) {
-                    const uint4 *from = kept_row + threadIdx.x;
-                    if constexpr (TWO) {
-                        for (; left > kStep - THREADS; left -= kStep, from += kStep, to += kStep) store_two<G, kBatch, THREADS, true>(to, from, left, f, k);
-                        if (left > 0) store_two<G, kBatch, THREADS, false>(to, from, left, f, k);
-                    } else {
-                        const Power power(f.m_rest, k);
-                        for (; left > kStep - THREADS; left -= kStep, from += kStep, to += kStep)
-                            store_batch<G, kBatch, THREADS, true>(to, from, left, power, f.rest);
-                        if (left > 0) store_batch<G, kBatch, THREADS, false>(to, from, left, power, f.rest);
-                    }
-                } else {
-                    for (; left > 0; left -= THREADS, to += THREADS) *to = make_uint4(0, 0, 0, 0);
-                }
-            } else {
-                for (int e = threadIdx.x; e < own.count * E; e += THREADS)
-                    store_value<G>(out, s.head + own.begin * E + e, f.active ? rest_gradient<TWO>(load_value<G>(kept_row, e), f, k) : 0.0f);
+                for (; left > kStep - THREADS; left -= kStep, from += kStep) take_rest<G, kBatch, THREADS, true, MODE>(&x, from, left, k);
+                if (left > 0) take_rest<G, kBatch, THREADS, false, MODE>(&x, from, left, k);
+                if (edge_at >= 0 && list.edge[threadIdx.x] < 0) x = take_one(x, edge, k);
             }
-            if (edge_at >= 0) store_value<G>(out, edge_at, f.active ? rest_gradient<TWO>(edge, f, k) : 0.0f);
-            __syncthreads();                                     // the row is read and written
-            if (f.active) {
-                // Who stores an element again: the block that has it.
-                const auto has = [&](int id) {
-                    const int at = id - s.head - own.begin * E;
-                    return id < s.head || id >= vocab - s.tail ? rank == 0 : at >= 0 && at < own.count * E;
-                };
-                const bool labelled = a.row.labels && f.hard != 0.0f;
-                if (first_own && has(id_own)) {
-                    float q = 0.0f;                              // of all entries with this id
-                    for (int i = threadIdx.x; i < a.k; ++i)
-                        if (list.id[i] == id_own) q = __fadd_rn(q, expf(listed_log(a, list.value[i], f.shift, f.log_sum)));
-                    const float p = expf(log_prob(x_own, MaxSum{f.m, f.s}, k, a.row.inv_temperature));
-                    float g = f.soft == 0.0f ? 0.0f : __fmul_rn(f.soft, __fmaf_rn(f.mass, p, -q));
+            x = warp_join<MODE>(x, k);
+            if (lane == 0) warp_part[warp] = x;
+            __syncthreads();
+            if (warp == 0) x = warp_join<MODE>(lane < kWarps ? warp_part[lane] : RestSums{-INFINITY, 0.0f, 0.0f}, k);
+            if (blocks > 1) {
+                if (warp == 0 && lane < static_cast<int>(blocks)) {
+                    const uint32_t at = peer_address(smem_address(&block_part[parity][rank]), lane);
+                    asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0 + 4], %2;\n\tst.shared::cluster.f32 [%0 + 8], %3;"
+                                 :: "r"(at), "f"(x.m), "f"(x.s), "f"(x.s1) : "memory");
+                }
+                cluster_sync();
+                if (warp == 0) x = warp_join<MODE>(lane < static_cast<int>(blocks) ? block_part[parity][lane] : RestSums{-INFINITY, 0.0f, 0.0f}, k);
+            }
+            if (warp == 0) {
+                const RestSums listed = warp_join<MODE>(lane * 32 < a.k ? list.part[lane] : RestSums{-INFINITY, 0.0f, 0.0f}, k);
+                DistillFactors f = make_factors<MODE>(a, list.teacher, x, listed, list.weight);
+                f.late = late[parity];
+                if (lane == 0) factors = f;
+            }
+            float x_next = 0.0f;
+            take_list(t + step, next, &x_next, &label_logit);    // while the others wait for the factors
+            __syncthreads();
+            const DistillFactors &f = factors;
+            if (f.late) break;
+            active = f.active;
+            const RestFactors g{f.m_rest, f.rest, f.rest1};
+            // The listed elements' gradients, and terms of the loss.
+            float listed_gradient = 0.0f;
+            if (active && works) {
+                float term = 0.0f;
+                if (id >= 0) {
+                    const float p = __fmul_rn(exp2_fast(exponent(x_own, f.m, k)), f.inv_s);
+                    const float log_q = listed_log(a, list.value[at_list], list.teacher);
+                    float q = expf(log_q);
+                    term = divergence(q, p, __fsub_rn(__fsub_rn(__fmul_rn(__fsub_rn(x_own, pivot(f.m)), a.row.inv_temperature), f.log_s), log_q));
+                    if (!first) term = __fsub_rn(term, p);       // its probability has been counted
+                    for (int i = at_list + 1; list.twice && i < a.k; ++i)        // q of all entries with this id
+                        if (list.ids()[i] == id) q = __fadd_rn(q, expf(listed_log(a, list.value[i], list.teacher)));
+                    if (f.soft != 0.0f) listed_gradient = __fmul_rn(f.soft, __fmaf_rn(f.mass, p, -q));
                     if (f.hard != 0.0f) {
-                        const float p1 = TWO ? expf(log_prob(x_own, MaxSum{f.m, f.s1}, kLog2e, 1.0f)) : p;
-                        g = __fmaf_rn(f.hard, __fsub_rn(p1, labelled && id_own == label ? 1.0f : 0.0f), g);
+                        const float p1 = MODE != kOne ? __fmul_rn(exp2_fast(exponent(x_own, f.m, kLog2e)), reciprocal_fast(f.s1)) : p;
+                        listed_gradient = __fmaf_rn(f.hard, __fsub_rn(p1, id == list.label ? 1.0f : 0.0f), listed_gradient);
                     }
-                    store_value<G>(out, id_own, g);
                 }
-                // The label, where it is not listed.
-                if (labelled && warp == kWarps - 1 && has(static_cast<int>(label))) {
-                    bool listed = false;
-                    for (int i = lane; i < a.k; i += 32) listed |= list.id[i] == label;
-                    if (!__any_sync(0xffffffffu, listed) && lane == 0)
-                        store_value<G>(out, label, __fsub_rn(rest_gradient<TWO>(row_label_logit, f, k), f.hard));
+                term = warp_sum(term);
+                if (lane == 0) list.terms[list_warp] = term;
+            }
+            x_own = x_next;
+            if (writes && active) {
+                char *out = out_of();
+                if (same_phase()) {
+                    uint4 *to = reinterpret_cast<uint4 *>(out + s.head * G::kBytes) + own.begin + threadIdx.x;
+                    int left = own.count - static_cast<int>(threadIdx.x);
+                    const uint4 *from = kept_row + threadIdx.x;
+                    for (; left > kStep - THREADS; left -= kStep, from += kStep, to += kStep) store_rest<G, kBatch, THREADS, true, MODE>(to, from, left, g, k);
+                    if (left > 0) store_rest<G, kBatch, THREADS, false, MODE>(to, from, left, g, k);
+                } else {
+                    for (int i = threadIdx.x; i < own.count * E; i += THREADS)
+                        store_value<G>(out, s.head + own.begin * E + i, rest_gradient<MODE>(load_value<G>(kept_row, i), g, k));
+                }
+                if (edge_at >= 0) store_value<G>(out, edge_at, rest_gradient<MODE>(edge, g, k));
+            }
+            __syncthreads();                                     // the row is read and written
+            if (next.wanted && threadIdx.x == 0) fetch(t + step);
+            // While that is on its way: the listed elements and the label again, and the row's loss.
+            if (writes && active) {
+                char *out = out_of();
+                // Who stores an element again: the block that has it.
+                const auto has = [&](int i) {
+                    const int at = i - s.head - own.begin * E;
+                    return i < s.head || i >= vocab - s.tail ? rank == 0 : at >= 0 && at < own.count * E;
+                };
+                if (first && has(id)) store_value<G>(out, id, listed_gradient);
+                if (threadIdx.x == THREADS - 1 && list.label >= 0 && f.hard != 0.0f && !list.has_label && has(list.label))
+                    store_value<G>(out, list.label, __fsub_rn(rest_gradient<MODE>(list.label_logit, g, k), f.hard));
+            }
+            if (rank == 0 && threadIdx.x == 32) {
+                float kl = 0.0f, ce = 0.0f;
+                if (active) {
+                    float terms = 0.0f;
+                    for (int w = 0; w * 32 < a.k; ++w) terms = __fadd_rn(terms, list.terms[w]);
+                    row_loss(a, list.teacher, f, terms, list.label_logit, &kl, &ce);
+                }
+                // A coefficient of exactly 0 takes its term out.
+                const float loss = __fadd_rn(a.soft == 0.0f ? 0.0f : __fmul_rn(a.soft, kl), a.hard == 0.0f ? 0.0f : __fmul_rn(a.hard, ce));
+                a.token_loss[t] = loss;
+                if (active) {
+                    const double w = list.weight;
+                    sums.loss += w * loss;
+                    sums.kl += w * kl;
+                    sums.ce += w * ce;
+                    sums.weight += w;
                 }
             }
+        } else {
+            __syncthreads();                                     // the last row's list has been read
+            ask(t + step, next);
+            if (threadIdx.x == 0 && rank == 0) a.token_loss[t] = 0.0f;
         }
-        // The row's memory and list are free: what was written over the row comes before the next copy.
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncthreads();
+        if (writes && !active) {
+            char *out = out_of();
+            if (same_phase()) {
+                uint4 *to = reinterpret_cast<uint4 *>(out + s.head * G::kBytes) + own.begin;
+                for (int i = threadIdx.x; i < own.count; i += THREADS) to[i] = make_uint4(0, 0, 0, 0);
+            } else {
+                for (int i = threadIdx.x; i < own.count * E; i += THREADS) store_value<G>(out, s.head + own.begin * E + i, 0.0f);
+            }
+            if (edge_at >= 0) store_value<G>(out, edge_at, 0.0f);
+        }
+        if (!list.wanted) {
+            take_list(t + step, next, &x_own, &label_logit);
+            __syncthreads();
+            if (next.wanted && threadIdx.x == 0) fetch(t + step);
+        }
     }
-    if (threadIdx.x == 0 && factors.late) {
-        barrier_wait(smem_address(&landed), phase ^ 1, kWaitTries);      // the copy in flight, if any
-        sums.loss = sums.kl = sums.ce = sums.weight = NAN;
+    __syncthreads();                                             // the sums
+    if (threadIdx.x == 0) {
+        if (t < a.row.rows) {                                    // a wait ran out
+            barrier_wait(smem_address(&landed), phase ^ 1, kWaitTries);  // the copy in flight, if any
+            sums.loss = sums.kl = sums.ce = sums.weight = NAN;
+        }
+        if (rank == 0)
+            a.partial[first_row] = make_float4(static_cast<float>(sums.loss), static_cast<float>(sums.kl), static_cast<float>(sums.ce), static_cast<float>(sums.weight));
     }
-    if (threadIdx.x == 0 && rank == 0)
-        a.partial[first_row] = make_float4(static_cast<float>(sums.loss), static_cast<float>(sums.kl), static_cast<float>(sums.ce), static_cast<float>(sums.weight));
     if (blocks > 1) cluster_sync();                              // nobody leaves while a peer writes to its memory
 }
 

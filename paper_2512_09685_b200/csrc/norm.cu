@@ -2,9 +2,11 @@
 // the launches.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "checkpoint_host.h"
 #include "norm.cuh"
+#include "rows_host.h"
 
 namespace {
 
@@ -28,6 +30,66 @@ star_status_t check_optional_kept(const int8_t *codes, const uint8_t *scales, in
     at[0] = at[1] = Extent{};
     if (!codes && !scales) return STAR_OK;
     return check_kept(codes, scales, rows, cols, out, at);
+}
+
+// Whether every row of an optional matrix starts on a boundary of `bytes`.
+bool on_grid(const void *p, int64_t ld, int size, int bytes)
+{
+    return !p || (reinterpret_cast<uintptr_t>(p) % static_cast<unsigned>(bytes) == 0 && (ld * size) % bytes == 0);
+}
+
+constexpr int kBackEach = 2;
+
+// The threads that share a row, `each` columns to one: the next power of two.  0: a
+// row is too long for a block.
+int row_threads(int64_t cols, int each)
+{
+    for (int t : {32, 64, 128, 256, 512, 1024})
+        if (cols <= int64_t{t} * each) return t;
+    return 0;
+}
+
+template <typename F> star_status_t with_threads(int threads, F f)
+{
+    switch (threads) {
+    case 32: return f(std::integral_constant<int, 32>());
+    case 64: return f(std::integral_constant<int, 64>());
+    case 128: return f(std::integral_constant<int, 128>());
+    case 256: return f(std::integral_constant<int, 256>());
+    case 512: return f(std::integral_constant<int, 512>());
+    default: return f(std::integral_constant<int, 1024>());
+    }
+}
+
+template <typename G, int EACH> star_status_t run_norm(const NormArgs &a, int threads, cudaStream_t stream)
+{
+    if (threads == 0)
+        return launch(star_rms_norm_loose_kernel<G>, dim3(static_cast<unsigned>(std::min<int64_t>(a.rows, 148 * 32))), kNormThreads, 0, dim3(1), stream, a);
+    return with_threads(threads, [&](auto t) {
+        constexpr int kThreads = decltype(t)::value, kBlock = norm_block(kThreads);
+        const int64_t blocks = (a.rows * kThreads + kBlock - 1) / kBlock;
+        return launch(star_rms_norm_kernel<G, kThreads, EACH>, dim3(static_cast<unsigned>(std::min<int64_t>(blocks, 148 * 32))), kBlock, 0, dim3(1), stream, a);
+    });
+}
+
+template <typename G, bool KEPT> star_status_t run_backward(const NormGradArgs &a, int threads, int64_t *parts, cudaStream_t stream)
+{
+    if (threads == 0) {
+        *parts = std::min(a.rows, kMostParts);
+        return launch(star_rms_norm_backward_loose_kernel<G>, dim3(static_cast<unsigned>(*parts)), kNormThreads, 0, dim3(1), stream, a);
+    }
+    return with_threads(threads, [&](auto t) {
+        constexpr int kThreads = decltype(t)::value, kBlock = norm_block(kThreads);
+        constexpr int kStages = G::kBytes == 4 && kThreads <= 512 ? 3 : 2;
+        constexpr int kKib = (NormRing<G, KEPT, kBackEach, kStages>::kThread * kBlock + 1023) / 1024;
+        static Held known;
+        int held = 0;
+        constexpr auto kernel = star_rms_norm_backward_kernel<G, KEPT, kThreads, kBackEach, kStages>;
+        const cudaError_t e = held_clusters(kernel, known, kBlock, 1, kKib, &held);
+        if (e != cudaSuccess) return cuda_failed(e);
+        *parts = std::min<int64_t>({(a.rows * kThreads + kBlock - 1) / kBlock, held, kMostParts});
+        return launch(kernel, dim3(static_cast<unsigned>(*parts)), kBlock, kKib * 1024, dim3(1), stream, a);
+    });
 }
 
 bool same(const void *a, int64_t ld_a, const void *b, int64_t ld_b, int64_t rows) { return a == b && (ld_a == ld_b || rows <= 1); }
@@ -73,15 +135,17 @@ extern "C" star_status_t star_rms_norm(void *y, int64_t ld_y, const void *x, int
     a.rows = rows;
     a.cols = static_cast<int>(cols);
     a.eps = eps;
-    a.inv_cols = static_cast<float>(1.0 / static_cast<double>(cols));
+    a.inv_cols = 1.0 / static_cast<double>(cols);
+    a.gain_wide = gain_dtype == STAR_DTYPE_F32;
+    const auto grid = [&](int bytes) {
+        return on_grid(x, ld_x, size, bytes) && on_grid(residual, ld_residual, size, bytes) && on_grid(total, ld_total, size, bytes) &&
+               on_grid(y, ld_y, size, bytes);
+    };
+    a.wide = grid(32);
+    const int each = cols <= 4096 ? 1 : 2, threads = grid(16) ? row_threads(cols, each * 16) : 0;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    const dim3 grid(static_cast<unsigned>(std::min<int64_t>(rows, 148 * 32)));
-    const bool wide_gain = gain_dtype == STAR_DTYPE_F32;
-    if (dtype == STAR_DTYPE_BF16)
-        return wide_gain ? launch(star_rms_norm_loose_kernel<GradBF16, GradF32>, grid, kNormThreads, 0, dim3(1), stream, a)
-                         : launch(star_rms_norm_loose_kernel<GradBF16, GradBF16>, grid, kNormThreads, 0, dim3(1), stream, a);
-    return wide_gain ? launch(star_rms_norm_loose_kernel<GradF32, GradF32>, grid, kNormThreads, 0, dim3(1), stream, a)
-                     : launch(star_rms_norm_loose_kernel<GradF32, GradBF16>, grid, kNormThreads, 0, dim3(1), stream, a);
+    if (each == 1) return dtype == STAR_DTYPE_BF16 ? run_norm<GradBF16, 1>(a, threads, stream) : run_norm<GradF32, 1>(a, threads, stream);
+    return dtype == STAR_DTYPE_BF16 ? run_norm<GradBF16, 2>(a, threads, stream) : run_norm<GradF32, 2>(a, threads, stream);
 }
 
 extern "C" star_status_t star_rms_norm_workspace_bytes(int64_t rows, int64_t cols, size_t *bytes_out)
@@ -141,25 +205,28 @@ extern "C" star_status_t star_rms_norm_backward(void *dx, int64_t ld_dx, void *d
     a.ld_d_total = ld_d_total;
     a.rows = rows;
     a.cols = static_cast<int>(cols);
-    a.inv_cols = static_cast<float>(1.0 / static_cast<double>(cols));
+    a.inv_cols = 1.0 / static_cast<double>(cols);
+    a.gain_wide = gain_dtype == STAR_DTYPE_F32;
     a.partial = dgain ? static_cast<float *>(workspace) : nullptr;
+    const auto grid = [&](int bytes) {
+        return on_grid(dx, ld_dx, size, bytes) && on_grid(dy, ld_dy, size, bytes) && on_grid(total, ld_total, size, bytes) &&
+               on_grid(d_total, ld_d_total, size, bytes);
+    };
+    a.wide = grid(32);
+    const int threads = grid(16) ? row_threads(cols, kBackEach * 16 / size) : 0;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    const int64_t parts = std::min(rows, kMostParts);
+    int64_t parts = 0;
     if (rows > 0) {
-        const dim3 grid(static_cast<unsigned>(parts));
-        const bool wide_gain = gain_dtype == STAR_DTYPE_F32;
         if (dtype == STAR_DTYPE_BF16)
-            st = wide_gain ? launch(star_rms_norm_backward_loose_kernel<GradBF16, GradF32>, grid, kNormThreads, 0, dim3(1), stream, a)
-                           : launch(star_rms_norm_backward_loose_kernel<GradBF16, GradBF16>, grid, kNormThreads, 0, dim3(1), stream, a);
+            st = total ? run_backward<GradBF16, false>(a, threads, &parts, stream) : run_backward<GradBF16, true>(a, threads, &parts, stream);
         else
-            st = wide_gain ? launch(star_rms_norm_backward_loose_kernel<GradF32, GradF32>, grid, kNormThreads, 0, dim3(1), stream, a)
-                           : launch(star_rms_norm_backward_loose_kernel<GradF32, GradBF16>, grid, kNormThreads, 0, dim3(1), stream, a);
+            st = total ? run_backward<GradF32, false>(a, threads, &parts, stream) : run_backward<GradF32, true>(a, threads, &parts, stream);
         if (st != STAR_OK) return st;
     }
     if (!dgain) return STAR_OK;
-    const dim3 grid(static_cast<unsigned>(std::min<int64_t>((cols + 31) / 32, 148 * 16)));
+    const dim3 gain_grid(static_cast<unsigned>(std::min<int64_t>((cols + 31) / 32, 148 * 16)));
     const float *partial = static_cast<const float *>(workspace);
     return dgain_dtype == STAR_DTYPE_BF16
-               ? launch(star_rms_norm_gain_kernel<GradBF16>, grid, kGainThreads, 0, dim3(1), stream, partial, parts, a.cols, dgain, accumulate)
-               : launch(star_rms_norm_gain_kernel<GradF32>, grid, kGainThreads, 0, dim3(1), stream, partial, parts, a.cols, dgain, accumulate);
+               ? launch(star_rms_norm_gain_kernel<GradBF16>, gain_grid, kGainThreads, 0, dim3(1), stream, partial, parts, a.cols, dgain, accumulate)
+               : launch(star_rms_norm_gain_kernel<GradF32>, gain_grid, kGainThreads, 0, dim3(1), stream, partial, parts, a.cols, dgain, accumulate);
 }

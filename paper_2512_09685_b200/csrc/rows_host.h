@@ -10,7 +10,7 @@
 
 namespace star {
 
-constexpr int kMostKib = 224;        // shared memory of a block that keeps a row
+constexpr int kMostKib = 224;        // shared memory of a block that keeps a row, beside little of its own
 
 constexpr int kMaxDevices = 64;
 
@@ -21,7 +21,7 @@ struct Held {
     std::atomic<int> clusters[kMaxDevices][4][kMostKib + 1];
 };
 
-template <typename Kernel> inline cudaError_t held_clusters(Kernel kernel, Held &known, int threads, int cluster, int kib, int *out)
+template <typename Kernel> inline cudaError_t held_clusters(Kernel kernel, Held &known, int threads, int cluster, int kib, int *out, int most_kib = kMostKib)
 {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -30,7 +30,7 @@ template <typename Kernel> inline cudaError_t held_clusters(Kernel kernel, Held 
     std::atomic<int> &slot = known.clusters[dev][cluster == 1 ? 0 : cluster == 2 ? 1 : cluster == 4 ? 2 : 3][kib];
     int n = slot.load(std::memory_order_relaxed);
     if (n == 0) {
-        if (kib > 0) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostKib * 1024);
+        if (kib > 0) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most_kib * 1024);
         if (e != cudaSuccess) return e;
         if (cluster == 1) {
             int sms = 0, per_sm = 0;
