@@ -933,18 +933,26 @@ def star_preference_loss(logits: torch.Tensor, labels: torch.Tensor, seq_offsets
 STAR_MAX_ALTERNATIVES = 128
 
 
-def _listed(t: Optional[torch.Tensor], rows: int, k: int, what: str, dtype) -> Tuple[Optional[int], int]:
+def _like(t: torch.Tensor, what: str, shape, dtype) -> Tuple[int, int]:
+    """(address, row stride) of a matrix of a shape and dtype that another argument gave."""
+    if t.shape == shape and t.dtype is dtype and t.is_cuda:
+        ld, step = t.stride()
+        if step == 1 and ld >= shape[1]:
+            return t.data_ptr(), ld
+    p, _, ld = _matrix(t, what, tuple(shape), dtype)
+    return p, ld
+
+
+def _listed(t: torch.Tensor, rows: int, k: int, what: str, dtype) -> Tuple[int, int]:
     """(address, row stride) of a rows x k matrix of a teacher's or of top entries."""
-    if t is None:
-        return None, k
     if t.dtype is not dtype or t.dim() != 2 or not t.is_cuda:
         raise TypeError("%s must be a 2-D %s CUDA tensor" % (what, dtype))
-    if tuple(t.shape) != (rows, k):
+    if t.shape != (rows, k):
         raise ValueError("%s has shape %s, expected %s" % (what, tuple(t.shape), (rows, k)))
     ld, step = t.stride()
     if (step != 1 and k > 1) or (ld < k and rows > 1):
         raise TypeError("%s must have contiguous rows that do not overlap" % what)
-    return t.data_ptr(), max(ld, k)
+    return t.data_ptr(), ld if ld > k else k
 
 
 def star_token_alternatives(logits: torch.Tensor, top_ids: Optional[torch.Tensor] = None,
@@ -953,17 +961,20 @@ def star_token_alternatives(logits: torch.Tensor, top_ids: Optional[torch.Tensor
                             entropy: Optional[torch.Tensor] = None, temperature: float = 1.0, stream=None) -> None:
     """The largest logits' ids (int32, rows x k) and log-probabilities, with lse,
     entropy and the labels' logp where asked for; without labels every row takes part."""
-    rows, vocab = logits.shape
     x, dtype, ld = _matrix(logits, "logits")
-    if (top_ids is None) != (top_logp is None):
+    rows, vocab = logits.shape
+    k = ld_top = 0
+    ids = top = None
+    if top_ids is not None and top_logp is not None:
+        k = top_ids.shape[-1]
+        ids, ld_top = _listed(top_ids, rows, k, "top_ids", torch.int32)
+        top, ld_logp = _listed(top_logp, rows, k, "top_logp", torch.float32)
+        if ld_logp != ld_top and rows > 1:
+            raise ValueError("top_ids and top_logp must have one row stride")
+    elif top_ids is not top_logp:
         raise ValueError("top_ids and top_logp come together")
-    k = 0 if top_ids is None else top_ids.shape[-1]
-    ids, ld_ids = _listed(top_ids, rows, k, "top_ids", torch.int32)
-    top, ld_top = _listed(top_logp, rows, k, "top_logp", torch.float32)
-    if ld_ids != ld_top and rows > 1:
-        raise ValueError("top_ids and top_logp must have one row stride")
     _check(_lib.star_token_alternatives(x, dtype, rows, vocab, ld, _vector(labels, rows, "labels", torch.int64), temperature, k,
-                                        ids, top, max(ld_ids, ld_top), _vector(logp, rows, "logp"), _vector(lse, rows, "lse"),
+                                        ids, top, ld_top, _vector(logp, rows, "logp"), _vector(lse, rows, "lse"),
                                         _vector(entropy, rows, "entropy"), _stream(stream)), "star_token_alternatives")
 
 
@@ -974,14 +985,18 @@ def star_token_alternatives_backward(dlogits: torch.Tensor, logits: torch.Tensor
                                      temperature: float = 1.0, stream=None) -> None:
     """The gradient of the logits (which it may replace) from those of
     star_token_alternatives' results, with that call's lse and entropy."""
-    rows, vocab = logits.shape
     x, dtype, ld = _matrix(logits, "logits")
-    d, _, ld_d = _matrix(dlogits, "dlogits", (rows, vocab), logits.dtype)
-    if (top_ids is None) != (d_top_logp is None):
+    shape = logits.shape
+    rows, vocab = shape
+    d, ld_d = _like(dlogits, "dlogits", shape, logits.dtype)
+    k = ld_ids = ld_top = 0
+    ids = top = None
+    if top_ids is not None and d_top_logp is not None:
+        k = top_ids.shape[-1]
+        ids, ld_ids = _listed(top_ids, rows, k, "top_ids", torch.int32)
+        top, ld_top = _listed(d_top_logp, rows, k, "d_top_logp", torch.float32)
+    elif top_ids is not d_top_logp:
         raise ValueError("top_ids and d_top_logp come together")
-    k = 0 if top_ids is None else top_ids.shape[-1]
-    ids, ld_ids = _listed(top_ids, rows, k, "top_ids", torch.int32)
-    top, ld_top = _listed(d_top_logp, rows, k, "d_top_logp", torch.float32)
     _check(_lib.star_token_alternatives_backward(d, ld_d, x, dtype, rows, vocab, ld, _vector(labels, rows, "labels", torch.int64),
                                                  temperature, _vector(lse, rows, "lse"), _vector(entropy, rows, "entropy"),
                                                  _vector(d_logp, rows, "d_logp"), _vector(d_entropy, rows, "d_entropy"), k, ids,
@@ -996,14 +1011,15 @@ def star_distillation_loss(logits: torch.Tensor, teacher_ids: torch.Tensor, teac
     """Distillation from a teacher's k ids and values a row (logits, or with
     ``rest`` log-probabilities whose remainder counts too): token_loss, the four
     sums and, unless None, the gradient of the logits (which may be the logits)."""
-    rows, vocab = logits.shape
     x, dtype, ld = _matrix(logits, "logits")
-    d, _, ld_d = (None, dtype, vocab) if dlogits is None else _matrix(dlogits, "dlogits", (rows, vocab), logits.dtype)
+    shape = logits.shape
+    rows, vocab = shape
+    d, ld_d = (None, vocab) if dlogits is None else _like(dlogits, "dlogits", shape, logits.dtype)
     k = teacher_ids.shape[-1]
     ids, ld_ids = _listed(teacher_ids, rows, k, "teacher_ids", torch.int32)
     values, ld_values = _listed(teacher_values, rows, k, "teacher_values", torch.float32)
     ws, ws_bytes = _workspace(workspace)
-    _check(_lib.star_distillation_loss(x, dtype, rows, vocab, ld, ids, ld_ids, values, ld_values, k, int(rest), teacher_temperature,
+    _check(_lib.star_distillation_loss(x, dtype, rows, vocab, ld, ids, ld_ids, values, ld_values, k, rest, teacher_temperature,
                                        _vector(labels, rows, "labels", torch.int64), _vector(weights, rows, "weights"), temperature,
                                        soft_coef, label_coef, _vector(token_loss, rows, "token_loss"), _vector(sums, 4, "sums"), d,
                                        ld_d, ws, ws_bytes, _stream(stream)), "star_distillation_loss")
@@ -1085,16 +1101,11 @@ def _gain(t: Optional[torch.Tensor], cols: int, what: str) -> Tuple[Optional[int
     """(address, dtype code) of a vector of float32 or bfloat16."""
     if t is None:
         return None, STAR_DTYPE_F32
-    if t.dtype not in _DTYPES:
+    kind = t.dtype
+    code = _DTYPES.get(kind)
+    if code is None:
         raise TypeError("%s must be a contiguous float32 or bfloat16 CUDA tensor" % what)
-    return _vector(t, cols, what, t.dtype), _DTYPES[t.dtype]
-
-
-def _optional_matrix(t: Optional[torch.Tensor], what: str, shape, dtype) -> Tuple[Optional[int], int]:
-    if t is None:
-        return None, shape[1]
-    p, _, ld = _matrix(t, what, shape, dtype)
-    return p, ld
+    return _vector(t, cols, what, kind), code
 
 
 def _optional_kept(codes, scales, rows: int, cols: int) -> Tuple[Optional[int], Optional[int]]:
@@ -1109,13 +1120,14 @@ def star_rms_norm(y: torch.Tensor, x: torch.Tensor, gain: Optional[torch.Tensor]
                   stream=None) -> None:
     """y = the root-mean-square norm of x + residual; the sum goes to total (which may
     be x or the residual), and y is kept in 8 bits in codes and scales, where given."""
-    rows, cols = x.shape
     p, dtype, ld = _matrix(x, "x")
-    o, _, ld_o = _matrix(y, "y", (rows, cols), x.dtype)
-    r, ld_r = _optional_matrix(residual, "residual", (rows, cols), x.dtype)
-    s, ld_s = _optional_matrix(total, "total", (rows, cols), x.dtype)
+    shape, kind = x.shape, x.dtype
+    rows, cols = shape
+    o, ld_o = _like(y, "y", shape, kind)
+    r, ld_r = (None, cols) if residual is None else _like(residual, "residual", shape, kind)
+    s, ld_s = (None, cols) if total is None else _like(total, "total", shape, kind)
     g, g_dtype = _gain(gain, cols, "gain")
-    q, b = _optional_kept(codes, scales, rows, cols)
+    q, b = (None, None) if codes is None and scales is None else _optional_kept(codes, scales, rows, cols)
     _check(_lib.star_rms_norm(o, ld_o, p, ld, r, ld_r, s, ld_s, dtype, rows, cols, g, g_dtype, eps, _vector(rstd, rows, "rstd"),
                               q, b, _stream(stream)), "star_rms_norm")
 
@@ -1132,16 +1144,17 @@ def star_rms_norm_backward(dx: torch.Tensor, dgain: Optional[torch.Tensor], dy: 
                            d_total: Optional[torch.Tensor] = None, accumulate: bool = False, stream=None) -> None:
     """dx (which may be dy or d_total) and, unless None, dgain = or += its sums, from
     the normalized stream: total, or a checkpoint of it in codes and scales."""
-    rows, cols = dy.shape
     p, dtype, ld = _matrix(dy, "dy")
-    d, _, ld_d = _matrix(dx, "dx", (rows, cols), dy.dtype)
-    s, ld_s = _optional_matrix(total, "total", (rows, cols), dy.dtype)
-    e, ld_e = _optional_matrix(d_total, "d_total", (rows, cols), dy.dtype)
+    shape, kind = dy.shape, dy.dtype
+    rows, cols = shape
+    d, ld_d = _like(dx, "dx", shape, kind)
+    s, ld_s = (None, cols) if total is None else _like(total, "total", shape, kind)
+    e, ld_e = (None, cols) if d_total is None else _like(d_total, "d_total", shape, kind)
     g, g_dtype = _gain(gain, cols, "gain")
     dg, dg_dtype = _gain(dgain, cols, "dgain")
-    q, b = _optional_kept(codes, scales, rows, cols)
+    q, b = (None, None) if codes is None and scales is None else _optional_kept(codes, scales, rows, cols)
     ws, ws_bytes = (None, 0) if workspace is None else _workspace(workspace)
-    _check(_lib.star_rms_norm_backward(d, ld_d, dg, dg_dtype, int(accumulate), p, ld, s, ld_s, q, b, e, ld_e, dtype, rows, cols, g,
+    _check(_lib.star_rms_norm_backward(d, ld_d, dg, dg_dtype, accumulate, p, ld, s, ld_s, q, b, e, ld_e, dtype, rows, cols, g,
                                        g_dtype, _vector(rstd, rows, "rstd"), ws, ws_bytes, _stream(stream)),
            "star_rms_norm_backward")
 

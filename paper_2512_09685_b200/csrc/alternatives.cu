@@ -18,6 +18,40 @@ star_status_t check_top(const void *p, int64_t rows, int k, int64_t ld, Extent *
     return k > 0 ? check_matrix(p, rows, k, ld, 4, out) : STAR_OK;
 }
 
+template <typename G, int THREADS, bool CLUSTER> star_status_t launch_rows(const AlternativesArgs &a, int cluster, cudaStream_t stream)
+{
+    const int64_t clusters = std::min<int64_t>(a.row.rows, int64_t{1} << 20);
+    return launch(star_alternatives_kernel<G, THREADS, CLUSTER>, dim3(static_cast<unsigned>(clusters * cluster)), THREADS, 0,
+                  dim3(static_cast<unsigned>(cluster)), stream, a);
+}
+
+// Threads to a row: few for short rows, as for the rows' statistics (walk_rows of the
+// losses), but at least two groups of them to an alternative, four in rows where the
+// second look costs less than what it finds; more where there are few rows.  us:
+//     rows x vocab, k            64 threads    128    256
+//     16384 x  4000,  8  bf16          63.8   80.9    132
+//     16384 x  4000, 64  bf16                  153    193
+//      4096 x 16000, 20  bf16          44.1   42.0   55.1
+//      4096 x 50257,  8  bf16                 87.7   97.3
+//      4096 x 50257, 64  bf16                  126    116
+//      2048 x 50257, 64  fp32                  125   95.4
+// Few long rows: clusters of up to eight blocks.  Blocks of 256 threads and a row to
+// each against clusters: 1 x 50257, 20 bf16 10.4 -> 7.2 us.
+template <typename G> star_status_t run_rows(const AlternativesArgs &a, cudaStream_t stream)
+{
+    const int64_t granules = a.row.vocab * G::kBytes / 16;
+    int cluster = 1;
+    while (granules > 2048 && cluster < 8 && a.row.rows * cluster * 2 <= 148 * 4 && granules / (cluster * 2) >= 448) cluster *= 2;
+    if (cluster > 1) return launch_rows<G, 256, true>(a, cluster, stream);
+    int threads = granules <= 2048 ? 64 : granules <= 8192 ? 128 : 256;
+    while (threads < 256 && (threads < (granules > 2048 ? 4 : 2) * a.k || (threads < granules && a.row.rows * threads < 148 * 800))) threads *= 2;
+    switch (threads) {
+    case 64: return launch_rows<G, 64, false>(a, 1, stream);
+    case 128: return launch_rows<G, 128, false>(a, 1, stream);
+    default: return launch_rows<G, 256, false>(a, 1, stream);
+    }
+}
+
 }  // namespace
 
 extern "C" star_status_t star_token_alternatives(const void *logits, star_dtype_t dtype, int64_t rows, int64_t vocab, int64_t ld,
@@ -45,11 +79,8 @@ extern "C" star_status_t star_token_alternatives(const void *logits, star_dtype_
     a.logp = logp;
     a.lse = lse;
     a.entropy = entropy;
-    constexpr int kThreads = 256;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    const dim3 grid(static_cast<unsigned>(std::min<int64_t>(rows, int64_t{1} << 20)));
-    return dtype == STAR_DTYPE_BF16 ? launch(star_alternatives_kernel<GradBF16, kThreads>, grid, kThreads, 0, dim3(1), stream, a)
-                                    : launch(star_alternatives_kernel<GradF32, kThreads>, grid, kThreads, 0, dim3(1), stream, a);
+    return dtype == STAR_DTYPE_BF16 ? run_rows<GradBF16>(a, stream) : run_rows<GradF32>(a, stream);
 }
 
 extern "C" star_status_t star_token_alternatives_backward(void *dlogits, int64_t ld_dlogits, const void *logits, star_dtype_t dtype,

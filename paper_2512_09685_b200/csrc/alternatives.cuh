@@ -95,36 +95,50 @@ __device__ __forceinline__ uint32_t order_of(float x)
 constexpr uint32_t kLowest = 0x007fffffu;    // order_of(-inf)
 
 // ---------------------------------------------------------------------------
-// Statistics and the k largest logits of a row, in one reading of it from memory.
+// Statistics and the k largest logits of a row, in one reading of it from memory, by a
+// block, or by a cluster of blocks that share it where there are few rows.
 //
-// A row is split among the threads, and every thread knows the largest logit of
-// its part when the statistics are done.  The k-th largest of these is at most the
-// k-th largest logit, so no logit below it is wanted, and in a row whose large
-// logits lie anywhere little more than k are not: those are gathered by a second
-// look at the parts that hold one (from L2), and each finds its rank by comparing
-// itself with the others.  Rows that leave too many (many equal logits, or the
-// large ones side by side) are searched for the k-th largest by counting.
+// A row falls into groups: what a thread takes (or what up to four neighbours take).
+// The k-th largest of the groups' largest logits is at most the k-th largest logit, so
+// no logit below it is wanted; and in a row whose large logits lie anywhere little more
+// than k are not below it.  (The j-th largest within each warp, joined, needs no warp to
+// look at all groups, but leaves a third more: 4096 x 50257, k = 64, 131 us against 117.)
+// Every thread has kept the largest logit of each few batches that it took; the whole
+// block looks again (in L2) at those that reach the bound, and what it finds are the
+// candidates, whose ranks are counted.  Rows that leave too many of them (many equal
+// logits, or the large ones side by side) are searched for the k-th largest by counting.
 // ---------------------------------------------------------------------------
-constexpr int kMostCandidates = 1088;        // k groups of a thread's one granule, and the edges
+constexpr int kMostCandidates = 1088;        // of bf16: 128 threads' one granule, and the edges
+constexpr int kMostGroups = 512;             // of a cluster; of a block: its threads
+constexpr int kSlots = 8;                    // of a thread
 
 struct Candidates {
     uint64_t key[kMostCandidates];           // order in the upper half, 2^31 - 1 - index below
     int count;
 };
-__device__ __forceinline__ void put_candidate(Candidates &c, uint32_t order, int index)
+// `found` is the first block's.
+template <bool CLUSTER> __device__ __forceinline__ void put_candidate(Candidates &found, uint32_t order, int index)
 {
-    const int at = atomicAdd(&c.count, 1);
-    if (at < kMostCandidates) c.key[at] = static_cast<uint64_t>(order) << 32 | static_cast<uint32_t>(0x7fffffff - index);
+    const uint64_t key = static_cast<uint64_t>(order) << 32 | static_cast<uint32_t>(0x7fffffff - index);
+    if constexpr (CLUSTER) {
+        int at;
+        asm volatile("atom.relaxed.cluster.shared::cluster.add.u32 %0, [%1], 1;" : "=r"(at) : "r"(peer_address(smem_address(&found.count), 0)) : "memory");
+        if (at < kMostCandidates) asm volatile("st.shared::cluster.u64 [%0], %1;" :: "r"(peer_address(smem_address(&found.key[at]), 0)), "l"(key) : "memory");
+    } else {
+        const int at = atomicAdd(&found.count, 1);
+        if (at < kMostCandidates) found.key[at] = key;
+    }
 }
 
-// The largest bound that at least k of the values (`EACH` to a lane) reach, or one
-// that few more reach.
-template <int EACH> __device__ __forceinline__ uint32_t bound_of(const uint32_t (&x)[EACH], int k)
+// By a warp: the largest bound that at least k of n orders reach, or one that few more reach.
+template <int EACH> __device__ __forceinline__ uint32_t bound_of(const uint32_t *order, int n, int k)
 {
-    uint32_t low = 0xffffffffu, high = 0;
+    uint32_t x[EACH], low = 0xffffffffu, high = 0;
 #pragma unroll
     for (int q = 0; q < EACH; ++q) {
-        low = min(low, x[q]);
+        const int i = q * 32 + static_cast<int>(threadIdx.x % 32);
+        x[q] = i < n ? order[i] : 0;
+        if (i < n) low = min(low, x[q]);
         high = max(high, x[q]);
     }
     low = __reduce_min_sync(0xffffffffu, low);
@@ -132,14 +146,14 @@ template <int EACH> __device__ __forceinline__ uint32_t bound_of(const uint32_t 
     uint32_t width = high - low;             // the bound lies in [low, low + width]
     while (width > 0) {
         const uint32_t mid = low + (width - width / 2);
-        int n = 0;
+        int reach = 0;
 #pragma unroll
-        for (int q = 0; q < EACH; ++q) n += x[q] >= mid ? 1 : 0;
-        n = __reduce_add_sync(0xffffffffu, n);
-        if (n >= k) {
+        for (int q = 0; q < EACH; ++q) reach += x[q] >= mid ? 1 : 0;
+        reach = __reduce_add_sync(0xffffffffu, reach);
+        if (reach >= k) {
             width -= mid - low;
             low = mid;
-            if (n <= k + k / 8) break;
+            if (reach <= k + k / 8) break;
         } else {
             width = mid - low - 1;
         }
@@ -161,11 +175,11 @@ template <typename G, int THREADS> __device__ int count_row(const void *base, in
     return *total;
 }
 
-// The candidates of a row that `low` leaves too many of (but at least k): counting
-// finds a bound that leaves few enough, or the k-th largest logit itself, whose
+// The candidates of a row that `low` leaves too many of (but at least k), by one block:
+// counting finds a bound that leaves few enough, or the k-th largest logit itself, whose
 // equals are then taken by ascending index.
 template <typename G, int THREADS>
-__device__ void search_row(const void *base, int vocab, int k, uint32_t low, Candidates &found, int *scratch)
+__device__ __noinline__ void search_row(const void *base, int vocab, int k, uint32_t low, Candidates &found, int *scratch)
 {
     uint32_t width = 0xffffffffu - low;
     int reach = kMostCandidates + 1;         // logits at or above low
@@ -186,7 +200,7 @@ __device__ void search_row(const void *base, int vocab, int k, uint32_t low, Can
     const bool ties = reach > kMostCandidates;               // low is the k-th largest, and many equal it
     for (int i = threadIdx.x; i < vocab; i += THREADS) {
         const uint32_t order = order_of(load_value<G>(base, i));
-        if (ties ? order > low : order >= low) put_candidate(found, order, i);
+        if (ties ? order > low : order >= low) put_candidate<false>(found, order, i);
     }
     __syncthreads();
     if (!ties) return;
@@ -206,108 +220,174 @@ __device__ void search_row(const void *base, int vocab, int k, uint32_t low, Can
     __syncthreads();
 }
 
-template <typename G, int THREADS>
-__global__ void __launch_bounds__(THREADS, row_blocks(THREADS)) star_alternatives_kernel(const __grid_constant__ AlternativesArgs a)
+template <typename G, int THREADS, bool CLUSTER>
+__global__ void __launch_bounds__(THREADS, CLUSTER ? policy_blocks(THREADS) : row_blocks(THREADS)) star_alternatives_kernel(const __grid_constant__ AlternativesArgs a)
 {
     constexpr int E = Granule<G>::kCount, kWarps = THREADS / 32, kStep = kBatch * THREADS;
-    __shared__ MaxSums warp_part[kWarps];
+    constexpr int kGroups = CLUSTER ? kMostGroups : THREADS;
+    __shared__ alignas(16) float4 parts[CLUSTER ? 8 * kWarps : kWarps];  // of all warps
     __shared__ MaxSums row_sums;
-    __shared__ uint32_t group_order[THREADS];
-    __shared__ Candidates found;
     __shared__ uint32_t row_bound;
-    __shared__ int scratch;
+    __shared__ uint32_t group_order[kGroups];                    // the first block's
+    __shared__ uint32_t slot_order[kSlots][THREADS];
+    __shared__ unsigned short hits[kSlots * THREADS];
+    __shared__ int n_hits, scratch;
+    __shared__ Candidates found;                                 // the first block's
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t blocks = CLUSTER ? cluster_size() : 1, rank = CLUSTER ? cluster_rank() : 0;
+    const int log_blocks = CLUSTER ? 31 - __clz(static_cast<int>(blocks)) : 0;
+    const int warps = kWarps << log_blocks;
     const float k = __fmul_rn(a.row.inv_temperature, kLog2e);
     const int vocab = static_cast<int>(a.row.vocab);
     launch_dependents();
+    if constexpr (CLUSTER) cluster_sync();                       // the others have started
     wait_for_primary();
 
-    for (int64_t t = blockIdx.x; t < a.row.rows; t += gridDim.x) {
+    for (int64_t t = blockIdx.x >> log_blocks; t < a.row.rows; t += gridDim.x >> log_blocks) {
         const char *base = static_cast<const char *>(a.row.logits) + t * a.row.ld * G::kBytes;
         const int64_t label = a.row.labels ? a.row.labels[t] : 0;
-        const bool wanted = label >= 0 && label < vocab;     // vocab of 0: none
-        const RowSplit s = split_row<G>(base, vocab);
-        const uint4 *granules = reinterpret_cast<const uint4 *>(base + s.head * G::kBytes);
+        const bool wanted = label >= 0 && label < vocab;         // vocab of 0: none
         MaxSums x{-INFINITY, 0.0f, 0.0f};
-        float edge = -INFINITY;
+        float label_logit = 0.0f;
         if (wanted) {
-            int left = s.granules - static_cast<int>(threadIdx.x);
+            const RowSplit s = split_row<G>(base, vocab);
+            const RowShare own = row_share(s.granules, rank, log_blocks);
+            const uint4 *granules = reinterpret_cast<const uint4 *>(base + s.head * G::kBytes) + own.begin;
+            const int edge_at = rank == 0 ? edge_element(s, threadIdx.x, vocab) : -1;
+            const float edge = edge_at >= 0 ? load_value<G>(base, edge_at) : -INFINITY;
+            if (threadIdx.x == THREADS - 1 && rank == 0 && a.logp) label_logit = load_value<G>(base, label);
+            // Batches to a slot: a power of two.
+            const int batches = (own.count + kStep - 1) / kStep, log_each = batches > kSlots ? 32 - __clz((batches - 1) / kSlots) : 0;
+            int left = own.count - static_cast<int>(threadIdx.x), batch = 0;
+            float most = -INFINITY;
             const uint4 *from = granules + threadIdx.x;
-            for (; left > kStep - THREADS; left -= kStep, from += kStep) take_batch_with_entropy<G, kBatch, THREADS, true>(&x, from, left, k);
-            if (left > 0) take_batch_with_entropy<G, kBatch, THREADS, false>(&x, from, left, k);
-            const int edge_at = edge_element(s, threadIdx.x, vocab);
-            if (edge_at >= 0) {
-                edge = load_value<G>(base, edge_at);
-                x = take_one(x, edge, k);
-            }
-            if (a.k > 0) group_order[threadIdx.x] = order_of(x.m);
-            const float own = x.m;
-            x = warp_join(x, k);
-            if (lane == 0) warp_part[warp] = x;
-            if (threadIdx.x == 0) found.count = 0;
-            __syncthreads();
-            if (warp == 0) {
-                x = warp_join(lane < kWarps ? warp_part[lane] : MaxSums{-INFINITY, 0.0f, 0.0f}, k);
-                if (lane == 0) row_sums = x;
-                if (a.k > 0) {
-                    uint32_t most[THREADS / 32];
-#pragma unroll
-                    for (int q = 0; q < THREADS / 32; ++q) most[q] = group_order[q * 32 + lane];
-                    // No bound where there are fewer parts than alternatives.
-                    const uint32_t bound = a.k <= THREADS ? bound_of(most, a.k) : 0;
-                    if (lane == 0) row_bound = max(bound, kLowest + 1);
+            for (; left > 0; left -= kStep, from += kStep) {
+                const float m = left > kStep - THREADS ? take_batch_with_entropy<G, kBatch, THREADS, true>(&x, from, left, k)
+                                                       : take_batch_with_entropy<G, kBatch, THREADS, false>(&x, from, left, k);
+                most = fmaxf(most, m);
+                ++batch;
+                if ((batch & ((1 << log_each) - 1)) == 0) {
+                    slot_order[(batch >> log_each) - 1][threadIdx.x] = order_of(most);
+                    most = -INFINITY;
                 }
             }
-            __syncthreads();
-            x = row_sums;
-            // A second look at the parts that reach the bound.
-            if (a.k > 0 && x.s > 0.0f) {
+            if ((batch & ((1 << log_each) - 1)) != 0) slot_order[batch >> log_each][threadIdx.x] = order_of(most);
+            const int slots = (batch + (1 << log_each) - 1) >> log_each;
+            if (edge_at >= 0) x = take_one(x, edge, k);
+            if (a.k > 0) {
+                uint32_t group = order_of(x.m);
+                if constexpr (CLUSTER) {
+                    const uint32_t width = blocks / 2;
+                    for (uint32_t o = 1; o < width; o *= 2) group = max(group, __shfl_xor_sync(0xffffffffu, group, o));
+                    if (threadIdx.x % width == 0)
+                        asm volatile("st.shared::cluster.u32 [%0], %1;" :: "r"(peer_address(smem_address(&group_order[(rank * THREADS + threadIdx.x) / width]), 0)), "r"(group) : "memory");
+                } else {
+                    group_order[threadIdx.x] = group;
+                }
+            }
+            x = warp_join(x, k);
+            if constexpr (CLUSTER) {
+                if (lane == 0)
+                    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %3};" :: "r"(peer_address(smem_address(&parts[rank * kWarps + warp]), 0)),
+                                 "f"(x.m), "f"(x.s), "f"(x.t) : "memory");
+            } else if (lane == 0) {
+                parts[warp] = make_float4(x.m, x.s, x.t, 0.0f);
+            }
+            if (threadIdx.x == 0) found.count = n_hits = 0;
+            if constexpr (CLUSTER) cluster_sync(); else __syncthreads();
+            // One warp joins the sums, another one finds the bound.
+            if (warp == 0 && rank == 0) {
+                const float4 none = make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
+                const float4 part = lane < warps ? parts[lane] : none;
+                x = MaxSums{part.x, part.y, part.z};
+                if constexpr (CLUSTER) {
+                    const float4 more = lane + 32 < warps ? parts[lane + 32] : none;
+                    const float m = fmaxf(part.x, more.x);
+                    x = add(move_to(x, m, k), move_to(MaxSums{more.x, more.y, more.z}, m, k));
+                }
+                x = warp_join(x, k);
+                if (lane == 0) row_sums = x;
+                if constexpr (CLUSTER) {
+                    if (lane > 0 && lane < static_cast<int>(blocks))
+                        asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(peer_address(smem_address(&row_sums.s), lane)), "f"(x.s) : "memory");
+                }
+            }
+            if (warp == 1 && rank == 0 && a.k > 0) {
+                const uint32_t bound = max(bound_of<kGroups / 32>(group_order, CLUSTER ? 2 * THREADS : THREADS, a.k), kLowest + 1);
+                if constexpr (CLUSTER) {
+                    if (lane < static_cast<int>(blocks))
+                        asm volatile("st.shared::cluster.u32 [%0], %1;" :: "r"(peer_address(smem_address(&row_bound), lane)), "r"(bound) : "memory");
+                } else if (lane == 0) {
+                    row_bound = bound;
+                }
+            }
+            if constexpr (CLUSTER) cluster_sync(); else __syncthreads();
+            x = row_sums;                                        // the first block's; another's has the sum alone
+            // A second look at what reaches the bound.
+            if (a.k > 0 && x.s > 0.0f && x.s < INFINITY) {
                 const uint32_t bound = row_bound;
-                if (order_of(own) >= bound) {
-                    if (edge_at >= 0 && order_of(edge) >= bound) put_candidate(found, order_of(edge), edge_at);
-                    for (int g = threadIdx.x; g < s.granules; g += THREADS) {
-                        const uint4 v = granules[g];
-                        RunningMax<G> most;
-                        most.take(v);
-                        if (order_of(most.value()) < bound) continue;
-                        for (int e = 0; e < E; ++e) {
-                            const float f = load_value<G>(granules, static_cast<int64_t>(g) * E + e);
-                            if (order_of(f) >= bound) put_candidate(found, order_of(f), s.head + g * E + e);
-                        }
+                if (edge_at >= 0 && order_of(edge) >= bound) put_candidate<CLUSTER>(found, order_of(edge), edge_at);
+                for (int q = 0; q < slots; ++q)
+                    if (slot_order[q][threadIdx.x] >= bound) hits[atomicAdd(&n_hits, 1)] = static_cast<unsigned short>(q * THREADS + threadIdx.x);
+                __syncthreads();
+                const int n = n_hits << (log_each + 2);          // granules
+                for (int i = threadIdx.x; i < n; i += THREADS) {
+                    const int hit = hits[i >> (log_each + 2)], slot = hit / THREADS;
+                    const int g = hit % THREADS + ((slot << (log_each + 2)) + (i & ((4 << log_each) - 1))) * THREADS;
+                    if (g >= own.count) continue;
+                    const uint4 v = granules[g];
+                    RunningMax<G> high;
+                    high.take(v);
+                    if (order_of(high.value()) < bound) continue;
+                    Pair f[E / 2];
+                    Granule<G>::widen(v, f);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        float lo, hi;
+                        split_pair(f[e / 2], &lo, &hi);
+                        const uint32_t order = order_of(e % 2 ? hi : lo);
+                        if (order >= bound) put_candidate<CLUSTER>(found, order, s.head + (own.begin + g) * E + e);
                     }
                 }
-                __syncthreads();
-                if (found.count > kMostCandidates) search_row<G, THREADS>(base, vocab, a.k, bound, found, &scratch);
+                if constexpr (CLUSTER) cluster_sync(); else __syncthreads();
+                if (rank == 0 && found.count > kMostCandidates) search_row<G, THREADS>(base, vocab, a.k, bound, found, &scratch);
             }
         }
-        const bool active = wanted && !(x.s == 0.0f), whole = active && x.s < INFINITY;
-        if (threadIdx.x == 0) {
-            const float nan = x.s;                           // where the row has no sum
-            if (a.logp) a.logp[t] = active ? log_prob(load_value<G>(base, label), MaxSum{x.m, x.s}, k, a.row.inv_temperature) : 0.0f;
-            if (a.lse) a.lse[t] = active ? log_sum_exp(MaxSum{x.m, x.s}, a.row.inv_temperature) : -INFINITY;
-            if (a.entropy) a.entropy[t] = whole ? __fsub_rn(logf(x.s), __fmul_rn(kLn2, __fdiv_rn(x.t, x.s))) : active ? nan : 0.0f;
-        }
-        if (a.k > 0) {
-            const int n = whole ? found.count : 0, have = min(n, a.k);
-            int32_t *ids = a.top_ids + t * a.ld_top;
-            float *top = a.top_logp + t * a.ld_top;
-            for (int i = threadIdx.x; i < n; i += THREADS) {
-                const uint64_t key = found.key[i];
-                int rank = 0;
-                for (int j = 0; j < n; ++j) rank += found.key[j] > key ? 1 : 0;
-                if (rank < a.k) {
-                    const uint32_t order = static_cast<uint32_t>(key >> 32);
-                    const float f = __uint_as_float(order & 0x80000000u ? order & 0x7fffffffu : ~order);
-                    ids[rank] = 0x7fffffff - static_cast<int32_t>(key & 0xffffffffu);
-                    top[rank] = log_prob(f, MaxSum{x.m, x.s}, k, a.row.inv_temperature);
+        if (rank == 0) {                                         // the rest is the first block's
+            const bool active = wanted && !(x.s == 0.0f), whole = active && x.s < INFINITY;
+            if (threadIdx.x == THREADS - 1) {
+                const float nan = x.s;                           // where the row has no sum
+                if (a.logp) a.logp[t] = active ? log_prob(label_logit, MaxSum{x.m, x.s}, k, a.row.inv_temperature) : 0.0f;
+                if (a.lse) a.lse[t] = active ? log_sum_exp(MaxSum{x.m, x.s}, a.row.inv_temperature) : -INFINITY;
+                if (a.entropy) a.entropy[t] = whole ? __fsub_rn(logf(x.s), __fmul_rn(kLn2, __fdiv_rn(x.t, x.s))) : active ? nan : 0.0f;
+            }
+            if (a.k > 0) {
+                const int n = whole ? found.count : 0, have = min(n, a.k);
+                int32_t *ids = a.top_ids + t * a.ld_top;
+                float *top = a.top_logp + t * a.ld_top;
+                // Four lanes count a candidate's betters.
+                for (int i = threadIdx.x / 4; i - static_cast<int>(threadIdx.x / 4) < n; i += THREADS / 4) {
+                    const uint64_t key = i < n ? found.key[i] : 0;
+                    int rank_of = 0;
+                    for (int j = threadIdx.x % 4; j < n; j += 4) rank_of += found.key[j] > key ? 1 : 0;
+                    rank_of += __shfl_xor_sync(0xffffffffu, rank_of, 1);
+                    rank_of += __shfl_xor_sync(0xffffffffu, rank_of, 2);
+                    if (i < n && rank_of < a.k && threadIdx.x % 4 == 0) {
+                        const uint32_t order = static_cast<uint32_t>(key >> 32);
+                        const float f = __uint_as_float(order & 0x80000000u ? order & 0x7fffffffu : ~order);
+                        ids[rank_of] = 0x7fffffff - static_cast<int32_t>(key & 0xffffffffu);
+                        top[rank_of] = log_prob(f, MaxSum{x.m, x.s}, k, a.row.inv_temperature);
+                    }
+                }
+                for (int i = have + threadIdx.x; i < a.k; i += THREADS) {
+                    ids[i] = -1;
+                    top[i] = active && !whole ? x.s : -INFINITY;
                 }
             }
-            for (int i = have + threadIdx.x; i < a.k; i += THREADS) {
-                ids[i] = -1;
-                top[i] = active && !whole ? x.s : -INFINITY;
-            }
         }
-        __syncthreads();                                     // the candidates are read
+        if (wanted) {                                            // what is shared has been read
+            if constexpr (CLUSTER) cluster_sync(); else __syncthreads();
+        }
     }
 }
 

@@ -403,8 +403,8 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
         }
         return first;
     };
-    // ... and there: what the teacher's list says by itself, and a thread's entry's logit (or the label's, by
-    // the thread behind the list's last), which are then on their way.
+    // ... and there: what the teacher's list says by itself.  Where other blocks share the row, a thread's entry's
+    // logit, and the label's, are then on their way; a block on its own finds them in its row.
     const auto take_list = [&](int64_t t, Listed &list, float *x, float *label_logit) {
         if (t >= a.row.rows) {
             if (lists_it && at_list == 0) list.wanted = 0;
@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
             id = -1;
             reinterpret_cast<int *>(list.id4)[at_list] = -1;
         }
-        if (id >= 0) *x = load_value<G>(base, id);
+        if (blocks > 1 && id >= 0) *x = load_value<G>(base, id);
         if (at_list < 32) list.edge[at_list] = -1;
         if (at_list == 0) {
             const int64_t asked = list.asked_label;
@@ -426,7 +426,7 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
             list.label = label;
             list.wanted = (label >= 0 || !a.row.labels) && list.weight != 0.0f;
             list.twice = list.has_label = 0;
-            if (label >= 0 && a.hard != 0.0f) *label_logit = load_value<G>(base, label);
+            if (blocks > 1 && label >= 0 && a.hard != 0.0f) *label_logit = load_value<G>(base, label);
         }
         if (works) {
             const float v = id >= 0 ? list.value[at_list] : -INFINITY, most = warp_max(v);
@@ -471,7 +471,7 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
         bool active = false;
         if (list.wanted) {
             const float edge = edge_at >= 0 ? load_value<G>(row_base(t), edge_at) : 0.0f;
-            if (lists_it && at_list == 0) list.label_logit = label_logit;
+            if (blocks > 1 && lists_it && at_list == 0) list.label_logit = label_logit;
             // This thread's entry, and where it lies in the block's share.
             const int id = lists_it ? list.ids()[at_list] : -1, in_own = id - s.head - own.begin * E;
             const bool in_share = id >= s.head && in_own >= 0 && in_own < own.count * E;
@@ -484,6 +484,13 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
                 phase ^= 1;
             }
             if (blocks == 1 && lists_it) {
+                const auto logit = [&](int i) {
+                    const int at = i - s.head;
+                    return i >= s.head && at < own.count * E ? load_value<G>(kept_row, at) : load_value<G>(row_base(t), i);
+                };
+                if (id >= 0) x_own = logit(id);
+                if (at_list == 0 && list.label >= 0) list.label_logit = logit(list.label);
+                list_sync();
                 // Whether an id is listed twice: each entry leaves its number in its element's place and looks who was last.
                 const int edge_of = id < 0 || in_share ? -1 : id < s.head ? id : s.head + id - (vocab - s.tail);
                 if (in_share) mark<G>(kept_row, in_own, at_list);
