@@ -117,10 +117,18 @@ extern "C" star_status_t star_token_alternatives_backward(void *dlogits, int64_t
     a.ld_d_top = ld_d_top;
     a.dlogits = dlogits;
     a.ld_dlogits = ld_dlogits;
-    const int64_t per_row = vocab * dtype_size(dtype) / 16 / kAltGranules + 1;           // of a warp
-    const int64_t most = 148 * 64, warps = kAltThreads / 32;
-    const dim3 grid(static_cast<unsigned>(rows > most * warps / per_row ? most : (rows * per_row + warps - 1) / warps));
+    // Blocks to a row: until every SM has five, as long as each has a step of its own.  Half a block for short
+    // rows, if it has a thread for the label beside the alternatives'.
+    const int64_t granules = vocab * dtype_size(dtype) / 16;
+    const bool small = granules <= 1024 && k < 128;
+    int64_t parts = 1;
+    while (parts * 2 * kBatch * 256 <= granules && rows * parts < 148 * 5) parts *= 2;
+    const dim3 grid(static_cast<unsigned>(std::min<int64_t>(rows * parts, 0x7fffffff)));
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    return dtype == STAR_DTYPE_BF16 ? launch(star_alternatives_backward_kernel<GradBF16>, grid, kAltThreads, 0, dim3(1), stream, a)
-                                    : launch(star_alternatives_backward_kernel<GradF32>, grid, kAltThreads, 0, dim3(1), stream, a);
+    const int n = static_cast<int>(parts);
+    if (dtype == STAR_DTYPE_BF16)
+        return small ? launch(star_alternatives_backward_kernel<GradBF16, 128>, grid, 128, 0, dim3(1), stream, a, n)
+                     : launch(star_alternatives_backward_kernel<GradBF16, 256>, grid, 256, 0, dim3(1), stream, a, n);
+    return small ? launch(star_alternatives_backward_kernel<GradF32, 128>, grid, 128, 0, dim3(1), stream, a, n)
+                 : launch(star_alternatives_backward_kernel<GradF32, 256>, grid, 256, 0, dim3(1), stream, a, n);
 }

@@ -395,8 +395,10 @@ __global__ void __launch_bounds__(THREADS, CLUSTER ? policy_blocks(THREADS) : ro
 // The backward pass.  With u = z - lse and p = exp(u),
 //     dlogits[j] = (sum of the gradients of what names j - p (G + h (u + H))) / temperature,
 // G the sum of the gradients of a row's log-probabilities, h that of its entropy H.
-// A warp takes a run of granules of a row at a time, as for the losses' gradients;
-// elements that the label or an alternative names are made by the same warp.
+// A block takes a row, or a part of one where there are few.  What the label or an
+// alternative names is found out once for all of it, a thread to an entry; their
+// elements' logits are read before anything is stored (the gradient may replace the
+// logits) and their gradients stored after it.
 // ---------------------------------------------------------------------------
 struct AlternativesGradArgs {
     RowArgs row;                 // labels may be null
@@ -420,120 +422,139 @@ __device__ __forceinline__ float dense_gradient(float x, const AlternativesRow &
     return __fmul_rn(exp2_fast(__fmul_rn(u, kLog2e)), __fmaf_rn(r.slope, u, r.plain));
 }
 
-constexpr int kAltThreads = 256;
-constexpr int kAltPerThread = 4;
-constexpr int kAltGranules = 32 * kAltPerThread;
-constexpr int kAltSlots = kMostAlternatives / 32 + 1;        // what names an element, to a lane
-
-template <typename G> __global__ void __launch_bounds__(kAltThreads, 4) star_alternatives_backward_kernel(const __grid_constant__ AlternativesGradArgs a)
+// Two elements.  The bound keeps 0 * -inf out.
+__device__ __forceinline__ Pair dense_gradient(Pair x, const AlternativesRow &r)
 {
-    constexpr int E = Granule<G>::kCount, P = Granule<G>::kPairs;
+    float lo, hi;
+    split_pair(pair_fma(x, pair_of(r.inv_temperature), pair_of(-r.lse)), &lo, &hi);
+    const Pair u = make_pair(fmaxf(lo, -200.0f), fmaxf(hi, -200.0f));
+    return pair_mul(pair_exp2(pair_mul(u, pair_of(kLog2e))), pair_fma(pair_of(r.slope), u, pair_of(r.plain)));
+}
+
+template <typename G, int THREADS> __global__ void __launch_bounds__(THREADS, row_blocks(THREADS)) star_alternatives_backward_kernel(const __grid_constant__ AlternativesGradArgs a, int parts)
+{
+    constexpr int E = Granule<G>::kCount, P = Granule<G>::kPairs, kStep = kBatch * THREADS;
+    __shared__ int4 id4[kMostAlternatives / 4];
+    __shared__ float grads[kMostAlternatives], warp_sums[kMostAlternatives / 32];
+    __shared__ int label_listed;
+    const int *ids = reinterpret_cast<const int *>(id4);
     launch_dependents();
     wait_for_primary();
-    const int vocab = static_cast<int>(a.row.vocab);
-    const int64_t per_row = (a.row.vocab / E + kAltGranules) / kAltGranules;             // the last run may be empty
-    const int64_t items = a.row.rows * per_row;
-    const int lane = threadIdx.x % 32, warps = kAltThreads / 32;
-    for (int64_t item = static_cast<int64_t>(blockIdx.x) * warps + threadIdx.x / 32; item < items; item += static_cast<int64_t>(gridDim.x) * warps) {
-        const int64_t t = items <= 0xffffffff ? static_cast<uint32_t>(item) / static_cast<uint32_t>(per_row) : item / per_row;
-        const int64_t run = item - t * per_row;
+    const int vocab = static_cast<int>(a.row.vocab), lane = threadIdx.x % 32;
+    for (int64_t item = blockIdx.x; item < a.row.rows * parts; item += gridDim.x) {
+        const int64_t t = parts == 1 ? item : item / parts;
+        const int part = static_cast<int>(item - t * parts);
         const char *base = static_cast<const char *>(a.row.logits) + t * a.row.ld * G::kBytes;
         char *out = static_cast<char *>(a.dlogits) + t * a.ld_dlogits * G::kBytes;
         const RowSplit s = split_row<G>(base, vocab);
-        const int begin = static_cast<int>(run) * kAltGranules, end = min(begin + kAltGranules, s.granules);
-        const int first = s.head + begin * E, last = s.head + end * E;                   // the run's elements; run 0 has the edges too
-        const int edge_at = run == 0 ? edge_element(s, lane, vocab) : -1;
+        const int each = (s.granules + parts - 1) / parts, begin = min(each * part, s.granules), end = min(begin + each, s.granules);
+        const int edge_at = part == 0 ? edge_element(s, threadIdx.x, vocab) : -1;
         const float lse = a.lse[t];
         const int64_t label = a.row.labels ? a.row.labels[t] : 0;
         const bool active = lse != -INFINITY && label >= 0 && label < vocab;
-        // What names an element, and its gradient: the alternatives, then the label.
-        int named[kAltSlots];
-        float grad[kAltSlots], each = 0.0f;
+        const bool same_phase = (reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(base)) % 16 == 0;
+        const auto here = [&](int id) {
+            const int at = id - s.head;
+            return id < s.head || id >= vocab - s.tail ? part == 0 : at >= begin * E && at < end * E;
+        };
         AlternativesRow r{lse, a.row.inv_temperature, 0.0f, 0.0f};
+        const float d_logp = active && a.d_logp ? a.d_logp[t] : 0.0f;
+        // This thread's entry: the elements' logit and the gradients of all that names it.  -1: none, or none of its own.
+        int named = -1;
+        float logit = 0.0f, sum = 0.0f;
         if (active) {
-#pragma unroll
-            for (int q = 0; q < kAltSlots; ++q) {
-                const int i = q * 32 + lane;
-                named[q] = -1;
-                grad[q] = 0.0f;
-                if (i < a.k) {
-                    const int id = a.top_ids[t * a.ld_top + i];
-                    if (id >= 0 && id < vocab) {
-                        named[q] = id;
-                        grad[q] = a.d_top[t * a.ld_d_top + i];
-                    }
-                } else if (i == a.k && a.d_logp) {
-                    named[q] = static_cast<int>(label);
-                    grad[q] = a.d_logp[t];
-                }
-                each = __fadd_rn(each, grad[q]);
-            }
-            each = warp_sum(each);
             const float h = a.d_entropy ? a.d_entropy[t] : 0.0f;
-            float plain = h == 0.0f ? each : __fmaf_rn(h, a.entropy[t], each);
+            float all = d_logp;
+            if (a.k > 0) {
+                if (threadIdx.x < kMostAlternatives) {
+                    int id = -1;
+                    if (static_cast<int>(threadIdx.x) < a.k) {
+                        id = a.top_ids[t * a.ld_top + threadIdx.x];
+                        if (id < 0 || id >= vocab)
+                            id = -1;
+                        else
+                            sum = a.d_top[t * a.ld_d_top + threadIdx.x];
+                    }
+                    const float total = warp_sum(sum);
+                    if (lane == 0) warp_sums[threadIdx.x / 32] = total;
+                    grads[threadIdx.x] = sum;
+                    reinterpret_cast<int *>(id4)[threadIdx.x] = id;
+                    named = id;
+                }
+                if (threadIdx.x == 0) label_listed = 0;
+                __syncthreads();
+                for (int w = 0; w * 32 < a.k; ++w) all = __fadd_rn(all, warp_sums[w]);
+                if (named >= 0 && here(named)) {
+                    // The first entry with an id takes the gradients of all of them.
+                    const int mine = static_cast<int>(threadIdx.x);
+                    for (int i = 0; i < a.k; i += 4) {
+                        const int4 other = id4[i / 4];
+                        if (other.x != named && other.y != named && other.z != named && other.w != named) continue;
+                        for (int q = i; q < i + 4; ++q) {
+                            if (ids[q] != named || q == mine) continue;
+                            if (q < mine) named = -2;
+                            sum = __fadd_rn(sum, grads[q]);
+                        }
+                        if (named < 0) break;
+                    }
+                    if (named >= 0) {
+                        logit = load_value<G>(base, named);
+                        if (a.d_logp && named == label) {
+                            sum = __fadd_rn(sum, d_logp);
+                            label_listed = 1;
+                        }
+                    }
+                } else {
+                    named = -1;
+                }
+            }
+            if (threadIdx.x == THREADS - 1 && a.d_logp && here(static_cast<int>(label))) {
+                named = static_cast<int>(label);
+                logit = load_value<G>(base, named);
+                sum = d_logp;
+            }
+            if (a.k > 0 || a.d_logp) __syncthreads();        // the named elements' logits are read
+            float plain = h == 0.0f ? all : __fmaf_rn(h, a.entropy[t], all);
             if (lse != lse) plain = lse;                     // a NaN row's gradient is NaN
             r.plain = -__fmul_rn(plain, r.inv_temperature);
             r.slope = -__fmul_rn(h, r.inv_temperature);
         }
-        // The named elements' logits, before anything is stored in place.
-        float at_named[kAltSlots];
-        uint32_t here[kAltSlots];
-        if (active) {
-#pragma unroll
-            for (int q = 0; q < kAltSlots; ++q) {
-                const bool in = named[q] >= 0 && ((named[q] >= first && named[q] < last) || (run == 0 && (named[q] < s.head || named[q] >= vocab - s.tail)));
-                here[q] = __ballot_sync(0xffffffffu, in);
-                at_named[q] = in ? load_value<G>(base, named[q]) : 0.0f;
-            }
-            __syncwarp();
-        }
         const float edge = active && edge_at >= 0 ? load_value<G>(base, edge_at) : 0.0f;
-        const bool same_phase = (reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(base)) % 16 == 0;
         if (same_phase) {
-            const uint4 *src = reinterpret_cast<const uint4 *>(base + s.head * G::kBytes) + begin + lane;
-            uint4 *dst = reinterpret_cast<uint4 *>(out + s.head * G::kBytes) + begin + lane;
-            const int left = end - begin - lane;
-            if (active) {
-                uint4 v[kAltPerThread];
+            const uint4 *src = reinterpret_cast<const uint4 *>(base + s.head * G::kBytes) + begin + threadIdx.x;
+            uint4 *dst = reinterpret_cast<uint4 *>(out + s.head * G::kBytes) + begin + threadIdx.x;
+            for (int left = end - begin - static_cast<int>(threadIdx.x); left > 0; left -= kStep, src += kStep, dst += kStep) {
+                if (!active) {
 #pragma unroll
-                for (int q = 0; q < kAltPerThread; ++q)
-                    if (q * 32 < left) v[q] = src[q * 32];
+                    for (int q = 0; q < kBatch; ++q)
+                        if (q * THREADS < left) dst[q * THREADS] = make_uint4(0, 0, 0, 0);
+                    continue;
+                }
+                uint4 v[kBatch];
 #pragma unroll
-                for (int q = 0; q < kAltPerThread; ++q) {
-                    if (q * 32 < left) {
+                for (int q = 0; q < kBatch; ++q)
+                    if (q * THREADS < left) v[q] = src[q * THREADS];
+#pragma unroll
+                for (int q = 0; q < kBatch; ++q) {
+                    if (q * THREADS < left) {
                         Pair g[P];
                         Granule<G>::widen(v[q], g);
 #pragma unroll
-                        for (int e = 0; e < P; ++e) {
-                            float lo, hi;
-                            split_pair(g[e], &lo, &hi);
-                            g[e] = make_pair(dense_gradient(lo, r), dense_gradient(hi, r));
-                        }
-                        dst[q * 32] = Granule<G>::narrow(g);
+                        for (int e = 0; e < P; ++e) g[e] = dense_gradient(g[e], r);
+                        dst[q * THREADS] = Granule<G>::narrow(g);
                     }
                 }
-            } else {
-#pragma unroll
-                for (int q = 0; q < kAltPerThread; ++q)
-                    if (q * 32 < left) dst[q * 32] = make_uint4(0, 0, 0, 0);
             }
         } else {
-            for (int at = first + lane; at < last; at += 32) store_value<G>(out, at, active ? dense_gradient(load_value<G>(base, at), r) : 0.0f);
+            for (int at = s.head + begin * E + threadIdx.x; at < s.head + end * E; at += THREADS)
+                store_value<G>(out, at, active ? dense_gradient(load_value<G>(base, at), r) : 0.0f);
         }
         if (edge_at >= 0) store_value<G>(out, edge_at, active ? dense_gradient(edge, r) : 0.0f);
-        if (!active) continue;
-        __syncwarp();                                        // the run is stored
-#pragma unroll
-        for (int q = 0; q < kAltSlots; ++q) {
-            for (uint32_t rest = here[q]; rest; rest &= rest - 1) {
-                const int who = __ffs(rest) - 1;
-                const int id = __shfl_sync(0xffffffffu, named[q], who);
-                float sum = 0.0f;                            // of all that name it
-#pragma unroll
-                for (int p = 0; p < kAltSlots; ++p) sum = __fadd_rn(sum, named[p] == id ? grad[p] : 0.0f);
-                sum = warp_sum(sum);
-                if (lane == who) store_value<G>(out, id, __fmaf_rn(sum, r.inv_temperature, dense_gradient(at_named[q], r)));
-            }
+        if (active && (a.k > 0 || a.d_logp)) {
+            __syncthreads();                                 // the part is stored
+            if (threadIdx.x == THREADS - 1 && a.k > 0 && label_listed) named = -1;
+            if (named >= 0) store_value<G>(out, named, __fmaf_rn(sum, r.inv_temperature, dense_gradient(logit, r)));
+            if (a.k > 0 && gridDim.x < a.row.rows * parts) __syncthreads();              // the list is read
         }
     }
 }

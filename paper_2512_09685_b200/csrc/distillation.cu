@@ -30,7 +30,18 @@ star_status_t launch_loss(const DistillArgs &a, int cluster, int *parts_out, cud
     if (e != cudaSuccess) return cuda_failed(e);
     const int64_t clusters = std::min<int64_t>(a.row.rows, held);
     *parts_out = static_cast<int>(clusters);
-    return launch(kernel, dim3(static_cast<unsigned>(clusters * cluster)), THREADS, static_cast<size_t>(kib) * 1024, dim3(static_cast<unsigned>(cluster)), stream, a);
+    // Rows in order of taking part, where some may not, every block has a few, and there is enough to do to make up
+    // for finding it: 8192 x 50257, 35 % masked, 299 -> 273 us; none masked, 4096 x 50257 179 -> 184, 16384 x 4000
+    // 113 -> 130 (not taken).
+    DistillArgs work = a;
+    if ((!a.row.labels && !a.row.weights) || a.row.rows < 4 * clusters || a.row.rows > kMostOrdered ||
+        a.row.rows * a.row.vocab * G::kBytes < 200'000'000) {
+        work.order = nullptr;
+    } else {
+        const star_status_t st = launch(star_distillation_order_kernel, dim3(1), kOrderThreads, 0, dim3(1), stream, a.row, work.order);
+        if (st != STAR_OK) return st;
+    }
+    return launch(kernel, dim3(static_cast<unsigned>(clusters * cluster)), THREADS, static_cast<size_t>(kib) * 1024, dim3(static_cast<unsigned>(cluster)), stream, work);
 }
 
 template <typename G, int MODE> star_status_t run_threads(const DistillArgs &a, int threads, int cluster, int *parts_out, cudaStream_t stream)
@@ -78,7 +89,7 @@ extern "C" star_status_t star_distillation_loss(const void *logits, star_dtype_t
     if (k < 0 || !std::isfinite(soft_coef) || !std::isfinite(label_coef) || !(teacher_temperature > 0.0f) ||
         !std::isfinite(teacher_temperature) || !std::isfinite(1.0f / teacher_temperature))
         return STAR_ERR_INVALID_ARG;
-    if (k > kMostListed) return STAR_ERR_UNSUPPORTED;
+    if (k > kMostListed || rows > 0x3fffffff) return STAR_ERR_UNSUPPORTED;
     DistillArgs a{};
     Extent read[5], written[4];
     star_status_t st = check_rows(logits, dtype, rows, vocab, ld, labels, temperature, &a.row, read, label_coef == 0.0f);
@@ -106,6 +117,7 @@ extern "C" star_status_t star_distillation_loss(const void *logits, star_dtype_t
     a.hard = label_coef;
     a.token_loss = token_loss;
     a.partial = static_cast<float4 *>(workspace);
+    a.order = reinterpret_cast<int32_t *>(a.partial + rows);     // 4 bytes for each row and 4 more: there are 16 and 16
     a.dlogits = dlogits;
     a.ld_dlogits = ld_dlogits;
     a.tries = wait_attempts();

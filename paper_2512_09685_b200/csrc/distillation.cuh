@@ -21,10 +21,17 @@ struct DistillArgs {
     float soft, hard;
     float *token_loss;
     float4 *partial;             // the four sums of each block's (cluster's) rows
+    int32_t *order;              // may be null: the rows that take part in front, the others behind them, then the number of the first
     void *dlogits;               // may be null
     int64_t ld_dlogits;
     int tries;                   // of a wait
 };
+
+// Whether a row takes part, as far as its label and weight say.
+__device__ __forceinline__ bool takes_part(const RowArgs &a, int64_t label, float weight)
+{
+    return (!a.labels || (label >= 0 && label < a.vocab)) && weight != 0.0f;
+}
 
 // Statistics of the elements that the teacher does not list: the largest, the sum of
 // 2^exponent at the loss's temperature, and at temperature 1 where that is another.
@@ -96,6 +103,7 @@ struct Listed {
     int label;                   // -1: none
     float label_logit;
     int wanted;                  // the label and the weight let the row take part
+    int row;
     RestSums part[kListWarps];   // the student's statistics of the first entries of each id
     float most[kListWarps];      // of the teacher's values: the largest, -inf, or NaN
     double sum[kListWarps];      // of exp((value - most) / temperature)
@@ -336,6 +344,7 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
     __shared__ DistillFactors factors;
     __shared__ DistillSums sums;
     __shared__ Listed lists[2];                                  // of every other row
+    __shared__ int ahead[2];                                     // of every other item: its row, where rows are taken in a given order
     __shared__ int late[2];                                      // of every other row, as in the policy loss
     __shared__ alignas(8) uint64_t landed;                       // the row's copy is in place
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -346,7 +355,7 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
     const int vocab = static_cast<int>(a.row.vocab);
     const uint32_t blocks = cluster_size(), rank = cluster_rank();
     const int log_blocks = 31 - __clz(static_cast<int>(blocks));
-    const int64_t first_row = blockIdx.x >> log_blocks, step = gridDim.x >> log_blocks;
+    const int first_item = static_cast<int>(blockIdx.x) >> log_blocks, step = static_cast<int>(gridDim.x) >> log_blocks, rows = static_cast<int>(a.row.rows);
     launch_dependents();
     if (threadIdx.x == 0) {
         sums = DistillSums{0.0, 0.0, 0.0, 0.0};
@@ -382,16 +391,21 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
         barrier_expect(bar, bytes);
         bulk_load(smem_address(kept_row), base + s.head * G::kBytes + static_cast<int64_t>(own.begin) * 16, bytes, bar);
     };
-    // Row t's list, label and weight, into shared memory by the list's threads: under way ...
-    const auto ask = [&](int64_t t, Listed &list) {
-        if (!lists_it || t >= a.row.rows) return;
+    const int items = a.order ? a.order[rows] : rows;
+    // An item's row, list, label and weight, into shared memory by the list's threads: under way ...
+    const auto ask = [&](int item, int parity) {
+        Listed &list = lists[parity];
+        if (!lists_it || item >= items) return;
+        const int64_t t = a.order ? ahead[parity] : item;
         if (at_list < a.k) {
             copy_word<4>(reinterpret_cast<int *>(list.id4) + at_list, a.ids + t * a.ld_ids + at_list);
             copy_word<4>(list.value + at_list, a.values + t * a.ld_values + at_list);
         }
         if (at_list == 0) {
+            list.row = static_cast<int>(t);
             if (a.row.labels) copy_word<8>(&list.asked_label, a.row.labels + t);
             if (a.row.weights) copy_word<4>(&list.weight, a.row.weights + t);
+            if (a.order && item + step < items) copy_word<4>(&ahead[parity ^ 1], a.order + item + step);
         }
     };
     // No entry in front has its id.
@@ -405,28 +419,25 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
     };
     // ... and there: what the teacher's list says by itself.  Where other blocks share the row, a thread's entry's
     // logit, and the label's, are then on their way; a block on its own finds them in its row.
-    const auto take_list = [&](int64_t t, Listed &list, float *x, float *label_logit) {
-        if (t >= a.row.rows) {
+    const auto take_list = [&](int item, Listed &list, float *x, float *label_logit) {
+        if (item >= items) {
             if (lists_it && at_list == 0) list.wanted = 0;
             return;
         }
         if (!lists_it) return;
         asm volatile("cp.async.wait_all;" ::: "memory");
-        const char *base = row_base(t);
         int id = list.ids()[at_list];
         if (id >= vocab) {
             id = -1;
             reinterpret_cast<int *>(list.id4)[at_list] = -1;
         }
-        if (blocks > 1 && id >= 0) *x = load_value<G>(base, id);
         if (at_list < 32) list.edge[at_list] = -1;
         if (at_list == 0) {
             const int64_t asked = list.asked_label;
             const int label = asked >= 0 && asked < vocab ? static_cast<int>(asked) : -1;
             list.label = label;
-            list.wanted = (label >= 0 || !a.row.labels) && list.weight != 0.0f;
+            list.wanted = takes_part(a.row, asked, list.weight);
             list.twice = list.has_label = 0;
-            if (blocks > 1 && label >= 0 && a.hard != 0.0f) *label_logit = load_value<G>(base, label);
         }
         if (works) {
             const float v = id >= 0 ? list.value[at_list] : -INFINITY, most = warp_max(v);
@@ -444,7 +455,10 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
             const Teacher teacher = make_teacher(a, list);
             if (lane == 0) list.teacher = teacher;
         }
+        if (blocks > 1 && at_list == 0 && list.label >= 0) *label_logit = load_value<G>(row_base(list.row), list.label);
         if (blocks > 1 && id >= 0) {
+            const char *base = row_base(list.row);
+            *x = load_value<G>(base, id);
             const RowSplit s = split_row<G>(base, vocab);
             if (id < s.head) list.edge[id] = at_list;
             if (id >= vocab - s.tail) list.edge[s.head + id - (vocab - s.tail)] = at_list;
@@ -452,16 +466,40 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
         }
     };
 
+    // A row that takes no part.
+    const auto clear = [&](int64_t t) {
+        if (threadIdx.x == 0 && rank == 0) a.token_loss[t] = 0.0f;
+        if (!a.dlogits) return;
+        const RowSplit s = split_row<G>(row_base(t), vocab);
+        const RowShare own = row_share(s.granules, rank, log_blocks);
+        char *out = static_cast<char *>(a.dlogits) + t * a.ld_dlogits * G::kBytes;
+        if ((reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(row_base(t))) % 16 == 0) {
+            uint4 *to = reinterpret_cast<uint4 *>(out + s.head * G::kBytes) + own.begin;
+            for (int i = threadIdx.x; i < own.count; i += THREADS) to[i] = make_uint4(0, 0, 0, 0);
+        } else {
+            for (int i = threadIdx.x; i < own.count * E; i += THREADS) store_value<G>(out, s.head + own.begin * E + i, 0.0f);
+        }
+        const int edge_at = rank == 0 ? edge_element(s, threadIdx.x, vocab) : -1;
+        if (edge_at >= 0) store_value<G>(out, edge_at, 0.0f);
+    };
+    // In a given order, the rows that take no part are cleared between the others; this block's next one's place.
+    int idle = a.order ? items + first_item : rows;
+
     uint32_t phase = 0;
     int parity = 0;
     float x_own = 0.0f, label_logit = 0.0f;
-    ask(first_row, lists[0]);
-    take_list(first_row, lists[0], &x_own, &label_logit);
+    if (a.order && lists_it && first_item < items) {
+        if (at_list == 0) ahead[0] = a.order[first_item];
+        list_sync();
+    }
+    ask(first_item, 0);
+    take_list(first_item, lists[0], &x_own, &label_logit);
     __syncthreads();
-    if (lists[0].wanted && threadIdx.x == 0) fetch(first_row);
-    int64_t t = first_row;
-    for (; t < a.row.rows; t += step, parity ^= 1) {
+    if (lists[0].wanted && threadIdx.x == 0) fetch(lists[0].row);
+    int item = first_item;
+    for (; item < items; item += step, parity ^= 1) {
         Listed &list = lists[parity], &next = lists[parity ^ 1];
+        const int64_t t = list.row;
         const bool writes = a.dlogits != nullptr;
         const auto out_of = [&] { return static_cast<char *>(a.dlogits) + t * a.ld_dlogits * G::kBytes; };
         const auto same_phase = [&] { return (reinterpret_cast<uintptr_t>(out_of()) - reinterpret_cast<uintptr_t>(row_base(t))) % 16 == 0; };
@@ -510,7 +548,7 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
                 const RestSums part = warp_join<MODE>(RestSums{first ? x_own : -INFINITY, one, one}, k);
                 if (lane == 0) list.part[list_warp] = part;
             }
-            ask(t + step, next);                                 // while the walk goes on
+            ask(item + step, parity ^ 1);                        // while the walk goes on
             RestSums x{-INFINITY, 0.0f, 0.0f};
             {
                 const uint4 *from = kept_row + threadIdx.x;
@@ -539,7 +577,7 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
                 if (lane == 0) factors = f;
             }
             float x_next = 0.0f;
-            take_list(t + step, next, &x_next, &label_logit);    // while the others wait for the factors
+            take_list(item + step, next, &x_next, &label_logit); // while the others wait for the factors
             __syncthreads();
             const DistillFactors &f = factors;
             if (f.late) break;
@@ -582,7 +620,7 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
                 if (edge_at >= 0) store_value<G>(out, edge_at, rest_gradient<MODE>(edge, g, k));
             }
             __syncthreads();                                     // the row is read and written
-            if (next.wanted && threadIdx.x == 0) fetch(t + step);
+            if (next.wanted && threadIdx.x == 0) fetch(next.row);
             // While that is on its way: the listed elements and the label again, and the row's loss.
             if (writes && active) {
                 char *out = out_of();
@@ -615,35 +653,88 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
             }
         } else {
             __syncthreads();                                     // the last row's list has been read
-            ask(t + step, next);
-            if (threadIdx.x == 0 && rank == 0) a.token_loss[t] = 0.0f;
-        }
-        if (writes && !active) {
-            char *out = out_of();
-            if (same_phase()) {
-                uint4 *to = reinterpret_cast<uint4 *>(out + s.head * G::kBytes) + own.begin;
-                for (int i = threadIdx.x; i < own.count; i += THREADS) to[i] = make_uint4(0, 0, 0, 0);
-            } else {
-                for (int i = threadIdx.x; i < own.count * E; i += THREADS) store_value<G>(out, s.head + own.begin * E + i, 0.0f);
-            }
-            if (edge_at >= 0) store_value<G>(out, edge_at, 0.0f);
-        }
-        if (!list.wanted) {
-            take_list(t + step, next, &x_own, &label_logit);
+            ask(item + step, parity ^ 1);
+            take_list(item + step, next, &x_own, &label_logit);
             __syncthreads();
-            if (next.wanted && threadIdx.x == 0) fetch(t + step);
+            if (next.wanted && threadIdx.x == 0) fetch(next.row);
+        }
+        // What has no gradient: this row, and as many of the idle ones as keep step with the others.
+        int others = idle < rows ? ((rows - idle + step - 1) / step * step + items - item - 1) / (items - item) : 0;
+        for (int64_t zero = active ? -1 : t;;) {
+            if (zero >= 0) clear(zero);
+            if (others-- <= 0 || idle >= rows) break;
+            zero = a.order[idle];
+            idle += step;
         }
     }
+    for (; idle < rows; idle += step) clear(a.order[idle]);      // of a block that had no other row
     __syncthreads();                                             // the sums
     if (threadIdx.x == 0) {
-        if (t < a.row.rows) {                                    // a wait ran out
+        if (item < items) {                                      // a wait ran out
             barrier_wait(smem_address(&landed), phase ^ 1, kWaitTries);  // the copy in flight, if any
             sums.loss = sums.kl = sums.ce = sums.weight = NAN;
         }
         if (rank == 0)
-            a.partial[first_row] = make_float4(static_cast<float>(sums.loss), static_cast<float>(sums.kl), static_cast<float>(sums.ce), static_cast<float>(sums.weight));
+            a.partial[first_item] = make_float4(static_cast<float>(sums.loss), static_cast<float>(sums.kl), static_cast<float>(sums.ce), static_cast<float>(sums.weight));
     }
     if (blocks > 1) cluster_sync();                              // nobody leaves while a peer writes to its memory
+}
+
+// The order of the rows: those that take part in front.  A mask leaves one block more
+// rows than another, in the largest of hundreds by a third at 28 rows each; taken from a
+// list of those that take part they are dealt out evenly, and the others' zeros are
+// written beside them.  One block; a thread has every 1024th row and up to 64 of them.
+constexpr int kOrderThreads = 1024;
+constexpr int kMostOrdered = 64 * kOrderThreads;
+
+__global__ void __launch_bounds__(kOrderThreads) star_distillation_order_kernel(const __grid_constant__ RowArgs a, int32_t *order)
+{
+    __shared__ int warp_sums[32];
+    launch_dependents();
+    wait_for_primary();
+    const int rows = static_cast<int>(a.rows), lane = threadIdx.x % 32;
+    uint64_t taken = 0;
+    int have = 0;                            // rows of this thread
+    for (int first = threadIdx.x; first < rows; first += 8 * kOrderThreads) {
+        int64_t label[8];
+        float weight[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int t = first + q * kOrderThreads;
+            label[q] = t < rows && a.labels ? a.labels[t] : 0;
+            weight[q] = t < rows && a.weights ? a.weights[t] : 1.0f;
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            if (first + q * kOrderThreads < rows) {
+                taken |= static_cast<uint64_t>(takes_part(a, label[q], weight[q])) << have;
+                ++have;
+            }
+        }
+    }
+    const int mine = __popcll(taken);
+    int up_to = mine;                        // of the warp's threads up to this one
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        const int other = __shfl_up_sync(0xffffffffu, up_to, o);
+        if (lane >= o) up_to += other;
+    }
+    if (lane == 31) warp_sums[threadIdx.x / 32] = up_to;
+    __syncthreads();
+    int total = 0, in_front = 0;
+#pragma unroll
+    for (int w = 0; w < 32; ++w) {
+        if (w == static_cast<int>(threadIdx.x) / 32) in_front = total;
+        total += warp_sums[w];
+    }
+    // The rows in front of this thread's: every thread below has as many as this one or one more.
+    const int full = rows / kOrderThreads, rest = rows % kOrderThreads, threads = static_cast<int>(threadIdx.x);
+    int at = in_front + up_to - mine, other = total + full * threads + min(threads, rest) - at;
+    for (int i = 0; i < have; ++i) {
+        const int t = threads + i * kOrderThreads;
+        order[taken >> i & 1 ? at++ : other++] = t;
+    }
+    if (threadIdx.x == 0) order[rows] = total;
 }
 
 constexpr int kDistillSumThreads = 1024;

@@ -124,6 +124,43 @@ def test_strides_in_place_and_other_phases(dtype, offset, extra):
     assert torch.equal(apart, inside)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("kind", ["labels", "weights", "none", "one", "runs"])
+def test_many_rows_of_which_some_take_part(kind, dtype):
+    """Enough rows for every block to have several: they are taken in an order of their own."""
+    rows = 6007
+    x, ids, values, labels, w = make(rows, 501, 5, dtype, seed=20, rest=True)
+    drop = torch.rand(rows, generator=gpu(21), device="cuda") < 0.4
+    if kind == "labels":
+        labels[drop] = -100
+    elif kind == "weights":
+        w[drop] = 0.0
+    elif kind == "none":
+        w[:] = 0.0
+    elif kind == "one":
+        labels[:] = -1
+        labels[3000] = 7
+    else:
+        labels[100:4000] = 501
+    off = (labels < 0) | (labels >= 501) | (w == 0)
+    x[off] = math.nan
+    values[off] = math.nan
+    more = dict(rest=True, labels=labels, weights=w, label_coef=0.5, temperature=1.3)
+    loss, sums, dx = call(x, ids, values, **more)
+    on = torch.nonzero(~off)[:, 0]
+    pick = on[torch.randperm(len(on), generator=gpu(22), device="cuda")[:40]]
+    assert bool((loss[off] == 0).all()) and bool((dx[off] == 0).all())
+    if len(pick):
+        want = R.distillation(x[pick], ids[pick], values[pick], labels=labels[pick], weights=w[pick], temperature=1.3, rest=True, hard=0.5)
+        near(loss[pick], want["token_loss"], want["token_bound"])
+        near(dx[pick], want["dlogits"], want["grad_bound"] + R.half_step(dtype) * want["dlogits"].abs())
+    part = torch.where(off, torch.zeros_like(w), w).double()
+    assert abs(float(sums[0]) - float((part * loss.double()).sum())) <= 8 * R.ULP * float((part * loss.double().abs()).sum())
+    assert abs(float(sums[3]) - float(part.sum())) <= 8 * R.ULP * float(part.sum())
+    again = call(x, ids, values, in_place=True, **more)
+    assert torch.equal(again[0], loss) and torch.equal(again[1], sums) and torch.equal(again[2], dx)
+
+
 def test_inactive_rows_are_not_read():
     x, ids, values, labels, w = make(7, 3001, 9, BF16, seed=5)
     labels[1], labels[2], w[3] = -100, 3001, 0.0
