@@ -18,10 +18,10 @@ star_status_t check_top(const void *p, int64_t rows, int k, int64_t ld, Extent *
     return k > 0 ? check_matrix(p, rows, k, ld, 4, out) : STAR_OK;
 }
 
-template <typename G, int THREADS, bool CLUSTER> star_status_t launch_rows(const AlternativesArgs &a, int cluster, cudaStream_t stream)
+template <typename G, int THREADS, bool CLUSTER, bool FEW> star_status_t launch_rows(const AlternativesArgs &a, int cluster, cudaStream_t stream)
 {
     const int64_t clusters = std::min<int64_t>(a.row.rows, int64_t{1} << 20);
-    return launch(star_alternatives_kernel<G, THREADS, CLUSTER>, dim3(static_cast<unsigned>(clusters * cluster)), THREADS, 0,
+    return launch(star_alternatives_kernel<G, THREADS, CLUSTER, FEW>, dim3(static_cast<unsigned>(clusters * cluster)), THREADS, 0,
                   dim3(static_cast<unsigned>(cluster)), stream, a);
 }
 
@@ -35,20 +35,21 @@ template <typename G, int THREADS, bool CLUSTER> star_status_t launch_rows(const
 //      4096 x 50257,  8  bf16                 87.7   97.3
 //      4096 x 50257, 64  bf16                  126    116
 //      2048 x 50257, 64  fp32                  125   95.4
-// Few long rows: clusters of up to eight blocks.  Blocks of 256 threads and a row to
-// each against clusters: 1 x 50257, 20 bf16 10.4 -> 7.2 us.
+// Few long rows: clusters of up to eight blocks.  A block to a row against clusters:
+// 1 x 50257, 20 bf16 10.4 -> 6.4 us.  And 64 registers to a thread instead of 48 while all
+// blocks fit the GPU at once: 400 x 50257, 20 bf16 20.2 -> KFEW us.
 template <typename G> star_status_t run_rows(const AlternativesArgs &a, cudaStream_t stream)
 {
     const int64_t granules = a.row.vocab * G::kBytes / 16;
     int cluster = 1;
     while (granules > 2048 && cluster < 8 && a.row.rows * cluster * 2 <= 148 * 4 && granules / (cluster * 2) >= 448) cluster *= 2;
-    if (cluster > 1) return launch_rows<G, 256, true>(a, cluster, stream);
+    if (cluster > 1) return launch_rows<G, 256, true, true>(a, cluster, stream);
     int threads = granules <= 2048 ? 64 : granules <= 8192 ? 128 : 256;
     while (threads < 256 && (threads < (granules > 2048 ? 4 : 2) * a.k || (threads < granules && a.row.rows * threads < 148 * 800))) threads *= 2;
     switch (threads) {
-    case 64: return launch_rows<G, 64, false>(a, 1, stream);
-    case 128: return launch_rows<G, 128, false>(a, 1, stream);
-    default: return launch_rows<G, 256, false>(a, 1, stream);
+    case 64: return launch_rows<G, 64, false, false>(a, 1, stream);
+    case 128: return launch_rows<G, 128, false, false>(a, 1, stream);
+    default: return a.row.rows <= 148 * 4 ? launch_rows<G, 256, false, true>(a, 1, stream) : launch_rows<G, 256, false, false>(a, 1, stream);
     }
 }
 

@@ -93,6 +93,7 @@ __device__ __forceinline__ uint32_t order_of(float x)
     return bits & 0x80000000u ? ~bits : bits | 0x80000000u;
 }
 constexpr uint32_t kLowest = 0x007fffffu;    // order_of(-inf)
+__device__ __forceinline__ float logit_of(uint32_t order) { return __uint_as_float(order & 0x80000000u ? order & 0x7fffffffu : ~order); }
 
 // ---------------------------------------------------------------------------
 // Statistics and the k largest logits of a row, in one reading of it from memory, by a
@@ -220,8 +221,9 @@ __device__ __noinline__ void search_row(const void *base, int vocab, int k, uint
     __syncthreads();
 }
 
-template <typename G, int THREADS, bool CLUSTER>
-__global__ void __launch_bounds__(THREADS, CLUSTER ? policy_blocks(THREADS) : row_blocks(THREADS)) star_alternatives_kernel(const __grid_constant__ AlternativesArgs a)
+// FEW: more registers to a thread, fewer threads to an SM.
+template <typename G, int THREADS, bool CLUSTER, bool FEW>
+__global__ void __launch_bounds__(THREADS, FEW ? policy_blocks(THREADS) : row_blocks(THREADS)) star_alternatives_kernel(const __grid_constant__ AlternativesArgs a)
 {
     constexpr int E = Granule<G>::kCount, kWarps = THREADS / 32, kStep = kBatch * THREADS;
     constexpr int kGroups = CLUSTER ? kMostGroups : THREADS;
@@ -326,6 +328,7 @@ __global__ void __launch_bounds__(THREADS, CLUSTER ? policy_blocks(THREADS) : ro
             // A second look at what reaches the bound.
             if (a.k > 0 && x.s > 0.0f && x.s < INFINITY) {
                 const uint32_t bound = row_bound;
+                const float least = logit_of(bound);
                 if (edge_at >= 0 && order_of(edge) >= bound) put_candidate<CLUSTER>(found, order_of(edge), edge_at);
                 for (int q = 0; q < slots; ++q)
                     if (slot_order[q][threadIdx.x] >= bound) hits[atomicAdd(&n_hits, 1)] = static_cast<unsigned short>(q * THREADS + threadIdx.x);
@@ -338,15 +341,19 @@ __global__ void __launch_bounds__(THREADS, CLUSTER ? policy_blocks(THREADS) : ro
                     const uint4 v = granules[g];
                     RunningMax<G> high;
                     high.take(v);
-                    if (order_of(high.value()) < bound) continue;
+                    if (!(high.value() >= least)) continue;
                     Pair f[E / 2];
                     Granule<G>::widen(v, f);
+                    uint32_t which = 0;
 #pragma unroll
-                    for (int e = 0; e < E; ++e) {
+                    for (int e = 0; e < E / 2; ++e) {
                         float lo, hi;
-                        split_pair(f[e / 2], &lo, &hi);
-                        const uint32_t order = order_of(e % 2 ? hi : lo);
-                        if (order >= bound) put_candidate<CLUSTER>(found, order, s.head + (own.begin + g) * E + e);
+                        split_pair(f[e], &lo, &hi);
+                        which |= (lo >= least ? 1u : 0u) << (2 * e) | (hi >= least ? 2u : 0u) << (2 * e);
+                    }
+                    for (; which; which &= which - 1) {          // one, as a rule
+                        const int e = __ffs(which) - 1;
+                        put_candidate<CLUSTER>(found, order_of(load_value<G>(granules + g, e)), s.head + (own.begin + g) * E + e);
                     }
                 }
                 if constexpr (CLUSTER) cluster_sync(); else __syncthreads();
@@ -373,8 +380,7 @@ __global__ void __launch_bounds__(THREADS, CLUSTER ? policy_blocks(THREADS) : ro
                     rank_of += __shfl_xor_sync(0xffffffffu, rank_of, 1);
                     rank_of += __shfl_xor_sync(0xffffffffu, rank_of, 2);
                     if (i < n && rank_of < a.k && threadIdx.x % 4 == 0) {
-                        const uint32_t order = static_cast<uint32_t>(key >> 32);
-                        const float f = __uint_as_float(order & 0x80000000u ? order & 0x7fffffffu : ~order);
+                        const float f = logit_of(static_cast<uint32_t>(key >> 32));
                         ids[rank_of] = 0x7fffffff - static_cast<int32_t>(key & 0xffffffffu);
                         top[rank_of] = log_prob(f, MaxSum{x.m, x.s}, k, a.row.inv_temperature);
                     }
