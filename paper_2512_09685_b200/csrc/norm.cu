@@ -40,56 +40,91 @@ bool on_grid(const void *p, int64_t ld, int size, int bytes)
 
 constexpr int kBackEach = 2;
 
-// The threads that share a row, `each` columns to one: the next power of two.  0: a
-// row is too long for a block.
+// The threads that share a row, `each` columns to one: the next power of two.
 int row_threads(int64_t cols, int each)
 {
-    for (int t : {32, 64, 128, 256, 512, 1024})
-        if (cols <= int64_t{t} * each) return t;
-    return 0;
+    int t = 32;
+    while (t < 1024 && cols > int64_t{t} * each) t *= 2;
+    return t;
 }
 
-template <typename F> star_status_t with_threads(int threads, F f)
+// f with the number of threads at compile time, of those between LEAST and MOST.
+template <int LEAST, int MOST, typename F> star_status_t with_threads(int threads, F f)
 {
-    switch (threads) {
-    case 32: return f(std::integral_constant<int, 32>());
-    case 64: return f(std::integral_constant<int, 64>());
-    case 128: return f(std::integral_constant<int, 128>());
-    case 256: return f(std::integral_constant<int, 256>());
-    case 512: return f(std::integral_constant<int, 512>());
-    default: return f(std::integral_constant<int, 1024>());
+    if constexpr (LEAST < MOST)
+        if (threads > LEAST) return with_threads<LEAST * 2, MOST>(threads, f);
+    return f(std::integral_constant<int, LEAST>());
+}
+
+// How a row falls to threads: whole pieces of 16 bytes, single columns, or in turns.
+enum Way { kPieces, kColumns, kLong };
+
+template <typename G> star_status_t run_norm(const NormArgs &a, Way way, cudaStream_t stream)
+{
+    const auto blocks = [&](int threads) {
+        const int block = norm_block(threads);
+        return dim3(static_cast<unsigned>(std::min<int64_t>((a.rows * threads + block - 1) / block, 148 * 32)));
+    };
+    const int64_t cols = a.cols;
+    if (way == kPieces) {
+        // Half a block of 32 to a thread, or one: 4096 x 8192 bf16 49.7 and 43.2 us, 8192 x 4096 fp32 79.9 and 84.6.
+        if (cols <= 4096)
+            return with_threads<32, 256>(row_threads(cols, 16), [&](auto t) {
+                return launch(star_rms_norm_kernel<G, decltype(t)::value, 1>, blocks(t), norm_block(t), 0, dim3(1), stream, a);
+            });
+        return with_threads<256, 512>(row_threads(cols, 32), [&](auto t) {
+            return launch(star_rms_norm_kernel<G, decltype(t)::value, 2>, blocks(t), norm_block(t), 0, dim3(1), stream, a);
+        });
     }
-}
-
-template <typename G, int EACH> star_status_t run_norm(const NormArgs &a, int threads, cudaStream_t stream)
-{
-    if (threads == 0)
-        return launch(star_rms_norm_loose_kernel<G>, dim3(static_cast<unsigned>(std::min<int64_t>(a.rows, 148 * 32))), kNormThreads, 0, dim3(1), stream, a);
-    return with_threads(threads, [&](auto t) {
-        constexpr int kThreads = decltype(t)::value, kBlock = norm_block(kThreads);
-        const int64_t blocks = (a.rows * kThreads + kBlock - 1) / kBlock;
-        return launch(star_rms_norm_kernel<G, kThreads, EACH>, dim3(static_cast<unsigned>(std::min<int64_t>(blocks, 148 * 32))), kBlock, 0, dim3(1), stream, a);
-    });
-}
-
-template <typename G, bool KEPT> star_status_t run_backward(const NormGradArgs &a, int threads, int64_t *parts, cudaStream_t stream)
-{
-    if (threads == 0) {
-        *parts = std::min(a.rows, kMostParts);
-        return launch(star_rms_norm_backward_loose_kernel<G>, dim3(static_cast<unsigned>(*parts)), kNormThreads, 0, dim3(1), stream, a);
+    if (way == kColumns) {
+        if (cols <= 128) return launch(star_rms_norm_columns_kernel<G, 32, 4>, blocks(32), norm_block(32), 0, dim3(1), stream, a);
+        if (cols <= 8192)
+            return with_threads<32, 1024>(row_threads(cols, 8), [&](auto t) {
+                return launch(star_rms_norm_columns_kernel<G, decltype(t)::value, 8>, blocks(t), norm_block(t), 0, dim3(1), stream, a);
+            });
+        return launch(star_rms_norm_columns_kernel<G, 1024, 16>, blocks(1024), 1024, 0, dim3(1), stream, a);
     }
-    return with_threads(threads, [&](auto t) {
-        constexpr int kThreads = decltype(t)::value, kBlock = norm_block(kThreads);
-        constexpr int kStages = G::kBytes == 4 && kThreads <= 512 ? 3 : 2;
-        constexpr int kKib = (NormRing<G, KEPT, kBackEach, kStages>::kThread * kBlock + 1023) / 1024;
+    return launch(star_rms_norm_long_kernel<G>, dim3(static_cast<unsigned>(std::min<int64_t>(a.rows, 148 * 32))), kNormThreads, 0, dim3(1), stream, a);
+}
+
+// Blocks that stay, each with a row of sums: as many as the GPU holds.
+template <int THREADS, typename Kernel>
+star_status_t launch_backward(Kernel kernel, Held &known, int kib, const NormGradArgs &a, int64_t *parts, cudaStream_t stream)
+{
+    constexpr int kBlock = norm_block(THREADS);
+    int held = 0;
+    const cudaError_t e = held_clusters(kernel, known, kBlock, 1, kib, &held);
+    if (e != cudaSuccess) return cuda_failed(e);
+    *parts = std::min<int64_t>({(a.rows * THREADS + kBlock - 1) / kBlock, held, kMostParts});
+    return launch(kernel, dim3(static_cast<unsigned>(*parts)), kBlock, static_cast<size_t>(kib) * 1024, dim3(1), stream, a);
+}
+
+template <typename G, bool KEPT> star_status_t run_backward(const NormGradArgs &a, Way way, int64_t *parts, cudaStream_t stream)
+{
+    const int64_t cols = a.cols;
+    if (way == kPieces)
+        return with_threads<32, 1024>(row_threads(cols, kBackEach * 16 / G::kBytes), [&](auto t) {
+            constexpr int kThreads = decltype(t)::value;
+            // Rows on their way: 16384 x 4096 bf16 with 2, 3 and 4 of them 88.4, 89.1, 90.0 us, 8192 x 4096 fp32 88.6, 82.2, 89.2.
+            constexpr int kStages = G::kBytes == 4 && kThreads <= 512 ? 3 : 2;
+            constexpr int kKib = (NormRing<G, KEPT, kBackEach, kStages>::kThread * norm_block(kThreads) + 1023) / 1024;
+            static Held known;
+            return launch_backward<kThreads>(star_rms_norm_backward_kernel<G, KEPT, kThreads, kBackEach, kStages>, known, kKib, a, parts, stream);
+        });
+    // Four columns to a thread, or eight where a block has no more threads: 4096 x 4095 66.4 and 103 us.  (Forward the
+    // other way round, 130 and 89.5.)
+    if (way == kColumns && cols <= 4096)
+        return with_threads<32, 1024>(row_threads(cols, 4), [&](auto t) {
+            constexpr int kThreads = decltype(t)::value;
+            static Held known;
+            return launch_backward<kThreads>(star_rms_norm_backward_columns_kernel<G, KEPT, kThreads, 4>, known, 0, a, parts, stream);
+        });
+    if (way == kColumns) {
         static Held known;
-        int held = 0;
-        constexpr auto kernel = star_rms_norm_backward_kernel<G, KEPT, kThreads, kBackEach, kStages>;
-        const cudaError_t e = held_clusters(kernel, known, kBlock, 1, kKib, &held);
-        if (e != cudaSuccess) return cuda_failed(e);
-        *parts = std::min<int64_t>({(a.rows * kThreads + kBlock - 1) / kBlock, held, kMostParts});
-        return launch(kernel, dim3(static_cast<unsigned>(*parts)), kBlock, kKib * 1024, dim3(1), stream, a);
-    });
+        return launch_backward<1024>(star_rms_norm_backward_columns_kernel<G, KEPT, 1024, 8>, known, 0, a, parts, stream);
+    }
+    *parts = std::min(a.rows, kMostParts);
+    return launch(star_rms_norm_backward_long_kernel<G>, dim3(static_cast<unsigned>(*parts)), kNormThreads, 0, dim3(1), stream, a);
 }
 
 bool same(const void *a, int64_t ld_a, const void *b, int64_t ld_b, int64_t rows) { return a == b && (ld_a == ld_b || rows <= 1); }
@@ -142,10 +177,9 @@ extern "C" star_status_t star_rms_norm(void *y, int64_t ld_y, const void *x, int
                on_grid(y, ld_y, size, bytes);
     };
     a.wide = grid(32);
-    const int each = cols <= 4096 ? 1 : 2, threads = grid(16) ? row_threads(cols, each * 16) : 0;
+    const Way way = cols > 16384 ? kLong : grid(16) ? kPieces : kColumns;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (each == 1) return dtype == STAR_DTYPE_BF16 ? run_norm<GradBF16, 1>(a, threads, stream) : run_norm<GradF32, 1>(a, threads, stream);
-    return dtype == STAR_DTYPE_BF16 ? run_norm<GradBF16, 2>(a, threads, stream) : run_norm<GradF32, 2>(a, threads, stream);
+    return dtype == STAR_DTYPE_BF16 ? run_norm<GradBF16>(a, way, stream) : run_norm<GradF32>(a, way, stream);
 }
 
 extern "C" star_status_t star_rms_norm_workspace_bytes(int64_t rows, int64_t cols, size_t *bytes_out)
@@ -213,14 +247,14 @@ extern "C" star_status_t star_rms_norm_backward(void *dx, int64_t ld_dx, void *d
                on_grid(d_total, ld_d_total, size, bytes);
     };
     a.wide = grid(32);
-    const int threads = grid(16) ? row_threads(cols, kBackEach * 16 / size) : 0;
+    const Way way = grid(16) && cols <= 1024 * kBackEach * 16 / size ? kPieces : cols <= 1024 * 8 ? kColumns : kLong;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     int64_t parts = 0;
     if (rows > 0) {
         if (dtype == STAR_DTYPE_BF16)
-            st = total ? run_backward<GradBF16, false>(a, threads, &parts, stream) : run_backward<GradBF16, true>(a, threads, &parts, stream);
+            st = total ? run_backward<GradBF16, false>(a, way, &parts, stream) : run_backward<GradBF16, true>(a, way, &parts, stream);
         else
-            st = total ? run_backward<GradF32, false>(a, threads, &parts, stream) : run_backward<GradF32, true>(a, threads, &parts, stream);
+            st = total ? run_backward<GradF32, false>(a, way, &parts, stream) : run_backward<GradF32, true>(a, way, &parts, stream);
         if (st != STAR_OK) return st;
     }
     if (!dgain) return STAR_OK;
