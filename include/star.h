@@ -494,7 +494,8 @@ STAR_API star_status_t star_group_update_host_ex(float *h_params, float *h_momen
  * side by side in the rows of one buffer, those with different strides may not.
  * All sums, softmax statistics
  * and activation values are held in binary32; results are rounded once.  The
- * same call on the same inputs gives the same bits.
+ * same call on the same inputs gives the same bits.  A workspace belongs to one call at
+ * a time: calls, or captured graphs, that may run at once need one each.
  * ------------------------------------------------------------------------- */
 
 /* Rows of logits x[t][0 .. vocab), one label each.  With z = x / temperature,
@@ -640,14 +641,15 @@ STAR_API star_status_t star_token_alternatives_backward(void *dlogits, int64_t l
  *   labels  : NULL only where label_coef is 0.  A row is active iff its label, where
  *             labels are given, lies in [0, vocab), its weight is not 0 (1 without
  *             weights) and not every logit is -inf; the others have token_loss 0 and a
- *             zero gradient, and their logits and lists are not read
+ *             zero gradient, and their logits and lists may hold anything
  *   teacher_ids, teacher_values : rows x k, strides ld_ids and ld_values
  *   dlogits : as for the policy loss (NULL: forward alone; may be the logits)
  *   token_loss : rows entries;  sums : 4 entries
  *   workspace : device, 16-byte aligned, star_loss_workspace_bytes(rows, 0) bytes
  * Coefficients and temperatures finite, the latter > 0.  k up to STAR_MAX_ALTERNATIVES,
- * rows of logits up to 1.6 MiB (851968 of bf16, 425984 of fp32): STAR_ERR_UNSUPPORTED
- * beyond.  Two kernel launches.  It waits inside its kernel as the policy loss does. */
+ * rows of logits up to 1.6 MiB (851968 of bf16, 425984 of fp32), fewer than 2^30 of
+ * them: STAR_ERR_UNSUPPORTED beyond.  Two or three kernel launches.  It waits inside its
+ * kernel as the policy loss does. */
 STAR_API star_status_t star_distillation_loss(const void *logits, star_dtype_t dtype, int64_t rows,
                                               int64_t vocab, int64_t ld, const int32_t *teacher_ids,
                                               int64_t ld_ids, const float *teacher_values, int64_t ld_values,

@@ -178,11 +178,12 @@ template <typename G, int THREADS> __device__ int count_row(const void *base, in
 
 // The candidates of a row that `low` leaves too many of (but at least k), by one block:
 // counting finds a bound that leaves few enough, or the k-th largest logit itself, whose
-// equals are then taken by ascending index.
+// equals are then taken by ascending index.  `high`: the largest logit's.  A row of one
+// value needs no counting, others up to 32 passes over the row (from L2).
 template <typename G, int THREADS>
-__device__ __noinline__ void search_row(const void *base, int vocab, int k, uint32_t low, Candidates &found, int *scratch)
+__device__ __noinline__ void search_row(const void *base, int vocab, int k, uint32_t low, uint32_t high, Candidates &found, int *scratch)
 {
-    uint32_t width = 0xffffffffu - low;
+    uint32_t width = high - low;
     int reach = kMostCandidates + 1;         // logits at or above low
     while (width > 0 && reach > kMostCandidates) {
         const uint32_t mid = low + (width - width / 2);
@@ -357,7 +358,7 @@ __global__ void __launch_bounds__(THREADS, FEW ? policy_blocks(THREADS) : row_bl
                     }
                 }
                 if constexpr (CLUSTER) cluster_sync(); else __syncthreads();
-                if (rank == 0 && found.count > kMostCandidates) search_row<G, THREADS>(base, vocab, a.k, bound, found, &scratch);
+                if (rank == 0 && found.count > kMostCandidates) search_row<G, THREADS>(base, vocab, a.k, bound, order_of(x.m), found, &scratch);
             }
         }
         if (rank == 0) {                                         // the rest is the first block's

@@ -488,6 +488,10 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
     uint32_t phase = 0;
     int parity = 0;
     float x_own = 0.0f, label_logit = 0.0f;
+    if (threadIdx.x == 0 && first_item < items) {                // the first row's copy does not wait for its list
+        const int64_t t = a.order ? a.order[first_item] : first_item;
+        if (takes_part(a.row, a.row.labels ? a.row.labels[t] : 0, a.row.weights ? a.row.weights[t] : 1.0f)) fetch(t);
+    }
     if (a.order && lists_it && first_item < items) {
         if (at_list == 0) ahead[0] = a.order[first_item];
         list_sync();
@@ -495,7 +499,6 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
     ask(first_item, 0);
     take_list(first_item, lists[0], &x_own, &label_logit);
     __syncthreads();
-    if (lists[0].wanted && threadIdx.x == 0) fetch(lists[0].row);
     int item = first_item;
     for (; item < items; item += step, parity ^= 1) {
         Listed &list = lists[parity], &next = lists[parity ^ 1];
