@@ -63,8 +63,9 @@ template <typename G> star_status_t run_mode(const DistillArgs &a, int threads, 
 }
 
 // The smallest block whose part of the SM's shared memory holds a row, or a cluster
-// of them; the cluster's blocks may take an SM's shared memory each.  More blocks to
-// a row where there are few.
+// of them; the cluster's blocks may take an SM's shared memory each.  More threads and
+// more blocks to a row where there are few: 302 x 3071 bf16 with 512 threads instead of
+// 128, and few to the sums, 11.5 -> 8.4 us; 37 x 32001 fp32 17.9 -> 15.3.
 bool shape(int64_t rows, int64_t vocab, int size, int *threads, int *cluster)
 {
     const int64_t bytes = vocab * size;
@@ -73,6 +74,7 @@ bool shape(int64_t rows, int64_t vocab, int size, int *threads, int *cluster)
     for (int t : {512, 256, 128})
         if (bytes <= int64_t{kDistillBytesPerThread} * t) *threads = t;
     while (*cluster < 8 && bytes > int64_t{kDistillBytesPerThread} * *threads * *cluster) *cluster *= 2;
+    while (*threads < 512 && rows * *threads < 148 * 512 && bytes > 16 * *threads) *threads *= 2;
     while (*cluster < 8 && rows * *cluster * 2 <= 148 * 2 && bytes / (*cluster * 2) >= 448 * 16) *cluster *= 2;
     return bytes <= int64_t{kDistillBytesPerThread} * 1024 * *cluster;
 }
@@ -126,6 +128,8 @@ extern "C" star_status_t star_distillation_loss(const void *logits, star_dtype_t
         st = dtype == STAR_DTYPE_BF16 ? run_mode<GradBF16>(a, threads, cluster, &parts, stream) : run_mode<GradF32>(a, threads, cluster, &parts, stream);
         if (st != STAR_OK) return st;
     }
-    return launch(star_distillation_sums_kernel, dim3(1), kDistillSumThreads, 0, dim3(1), stream, static_cast<const float4 *>(a.partial),
+    int sum_threads = 32;
+    while (sum_threads < kDistillSumThreads && sum_threads * 2 <= parts) sum_threads *= 2;
+    return launch(star_distillation_sums_kernel, dim3(1), sum_threads, 0, dim3(1), stream, static_cast<const float4 *>(a.partial),
                   static_cast<int64_t>(parts), sums);
 }

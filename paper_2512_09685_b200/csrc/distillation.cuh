@@ -740,21 +740,28 @@ __global__ void __launch_bounds__(kOrderThreads) star_distillation_order_kernel(
     if (threadIdx.x == 0) order[rows] = total;
 }
 
-constexpr int kDistillSumThreads = 1024;
+constexpr int kDistillSumThreads = 1024;     // at most; fewer for few parts
 
 __global__ void __launch_bounds__(kDistillSumThreads) star_distillation_sums_kernel(const float4 *partial, int64_t n, float *sums)
 {
-    __shared__ double shared[kDistillSumThreads / 32];
+    __shared__ double shared[kDistillSumThreads / 32][4];
     wait_for_primary();
     double s[4] = {0.0, 0.0, 0.0, 0.0};
-    for (int64_t i = threadIdx.x; i < n; i += kDistillSumThreads) {
+    for (int64_t i = threadIdx.x; i < n; i += blockDim.x) {
         const float4 x = partial[i];
         s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
     }
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const double total = block_sum(s[q], shared);
-        if (threadIdx.x == 0) sums[q] = static_cast<float>(total);
+    for (int q = 0; q < 4; ++q) s[q] = warp_sum_wide(s[q]);
+    if (threadIdx.x % 32 == 0) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) shared[threadIdx.x / 32][q] = s[q];
+    }
+    __syncthreads();
+    if (threadIdx.x < 4) {
+        double total = 0.0;
+        for (unsigned w = 0; w < blockDim.x / 32; ++w) total += shared[w][threadIdx.x];
+        sums[threadIdx.x] = static_cast<float>(total);
     }
 }
 

@@ -260,7 +260,9 @@ extern "C" star_status_t star_rms_norm_backward(void *dx, int64_t ld_dx, void *d
     if (!dgain) return STAR_OK;
     const dim3 gain_grid(static_cast<unsigned>(std::min<int64_t>((cols + 31) / 32, 148 * 16)));
     const float *partial = static_cast<const float *>(workspace);
+    int gain_threads = 32;                               // four rows of sums to a warp, up to 32 warps
+    while (gain_threads < kGainThreads && gain_threads / 8 < parts) gain_threads *= 2;
     return dgain_dtype == STAR_DTYPE_BF16
-               ? launch(star_rms_norm_gain_kernel<GradBF16>, gain_grid, kGainThreads, 0, dim3(1), stream, partial, parts, a.cols, dgain, accumulate)
-               : launch(star_rms_norm_gain_kernel<GradF32>, gain_grid, kGainThreads, 0, dim3(1), stream, partial, parts, a.cols, dgain, accumulate);
+               ? launch(star_rms_norm_gain_kernel<GradBF16>, gain_grid, gain_threads, 0, dim3(1), stream, partial, parts, a.cols, dgain, accumulate)
+               : launch(star_rms_norm_gain_kernel<GradF32>, gain_grid, gain_threads, 0, dim3(1), stream, partial, parts, a.cols, dgain, accumulate);
 }

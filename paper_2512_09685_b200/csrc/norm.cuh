@@ -604,7 +604,7 @@ star_rms_norm_backward_kernel(const __grid_constant__ NormGradArgs a)
     }
 }
 
-// dgain from the blocks' sums: 32 columns to a block, 32 warps that share the rows.
+// dgain from the blocks' sums: 32 columns to a block, up to 32 warps that share the rows.
 constexpr int kGainThreads = 1024;
 
 template <typename W>
@@ -612,17 +612,17 @@ __global__ void __launch_bounds__(kGainThreads) star_rms_norm_gain_kernel(const 
 {
     __shared__ float part[32][33];
     wait_for_primary();
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = blockDim.x / 32;
     for (int base = blockIdx.x * 32; base < cols; base += gridDim.x * 32) {
         const int c = base + lane;
         float x = 0.0f;
         if (c < cols)
-            for (int64_t q = warp; q < parts; q += 32) x = __fadd_rn(x, partial[q * cols + c]);
+            for (int64_t q = warp; q < parts; q += warps) x = __fadd_rn(x, partial[q * cols + c]);
         part[warp][lane] = x;
         __syncthreads();
         if (warp == 0 && c < cols) {
             double sum = accumulate ? static_cast<double>(load_value<W>(dgain, c)) : 0.0;
-            for (int w = 0; w < 32; ++w) sum += part[w][lane];
+            for (int w = 0; w < warps; ++w) sum += part[w][lane];
             store_value<W>(dgain, c, static_cast<float>(sum));
         }
         __syncthreads();
