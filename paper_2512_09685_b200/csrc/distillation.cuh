@@ -44,8 +44,9 @@ struct alignas(16) DistillFactors {
     float m_rest;        // the largest element that is not listed
     float rest, rest1;   // dlogits[j] = rest 2^exponent(x, m_rest) + rest1 2^exponent1(x, m_rest)
     float m, s, s1;      // of the whole row
-    float inv_s, log_s;
+    float inv_s;
     float rest_s;        // of what is not listed, at m_rest
+    float p_listed;      // the student's probability of the listed
     float p0, q0;        // the probabilities of what is not listed, the student's and the teacher's; q0 of 0: no such term
     float mass;          // what the teacher's probabilities that count add up to
     float soft, hard;    // weight and coefficients in front of the gradient's parts
@@ -83,13 +84,23 @@ __device__ __forceinline__ double warp_sum_wide(double x)
 // log-probability of a value v, the difference first, as for the student's; log_sum =
 // -inf: nothing is listed.
 struct Teacher {
-    float shift, log_sum;
+    double log_sum;
+    float shift;
     float mass;          // of the listed
     float missing;       // 1 - mass where the rest counts, else 0
 };
-__device__ __forceinline__ float listed_log(const DistillArgs &a, float v, const Teacher &t)
+// log s of a normal number, to half a step of its mantissa's part: the exponent's part is exact in binary64.
+__device__ __forceinline__ double log_wide(float s)
 {
-    return t.log_sum == -INFINITY ? -INFINITY : __fsub_rn(__fmul_rn(__fsub_rn(v, t.shift), a.inv_teacher_temperature), t.log_sum);
+    if (!(s < INFINITY)) return s;                               // NaN
+    const int bits = __float_as_int(s);
+    return static_cast<double>((bits >> 23) - 127) * 0.693147180559945309417 + static_cast<double>(logf(__int_as_float((bits & 0x007fffff) | 0x3f800000)));
+}
+// In binary64: a loss near 0 is made of small differences of such logarithms.
+__device__ __forceinline__ double listed_log(const DistillArgs &a, float v, const Teacher &t)
+{
+    if (t.log_sum == -INFINITY) return -INFINITY;
+    return (static_cast<double>(v) - static_cast<double>(t.shift)) * static_cast<double>(a.inv_teacher_temperature) - t.log_sum;
 }
 
 // A row's list, with a thread for each entry, and what else there is to know of a row
@@ -144,13 +155,13 @@ __device__ __forceinline__ Teacher make_teacher(const DistillArgs &a, const List
         bad |= list.most[w] != list.most[w];
         shift = fmaxf(shift, list.most[w]);
     }
-    if (bad || shift == INFINITY) return Teacher{0.0f, NAN, NAN, NAN};
-    if (shift == -INFINITY) return a.rest ? Teacher{0.0f, 0.0f, 0.0f, 1.0f} : Teacher{0.0f, -INFINITY, 0.0f, 0.0f};
+    if (bad || shift == INFINITY) return Teacher{NAN, 0.0f, NAN, NAN};
+    if (shift == -INFINITY) return a.rest ? Teacher{0.0, 0.0f, 0.0f, 1.0f} : Teacher{-INFINITY, 0.0f, 0.0f, 0.0f};
     double sum = 0.0;
     for (int w = 0; w < warps; ++w)
         if (list.most[w] > -INFINITY) sum += list.sum[w] * static_cast<double>(a.rest ? 1.0f : expf(__fmul_rn(__fsub_rn(list.most[w], shift), a.inv_teacher_temperature)));
-    if (a.rest) return Teacher{0.0f, 0.0f, static_cast<float>(sum), static_cast<float>(1.0 - sum)};      // log-probabilities already
-    return Teacher{shift, logf(static_cast<float>(sum)), 1.0f, 0.0f};
+    if (a.rest) return Teacher{0.0, 0.0f, static_cast<float>(sum), static_cast<float>(1.0 - sum)};      // log-probabilities already
+    return Teacher{log_wide(static_cast<float>(sum)), shift, 1.0f, 0.0f};
 }
 
 // A row's factors from its statistics without and of the listed elements, by a warp: what
@@ -165,10 +176,12 @@ __device__ __forceinline__ DistillFactors make_factors(const DistillArgs &a, con
     f.m = fmaxf(rest.m, listed.m);
     const float down = rest.s == 0.0f ? 0.0f : rebase(rest.m, f.m, k);
     const float rest_s = __fmul_rn(rest.s, down);                // what is not listed, at the row's reference
-    f.s = __fadd_rn(__fmul_rn(listed.s, rebase(listed.m, f.m, k)), rest_s);
+    const float listed_s = __fmul_rn(listed.s, rebase(listed.m, f.m, k));
+    f.s = __fadd_rn(listed_s, rest_s);
     f.active = !(f.s == 0.0f);
     f.inv_s = reciprocal_fast(f.s);                              // sums are near 1 or more
     f.p0 = __fmul_rn(rest_s, f.inv_s);
+    f.p_listed = __fmul_rn(listed_s, f.inv_s);
     f.q0 = teacher.missing > 0.0f && rest.s > 0.0f ? teacher.missing : 0.0f;
     f.mass = f.q0 > 0.0f ? 1.0f : teacher.mass;
     f.soft = __fmul_rn(__fmul_rn(weight, a.soft), inv_t);
@@ -183,7 +196,6 @@ __device__ __forceinline__ DistillFactors make_factors(const DistillArgs &a, con
     } else {
         f.rest = __fmaf_rn(f.hard, __fmul_rn(down, f.inv_s), f.rest);
     }
-    f.log_s = logf(f.s);
     return f;
 }
 
@@ -196,9 +208,13 @@ __device__ __forceinline__ void row_loss(const DistillArgs &a, const Teacher &te
 {
     const float inv_t = a.row.inv_temperature, k = __fmul_rn(inv_t, kLog2e);
     const MaxSum row{f.m, f.s};
-    // log p0 by its parts: it exists where p0 itself is below binary32.
     float d = 0.0f;
-    if (f.q0 > 0.0f) d = __fsub_rn(__fadd_rn(log_prob(f.m_rest, row, k, inv_t), logf(f.rest_s)), logf(f.q0));
+    if (f.q0 > 0.0f) {
+        // log p0 and log q0 keep their digits near 0 by way of what is listed, and p0's exists where p0 itself is
+        // below binary32 by its parts.
+        const float log_p0 = f.p_listed < 0.5f ? log1pf(-f.p_listed) : f.p0 > 1e-30f ? logf(f.p0) : __fadd_rn(log_prob(f.m_rest, row, k, inv_t), logf(f.rest_s));
+        d = __fsub_rn(log_p0, teacher.mass < 0.5f ? log1pf(-teacher.mass) : logf(f.q0));
+    }
     const float off = f.q0 > 0.0f ? 0.0f : a.rest ? -teacher.missing : __fsub_rn(f.mass, 1.0f);      // the teacher's sum - 1
     *kl_out = __fadd_rn(__fadd_rn(terms, divergence(f.q0, f.p0, d)), off);
     *ce_out = 0.0f;
@@ -592,12 +608,13 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
                 float term = 0.0f;
                 if (id >= 0) {
                     const float p = __fmul_rn(exp2_fast(exponent(x_own, f.m, k)), f.inv_s);
-                    const float log_q = listed_log(a, list.value[at_list], list.teacher);
-                    float q = expf(log_q);
-                    term = divergence(q, p, __fsub_rn(__fsub_rn(__fmul_rn(__fsub_rn(x_own, pivot(f.m)), a.row.inv_temperature), f.log_s), log_q));
+                    const double log_q = listed_log(a, list.value[at_list], list.teacher), log_s = log_wide(f.s);
+                    const double log_p = (static_cast<double>(x_own) - static_cast<double>(pivot(f.m))) * static_cast<double>(a.row.inv_temperature) - log_s;
+                    float q = expf(static_cast<float>(log_q));
+                    term = divergence(q, p, static_cast<float>(log_p - log_q));
                     if (!first) term = __fsub_rn(term, p);       // its probability has been counted
                     for (int i = at_list + 1; list.twice && i < a.k; ++i)        // q of all entries with this id
-                        if (list.ids()[i] == id) q = __fadd_rn(q, expf(listed_log(a, list.value[i], list.teacher)));
+                        if (list.ids()[i] == id) q = __fadd_rn(q, expf(static_cast<float>(listed_log(a, list.value[i], list.teacher))));
                     if (f.soft != 0.0f) listed_gradient = __fmul_rn(f.soft, __fmaf_rn(f.mass, p, -q));
                     if (f.hard != 0.0f) {
                         const float p1 = MODE != kOne ? __fmul_rn(exp2_fast(exponent(x_own, f.m, kLog2e)), reciprocal_fast(f.s1)) : p;

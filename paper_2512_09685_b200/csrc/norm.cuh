@@ -327,17 +327,34 @@ __global__ void __launch_bounds__(norm_block(THREADS)) star_rms_norm_columns_ker
         }
         const NormFactor r = norm_factor(group_total<THREADS, kBlock>(static_cast<double>(squares), part[parity]), a.inv_cols, a.eps);
         if (at == 0 && a.rstd) a.rstd[t] = r.high;
+        float g[EACH];
+        if (a.gain == nullptr) {
+#pragma unroll
+            for (int q = 0; q < EACH; ++q) g[q] = 1.0f;
+        } else if (a.gain_wide) {
+#pragma unroll
+            for (int q = 0; q < EACH; ++q) g[q] = q * THREADS + at < a.cols ? load_value<GradF32>(a.gain, q * THREADS + at) : 0.0f;
+        } else {
+#pragma unroll
+            for (int q = 0; q < EACH; ++q) g[q] = q * THREADS + at < a.cols ? load_value<GradBF16>(a.gain, q * THREADS + at) : 0.0f;
+        }
         char *y = static_cast<char *>(a.y) + t * a.ld_y * G::kBytes;
 #pragma unroll
         for (int q = 0; q < EACH; ++q) {
-            const int c = q * THREADS + at;
-            if (q * THREADS + at / 32 * 32 >= a.cols) break;     // a warp's 32 columns, all beyond the row
-            const float w = c < a.cols ? as_stored<G>(scaled(__fmul_rn(v[q], gain_at(a.gain, a.gain_wide, c)), r)) : 0.0f;
-            if (c < a.cols) store_value<G>(y, c, w);
-            if (a.kept.codes) {
-                const int s = scale_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(w) & 0x7fffffffu));
-                if (c < a.kept.pitch) a.kept.codes[t * a.kept.pitch + c] = s == 255 ? 0 : static_cast<int8_t>(code_bits(w, scale_inverse(s)) & 0xffu);
-                if (at % 32 == 0) a.kept.scales[scale_at(a.kept, t, c / 32)] = static_cast<uint8_t>(s);
+            v[q] = as_stored<G>(scaled(__fmul_rn(v[q], g[q]), r));
+            if (q * THREADS + at < a.cols) store_value<G>(y, q * THREADS + at, v[q]);
+        }
+        if (a.kept.codes) {
+            int8_t *codes = a.kept.codes + t * a.kept.pitch + at;
+            const int pitch = static_cast<int>(a.kept.pitch), first = at / 32 * 32;
+#pragma unroll
+            for (int q = 0; q < EACH; ++q) {
+                if (q * THREADS + first < a.cols) {              // not a warp's 32 columns beyond the row
+                    const float w = q * THREADS + at < a.cols ? v[q] : 0.0f;
+                    const int s = scale_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(w) & 0x7fffffffu));
+                    if (q * THREADS + at < pitch) codes[q * THREADS] = s == 255 ? 0 : static_cast<int8_t>(code_bits(w, scale_inverse(s)) & 0xffu);
+                    if (at % 32 == 0) a.kept.scales[scale_at(a.kept, t, (q * THREADS + at) / 32)] = static_cast<uint8_t>(s);
+                }
             }
         }
     }

@@ -204,6 +204,19 @@ def test_a_student_that_is_sure(rest):
         check(x, ids, values, rest=rest, weights=w, labels=labels, label_coef=0.5)
 
 
+@pytest.mark.parametrize("temperature,k", [(4.0, 3), (2.0, 40), (3.3, 1), (1.0, 128)])
+@pytest.mark.parametrize("rest", [False, True])
+def test_small_losses_keep_their_digits(temperature, k, rest):
+    """Flat distributions, of which the list is a small part: the loss is made of logarithms that nearly cancel.  They are
+    off by what the student's sum is, 2 half steps, and by the temperature's rounding times an exponent of about 10; the
+    terms' d^2 / 2 with d of about 0.7 / temperature by that over d / 2."""
+    x, ids, values, _, _ = make(40, 20011, k, BF16, seed=30, rest=rest, temperature=temperature)
+    more = dict(rest=rest, temperature=temperature, teacher_temperature=1.0 if rest else temperature)
+    loss, _, _, want = check(x, ids, values, **more)
+    off = float((loss.double() - want["token_loss"]).norm() / want["token_loss"].norm())
+    assert off <= R.ULP * (2 + 10) * temperature / 0.7 * 2, off
+
+
 def test_teacher_and_student_alike():
     """Near 0 the loss keeps its digits: its terms are of one sign."""
     from paper_2512_09685_b200 import binding as B
