@@ -108,6 +108,10 @@ __device__ __forceinline__ float logit_of(uint32_t order) { return __uint_as_flo
 // block looks again (in L2) at those that reach the bound, and what it finds are the
 // candidates, whose ranks are counted.  Rows that leave too many of them (many equal
 // logits, or the large ones side by side) are searched for the k-th largest by counting.
+//
+// 4096 x 50257 bf16, k = 64: 111 us, of which the walk with its sums 77 (64 without the
+// entropy's), the second look 15, ranks 7, the bound 3; issue-bound more than by memory
+// (63).
 // ---------------------------------------------------------------------------
 constexpr int kMostCandidates = 1088;        // of bf16: 128 threads' one granule, and the edges
 constexpr int kMostGroups = 512;             // of a cluster; of a block: its threads
@@ -406,6 +410,10 @@ __global__ void __launch_bounds__(THREADS, FEW ? policy_blocks(THREADS) : row_bl
 // alternative names is found out once for all of it, a thread to an entry; their
 // elements' logits are read before anything is stored (the gradient may replace the
 // logits) and their gradients stored after it.
+//
+// Bound by memory: 4096 x 50257 bf16 135 us with entropy, 6.1 TB/s; 151 with 64
+// alternatives (a warp to each 1024 elements, which asked anew what names them, 174 and
+// 228).
 // ---------------------------------------------------------------------------
 struct AlternativesGradArgs {
     RowArgs row;                 // labels may be null

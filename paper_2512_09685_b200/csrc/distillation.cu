@@ -91,7 +91,7 @@ extern "C" star_status_t star_distillation_loss(const void *logits, star_dtype_t
     if (k < 0 || !std::isfinite(soft_coef) || !std::isfinite(label_coef) || !(teacher_temperature > 0.0f) ||
         !std::isfinite(teacher_temperature) || !std::isfinite(1.0f / teacher_temperature))
         return STAR_ERR_INVALID_ARG;
-    if (k > kMostListed || rows > 0x3fffffff) return STAR_ERR_UNSUPPORTED;
+    if (k > kMostListed) return STAR_ERR_UNSUPPORTED;
     DistillArgs a{};
     Extent read[5], written[4];
     star_status_t st = check_rows(logits, dtype, rows, vocab, ld, labels, temperature, &a.row, read, label_coef == 0.0f);
@@ -106,7 +106,7 @@ extern "C" star_status_t star_distillation_loss(const void *logits, star_dtype_t
     if (st == STAR_OK && (overlaps_any(written[3], read + 1, 4) || overlaps_any(written[3], written, 3))) st = STAR_ERR_INVALID_ARG;
     if (st != STAR_OK) return st;
     int threads = 0, cluster = 0, parts = 0;
-    if (!shape(rows, vocab, dtype_size(dtype), &threads, &cluster)) return STAR_ERR_UNSUPPORTED;
+    if (rows > 0x3fffffff || !shape(rows, vocab, dtype_size(dtype), &threads, &cluster)) return STAR_ERR_UNSUPPORTED;
     a.row.weights = weights;
     a.ids = teacher_ids;
     a.values = teacher_values;
