@@ -100,18 +100,22 @@ template <int THREADS, int BLOCK, typename T> __device__ __forceinline__ T group
 
 // ---------------------------------------------------------------------------
 // Rows longer than a block's registers hold: a block to a row, a warp on blocks of 32
-// columns, a lane to a column; the row is read again for its results.
+// columns, a lane to a column; the row is read again for its results.  A thread
+// counts its steps: a column beyond the last of up to 2^31 - 65 has no number.
 // ---------------------------------------------------------------------------
 constexpr int kNormThreads = 256;
+__device__ __forceinline__ int long_column(int step) { return step * kNormThreads + static_cast<int>(threadIdx.x); }
+__device__ __forceinline__ int long_steps(int cols) { return (cols - static_cast<int>(threadIdx.x) - 1) / kNormThreads + 1; }    // cols >= threads
 
 // The sum of f(c) over a thread's columns: runs of 16 in binary32, added up in binary64.  In
 // binary32 alone a million columns of one value, 4096 to a thread, are off by 3e-5.
-template <typename F> __device__ __forceinline__ double sum_of_runs(int cols, F f)
+template <typename F> __device__ __forceinline__ double sum_of_runs(int steps, F f)
 {
     double sum = 0.0;
-    for (int c = threadIdx.x; c < cols;) {
+    for (int i = 0; i < steps;) {
         float run = 0.0f;
-        for (const int end = min(cols - c, 16 * kNormThreads) + c; c < end; c += kNormThreads) run = f(c, run);
+#pragma unroll 4
+        for (const int end = min(steps, i + 16); i < end; ++i) run = f(long_column(i), run);
         sum += static_cast<double>(run);
     }
     return sum;
@@ -123,7 +127,7 @@ __global__ void __launch_bounds__(kNormThreads) star_rms_norm_long_kernel(const 
     __shared__ double part[2][kNormThreads / 32];
     wait_for_primary();
     int parity = 0;
-    const int padded = (a.cols + 31) / 32 * 32;
+    const int steps = long_steps(a.cols), padded_steps = long_steps((a.cols + 31) / 32 * 32);
     for (int64_t t = blockIdx.x; t < a.rows; t += gridDim.x, parity ^= 1) {
         const char *x = static_cast<const char *>(a.x) + t * a.ld_x * G::kBytes;
         const char *residual = static_cast<const char *>(a.residual) + t * a.ld_residual * G::kBytes;
@@ -132,7 +136,7 @@ __global__ void __launch_bounds__(kNormThreads) star_rms_norm_long_kernel(const 
             const float v = load_value<G>(x, c);
             return a.residual ? as_stored<G>(__fadd_rn(v, load_value<G>(residual, c))) : v;
         };
-        const double squares = sum_of_runs(a.cols, [&](int c, float run) {
+        const double squares = sum_of_runs(steps, [&](int c, float run) {
             const float s = stream(c);
             if (a.total) store_value<G>(total, c, s);
             return __fmaf_rn(s, s, run);
@@ -141,7 +145,8 @@ __global__ void __launch_bounds__(kNormThreads) star_rms_norm_long_kernel(const 
         if (threadIdx.x == 0 && a.rstd) a.rstd[t] = r.high;
         char *y = static_cast<char *>(a.y) + t * a.ld_y * G::kBytes;
         // What was written to `total` is read back by the thread that wrote it.
-        for (int c = threadIdx.x; c < padded; c += kNormThreads) {
+        for (int i = 0; i < padded_steps; ++i) {
+            const int c = long_column(i);
             float v = 0.0f;
             if (c < a.cols) {
                 v = a.total ? load_value<G>(total, c) : stream(c);
@@ -168,6 +173,7 @@ __global__ void __launch_bounds__(kNormThreads) star_rms_norm_backward_long_kern
     wait_for_primary();
     int parity = 0;
     float *sums = a.partial ? a.partial + static_cast<int64_t>(blockIdx.x) * a.cols : nullptr;
+    const int steps = long_steps(a.cols);
     for (int64_t t = blockIdx.x; t < a.rows; t += gridDim.x, parity ^= 1) {
         const char *dy = static_cast<const char *>(a.dy) + t * a.ld_dy * G::kBytes;
         const char *total = static_cast<const char *>(a.total) + t * a.ld_total * G::kBytes;
@@ -179,10 +185,11 @@ __global__ void __launch_bounds__(kNormThreads) star_rms_norm_backward_long_kern
             return __fmul_rn(s, r);
         };
         const auto weighted = [&](int c, float d) { return __fmul_rn(d, gain_at(a.gain, a.gain_wide, c)); };
-        const double inner = sum_of_runs(a.cols, [&](int c, float run) { return __fmaf_rn(weighted(c, load_value<G>(dy, c)), normal(c), run); });
+        const double inner = sum_of_runs(steps, [&](int c, float run) { return __fmaf_rn(weighted(c, load_value<G>(dy, c)), normal(c), run); });
         const float mean = static_cast<float>(group_total<kNormThreads, kNormThreads>(inner, part[parity]) * a.inv_cols);
         char *dx = static_cast<char *>(a.dx) + t * a.ld_dx * G::kBytes;
-        for (int c = threadIdx.x; c < a.cols; c += kNormThreads) {
+        for (int i = 0; i < steps; ++i) {
+            const int c = long_column(i);
             const float d = load_value<G>(dy, c), n = normal(c);
             float v = __fmul_rn(r, __fmaf_rn(-n, mean, weighted(c, d)));
             if (a.d_total) v = __fadd_rn(v, load_value<G>(d_total, c));
@@ -646,8 +653,8 @@ __global__ void __launch_bounds__(kGainThreads) star_rms_norm_gain_kernel(const 
     __shared__ float part[32][33];
     wait_for_primary();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = blockDim.x / 32;
-    for (int base = blockIdx.x * 32; base < cols; base += gridDim.x * 32) {
-        const int c = base + lane;
+    for (int64_t base = blockIdx.x * 32; base < cols; base += gridDim.x * 32) {
+        const int64_t c = base + lane;
         float x = 0.0f;
         if (c < cols)
             for (int64_t q = warp; q < parts; q += warps) x = __fadd_rn(x, partial[q * cols + c]);

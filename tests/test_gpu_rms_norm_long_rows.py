@@ -39,3 +39,40 @@ def test_sums_of_one_sign(cols, value, dtype):
     # n, the sum, the mean and the difference are rounded once each, then dx.
     bound = rstd.double()[:, None] * n * mean * (SUM + 4 * R.ULP) + R.half_step(dtype) * want.abs() + R.ULP * want.abs()
     near(dx, want, bound)
+
+
+def test_the_most_columns():
+    """Rows that are 0 but at their ends, whose sums are exact: every column's index counts."""
+    from paper_2512_09685_b200 import binding as B
+    cols, ends = (1 << 31) - 65, 5000
+    at = torch.cat([torch.arange(ends, device="cuda"), torch.arange(cols - ends, cols, device="cuda")])
+
+    def row(seed):
+        v = torch.randint(1, 17, (2 * ends,), generator=gpu(seed), device="cuda").to(BF16)
+        x = torch.zeros((1, cols), dtype=BF16, device="cuda")
+        x[0, at] = v
+        return x, v.double()
+
+    x, v = row(1)
+    y, rstd = torch.full_like(x, 5.0), torch.empty(1, device="cuda")
+    codes, scales = B.star_checkpoint_empty(1, cols)
+    B.star_rms_norm(y, x, rstd=rstd, codes=codes, scales=scales, eps=1e-5)
+    r = ((v * v).sum() / cols + 1e-5) ** -0.5
+    near(rstd, r[None], R.ULP * r[None])
+    near(y[0, at], v * r, (2 * R.ULP + R.half_step(BF16)) * v * r)
+    assert int(torch.count_nonzero(y)) == 2 * ends
+    again = B.star_checkpoint_empty(1, cols)
+    B.star_checkpoint_pack(*again, y)
+    assert torch.equal(codes, again[0]) and torch.equal(scales[:, 0], again[1][:, 0])
+    del y, codes, scales, again
+
+    dy, d = row(2)
+    dx, dgain = torch.full_like(x, 5.0), torch.full((cols,), 5.0, device="cuda")
+    ws = torch.empty(B.star_rms_norm_workspace_bytes(1, cols), dtype=torch.uint8, device="cuda")
+    B.star_rms_norm_backward(dx, dgain, dy, None, rstd, ws, total=x)
+    r = rstd.double()
+    n = v * r
+    near(dgain[at], d * n, 3 * R.ULP * d * n)
+    want = r * (d - n * (d * n).sum() / cols)
+    near(dx[0, at], want, R.half_step(BF16) * want.abs() + r * n * (d * n).sum() / cols * (SUM + 4 * R.ULP) + R.ULP * want.abs())
+    assert int(torch.count_nonzero(dgain)) == 2 * ends and int(torch.count_nonzero(dx[:, ends:cols - ends])) == 0
