@@ -166,11 +166,19 @@ template <int EACH> __device__ __forceinline__ uint32_t bound_of(const uint32_t 
     return low;
 }
 
+// A thread's steps along n elements.  They are counted rather than the elements: one beyond
+// the last of 2^31 - 1 has no number.
+template <int THREADS> __device__ __forceinline__ int row_steps(int n)
+{
+    return static_cast<int>((static_cast<unsigned>(n) + THREADS - 1 - threadIdx.x) / THREADS);
+}
+
 // How many logits of a row reach `bound`, by a block of THREADS; every thread gets it.
 template <typename G, int THREADS> __device__ int count_row(const void *base, int vocab, uint32_t bound, int *total)
 {
     int n = 0;
-    for (int i = threadIdx.x; i < vocab; i += THREADS) n += order_of(load_value<G>(base, i)) >= bound ? 1 : 0;
+    const int steps = row_steps<THREADS>(vocab);
+    for (int q = 0; q < steps; ++q) n += order_of(load_value<G>(base, q * THREADS + static_cast<int>(threadIdx.x))) >= bound ? 1 : 0;
     n = __reduce_add_sync(0xffffffffu, n);
     __syncthreads();
     if (threadIdx.x == 0) *total = 0;
@@ -204,7 +212,9 @@ __device__ __noinline__ void search_row(const void *base, int vocab, int k, uint
     if (threadIdx.x == 0) found.count = 0;
     __syncthreads();
     const bool ties = reach > kMostCandidates;               // low is the k-th largest, and many equal it
-    for (int i = threadIdx.x; i < vocab; i += THREADS) {
+    const int steps = row_steps<THREADS>(vocab);
+    for (int q = 0; q < steps; ++q) {
+        const int i = q * THREADS + static_cast<int>(threadIdx.x);
         const uint32_t order = order_of(load_value<G>(base, i));
         if (ties ? order > low : order >= low) put_candidate<false>(found, order, i);
     }
@@ -213,7 +223,8 @@ __device__ __noinline__ void search_row(const void *base, int vocab, int k, uint
     // One warp, in the order of the indexes.
     if (threadIdx.x < 32) {
         int have = found.count;
-        for (int i = threadIdx.x; i - static_cast<int>(threadIdx.x) < vocab && have < k; i += 32) {
+        for (int first = 0; first <= (vocab - 1) / 32 && have < k; ++first) {
+            const int i = first * 32 + static_cast<int>(threadIdx.x);
             const bool equal = i < vocab && order_of(load_value<G>(base, i)) == low;
             const uint32_t who = __ballot_sync(0xffffffffu, equal);
             const int at = have + __popc(who & ((1u << threadIdx.x) - 1));
@@ -561,8 +572,9 @@ template <typename G, int THREADS> __global__ void __launch_bounds__(THREADS, ro
                 }
             }
         } else {
-            for (int at = s.head + begin * E + threadIdx.x; at < s.head + end * E; at += THREADS)
-                store_value<G>(out, at, active ? dense_gradient(load_value<G>(base, at), r) : 0.0f);
+            const int first = s.head + begin * E + static_cast<int>(threadIdx.x);
+            for (int q = 0; q < row_steps<THREADS>((end - begin) * E); ++q)
+                store_value<G>(out, first + q * THREADS, active ? dense_gradient(load_value<G>(base, first + q * THREADS), r) : 0.0f);
         }
         if (edge_at >= 0) store_value<G>(out, edge_at, active ? dense_gradient(edge, r) : 0.0f);
         if (active && (a.k > 0 || a.d_logp)) {
