@@ -572,9 +572,10 @@ template <typename G, int THREADS> __global__ void __launch_bounds__(THREADS, ro
                 }
             }
         } else {
-            const int first = s.head + begin * E + static_cast<int>(threadIdx.x);
-            for (int q = 0; q < row_steps<THREADS>((end - begin) * E); ++q)
-                store_value<G>(out, first + q * THREADS, active ? dense_gradient(load_value<G>(base, first + q * THREADS), r) : 0.0f);
+            // Without a sign: one beyond the last of 2^31 - 1 needs the 32nd bit.
+            const unsigned last = s.head + end * E;
+            for (unsigned at = s.head + begin * E + threadIdx.x; at < last; at += THREADS)
+                store_value<G>(out, at, active ? dense_gradient(load_value<G>(base, at), r) : 0.0f);
         }
         if (edge_at >= 0) store_value<G>(out, edge_at, active ? dense_gradient(edge, r) : 0.0f);
         if (active && (a.k > 0 || a.d_logp)) {
