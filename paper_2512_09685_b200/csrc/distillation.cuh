@@ -63,8 +63,9 @@ struct DistillSums {
     double loss, kl, ce, weight;
 };
 
-// q log(q / p) - q + p, which is never negative; d = log(p / q).  Without the
-// cancellation where the two are near.
+// q log(q / p) - q + p, which is never negative; d = log(p / q).  Where the two are near,
+// p - q leaves no digits beside q d, and exp(d) - 1 - d is good to 2^-24 / |d| of itself, as
+// d^2 / 2 is by what d is off (a series of exp(d) - 1 - d gives the same errors of the loss).
 __device__ __forceinline__ float divergence(float q, float p, float d)
 {
     if (q == 0.0f) return p;
