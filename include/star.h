@@ -635,7 +635,9 @@ STAR_API star_status_t star_token_alternatives_backward(void *dlogits, int64_t l
  *     sums = { sum w token_loss, sum w kl, sum w ce, sum w }      over the active rows
  * and dlogits is the gradient of sums[0] (no factor of temperature^2 is put in).
  * Ids outside [0, vocab) are entries that are not there (a record's -1); a value of
- * -inf is a probability of 0; an id that is listed twice has the sum of its q.  Where
+ * -inf is a probability of 0.  An id that is listed twice counts in kl with each of its
+ * entries, q[i] log(q[i] / p), which is not the divergence of a teacher that has their
+ * sum; p counts once, and the gradient, the same for both, has the sum of its q.  Where
  * the student's rest has no logit but -inf, the term in q0 is left out.  A coefficient
  * of exactly 0 takes its term out.
  *   labels  : NULL only where label_coef is 0.  A row is active iff its label, where
