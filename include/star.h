@@ -756,7 +756,8 @@ STAR_API star_status_t star_rms_norm_workspace_bytes(int64_t rows, int64_t cols,
  *     dx = d_total + rstd (gain dy - n mean(gain dy n))
  *     dgain[c] = sum_t dy n           (+ dgain[c] before, if accumulate != 0)
  *   total  : the stream as star_rms_norm normalized it (rows x cols of dtype), or NULL
- *            and codes, scales instead: a checkpoint of it (star_checkpoint_pack)
+ *            and codes, scales instead: a checkpoint of it (star_checkpoint_pack of
+ *            total; not the codes that star_rms_norm made, which are y's)
  *   rstd   : of the forward pass
  *   d_total: what reaches the stream past the norm, or NULL
  *   dx     : the gradient of x and of the residual; may be dy or d_total (same pointer

@@ -1119,7 +1119,8 @@ def star_rms_norm(y: torch.Tensor, x: torch.Tensor, gain: Optional[torch.Tensor]
                   codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, eps: float = 1e-6,
                   stream=None) -> None:
     """y = the root-mean-square norm of x + residual; the sum goes to total (which may
-    be x or the residual), and y is kept in 8 bits in codes and scales, where given."""
+    be x or the residual), and y is kept in 8 bits in codes and scales, where given (for
+    what reads y; star_rms_norm_backward takes the stream's)."""
     p, dtype, ld = _matrix(x, "x")
     shape, kind = x.shape, x.dtype
     rows, cols = shape
@@ -1143,7 +1144,8 @@ def star_rms_norm_backward(dx: torch.Tensor, dgain: Optional[torch.Tensor], dy: 
                            codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
                            d_total: Optional[torch.Tensor] = None, accumulate: bool = False, stream=None) -> None:
     """dx (which may be dy or d_total) and, unless None, dgain = or += its sums, from
-    the normalized stream: total, or a checkpoint of it in codes and scales."""
+    the normalized stream: total, or a checkpoint of it in codes and scales, which
+    star_checkpoint_pack makes of total.  (star_rms_norm's codes are y's: not these.)"""
     p, dtype, ld = _matrix(dy, "dy")
     shape, kind = dy.shape, dy.dtype
     rows, cols = shape

@@ -7,7 +7,8 @@ A small language-model head over frozen token embeddings,
 
 is trained by the clipped policy loss with a KL term, by the preference loss, or by
 distillation from a teacher's recorded top alternatives; then the head reads y
-through a root-mean-square norm, whose result alone is kept (``star_rms_norm``).
+through a root-mean-square norm (``star_rms_norm``).  Its result is kept in 8 bits, for
+the head's weight gradient, and y itself in bf16, for the norm's backward pass.
 The forward pass keeps the inputs of the three linear layers and of the GELU in
 8 bits (``star_checkpoint_pack``; h in the same pass as u's checkpoint); the loss
 turns the logits into their gradient in place; the backward pass reads the
@@ -64,7 +65,7 @@ class Worker:
         self.workspace = torch.empty(B.star_loss_workspace_bytes(rows, rows), dtype=torch.uint8, device=device)
         self.norm = norm
         if norm:
-            # The stream and its norm; only the stream stays until the backward pass.
+            # The stream, which the norm's backward pass reads, and its norm, which the head reads in the forward pass.
             self.y, self.normed = (torch.empty((rows, d), dtype=torch.bfloat16, device=device) for _ in range(2))
             self.rstd = torch.empty(rows, device=device)
             self.norm_workspace = torch.empty(B.star_rms_norm_workspace_bytes(rows, d), dtype=torch.uint8, device=device)
