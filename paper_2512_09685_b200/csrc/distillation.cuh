@@ -369,7 +369,7 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
     __shared__ DistillSums sums;
     __shared__ Listed lists[2];                                  // of every other row
     __shared__ int ahead[2];                                     // of every other item: its row, where rows are taken in a given order
-    __shared__ int late[2];                                      // chosen by `turn`, as block_part
+    __shared__ int late[2];                                      // of every other row, as in the policy loss
     __shared__ alignas(8) uint64_t landed;                       // the row's copy is in place
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int at_list = static_cast<int>(threadIdx.x) - kListFirst, list_warp = at_list / 32;
@@ -509,12 +509,11 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
     // In a given order, the rows that take no part are cleared between the others; this block's next one's place.
     int idle = a.order ? items + first_item : rows;
 
-    // What peers write is chosen by `turn`, which flips with the rows that pass the cluster's barrier below, the same in
-    // every block: between a block's reading of a slot and the next writing to it lies the barrier of the row between.
-    // The items' parity would not do: a row that takes no part flips it and has no barrier, and of two rows around it a
-    // block at the second could write over what a slow one still reads of the first.
+    // A cluster's blocks meet once in every row, whether it takes part or not: between a block's reading of what peers
+    // wrote for a row, chosen by its parity, and their writing for the row after the next lies the barrier of the row
+    // between, and none depends on what the blocks read to leave together.
     uint32_t phase = 0;
-    int parity = 0, turn = 0;
+    int parity = 0;
     float x_own = 0.0f, label_logit = 0.0f;
     if (threadIdx.x == 0 && first_item < items) {                // the first row's copy does not wait for its list
         const int64_t t = a.order ? a.order[first_item] : first_item;
@@ -546,9 +545,9 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
             const bool in_share = id >= s.head && in_own >= 0 && in_own < own.count * E;
             if (own.count > 0) {
                 if (!barrier_wait(smem_address(&landed), phase, a.tries)) {
-                    late[turn] = 1;                              // what the walk below finds is not used
+                    late[parity] = 1;                            // what the walk below finds is not used
                     for (uint32_t q = 0; q < blocks; ++q)
-                        if (blocks > 1) asm volatile("st.shared::cluster.s32 [%0], 1;" :: "r"(peer_address(smem_address(&late[turn]), q)) : "memory");
+                        if (blocks > 1) asm volatile("st.shared::cluster.s32 [%0], 1;" :: "r"(peer_address(smem_address(&late[parity]), q)) : "memory");
                 }
                 phase ^= 1;
             }
@@ -594,20 +593,19 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
             if (warp == 0) x = warp_join<MODE>(lane < kWarps ? warp_part[lane] : RestSums{-INFINITY, 0.0f, 0.0f}, k);
             if (blocks > 1) {
                 if (warp == 0 && lane < static_cast<int>(blocks)) {
-                    const uint32_t at = peer_address(smem_address(&block_part[turn][rank]), lane);
+                    const uint32_t at = peer_address(smem_address(&block_part[parity][rank]), lane);
                     asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0 + 4], %2;\n\tst.shared::cluster.f32 [%0 + 8], %3;"
                                  :: "r"(at), "f"(x.m), "f"(x.s), "f"(x.s1) : "memory");
                 }
                 cluster_sync();
-                if (warp == 0) x = warp_join<MODE>(lane < static_cast<int>(blocks) ? block_part[turn][lane] : RestSums{-INFINITY, 0.0f, 0.0f}, k);
+                if (warp == 0) x = warp_join<MODE>(lane < static_cast<int>(blocks) ? block_part[parity][lane] : RestSums{-INFINITY, 0.0f, 0.0f}, k);
             }
             if (warp == 0) {
                 const RestSums listed = warp_join<MODE>(lane * 32 < a.k ? list.part[lane] : RestSums{-INFINITY, 0.0f, 0.0f}, k);
                 DistillFactors f = make_factors<MODE>(a, list.teacher, x, listed, list.weight);
-                f.late = late[turn];
+                f.late = late[parity];
                 if (lane == 0) factors = f;
             }
-            turn ^= 1;
             float x_next = 0.0f;
             take_list(item + step, next, &x_next, &label_logit); // while the others wait for the factors
             __syncthreads();
@@ -685,7 +683,12 @@ __global__ void __launch_bounds__(THREADS, policy_blocks(THREADS)) star_distilla
                 }
             }
         } else {
-            __syncthreads();                                     // the last row's list has been read
+            if (blocks > 1) {
+                cluster_sync();
+                if (late[parity]) break;
+            } else {
+                __syncthreads();                                 // the last row's list has been read
+            }
             ask(item + step, parity ^ 1);
             take_list(item + step, next, &x_own, &label_logit);
             __syncthreads();
