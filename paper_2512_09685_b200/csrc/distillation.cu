@@ -31,8 +31,15 @@ star_status_t launch_loss(const DistillArgs &a, int cluster, int *parts_out, cud
     const int64_t clusters = std::min<int64_t>(a.row.rows, held);
     *parts_out = static_cast<int>(clusters);
     // Rows in order of taking part, where some may not, every block has a few, and there is enough to do to make up
-    // for finding it: 8192 x 50257, 35 % masked, 299 -> 273 us; none masked, 4096 x 50257 179 -> 184, 16384 x 4000
-    // 113 -> 130 (not taken).
+    // for finding it, whether or not any are masked; us as they come -> in order:
+    //                             35 % masked        none
+    //      4096 x  12000 bf16     51.4 ->  47.2    51.8 ->  57.4     98 MB: not taken
+    //      8192 x  12200 bf16     95.7 ->  83.0    99.0 ->   109    200 MB
+    //     65536 x   2000 bf16      551 ->   376     454 ->   508
+    //      2048 x  50257 bf16     87.3 ->  85.1    94.3 ->  97.8
+    //      8192 x  50257 bf16      304 ->   275     340 ->   349
+    //      1024 x  50257 fp32     83.1 ->  83.8    93.6 ->  97.2    206 MB, clusters of two
+    //      2048 x 131072 bf16      291 ->   244     324 ->   328    clusters of four
     DistillArgs work = a;
     if ((!a.row.labels && !a.row.weights) || a.row.rows < 4 * clusters || a.row.rows > kMostOrdered ||
         a.row.rows * a.row.vocab * G::kBytes < 200'000'000) {
@@ -63,9 +70,19 @@ template <typename G> star_status_t run_mode(const DistillArgs &a, int threads, 
 }
 
 // The smallest block whose part of the SM's shared memory holds a row, or a cluster
-// of them; the cluster's blocks may take an SM's shared memory each.  More threads and
-// more blocks to a row where there are few: 302 x 3071 bf16 with 512 threads instead of
-// 128, and few to the sums, 11.5 -> 8.4 us; 37 x 32001 fp32 17.9 -> 15.3.
+// of them; the cluster's blocks may take an SM's shared memory each.  Where there are few
+// rows, more threads to one: 302 x 3071 bf16 with 128, 256 and 512 threads 9.0, 8.4 and 10
+// to 13 us (256 taken), 1 x 6661 with 128 and 512 8.2 and 7.5; 590 x 3071 with 128 and 256
+// 11.8 and 12.0.  And clusters of more blocks for few long rows; us by blocks to a row:
+//     rows x vocab        1      2      4      8  taken
+//      9 x  32001 bf16  10.0   11.7   10.9   10.8     1
+//      1 x  50257 bf16  10.9   11.2   10.7   10.2     8
+//      9 x  50257 bf16  11.1   11.7   11.1   10.6     8
+//     18 x  50257 bf16  12.1   13.1   12.3   13.0     4
+//     37 x  50257 bf16  12.1   13.0   12.8   17.9     1   (the GPU does not hold as many clusters of 8 at once)
+//      9 x 100001 bf16         13.4   11.7   11.1     8
+//     18 x 100001 bf16         13.9   12.2   12.3     4
+//     37 x 100001 bf16         14.2   13.8   19.1     2
 bool shape(int64_t rows, int64_t vocab, int size, int *threads, int *cluster)
 {
     const int64_t bytes = vocab * size;
@@ -75,7 +92,7 @@ bool shape(int64_t rows, int64_t vocab, int size, int *threads, int *cluster)
         if (bytes <= int64_t{kDistillBytesPerThread} * t) *threads = t;
     while (*cluster < 8 && bytes > int64_t{kDistillBytesPerThread} * *threads * *cluster) *cluster *= 2;
     while (*threads < 512 && rows * *threads < 148 * 512 && bytes > 16 * *threads) *threads *= 2;
-    while (*cluster < 8 && rows * *cluster * 2 <= 148 * 2 && bytes / (*cluster * 2) >= 448 * 16) *cluster *= 2;
+    while (*cluster < 8 && rows * *cluster * 2 < 148 / 2 && bytes >= 98304) *cluster *= 2;
     return bytes <= int64_t{kDistillBytesPerThread} * 1024 * *cluster;
 }
 
