@@ -35,14 +35,28 @@ template <typename G, int THREADS, bool CLUSTER, bool FEW> star_status_t launch_
 //      4096 x 50257,  8  bf16                 87.7   97.3
 //      4096 x 50257, 64  bf16                  126    116
 //      2048 x 50257, 64  fp32                  125   95.4
-// Few long rows: clusters of up to eight blocks.  A block to a row against clusters:
-// 1 x 50257, 20 bf16 10.4 -> 6.4 us.  And 64 registers to a thread instead of 48 while all
-// blocks fit the GPU at once: 400 x 50257, 20 bf16 20.2 -> 16.7 us.
+// Few long rows: clusters of up to eight blocks, half a block to an SM in all, one or two
+// of longer rows, beyond which some wait for others to end.  us by blocks to a row, k = 20:
+//     rows x vocab        1      2      4      8  taken
+//      1 x  20011 bf16   5.3    6.4    5.8    5.8     1
+//      9 x  32001 bf16   6.4    7.5    6.5    6.2     8
+//     74 x  32001 bf16   8.0    9.1    9.8   13.4     1
+//      9 x  50257 bf16   8.6    8.4    7.3    6.6     8
+//     37 x  50257 bf16   9.3    9.0    8.4    9.4     4
+//    148 x  50257 bf16  10.1   11.2   15.8   22.9     1
+//     37 x 128256 bf16  15.2   12.6   11.3   11.0     8
+//    148 x 128256 bf16  21.8   18.4   23.5   29.1     2
+//    296 x 128256 bf16  24.7   23.6   36.6   50.0     2
+//     74 x  32001 fp32   8.2    7.9    8.9   13.0     4
+//    148 x  32001 fp32  10.6    9.4   14.8   20.9     2
+// And 64 registers to a thread instead of 48 while all blocks fit the GPU at once:
+// 400 x 50257, 20 bf16 20.2 -> 16.7 us.
 template <typename G> star_status_t run_rows(const AlternativesArgs &a, cudaStream_t stream)
 {
     const int64_t granules = a.row.vocab * G::kBytes / 16;
+    const int64_t most = granules < 6000 ? 148 / 2 : granules < 8000 ? 148 : 148 * 2;
     int cluster = 1;
-    while (granules > 2048 && cluster < 8 && a.row.rows * cluster * 2 <= 148 * 4 && granules / (cluster * 2) >= 448) cluster *= 2;
+    while (granules >= 3600 && cluster < 8 && a.row.rows * cluster * 2 <= (cluster == 1 && granules >= 12000 ? 148 * 4 : most)) cluster *= 2;
     if (cluster > 1) return launch_rows<G, 256, true, true>(a, cluster, stream);
     int threads = granules <= 2048 ? 64 : granules <= 8192 ? 128 : 256;
     while (threads < 256 && (threads < (granules > 2048 ? 4 : 2) * a.k || (threads < granules && a.row.rows * threads < 148 * 800))) threads *= 2;
