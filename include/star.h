@@ -740,8 +740,8 @@ STAR_API star_status_t star_checkpoint_weight_grad(void *dw, star_dtype_t dw_dty
  *   total  : rows x cols, or NULL; may be x or the residual (same pointer and stride)
  *   rstd   : rows entries, or NULL;  codes, scales : both or neither (NULL)
  *   gain   : cols entries of gain_dtype
- * Sums and rstd are binary32.  A row whose squares' sum is not finite in binary32 is
- * NaN throughout.  eps finite, > 0.  One kernel launch. */
+ * rstd is binary32, sums are that or more.  A row whose squares' sum is not finite in
+ * binary32 is NaN throughout.  eps finite, > 0.  One kernel launch. */
 STAR_API star_status_t star_rms_norm(void *y, int64_t ld_y, const void *x, int64_t ld_x, const void *residual,
                                      int64_t ld_residual, void *total, int64_t ld_total, star_dtype_t dtype,
                                      int64_t rows, int64_t cols, const void *gain, star_dtype_t gain_dtype,

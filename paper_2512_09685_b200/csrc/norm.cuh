@@ -102,6 +102,9 @@ template <int THREADS, int BLOCK, typename T> __device__ __forceinline__ T group
 // Rows longer than a block's registers hold: a block to a row, a warp on blocks of 32
 // columns, a lane to a column; the row is read again for its results.  A thread
 // counts its steps: a column beyond the last of up to 2^31 - 65 has no number.
+//
+// Bound by the latency of single elements: 4096 x 20000 bf16 with residual and 8 bits 451 us,
+// backward 596; 2048 x 32768 fp32 521 and 568 (3 to 6 times what their bytes take).
 // ---------------------------------------------------------------------------
 constexpr int kNormThreads = 256;
 __device__ __forceinline__ int long_column(int step) { return step * kNormThreads + static_cast<int>(threadIdx.x); }
